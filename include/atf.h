@@ -449,6 +449,127 @@ int atf_decode_paged_unrotated(const void *q, const void *k_pages, const void *v
                                const double *rope_inv_freq, float softmax_scale, void *workspace,
                                size_t workspace_bytes, void *hip_stream);
 
+/* ---- Appends with the heads' norms, and 8-bit caches ---------------------------------
+ *
+ * Norm and rotation.  Models that norm their heads compute, for every query and key head,
+ *   x' = x * rsqrt(mean(x^2) + eps) * weight      (mean over the head's d numbers)
+ * before RoPE.  atf_cache_append_normed does that, the rotation and the append in one pass:
+ * token t of row b, at position p = pos0 + t, or pos_rows[b] + t, has its queries normed,
+ * turned to p (rotate-half convention of Sec. 2) and written to q_out, ready for atf_prefill
+ * or a decode, its keys normed, turned to p and written to the K cache, and its values copied
+ * to the V cache.  All in fp32 from the bf16 inputs, rounded once, to nearest even.
+ *   q        bf16 [batch][n_new][h_q][d], or NULL: no queries (q_out NULL, h_q ignored)
+ *   k_new, v_new  bf16 [batch][n_new][h_kv][d]                           (device, read)
+ *   q_out    bf16, like q; may be q itself                               (device, written)
+ *   k_cache, v_cache  as atf_cache_append, capacity cache_tokens         (device, written at the tokens)
+ *   pos_rows int32 [batch], DEVICE, or NULL: the first position of each row's tokens, for
+ *            batches whose rows are of different lengths (atf_decode_ragged); pos0 must be 0.
+ *            A row whose entry is negative is idle: nothing of it is read into an output, its
+ *            slots of q_out and the caches keep what they hold.  Tokens at or past the
+ *            capacity are not stored (their queries are written all the same).
+ *   q_weight, k_weight  fp32 [d], DEVICE, or NULL: those heads are turned but not normed
+ *   eps      finite, >= 0
+ *   w, rope_inv_freq  the rotation, as atf_cache_append_rotated; a frequency of 0 leaves its
+ *            pair as it is (all of them 0: no rotation)
+ * n_new == 0 is a no-op.
+ * Errors: ATF_EINVAL (NULL window, pointer or only one of q and q_out, misaligned pointer,
+ * written buffers that overlap another one (q_out == q aside), batch < 1, heads < 1, n_new < 0,
+ * pos0 < 0, pos0 != 0 with pos_rows, pos0 + n_new > cache_tokens, cache_tokens < 1 or
+ * > 2^31 - 1, batch * n_new > 2^31 - 1, a bad eps or rotation frequency); ATF_EUNSUPPORTED
+ * (d not 64 or 128, h_q + 2 h_kv above 65535); ATF_EHIP. */
+int atf_cache_append_normed(const void *q, const void *k_new, const void *v_new, void *q_out,
+                            void *k_cache, void *v_cache, int32_t batch, int64_t n_new,
+                            int64_t pos0, const int32_t *pos_rows, int32_t h_q, int32_t h_kv,
+                            int64_t cache_tokens, const atf_window *w, const double *rope_inv_freq,
+                            const float *q_weight, const float *k_weight, float eps,
+                            void *hip_stream);
+
+/* atf_cache_append_normed into pages (layouts and tables as atf_cache_append_paged; tokens whose
+ * table entry is outside [0, num_pages) or past the table are not stored). */
+int atf_cache_append_paged_normed(const void *q, const void *k_new, const void *v_new, void *q_out,
+                                  void *k_pages, void *v_pages, const int32_t *block_table,
+                                  int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                                  int32_t batch, int64_t n_new, int64_t pos0,
+                                  const int32_t *pos_rows, int32_t h_q, int32_t h_kv,
+                                  const atf_window *w, const double *rope_inv_freq,
+                                  const float *q_weight, const float *k_weight, float eps,
+                                  void *hip_stream);
+
+/* 8-bit caches: half the memory and half the traffic of a decode.  Every row (one token of one
+ * KV head, keys and values apart) holds e4m3 numbers (4 exponent, 3 fraction bits, largest 448,
+ * no infinities) and one power of two that they are multiplied by, as an e8m0 byte (exponent +
+ * 127): the smallest 2^e, e in [-60, 119], with max |x| <= 448 * 2^e (the maximum over the
+ * row's finite numbers, 2^-60 if they are all 0 or none is).  Numbers are x / 2^e rounded to
+ * nearest even, from fp32 and once (keys after norm and rotation); what is not finite is
+ * stored as NaN.
+ *   k_cache  e4m3 [batch][h_kv][d/16][cache_tokens][16]   pair-chunk-major as the bf16 K cache
+ *   v_cache  e4m3 [batch][h_kv][ceil(cache_tokens/16)][d][16]  16-token blocks stored d-major,
+ *            a block's tokens IN ORDER (unlike the bf16 V cache's)
+ *   k_scale, v_scale  bytes [batch][h_kv][16 ceil(cache_tokens/16)], 16-byte aligned
+ * and in pages [num_pages][h_kv][...] with cache_tokens = page_tokens.
+ *
+ * atf_cache_append_normed into 8-bit caches (q_weight and k_weight may both be NULL). */
+int atf_cache_append_q8(const void *q, const void *k_new, const void *v_new, void *q_out,
+                        void *k_cache, void *k_scale, void *v_cache, void *v_scale, int32_t batch,
+                        int64_t n_new, int64_t pos0, const int32_t *pos_rows, int32_t h_q,
+                        int32_t h_kv, int64_t cache_tokens, const atf_window *w,
+                        const double *rope_inv_freq, const float *q_weight, const float *k_weight,
+                        float eps, void *hip_stream);
+int atf_cache_append_paged_q8(const void *q, const void *k_new, const void *v_new, void *q_out,
+                              void *k_pages, void *k_scale, void *v_pages, void *v_scale,
+                              const int32_t *block_table, int32_t max_pages_per_row,
+                              int32_t num_pages, int32_t page_tokens, int32_t batch, int64_t n_new,
+                              int64_t pos0, const int32_t *pos_rows, int32_t h_q, int32_t h_kv,
+                              const atf_window *w, const double *rope_inv_freq,
+                              const float *q_weight, const float *k_weight, float eps,
+                              void *hip_stream);
+
+/* Read positions pos0 .. pos0 + n_k - 1 of every row of an 8-bit cache (or, paged, of the pages
+ * its table names; entries are clamped to [0, num_pages)) back into contiguous bf16 caches, for
+ * atf_prefill of the next chunk or turn: every number times its power, which bf16 holds exactly.
+ * Nothing else of the bf16 caches changes.
+ *   q8_tokens     capacity of the 8-bit caches
+ *   k_cache, v_cache  bf16, layouts of atf_cache_append, capacity cache_tokens (device, written)
+ * n_k == 0 is a no-op.
+ * Errors: ATF_EINVAL (NULL/misaligned pointer, overlapping buffers, batch < 1, h_kv < 1, n_k < 0,
+ * pos0 < 0, pos0 + n_k > q8_tokens (or what a row's pages hold) or cache_tokens, bad page
+ * arguments); ATF_EUNSUPPORTED (d not 64/128, batch * h_kv above 65535); ATF_EHIP. */
+int atf_cache_read_q8(const void *k_q8, const void *k_scale, const void *v_q8, const void *v_scale,
+                      void *k_cache, void *v_cache, int32_t batch, int64_t n_k, int64_t pos0,
+                      int32_t h_kv, int32_t head_dim, int64_t q8_tokens, int64_t cache_tokens,
+                      void *hip_stream);
+int atf_cache_read_paged_q8(const void *k_pages, const void *k_scale, const void *v_pages,
+                            const void *v_scale, const int32_t *block_table,
+                            int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                            void *k_cache, void *v_cache, int32_t batch, int64_t n_k, int64_t pos0,
+                            int32_t h_kv, int32_t head_dim, int64_t cache_tokens, void *hip_stream);
+
+/* Decode over 8-bit caches: atf_decode, atf_decode_ragged and atf_decode_paged with the keys and
+ * values read as number * power (widened exactly; scores, softmax and the products with the
+ * values as there).  Keys are the rotated ones.  Same windows, clamping, empty rows and workspace
+ * (atf_decode_workspace_bytes of the same arguments); power bytes must be 1 .. 254.  A row whose
+ * scores are NaN (a key that was not finite) gives NaN.
+ * Errors: as those, plus ATF_EINVAL for NULL or misaligned scales.  Any group size is built:
+ * up to 16 query heads of a KV head share a workgroup.  Deterministic: equal inputs give equal bits. */
+int atf_decode_q8(const void *q, const void *k_cache, const void *k_scale, const void *v_cache,
+                  const void *v_scale, void *o, float *lse, int32_t batch, int64_t n_k,
+                  int64_t q_pos, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                  const atf_window *w, float softmax_scale, void *workspace,
+                  size_t workspace_bytes, void *hip_stream);
+int atf_decode_ragged_q8(const void *q, const void *k_cache, const void *k_scale,
+                         const void *v_cache, const void *v_scale, void *o, float *lse,
+                         int32_t batch, const int32_t *n_k_rows, const int32_t *q_pos_rows,
+                         int64_t max_n_k, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                         const atf_window *w, float softmax_scale, void *workspace,
+                         size_t workspace_bytes, void *hip_stream);
+int atf_decode_paged_q8(const void *q, const void *k_pages, const void *k_scale,
+                        const void *v_pages, const void *v_scale, void *o, float *lse,
+                        int32_t batch, const int32_t *block_table, int32_t max_pages_per_row,
+                        int32_t num_pages, int32_t page_tokens, const int32_t *n_k_rows,
+                        const int32_t *q_pos_rows, int64_t max_n_k, int32_t h_q, int32_t h_kv,
+                        const atf_window *w, float softmax_scale, void *workspace,
+                        size_t workspace_bytes, void *hip_stream);
+
 /* Message of the most recent failed call on this thread ("" if none). */
 const char *atf_last_error(void);
 

@@ -23,6 +23,13 @@ The functions carry the C names of ``include/atf.h``:
 - :func:`atf_rotate_kcache` -- RoPE over a whole unrotated K cache in one pass, into a
   pre-rotated copy; :func:`atf_cache_append_rotated`, :func:`atf_cache_append_paged_rotated`
   -- the appends with RoPE on the way in.
+- :func:`atf_cache_append_normed`, :func:`atf_cache_append_paged_normed` -- queries and keys
+  normed per head, turned to their positions and appended in one pass; rows may be at
+  positions of their own.
+- :func:`atf_cache_append_q8`, :func:`atf_cache_append_paged_q8` -- the same into 8-bit caches
+  (e4m3 numbers and a power of two per row); :func:`atf_cache_read_q8`,
+  :func:`atf_cache_read_paged_q8` -- those read back into bf16 caches; :func:`atf_decode_q8`,
+  :func:`atf_decode_ragged_q8`, :func:`atf_decode_paged_q8` -- decode over them.
 """
 from __future__ import annotations
 
@@ -103,6 +110,23 @@ def _load():
         "atf_decode_paged_unrotated": (ctypes.c_int, [P, P, P, P, P, i32, P, i32, i32, i32, P, P,
                                                       i64, i32, i32, W, P, f32, P, ctypes.c_size_t,
                                                       P]),
+        "atf_cache_append_normed": (ctypes.c_int, [P, P, P, P, P, P, i32, i64, i64, P, i32, i32, i64, W,
+                                                   P, P, P, f32, P]),
+        "atf_cache_append_paged_normed": (ctypes.c_int, [P, P, P, P, P, P, P, i32, i32, i32, i32, i64,
+                                                         i64, P, i32, i32, W, P, P, P, f32, P]),
+        "atf_cache_append_q8": (ctypes.c_int, [P, P, P, P, P, P, P, P, i32, i64, i64, P, i32, i32, i64,
+                                               W, P, P, P, f32, P]),
+        "atf_cache_append_paged_q8": (ctypes.c_int, [P, P, P, P, P, P, P, P, P, i32, i32, i32, i32, i64,
+                                                     i64, P, i32, i32, W, P, P, P, f32, P]),
+        "atf_cache_read_q8": (ctypes.c_int, [P, P, P, P, P, P, i32, i64, i64, i32, i32, i64, i64, P]),
+        "atf_cache_read_paged_q8": (ctypes.c_int, [P, P, P, P, P, i32, i32, i32, P, P, i32, i64, i64, i32,
+                                                   i32, i64, P]),
+        "atf_decode_q8": (ctypes.c_int, [P, P, P, P, P, P, P, i32, i64, i64, i32, i32, i64, W, f32, P,
+                                         ctypes.c_size_t, P]),
+        "atf_decode_ragged_q8": (ctypes.c_int, [P, P, P, P, P, P, P, i32, P, P, i64, i32, i32, i64, W,
+                                                f32, P, ctypes.c_size_t, P]),
+        "atf_decode_paged_q8": (ctypes.c_int, [P, P, P, P, P, P, P, i32, P, i32, i32, i32, P, P, i64,
+                                               i32, i32, W, f32, P, ctypes.c_size_t, P]),
         "atf_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -120,7 +144,10 @@ EXPORTED = ("atf_window_table", "atf_retention_profile", "atf_count_terms", "atf
             "atf_decode_paged", "atf_rotate_kcache", "atf_cache_append_rotated",
             "atf_cache_append_paged_rotated",
             "atf_prefill_unrotated", "atf_decode_unrotated", "atf_decode_ragged_unrotated",
-            "atf_decode_paged_unrotated", "atf_last_error")
+            "atf_decode_paged_unrotated", "atf_cache_append_normed", "atf_cache_append_paged_normed",
+            "atf_cache_append_q8", "atf_cache_append_paged_q8", "atf_cache_read_q8",
+            "atf_cache_read_paged_q8", "atf_decode_q8", "atf_decode_ragged_q8",
+            "atf_decode_paged_q8", "atf_last_error")
 
 
 def library():
@@ -700,3 +727,234 @@ def atf_decode_paged_unrotated(q, k_pages, v_pages, o, lse, block_table, n_k_row
         ctypes.byref(cw), fp, float(softmax_scale), _dev_ptr(workspace, torch.uint8, "workspace"),
         workspace.numel(), _stream_ptr(stream))
     _check(rc)
+
+
+# ---------------------------------------------------------------------------
+# appends with the heads' norms, and 8-bit caches
+# ---------------------------------------------------------------------------
+def qscale_shape(batch: int, cache_tokens: int, h_kv: int):
+    """Shape of k_scale and v_scale beside 8-bit caches, torch.float8_e8m0fnu:
+    [B, h_kv, 16 ceil(C/16)] (pages: batch = num_pages, C = page_tokens).  The caches are
+    torch.float8_e4m3fn of kcache_shape and vcache_shape (kpages_shape, vpages_shape)."""
+    return (batch, h_kv, (cache_tokens + 15) // 16 * 16)
+
+
+def _opt_ptr(t, dtype, name, shape):
+    if t is None:
+        return None
+    p = _dev_ptr(t, dtype, name)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return p
+
+
+def _new_heads(fn, q, k_new, v_new, q_out, window, q_weight, k_weight, pos_rows):
+    """The arguments every append with norms shares: (pointers of q, k_new, v_new, q_out;
+    pointers of pos_rows and the weights; B, n_new, h_q, h_kv, d)."""
+    torch = _torch()
+    bf, f32 = torch.bfloat16, torch.float32
+    B, n_new, h_kv, d = k_new.shape
+    if v_new.shape != k_new.shape or window.head_dim != d:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    if (q is None) != (q_out is None):
+        raise ValueError(f"{fn}: q and q_out must be given together")
+    h_q = 0
+    if q is not None:
+        if q.dim() != 4 or q.shape[:2] != k_new.shape[:2] or q.shape[3] != d or q_out.shape != q.shape:
+            raise ValueError(f"{fn}: inconsistent shapes")
+        h_q = q.shape[2]
+    ptrs = (None if q is None else _dev_ptr(q, bf, "q"), _dev_ptr(k_new, bf, "k_new"),
+            _dev_ptr(v_new, bf, "v_new"), None if q is None else _dev_ptr(q_out, bf, "q_out"))
+    return (ptrs, _opt_ptr(pos_rows, torch.int32, "pos_rows", (B,)),
+            _opt_ptr(q_weight, f32, "q_weight", (d,)), _opt_ptr(k_weight, f32, "k_weight", (d,)),
+            B, n_new, h_q, h_kv, d)
+
+
+def _q8_ptrs(fn, k, k_scale, v, v_scale, scale_shape):
+    torch = _torch()
+    if tuple(k_scale.shape) != scale_shape or tuple(v_scale.shape) != scale_shape:
+        raise ValueError(f"{fn}: scales must be {list(scale_shape)} (see qscale_shape)")
+    e4, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    return (_dev_ptr(k, e4, "k"), _dev_ptr(k_scale, e8, "k_scale"), _dev_ptr(v, e4, "v"),
+            _dev_ptr(v_scale, e8, "v_scale"))
+
+
+def _caches(fn, k_cache, v_cache, B, h_kv, d):
+    """Token capacity of a pair of contiguous caches of these sizes."""
+    if k_cache.dim() != 5:
+        raise ValueError(f"{fn}: the K cache must be [B, h_kv, d/16, C, 16]")
+    cap = k_cache.shape[3]
+    if k_cache.shape != kcache_shape(B, cap, h_kv, d) or v_cache.shape != vcache_shape(B, cap, h_kv, d):
+        raise ValueError(f"{fn}: inconsistent shapes")
+    return cap
+
+
+def _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d):
+    num_pages, hk, pt, dd = _pages(k_pages, v_pages, fn)
+    if hk != h_kv or dd != d or block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    return num_pages, pt, _dev_ptr(block_table, _torch().int32, "block_table")
+
+
+def atf_cache_append_normed(q, k_new, v_new, q_out, k_cache, v_cache, pos0: int, window: Window,
+                            q_weight=None, k_weight=None, eps: float = 1e-6, pos_rows=None,
+                            rope_inv_freq=None, stream=None):
+    """Norm per head (RMS, weights fp32 [d] or None), rotation and append in one pass: q
+    [B, n_new, h_q, d] bf16 (or None) -> q_out, k_new and v_new [B, n_new, h_kv, d] -> the caches
+    of atf_cache_append, at positions pos0 .., or pos_rows[b] .. of each row (int32 device
+    tensor [B], negative: an idle row; pos0 is 0 then)."""
+    fn = "atf_cache_append_normed"
+    torch = _torch()
+    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
+                                                            k_weight, pos_rows)
+    cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    cw, keep = window.as_c()
+    fp, keep2 = _rope_freq(rope_inv_freq, d)
+    _check(_lib.atf_cache_append_normed(
+        *ptrs, _dev_ptr(k_cache, torch.bfloat16, "k_cache"), _dev_ptr(v_cache, torch.bfloat16, "v_cache"),
+        B, n_new, int(pos0), rows, h_q, h_kv, cap, ctypes.byref(cw), fp, qw, kw, float(eps),
+        _stream_ptr(stream)))
+
+
+def atf_cache_append_paged_normed(q, k_new, v_new, q_out, k_pages, v_pages, block_table, pos0: int,
+                                  window: Window, q_weight=None, k_weight=None, eps: float = 1e-6,
+                                  pos_rows=None, rope_inv_freq=None, stream=None):
+    """atf_cache_append_normed into the pages block_table [B, max_pages] (int32, device) names."""
+    fn = "atf_cache_append_paged_normed"
+    torch = _torch()
+    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
+                                                            k_weight, pos_rows)
+    num_pages, pt, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
+    cw, keep = window.as_c()
+    fp, keep2 = _rope_freq(rope_inv_freq, d)
+    _check(_lib.atf_cache_append_paged_normed(
+        *ptrs, _dev_ptr(k_pages, torch.bfloat16, "k_pages"), _dev_ptr(v_pages, torch.bfloat16, "v_pages"),
+        table, block_table.shape[1], num_pages, pt, B, n_new, int(pos0), rows, h_q, h_kv,
+        ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+
+
+def atf_cache_append_q8(q, k_new, v_new, q_out, k_cache, k_scale, v_cache, v_scale, pos0: int,
+                        window: Window, q_weight=None, k_weight=None, eps: float = 1e-6,
+                        pos_rows=None, rope_inv_freq=None, stream=None):
+    """atf_cache_append_normed into 8-bit caches: k_cache and v_cache torch.float8_e4m3fn of
+    kcache_shape and vcache_shape, k_scale and v_scale torch.float8_e8m0fnu of qscale_shape."""
+    fn = "atf_cache_append_q8"
+    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
+                                                            k_weight, pos_rows)
+    cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
+    cw, keep = window.as_c()
+    fp, keep2 = _rope_freq(rope_inv_freq, d)
+    _check(_lib.atf_cache_append_q8(*ptrs, *cache, B, n_new, int(pos0), rows, h_q, h_kv, cap,
+                                    ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+
+
+def atf_cache_append_paged_q8(q, k_new, v_new, q_out, k_pages, k_scale, v_pages, v_scale, block_table,
+                              pos0: int, window: Window, q_weight=None, k_weight=None,
+                              eps: float = 1e-6, pos_rows=None, rope_inv_freq=None, stream=None):
+    """atf_cache_append_q8 into the pages block_table [B, max_pages] (int32, device) names."""
+    fn = "atf_cache_append_paged_q8"
+    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
+                                                            k_weight, pos_rows)
+    num_pages, pt, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
+    cw, keep = window.as_c()
+    fp, keep2 = _rope_freq(rope_inv_freq, d)
+    _check(_lib.atf_cache_append_paged_q8(
+        *ptrs, *cache, table, block_table.shape[1], num_pages, pt, B, n_new, int(pos0), rows, h_q, h_kv,
+        ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+
+
+def atf_cache_read_q8(k_q8, k_scale, v_q8, v_scale, k_cache, v_cache, n_k: int, pos0: int = 0,
+                      stream=None):
+    """Positions pos0 .. pos0 + n_k - 1 of 8-bit caches -> the same positions of bf16 caches (of
+    any capacity that holds them), exactly."""
+    fn = "atf_cache_read_q8"
+    torch = _torch()
+    B, h_kv = k_q8.shape[:2]
+    d = 16 * k_q8.shape[2]
+    cap = _caches(fn, k_q8, v_q8, B, h_kv, d)
+    out = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_q8, k_scale, v_q8, v_scale, qscale_shape(B, cap, h_kv))
+    _check(_lib.atf_cache_read_q8(
+        *cache, _dev_ptr(k_cache, torch.bfloat16, "k_cache"), _dev_ptr(v_cache, torch.bfloat16, "v_cache"),
+        B, int(n_k), int(pos0), h_kv, d, cap, out, _stream_ptr(stream)))
+
+
+def atf_cache_read_paged_q8(k_pages, k_scale, v_pages, v_scale, block_table, k_cache, v_cache, n_k: int,
+                            pos0: int = 0, stream=None):
+    """atf_cache_read_q8 from the pages block_table [B, max_pages] names, into contiguous caches."""
+    fn = "atf_cache_read_paged_q8"
+    torch = _torch()
+    num_pages, h_kv, pt, d = _pages(k_pages, v_pages, fn)
+    B = k_cache.shape[0]
+    out = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    _, _, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
+    _check(_lib.atf_cache_read_paged_q8(
+        *cache, table, block_table.shape[1], num_pages, pt, _dev_ptr(k_cache, torch.bfloat16, "k_cache"),
+        _dev_ptr(v_cache, torch.bfloat16, "v_cache"), B, int(n_k), int(pos0), h_kv, d, out,
+        _stream_ptr(stream)))
+
+
+def _decode_out(fn, q, o, lse, workspace):
+    torch = _torch()
+    B, h_q, d = q.shape
+    if o.shape != q.shape or lse.shape != (B, h_q):
+        raise ValueError(f"{fn}: inconsistent shapes")
+    return ((_dev_ptr(o, torch.bfloat16, "o"), _dev_ptr(lse, torch.float32, "lse")),
+            (_dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()), B, h_q, d)
+
+
+def _decode_rows(fn, n_k_rows, q_pos_rows, B):
+    torch = _torch()
+    if n_k_rows.shape != (B,) or q_pos_rows.shape != (B,):
+        raise ValueError(f"{fn}: inconsistent shapes")
+    return _dev_ptr(n_k_rows, torch.int32, "n_k_rows"), _dev_ptr(q_pos_rows, torch.int32, "q_pos_rows")
+
+
+def atf_decode_q8(q, k_cache, k_scale, v_cache, v_scale, o, lse, q_pos: int, window: Window, workspace,
+                  softmax_scale: float = 0.0, stream=None, n_k: Optional[int] = None):
+    """atf_decode over 8-bit caches (atf_cache_append_q8); the other arguments as there."""
+    fn = "atf_decode_q8"
+    torch = _torch()
+    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
+    h_kv = k_cache.shape[1]
+    cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
+    cw, keep = window.as_c()
+    _check(_lib.atf_decode_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B,
+                              cap if n_k is None else int(n_k), int(q_pos), h_q, h_kv, cap,
+                              ctypes.byref(cw), float(softmax_scale), *ws, _stream_ptr(stream)))
+
+
+def atf_decode_ragged_q8(q, k_cache, k_scale, v_cache, v_scale, o, lse, n_k_rows, q_pos_rows,
+                         max_n_k: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
+    """atf_decode_ragged over 8-bit caches."""
+    fn = "atf_decode_ragged_q8"
+    torch = _torch()
+    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
+    h_kv = k_cache.shape[1]
+    cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
+    rows = _decode_rows(fn, n_k_rows, q_pos_rows, B)
+    cw, keep = window.as_c()
+    _check(_lib.atf_decode_ragged_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B, *rows, int(max_n_k),
+                                     h_q, h_kv, cap, ctypes.byref(cw), float(softmax_scale), *ws,
+                                     _stream_ptr(stream)))
+
+
+def atf_decode_paged_q8(q, k_pages, k_scale, v_pages, v_scale, o, lse, block_table, n_k_rows, q_pos_rows,
+                        max_n_k: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
+    """atf_decode_paged over 8-bit pages."""
+    fn = "atf_decode_paged_q8"
+    torch = _torch()
+    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
+    num_pages, h_kv, pt, _ = _pages(k_pages, v_pages, fn)
+    _, _, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
+    rows = _decode_rows(fn, n_k_rows, q_pos_rows, B)
+    cw, keep = window.as_c()
+    _check(_lib.atf_decode_paged_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B, table,
+                                    block_table.shape[1], num_pages, pt, *rows, int(max_n_k), h_q, h_kv,
+                                    ctypes.byref(cw), float(softmax_scale), *ws, _stream_ptr(stream)))

@@ -758,11 +758,12 @@ struct PagedArgs {
     int32_t max_pages = 0, num_pages = 0, page_tokens = 0;
 };
 
-int decode_impl(const char* fn, const void* q, const void* k_cache, const void* v_cache, void* o,
-                float* lse, int32_t batch, int64_t n_k, int64_t q_pos, const int32_t* n_k_rows,
-                const int32_t* q_pos_rows, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
-                const atf_window* w, float softmax_scale, void* workspace, size_t workspace_bytes,
-                void* hip_stream, const PagedArgs& pg = PagedArgs(), const RopeArgs& rope = RopeArgs()) {
+// Checks a decode's arguments and fills what does not depend on its kernel; 0 or an error.
+int decode_setup(const char* fn, const void* q, const void* k_cache, const void* v_cache, void* o,
+                 float* lse, int32_t batch, int64_t n_k, int64_t q_pos, const int32_t* n_k_rows,
+                 const int32_t* q_pos_rows, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                 const atf_window* w, float softmax_scale, void* workspace, size_t workspace_bytes,
+                 const PagedArgs& pg, const RopeArgs& rope, atf::DecodeParams& p) {
     const bool ragged = n_k_rows != nullptr || q_pos_rows != nullptr;
     if (w == nullptr) return fail(ATF_EINVAL, "%s: NULL window", fn);
     const int d = w->head_dim;
@@ -780,7 +781,6 @@ int decode_impl(const char* fn, const void* q, const void* k_cache, const void* 
                     (long long)cache_tokens, (long long)n_k);
     if (!std::isfinite(softmax_scale))
         return fail(ATF_EINVAL, "%s: softmax_scale must be finite", fn);
-    atf::DecodeParams p{};
     int rc = build_table(w, &p.win);
     if (rc != ATF_OK) return rc;
     if (rope.rotate) {
@@ -806,8 +806,6 @@ int decode_impl(const char* fn, const void* q, const void* k_cache, const void* 
                     workspace == nullptr ? size_t(0) : workspace_bytes);
     if (!aligned(workspace, 16)) return fail(ATF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(float(d));
-    const int32_t group = h_q / h_kv;
-    const int32_t hpb = decode_heads_per_block(group);
     char* ws = static_cast<char*>(workspace);
     p.q = static_cast<const uint16_t*>(q);
     p.kpcm = static_cast<const uint16_t*>(k_cache);
@@ -824,8 +822,7 @@ int decode_impl(const char* fn, const void* q, const void* k_cache, const void* 
     p.q_pos = static_cast<int32_t>(q_pos);
     p.h_q = h_q;
     p.h_kv = h_kv;
-    p.group = group;
-    p.heads_per_block = hpb;
+    p.group = h_q / h_kv;
     p.n_k_rows = n_k_rows;
     p.q_pos_rows = q_pos_rows;
     p.block_table = pg.block_table;
@@ -833,7 +830,26 @@ int decode_impl(const char* fn, const void* q, const void* k_cache, const void* 
     p.num_pages = pg.num_pages;
     p.page_tokens = pg.page_tokens;
     p.n_valid = static_cast<int32_t>(ragged ? n_k : std::min(q_pos, n_k - 1) + 1);
-    p.cols16 = atf::decode_cols16(batch, h_q, h_kv, d, p.n_valid, cache_tokens, hpb, ragged);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    return ATF_OK;
+}
+
+int decode_impl(const char* fn, const void* q, const void* k_cache, const void* v_cache, void* o,
+                float* lse, int32_t batch, int64_t n_k, int64_t q_pos, const int32_t* n_k_rows,
+                const int32_t* q_pos_rows, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                const atf_window* w, float softmax_scale, void* workspace, size_t workspace_bytes,
+                void* hip_stream, const PagedArgs& pg = PagedArgs(), const RopeArgs& rope = RopeArgs()) {
+    atf::DecodeParams p{};
+    const int rc = decode_setup(fn, q, k_cache, v_cache, o, lse, batch, n_k, q_pos, n_k_rows, q_pos_rows,
+                                h_q, h_kv, cache_tokens, w, softmax_scale, workspace, workspace_bytes,
+                                pg, rope, p);
+    if (rc != ATF_OK) return rc;
+    const bool ragged = n_k_rows != nullptr;
+    const int d = w->head_dim;
+    const int32_t group = p.group;
+    const int32_t hpb = decode_heads_per_block(group);
+    p.heads_per_block = hpb;
+    p.cols16 = atf::decode_cols16(batch, h_q, h_kv, d, p.n_valid, p.cache_tokens, hpb, ragged);
     if (ragged) {
         // the work items are laid out on the device from the row arrays: the batch's
         // keys in about `splits` equal spans (multiples of the workgroup's token step)
@@ -858,7 +874,6 @@ int decode_impl(const char* fn, const void* q, const void* k_cache, const void* 
             return fail(ATF_EINVAL, "%s: cache too long for the split plan", fn);
         p.split_tokens = static_cast<int32_t>(step_tokens);
     }
-    p.scale_log2 = scale * 1.4426950408889634f;
     hipError_t e = atf::launch_decode(p, d, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return ATF_OK;
@@ -1083,6 +1098,372 @@ int atf_cache_append_paged_rotated(const void* k_new, const void* v_new, void* k
     return cache_append_paged_impl(fn, k_new, v_new, k_pages, v_pages, block_table,
                                    max_pages_per_row, num_pages, page_tokens, batch, n_new, pos0,
                                    h_kv, d, hip_stream, &rp);
+}
+
+}  // extern "C"
+
+namespace {
+
+// ---- appends with the heads' norms, and the 8-bit caches
+
+struct Span {
+    const char* name;
+    const void* ptr;
+    size_t bytes;
+    bool written;
+};
+
+// Every buffer that is written apart from every other one.
+template <size_t N>
+int check_apart(const char* fn, const Span (&s)[N]) {
+    for (size_t i = 0; i < N; ++i)
+        for (size_t j = i + 1; j < N; ++j) {
+            if (!(s[i].written || s[j].written) || !s[i].ptr || !s[j].ptr) continue;
+            const char *a = static_cast<const char*>(s[i].ptr), *b = static_cast<const char*>(s[j].ptr);
+            if (a < b + s[j].bytes && b < a + s[i].bytes)
+                return fail(ATF_EINVAL, "%s: %s and %s overlap", fn, s[i].name, s[j].name);
+        }
+    return ATF_OK;
+}
+
+// The page arguments, and the tokens that a row's pages hold.
+int check_pages(const char* fn, const PagedArgs& pg, int64_t* row_cap) {
+    if (!pg.block_table) return fail(ATF_EINVAL, "%s: NULL block table", fn);
+    if (!aligned(pg.block_table, 4)) return fail(ATF_EINVAL, "%s: block table must be 4-byte aligned", fn);
+    if (pg.page_tokens < 32 || pg.page_tokens % 32 != 0)
+        return fail(ATF_EINVAL, "%s: page_tokens %d must be a positive multiple of 32", fn, pg.page_tokens);
+    if (pg.num_pages < 1 || pg.max_pages < 1)
+        return fail(ATF_EINVAL, "%s: need num_pages >= 1 and max_pages_per_row >= 1", fn);
+    *row_cap = int64_t(pg.max_pages) * pg.page_tokens;
+    if (*row_cap > kPosLimit)
+        return fail(ATF_EINVAL, "%s: a row's pages hold more than 2^31 - 1 tokens", fn);
+    return ATF_OK;
+}
+
+PagedArgs paged_args(const int32_t* block_table, int32_t max_pages, int32_t num_pages, int32_t page_tokens) {
+    PagedArgs pg;
+    pg.block_table = block_table;
+    pg.max_pages = max_pages;
+    pg.num_pages = num_pages;
+    pg.page_tokens = page_tokens;
+    return pg;
+}
+
+int32_t scale_tokens(int64_t cache_tokens) { return static_cast<int32_t>((cache_tokens + 15) / 16 * 16); }
+
+struct HeadNorms {
+    const float* q_weight;
+    const float* k_weight;
+    float eps;
+};
+
+struct CacheQ8 {
+    void* k;
+    void* k_scale;
+    void* v;
+    void* v_scale;
+};
+
+// Shared by the four appends; `scaled`: 8-bit caches.  pg nullptr: contiguous ones.
+int append_normed_impl(const char* fn, const void* q, const void* k_new, const void* v_new, void* q_out,
+                       const CacheQ8& cache, bool scaled, int32_t batch, int64_t n_new, int64_t pos0,
+                       const int32_t* pos_rows, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                       const PagedArgs* pg, const atf_window* w, const double* rope_inv_freq,
+                       const HeadNorms& norms, void* hip_stream) {
+    if (w == nullptr) return fail(ATF_EINVAL, "%s: NULL window", fn);
+    const int d = w->head_dim;
+    if (d != 64 && d != 128)
+        return fail(ATF_EUNSUPPORTED, "%s: head_dim %d not built (64 or 128)", fn, d);
+    if (batch < 1 || h_kv < 1 || n_new < 0 || pos0 < 0 || (q != nullptr && h_q < 1))
+        return fail(ATF_EINVAL, "%s: need batch >= 1, heads >= 1, n_new >= 0, pos0 >= 0", fn);
+    if (q == nullptr) h_q = 0;
+    if ((q == nullptr) != (q_out == nullptr))
+        return fail(ATF_EINVAL, "%s: q and q_out must be given together", fn);
+    if (!std::isfinite(norms.eps) || norms.eps < 0.f)
+        return fail(ATF_EINVAL, "%s: eps must be finite and >= 0 (got %g)", fn, double(norms.eps));
+    int64_t cap = cache_tokens, entries = batch;
+    if (pg != nullptr) {
+        const int rc = check_pages(fn, *pg, &cap);
+        if (rc != ATF_OK) return rc;
+        cache_tokens = pg->page_tokens;
+        entries = pg->num_pages;
+    } else if (cap < 1 || cap > kPosLimit) {
+        return fail(ATF_EINVAL, "%s: cache_tokens %lld must be in [1, 2^31 - 1]", fn, (long long)cap);
+    }
+    if (pos_rows != nullptr ? pos0 != 0 : pos0 > cap - n_new)
+        return fail(ATF_EINVAL, pos_rows != nullptr
+                    ? "%s: pos0 %lld with pos_rows (the rows' positions are theirs: pass 0), %lld new tokens"
+                    : "%s: %lld tokens at position %lld do not fit the cache", fn,
+                    (long long)(pos_rows != nullptr ? pos0 : n_new), (long long)(pos_rows != nullptr ? n_new : pos0));
+    if (n_new > kPosLimit || int64_t(batch) * n_new > kPosLimit)
+        return fail(ATF_EINVAL, "%s: too many tokens for one call", fn);
+    if (int64_t(h_q) + 2 * int64_t(h_kv) > 65535)
+        return fail(ATF_EUNSUPPORTED, "%s: more than 65535 heads", fn);
+    atf::AppendNormedParams p{};
+    const int rc = rope_fractions(fn, w, rope_inv_freq, p.rope_rho_hi, p.rope_rho_lo);
+    if (rc != ATF_OK) return rc;
+    if (!k_new || !v_new || !cache.k || !cache.v || (scaled && (!cache.k_scale || !cache.v_scale)))
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    for (const void* x : {q, k_new, v_new, static_cast<const void*>(q_out), static_cast<const void*>(cache.k),
+                          static_cast<const void*>(cache.k_scale), static_cast<const void*>(cache.v),
+                          static_cast<const void*>(cache.v_scale)})
+        if (!aligned(x, 16)) return fail(ATF_EINVAL, "%s: tensors must be 16-byte aligned", fn);
+    if (!aligned(norms.q_weight, 4) || !aligned(norms.k_weight, 4) || !aligned(pos_rows, 4))
+        return fail(ATF_EINVAL, "%s: weights and row positions must be 4-byte aligned", fn);
+    const size_t tokens = size_t(batch) * size_t(n_new), vec = size_t(d) * 2;
+    const size_t number = scaled ? 1 : 2;
+    const size_t k_bytes = size_t(entries) * h_kv * size_t(cache_tokens) * d * number;
+    const size_t v_bytes = size_t(entries) * h_kv * size_t(scale_tokens(cache_tokens)) * d * number;
+    const size_t s_bytes = scaled ? size_t(entries) * h_kv * size_t(scale_tokens(cache_tokens)) : 0;
+    const Span spans[] = {
+        {"q", q == q_out ? nullptr : q, tokens * h_q * vec, false},
+        {"k_new", k_new, tokens * h_kv * vec, false},
+        {"v_new", v_new, tokens * h_kv * vec, false},
+        {"q_out", q_out, tokens * h_q * vec, true},
+        {"the K cache", cache.k, k_bytes, true},
+        {"the V cache", cache.v, v_bytes, true},
+        {"k_scale", cache.k_scale, s_bytes, true},
+        {"v_scale", cache.v_scale, s_bytes, true},
+    };
+    const int apart = check_apart(fn, spans);
+    if (apart != ATF_OK) return apart;
+    if (n_new == 0) return ATF_OK;
+    p.q = static_cast<const uint16_t*>(q);
+    p.k_src = static_cast<const uint16_t*>(k_new);
+    p.v_src = static_cast<const uint16_t*>(v_new);
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.k_dst = cache.k;
+    p.v_dst = cache.v;
+    p.k_scale = static_cast<uint8_t*>(cache.k_scale);
+    p.v_scale = static_cast<uint8_t*>(cache.v_scale);
+    p.q_weight = norms.q_weight;
+    p.k_weight = norms.k_weight;
+    p.eps = norms.eps;
+    p.pos_rows = pos_rows;
+    p.batch = batch;
+    p.n_new = static_cast<int32_t>(n_new);
+    p.h_q = h_q;
+    p.h_kv = h_kv;
+    p.pos0 = static_cast<int32_t>(pos0);
+    p.cache_tokens = static_cast<int32_t>(cache_tokens);
+    p.scale_tokens = scale_tokens(cache_tokens);
+    if (pg != nullptr) {
+        p.block_table = pg->block_table;
+        p.max_pages = pg->max_pages;
+        p.num_pages = pg->num_pages;
+        p.page_tokens = pg->page_tokens;
+    }
+    const hipError_t e = atf::launch_append_normed(p, d, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+// Shared by atf_cache_read_q8 and atf_cache_read_paged_q8 (pg given).
+int read_q8_impl(const char* fn, const void* k_src, const void* k_scale, const void* v_src,
+                 const void* v_scale, void* k_dst, void* v_dst, int32_t batch, int64_t n_k, int64_t pos0,
+                 int32_t h_kv, int32_t head_dim, int64_t src_tokens, const PagedArgs* pg,
+                 int64_t cache_tokens, void* hip_stream) {
+    if (head_dim != 64 && head_dim != 128)
+        return fail(ATF_EUNSUPPORTED, "%s: head_dim %d not built", fn, head_dim);
+    if (batch < 1 || h_kv < 1 || n_k < 0 || pos0 < 0)
+        return fail(ATF_EINVAL, "%s: need batch >= 1, h_kv >= 1, n_k >= 0, pos0 >= 0", fn);
+    int64_t cap = src_tokens, entries = batch;
+    if (pg != nullptr) {
+        const int rc = check_pages(fn, *pg, &cap);
+        if (rc != ATF_OK) return rc;
+        src_tokens = pg->page_tokens;
+        entries = pg->num_pages;
+    }
+    if (cap < 1 || cap > kPosLimit || cache_tokens < 1 || cache_tokens > kPosLimit || pos0 > cap - n_k ||
+        pos0 > cache_tokens - n_k)
+        return fail(ATF_EINVAL, "%s: tokens %lld .. %lld do not fit a source of %lld and caches of %lld tokens",
+                    fn, (long long)pos0, (long long)pos0 + (long long)n_k, (long long)cap, (long long)cache_tokens);
+    if (int64_t(batch) * h_kv > 65535)
+        return fail(ATF_EUNSUPPORTED, "%s: batch * h_kv above 65535", fn);
+    if (!k_src || !k_scale || !v_src || !v_scale || !k_dst || !v_dst)
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    for (const void* x : {k_src, k_scale, v_src, v_scale, static_cast<const void*>(k_dst),
+                          static_cast<const void*>(v_dst)})
+        if (!aligned(x, 16)) return fail(ATF_EINVAL, "%s: tensors must be 16-byte aligned", fn);
+    const size_t src = size_t(entries) * h_kv, padded = size_t(scale_tokens(src_tokens)), d = size_t(head_dim);
+    const size_t dst = size_t(batch) * h_kv;
+    const Span spans[] = {
+        {"the 8-bit K cache", k_src, src * size_t(src_tokens) * d, false},
+        {"k_scale", k_scale, src * padded, false},
+        {"the 8-bit V cache", v_src, src * padded * d, false},
+        {"v_scale", v_scale, src * padded, false},
+        {"the K cache", k_dst, dst * size_t(cache_tokens) * d * 2, true},
+        {"the V cache", v_dst, dst * size_t(scale_tokens(cache_tokens)) * d * 2, true},
+    };
+    const int apart = check_apart(fn, spans);
+    if (apart != ATF_OK) return apart;
+    if (n_k == 0) return ATF_OK;
+    atf::ReadQ8Params p{};
+    p.k_src = static_cast<const uint8_t*>(k_src);
+    p.k_scale = static_cast<const uint8_t*>(k_scale);
+    p.v_src = static_cast<const uint8_t*>(v_src);
+    p.v_scale = static_cast<const uint8_t*>(v_scale);
+    p.k_dst = static_cast<uint16_t*>(k_dst);
+    p.v_dst = static_cast<uint16_t*>(v_dst);
+    p.batch = batch;
+    p.n_k = static_cast<int32_t>(n_k);
+    p.pos0 = static_cast<int32_t>(pos0);
+    p.h_kv = h_kv;
+    p.src_tokens = static_cast<int32_t>(src_tokens);
+    p.scale_tokens = scale_tokens(src_tokens);
+    p.dst_tokens = static_cast<int32_t>(cache_tokens);
+    if (pg != nullptr) {
+        p.block_table = pg->block_table;
+        p.max_pages = pg->max_pages;
+        p.num_pages = pg->num_pages;
+        p.page_tokens = pg->page_tokens;
+    }
+    const hipError_t e = atf::launch_read_q8(p, head_dim, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+// Shared by the three decodes over 8-bit caches.
+int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const void* k_scale,
+                   const void* v_cache, const void* v_scale, void* o, float* lse, int32_t batch, int64_t n_k,
+                   int64_t q_pos, const int32_t* n_k_rows, const int32_t* q_pos_rows, int32_t h_q,
+                   int32_t h_kv, int64_t cache_tokens, const PagedArgs& pg, const atf_window* w,
+                   float softmax_scale, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    atf::DecodeQ8Params p{};
+    const int rc = decode_setup(fn, q, k_cache, v_cache, o, lse, batch, n_k, q_pos, n_k_rows, q_pos_rows, h_q,
+                                h_kv, cache_tokens, w, softmax_scale, workspace, workspace_bytes, pg,
+                                RopeArgs(), p);
+    if (rc != ATF_OK) return rc;
+    if (!k_scale || !v_scale) return fail(ATF_EINVAL, "%s: NULL scale pointer", fn);
+    if (!aligned(k_scale, 16) || !aligned(v_scale, 16))
+        return fail(ATF_EINVAL, "%s: scales must be 16-byte aligned", fn);
+    p.k_scale = static_cast<const uint8_t*>(k_scale);
+    p.v_scale = static_cast<const uint8_t*>(v_scale);
+    p.scale_tokens = pg.block_table != nullptr ? pg.page_tokens : scale_tokens(p.cache_tokens);
+    // the heads of a KV head in workgroups of up to 16, as even as they come
+    p.subgroups = (p.group + 15) / 16;
+    p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
+    if (n_k_rows != nullptr) {
+        p.splits = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
+    } else {
+        const int64_t steps = (int64_t(p.n_valid) + atf::kDecodeQ8TokenStep - 1) / atf::kDecodeQ8TokenStep;
+        const int64_t s = std::min<int64_t>(atf::decode_splits(batch, h_kv, n_k), steps);
+        const int64_t per = (steps + s - 1) / s;
+        p.splits = static_cast<int32_t>((steps + per - 1) / per);
+        if (per * atf::kDecodeQ8TokenStep * p.splits >= kPosLimit)
+            return fail(ATF_EINVAL, "%s: cache too long for the split plan", fn);
+        p.split_tokens = static_cast<int32_t>(per * atf::kDecodeQ8TokenStep);
+    }
+    const hipError_t e = atf::launch_decode_q8(p, w->head_dim, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int atf_cache_append_normed(const void* q, const void* k_new, const void* v_new, void* q_out, void* k_cache,
+                            void* v_cache, int32_t batch, int64_t n_new, int64_t pos0,
+                            const int32_t* pos_rows, int32_t h_q, int32_t h_kv, int64_t cache_tokens,
+                            const atf_window* w, const double* rope_inv_freq, const float* q_weight,
+                            const float* k_weight, float eps, void* hip_stream) {
+    return append_normed_impl("cache_append_normed", q, k_new, v_new, q_out, {k_cache, nullptr, v_cache, nullptr},
+                              false, batch, n_new, pos0, pos_rows, h_q, h_kv, cache_tokens, nullptr, w,
+                              rope_inv_freq, {q_weight, k_weight, eps}, hip_stream);
+}
+
+int atf_cache_append_paged_normed(const void* q, const void* k_new, const void* v_new, void* q_out,
+                                  void* k_pages, void* v_pages, const int32_t* block_table,
+                                  int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                                  int32_t batch, int64_t n_new, int64_t pos0, const int32_t* pos_rows,
+                                  int32_t h_q, int32_t h_kv, const atf_window* w,
+                                  const double* rope_inv_freq, const float* q_weight,
+                                  const float* k_weight, float eps, void* hip_stream) {
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    return append_normed_impl("cache_append_paged_normed", q, k_new, v_new, q_out,
+                              {k_pages, nullptr, v_pages, nullptr}, false, batch, n_new, pos0, pos_rows, h_q,
+                              h_kv, 0, &pg, w, rope_inv_freq, {q_weight, k_weight, eps}, hip_stream);
+}
+
+int atf_cache_append_q8(const void* q, const void* k_new, const void* v_new, void* q_out, void* k_cache,
+                        void* k_scale, void* v_cache, void* v_scale, int32_t batch, int64_t n_new,
+                        int64_t pos0, const int32_t* pos_rows, int32_t h_q, int32_t h_kv,
+                        int64_t cache_tokens, const atf_window* w, const double* rope_inv_freq,
+                        const float* q_weight, const float* k_weight, float eps, void* hip_stream) {
+    return append_normed_impl("cache_append_q8", q, k_new, v_new, q_out, {k_cache, k_scale, v_cache, v_scale},
+                              true, batch, n_new, pos0, pos_rows, h_q, h_kv, cache_tokens, nullptr, w,
+                              rope_inv_freq, {q_weight, k_weight, eps}, hip_stream);
+}
+
+int atf_cache_append_paged_q8(const void* q, const void* k_new, const void* v_new, void* q_out, void* k_pages,
+                              void* k_scale, void* v_pages, void* v_scale, const int32_t* block_table,
+                              int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                              int32_t batch, int64_t n_new, int64_t pos0, const int32_t* pos_rows,
+                              int32_t h_q, int32_t h_kv, const atf_window* w, const double* rope_inv_freq,
+                              const float* q_weight, const float* k_weight, float eps, void* hip_stream) {
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    return append_normed_impl("cache_append_paged_q8", q, k_new, v_new, q_out,
+                              {k_pages, k_scale, v_pages, v_scale}, true, batch, n_new, pos0, pos_rows, h_q,
+                              h_kv, 0, &pg, w, rope_inv_freq, {q_weight, k_weight, eps}, hip_stream);
+}
+
+int atf_cache_read_q8(const void* k_q8, const void* k_scale, const void* v_q8, const void* v_scale,
+                      void* k_cache, void* v_cache, int32_t batch, int64_t n_k, int64_t pos0, int32_t h_kv,
+                      int32_t head_dim, int64_t q8_tokens, int64_t cache_tokens, void* hip_stream) {
+    return read_q8_impl("cache_read_q8", k_q8, k_scale, v_q8, v_scale, k_cache, v_cache, batch, n_k, pos0, h_kv,
+                        head_dim, q8_tokens, nullptr, cache_tokens, hip_stream);
+}
+
+int atf_cache_read_paged_q8(const void* k_pages, const void* k_scale, const void* v_pages, const void* v_scale,
+                            const int32_t* block_table, int32_t max_pages_per_row, int32_t num_pages,
+                            int32_t page_tokens, void* k_cache, void* v_cache, int32_t batch, int64_t n_k,
+                            int64_t pos0, int32_t h_kv, int32_t head_dim, int64_t cache_tokens,
+                            void* hip_stream) {
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    return read_q8_impl("cache_read_paged_q8", k_pages, k_scale, v_pages, v_scale, k_cache, v_cache, batch, n_k,
+                        pos0, h_kv, head_dim, 0, &pg, cache_tokens, hip_stream);
+}
+
+int atf_decode_q8(const void* q, const void* k_cache, const void* k_scale, const void* v_cache,
+                  const void* v_scale, void* o, float* lse, int32_t batch, int64_t n_k, int64_t q_pos,
+                  int32_t h_q, int32_t h_kv, int64_t cache_tokens, const atf_window* w, float softmax_scale,
+                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return decode_q8_impl("decode_q8", q, k_cache, k_scale, v_cache, v_scale, o, lse, batch, n_k, q_pos, nullptr,
+                          nullptr, h_q, h_kv, cache_tokens, PagedArgs(), w, softmax_scale, workspace,
+                          workspace_bytes, hip_stream);
+}
+
+int atf_decode_ragged_q8(const void* q, const void* k_cache, const void* k_scale, const void* v_cache,
+                         const void* v_scale, void* o, float* lse, int32_t batch, const int32_t* n_k_rows,
+                         const int32_t* q_pos_rows, int64_t max_n_k, int32_t h_q, int32_t h_kv,
+                         int64_t cache_tokens, const atf_window* w, float softmax_scale, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+    if (!n_k_rows || !q_pos_rows)
+        return fail(ATF_EINVAL, "decode_ragged_q8: NULL row-length or row-position array");
+    return decode_q8_impl("decode_ragged_q8", q, k_cache, k_scale, v_cache, v_scale, o, lse, batch, max_n_k, 0,
+                          n_k_rows, q_pos_rows, h_q, h_kv, cache_tokens, PagedArgs(), w, softmax_scale,
+                          workspace, workspace_bytes, hip_stream);
+}
+
+int atf_decode_paged_q8(const void* q, const void* k_pages, const void* k_scale, const void* v_pages,
+                        const void* v_scale, void* o, float* lse, int32_t batch, const int32_t* block_table,
+                        int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                        const int32_t* n_k_rows, const int32_t* q_pos_rows, int64_t max_n_k, int32_t h_q,
+                        int32_t h_kv, const atf_window* w, float softmax_scale, void* workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+    const char* fn = "decode_paged_q8";
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    int64_t row_cap = 0;
+    const int rc = check_pages(fn, pg, &row_cap);
+    if (rc != ATF_OK) return rc;
+    if (!n_k_rows || !q_pos_rows) return fail(ATF_EINVAL, "%s: NULL row-length or row-position array", fn);
+    if (max_n_k > row_cap)
+        return fail(ATF_EINVAL, "%s: max_n_k %lld exceeds the %lld tokens a row's pages hold", fn,
+                    (long long)max_n_k, (long long)row_cap);
+    return decode_q8_impl(fn, q, k_pages, k_scale, v_pages, v_scale, o, lse, batch, max_n_k, 0, n_k_rows,
+                          q_pos_rows, h_q, h_kv, row_cap, pg, w, softmax_scale, workspace, workspace_bytes,
+                          hip_stream);
 }
 
 }  // extern "C"

@@ -106,6 +106,57 @@ struct AppendRotParams : AppendParams {
     uint32_t rope_rho_lo[kMaxPairs];
 };
 
+// Decode over 8-bit caches (decode_q8.hip): kpcm and vpk hold e4m3 bytes in the layouts of
+// q8.hpp's caches, with a power-of-two byte per token.  heads_per_block is at most 16 and need
+// not divide the group: the last of the `subgroups` workgroups of a KV head takes what is left.
+struct DecodeQ8Params : DecodeParams {
+    const uint8_t* k_scale;   // [B][h_kv][scale_tokens], or pages [num_pages][h_kv][page_tokens]
+    const uint8_t* v_scale;
+    int32_t scale_tokens;     // cache_tokens rounded up to 16, or page_tokens
+    int32_t subgroups;
+};
+
+// Append with the heads' norms and the rotation (append_normed.hip), of bf16 caches or, with
+// k_scale set, 8-bit ones.
+struct AppendNormedParams {
+    const uint16_t* q;           // [B][n_new][h_q][d], or nullptr (h_q is 0 then)
+    const uint16_t* k_src;       // [B][n_new][h_kv][d]
+    const uint16_t* v_src;
+    uint16_t* q_out;             // like q
+    void* k_dst;                 // caches or page pools
+    void* v_dst;
+    uint8_t* k_scale;            // 8-bit caches: [B][h_kv][scale_tokens] or pages, else nullptr
+    uint8_t* v_scale;
+    const float* q_weight;       // [d], or nullptr: not normed
+    const float* k_weight;
+    float eps;
+    const int32_t* pos_rows;     // device [B] first position of each row (negative: idle), or
+                                 // nullptr: pos0
+    const int32_t* block_table;  // [B][max_pages], or nullptr: contiguous caches
+    int32_t batch, n_new, h_q, h_kv, pos0;
+    int32_t cache_tokens;        // capacity of the contiguous caches
+    int32_t scale_tokens;        // cache_tokens rounded up to 16, or page_tokens
+    int32_t max_pages, num_pages, page_tokens;
+    int32_t heads_per_wave;      // set by the launcher
+    uint32_t rope_rho_hi[kMaxPairs];
+    uint32_t rope_rho_lo[kMaxPairs];
+};
+
+// 8-bit caches (or pages) read back into contiguous bf16 caches (cache_q8.hip): positions
+// pos0 .. pos0 + n_k - 1 of every row.
+struct ReadQ8Params {
+    const uint8_t* k_src;
+    const uint8_t* k_scale;
+    const uint8_t* v_src;
+    const uint8_t* v_scale;
+    uint16_t* k_dst;             // [B][h_kv][d/16][dst_tokens][16]
+    uint16_t* v_dst;             // [B][h_kv][ceil(dst_tokens/16)][d][16]
+    const int32_t* block_table;  // [B][max_pages], or nullptr: contiguous source
+    int32_t batch, n_k, pos0, h_kv;
+    int32_t src_tokens, scale_tokens, dst_tokens;
+    int32_t max_pages, num_pages, page_tokens;
+};
+
 // One pass of RoPE over a pair-chunk-major K cache (rotate.hip): key t of every (batch,
 // kv head) turned to position t, tokens 0 .. n_k - 1.
 struct RotateParams {
@@ -116,7 +167,7 @@ struct RotateParams {
     uint32_t rope_rho_lo[kMaxPairs];
 };
 
-// Kernel launchers (prefill.hip, decode.hip, rotate.hip).  Return the HIP error of the launch.
+// Kernel launchers (prefill.hip, decode.hip, rotate.hip and the files named).  Return the HIP error of the launch.
 hipError_t launch_prefill(const PrefillParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_prefill_rotating(const PrefillRotParams& p, int head_dim, hipStream_t stream);
 // The kernel a prefill takes: 4 or 8 waves per row block of prefill_short_kernel, 0 for
@@ -124,6 +175,11 @@ hipError_t launch_prefill_rotating(const PrefillRotParams& p, int head_dim, hipS
 int32_t prefill_waves(int32_t batch, int32_t n_q, int32_t n_k, int32_t q_pos0, int32_t h_kv, int32_t group,
                       int32_t cache_tokens, const int32_t* thresholds, int32_t head_dim, bool rotate);
 hipError_t launch_decode(const DecodeParams& p, int head_dim, hipStream_t stream);
+// The merge of the partial states that decode_q8_kernel wrote (decode.hip).
+hipError_t launch_decode_merge_q8(const DecodeParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t stream);
+hipError_t launch_append_normed(const AppendNormedParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_read_q8(const ReadQ8Params& p, int head_dim, hipStream_t stream);
 hipError_t launch_append(const AppendRotParams& p, bool turn, int head_dim, hipStream_t stream);
 hipError_t launch_rotate_kcache(const RotateParams& p, int head_dim, hipStream_t stream);
 
@@ -145,6 +201,8 @@ bool decode_direct(int32_t batch, int32_t h_q, int32_t h_kv, int32_t head_dim, i
 constexpr int64_t kDecode16MaxTokens = (int64_t(1) << 27) - 64;
 // Tokens handled per decode workgroup iteration (the split granularity).
 constexpr int32_t kDecodeTokenStep = 128;
+// The same of the 8-bit caches' decode: four waves, 64 tokens each.
+constexpr int32_t kDecodeQ8TokenStep = 256;
 // Largest split count the merge kernel accepts.
 constexpr int32_t kDecodeMaxSplits = 4096;
 // Query heads one decode workgroup handles at most (columns of its MFMA tiles).

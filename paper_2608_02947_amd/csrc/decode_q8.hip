@@ -1,0 +1,373 @@
+// Windowed single-token decode over 8-bit caches (q8.hpp), gfx950: decode.hip's split-KV decode
+// with the keys and values read as e4m3 numbers and widened to bf16 in registers.
+//
+// Caches (written by append_normed.hip):
+//   K [B][h_kv][d/16][cache_tokens][16]: chunk c of a token is 16 bytes, pairs 8c .. 8c + 7,
+//     first components then second; a power per token, k_scale [B][h_kv][ceil16(cache_tokens)]
+//   V [B][h_kv][ceil(cache_tokens/16)][d][16]: 16-token blocks, dim-major, tokens in order; a
+//     power per token, v_scale
+//
+// The heads of one KV head (up to 16 a workgroup) are the columns of v_mfma_f32_16x16x32_bf16,
+// a wave's block is 64 tokens, and every load of K and V is 16 bytes a lane.  With r = lane % 16,
+// g = lane / 16:
+//   scores, tile s = 0 .. 3: A row r is token 16 (r / 4) + 4 s + r % 4, the lane's 16 bytes chunk
+//     4 m + g of it: its two halves are two operands of 8 dims, for two products.  The result
+//     gives the lane, for head r, tokens 16 g + 4 s + v.
+//   values: the lane's 16 bytes are the 16 tokens of block g for dim 16 i + r: two operands of 8
+//     tokens.  The tokens 16 g .. 16 g + 15 it needs probabilities of are those it has scores of.
+// A key's power is part of its conversion (v_cvt_scalef32_pk_bf16_fp8); a value's, which differs
+// along the product's sum, goes into its probability after the normaliser has taken it.
+//
+// A pair is kept at distance z iff z <= W_r.  Per block, two ballots give the pairs kept at some
+// token and at every token: chunks without a kept pair are read from a line of zeros, queries
+// lose the pairs kept nowhere, and where a window ends inside the block the keys' bytes are
+// masked lane by lane.
+#include "atf_internal.hpp"
+#include "decode_plan.hpp"
+#include "q8.hpp"
+
+namespace atf {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;
+constexpr int kBlock = 64;             // tokens of a wave's block
+constexpr float kRescale = 8.0f;       // lazy-rescale threshold, log2 units
+
+// what lanes read whose chunk no token keeps, or whose token is past the row's keys
+__device__ const uint32_t g_zeros[64] __attribute__((aligned(256))) = {};
+
+__device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                   __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 8 e4m3 numbers times a power of two as 8 bf16 numbers, exact
+__device__ __forceinline__ u32x4_t widen(uint32_t a, uint32_t b, float power) {
+    u32x4_t r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, power, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, power, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, power, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, power, true));
+    return r;
+}
+
+// bf16 pairs whose bit is set in `mask` (bit e = pair e of the chunk)
+__device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
+    u32x4_t r;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+        r[t] = x[t] & (((mask >> (2 * t)) & 1u ? 0x0000FFFFu : 0u) | ((mask >> (2 * t + 1)) & 1u ? 0xFFFF0000u : 0u));
+    return r;
+}
+
+template <int D>
+__global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ8Params p) {
+    constexpr int kChunks = D / 16;
+    constexpr int kHalf = D / 2;
+    constexpr int kM = D / 64;   // loads of a token: 4 chunks each
+    constexpr int kDB = D / 16;  // 16-dim blocks of the output
+    constexpr int kOStride = D + 4;
+    constexpr int NW = kWaves;
+    __shared__ float red_m[NW][16];
+    __shared__ float red_l[NW][16];
+    __shared__ int s_w[kHalf];
+    // the queries while the waves stream, then the waves' outputs [wave][head][D + 4]
+    constexpr int kMerge = NW * 16 * kOStride;
+    __shared__ __attribute__((aligned(16))) float shared[kMerge];
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15;
+    const int g4 = lane >> 4;
+    const int split = blockIdx.x;
+    const int subgroups = p.subgroups;
+    const int g = blockIdx.y / subgroups;
+    const int sub = blockIdx.y % subgroups;
+    const int hq0 = g * p.group + sub * p.heads_per_block;
+    const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
+    const bool head_ok = r16 < NH;
+
+    int b, n_k = p.n_k, q_pos = p.q_pos, n_valid = p.n_valid, t_begin, t_end;
+    int64_t slot0 = 0;
+    if (p.n_k_rows != nullptr) {
+        int64_t span;
+        int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
+        b = ragged_item(p, split, kDecodeQ8TokenStep, t_begin, span, plan);
+        if (b < 0) return;
+        n_k = min(max(p.n_k_rows[b], 0), p.n_k);
+        q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
+        n_valid = min(n_k, q_pos + 1);
+        t_end = int(min(int64_t(n_valid), int64_t(t_begin) + span));
+        slot0 = int64_t(split) * p.h_q + hq0;
+    } else {
+        b = blockIdx.z;
+        t_begin = split * p.split_tokens;
+        t_end = min(n_valid, t_begin + p.split_tokens);
+        slot0 = (int64_t(b) * p.h_q + hq0) * p.splits + split;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    q_pos = __builtin_amdgcn_readfirstlane(q_pos);
+    t_begin = __builtin_amdgcn_readfirstlane(t_begin);
+    t_end = __builtin_amdgcn_readfirstlane(t_end);
+    const int my_w = lane < kHalf ? p.win.W[lane] : -1;
+    if (tid < kHalf) s_w[tid] = p.win.W[tid];
+
+    // queries: operand (m, half) at 256 (2 m + half) + 4 lane
+    for (int o = wave; o < 2 * kM; o += NW) {
+        u32x4_t z = {0u, 0u, 0u, 0u};
+        if (head_ok)
+            z = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(b) * p.h_q + hq0 + r16) * D + (o & 1) * kHalf +
+                                                  8 * (4 * (o >> 1) + g4));
+        *reinterpret_cast<u32x4_t*>(&shared[256 * o + 4 * lane]) = z;
+    }
+    __syncthreads();
+
+    f32x4_t oacc[kDB];
+#pragma unroll
+    for (int i = 0; i < kDB; ++i) oacc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, m_thr = -INFINITY, m_neg = 0.f, l_run = 0.f;
+    const float sc = p.scale_log2;
+    uint64_t q_keep = 0;
+    u32x4_t qm[2 * kM];  // queries with the pairs outside q_keep zeroed
+#pragma unroll
+    for (int o = 0; o < 2 * kM; ++o) qm[o] = u32x4_t{0u, 0u, 0u, 0u};
+
+    const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
+    const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
+    const uint8_t* const zeros = reinterpret_cast<const uint8_t*>(g_zeros);
+    const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
+
+    for (int t0 = t_begin + kBlock * wave; t0 < t_end; t0 += kBlock * NW) {
+        // the entries of the caches that hold the block's two halves of 32 tokens (a page holds
+        // whole halves): rows of KV head g, and the place of token t0 in them
+        int64_t row_a = int64_t(b) * p.h_kv + g, row_b = row_a;
+        int at_a = t0, at_b = t0 + 32;
+        int64_t cap = p.cache_tokens;
+        if (p.block_table != nullptr) {
+            const int pt = p.page_tokens;
+            const int32_t* table = p.block_table + int64_t(b) * p.max_pages;
+            const int ia = t0 / pt, ib = min((t0 + 32) / pt, p.max_pages - 1);
+            row_a = int64_t(min(max(table[ia], 0), p.num_pages - 1)) * p.h_kv + g;
+            row_b = int64_t(min(max(table[ib], 0), p.num_pages - 1)) * p.h_kv + g;
+            at_a = t0 - ia * pt;
+            at_b = (t0 + 32) % pt;
+            cap = pt;
+        }
+        const uint64_t full = __ballot(my_w >= q_pos - t0);
+        const uint64_t keep = __ballot(my_w >= max(0, q_pos - min(t0 + kBlock - 1, t_end - 1)));
+
+        // K operands
+        u32x4_t kf[4][kM];
+        u32x4_t kscale;
+        {
+            const bool hi = r16 >= 8;
+            const int64_t row = hi ? row_b : row_a;
+            const int at = (hi ? at_b : at_a) + (tk & 31);
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                const int c = 4 * m + g4;
+                const bool kept = (keep >> (8 * c)) & 0xFFull;
+                const uint8_t* src = keys + ((row * kChunks + c) * cap + at) * 16;
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    kf[s][m] = *reinterpret_cast<const u32x4_t*>(kept && t0 + tk + 4 * s < t_end ? src + 64 * s : zeros);
+            }
+            const uint8_t* src = p.k_scale + row * p.scale_tokens + (at & ~15);
+            kscale = *reinterpret_cast<const u32x4_t*>(t0 + (tk & ~15) < t_end ? src : zeros);
+        }
+        // V^T operands
+        u32x4_t vf[kDB], vscale;
+        {
+            const bool hi = g4 >= 2;
+            const int64_t row = hi ? row_b : row_a;
+            const int at = (hi ? at_b : at_a) + 16 * (g4 & 1);
+            const bool in = t0 + 16 * g4 < t_end;
+            const uint8_t* src = values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16;
+#pragma unroll
+            for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(in ? src + 256 * i : zeros);
+            vscale = *reinterpret_cast<const u32x4_t*>(in ? p.v_scale + row * p.scale_tokens + at : zeros);
+        }
+
+        // windows that end inside the block: this lane's token and chunk, byte by byte
+        if (keep & ~full) {
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                int w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = s_w[8 * (4 * m + g4) + e];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int z = q_pos - (t0 + tk + 4 * s);
+                    uint32_t lo = 0, hi = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        lo |= w[e] >= z ? 0xFFu << (8 * e) : 0u;
+                        hi |= w[4 + e] >= z ? 0xFFu << (8 * e) : 0u;
+                    }
+                    kf[s][m] &= u32x4_t{lo, hi, lo, hi};
+                }
+            }
+        }
+        if (keep != q_keep) {
+            q_keep = keep;
+#pragma unroll
+            for (int o = 0; o < 2 * kM; ++o)
+                qm[o] = keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
+                                   uint32_t(keep >> (8 * (4 * (o >> 1) + g4))) & 0xFFu);
+        }
+        f32x4_t sacc[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const float power = q8::power((kscale[s] >> (8 * (r16 & 3))) & 255u);
+            sacc[s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                sacc[s] = mfma16(widen(kf[s][m][0], kf[s][m][1], power), qm[2 * m], sacc[s]);
+                sacc[s] = mfma16(widen(kf[s][m][2], kf[s][m][3], power), qm[2 * m + 1], sacc[s]);
+            }
+        }
+        // tokens past the split's end: no probability, and no value that is not a number
+        if (t0 + kBlock > t_end) {
+            const int bound = t_end - (t0 + 16 * g4);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                uint32_t msk = 0;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    if (4 * s + v >= bound) sacc[s][v] = -INFINITY;
+                    msk |= 4 * s + v < bound ? 0xFFu << (8 * v) : 0u;
+                }
+                vscale[s] &= msk;
+#pragma unroll
+                for (int i = 0; i < kDB; ++i) vf[i][s] &= msk;
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sacc[s][v]);
+        if (__any(mx * sc > m_thr)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float m_new = fmaxf(m_run, mx * sc);
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = exp2_fast(m_run - m_use);
+            m_run = m_new;
+            m_thr = m_new + kRescale;
+            m_neg = -m_use;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < kDB; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) oacc[i][v] *= alpha;
+        }
+        // P times the values' powers as two bf16 numbers, what fits and what is left over: one
+        // would round every probability to 2^-9, and the output's own rounding is that size
+        u32x4_t ph[2], pl[2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float x[2];
+                uint32_t h[2];
+                bf16x2_t rest;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int v = 2 * t + k;
+                    const float e = exp2_fast(__builtin_fmaf(sacc[s][v], sc, m_neg));
+                    l_run += e;
+                    x[k] = e * q8::power((vscale[s] >> (8 * v)) & 255u);
+                    h[k] = __float_as_uint(x[k]) & 0xFFFF0000u;
+                    rest[k] = (__bf16)(x[k] - __uint_as_float(h[k]));
+                }
+                ph[s >> 1][2 * (s & 1) + t] = h[0] >> 16 | h[1];
+                pl[s >> 1][2 * (s & 1) + t] = __builtin_bit_cast(uint32_t, rest);
+            }
+#pragma unroll
+        for (int i = 0; i < kDB; ++i) {
+            const u32x4_t v0 = widen(vf[i][0], vf[i][1], 1.f), v1 = widen(vf[i][2], vf[i][3], 1.f);
+            oacc[i] = mfma16(v0, ph[0], oacc[i]);
+            oacc[i] = mfma16(v1, ph[1], oacc[i]);
+            oacc[i] = mfma16(v0, pl[0], oacc[i]);
+            oacc[i] = mfma16(v1, pl[1], oacc[i]);
+        }
+    }
+
+    // ---- combine the waves' states (in wave order) and write the split's partial
+    float l_lane = l_run + __shfl_xor(l_run, 16);
+    l_lane += __shfl_xor(l_lane, 32);
+    // every score NaN: any maximum will do for the normaliser to reach the output
+    if (m_run == -INFINITY && l_lane != l_lane) m_run = 0.f;
+    if (g4 == 0) {
+        red_m[wave][r16] = m_run;
+        red_l[wave][r16] = l_lane;
+    }
+    __syncthreads();
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, red_m[w][r16]);
+    const float f = m_run == -INFINITY ? 0.f : exp2_fast(m_run - m_all);
+    if (head_ok) {
+#pragma unroll
+        for (int i = 0; i < kDB; ++i)
+            *reinterpret_cast<f32x4_t*>(&shared[(16 * wave + r16) * kOStride + 16 * i + 4 * g4]) = oacc[i] * f;
+    }
+    __syncthreads();
+    for (int e = tid; e < NH * (D / 4); e += NW * 64) {
+        const int h = e / (D / 4), x = 4 * (e % (D / 4));
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, red_m[w][h]);
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) o += *reinterpret_cast<const f32x4_t*>(&shared[(16 * w + h) * kOStride + x]);
+        float L = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
+        const int64_t slot = p.n_k_rows != nullptr ? slot0 + h : slot0 + int64_t(h) * p.splits;
+        if (x == 0) {
+            p.ws_m[slot] = M;
+            p.ws_l[slot] = L;
+        }
+        *reinterpret_cast<f32x4_t*>(&p.ws_o[slot * D + x]) = o;
+    }
+}
+
+template <int D>
+hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
+    // ragged: one workgroup per possible work item (at most p.splits + batch)
+    const bool ragged = p.n_k_rows != nullptr;
+    const dim3 grid(unsigned(ragged ? p.splits + p.batch : p.splits), unsigned(p.h_kv * p.subgroups),
+                    unsigned(ragged ? 1 : p.batch));
+    hipLaunchKernelGGL(decode_q8_kernel<D>, grid, dim3(kWaves * 64), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_decode_merge_q8(p, D, stream);
+}
+
+}  // namespace
+
+hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t stream) {
+    if (p.splits < 1 || p.splits > kDecodeMaxSplits || p.heads_per_block < 1 || p.heads_per_block > 16 ||
+        p.subgroups < 1 || (p.subgroups - 1) * p.heads_per_block >= p.group ||
+        p.subgroups * p.heads_per_block < p.group)
+        return hipErrorInvalidValue;
+    if (p.n_k_rows == nullptr &&
+        (int64_t(p.splits) * p.split_tokens < p.n_valid || p.split_tokens % kDecodeQ8TokenStep != 0))
+        return hipErrorInvalidValue;
+    if (p.n_k_rows != nullptr && (p.q_pos_rows == nullptr || p.ws_plan == nullptr || p.splits > kDecodeMaxSplits - 1))
+        return hipErrorInvalidValue;
+    (void)hipGetLastError();
+    return head_dim == 64 ? launch_d<64>(p, stream) : launch_d<128>(p, stream);
+}
+
+}  // namespace atf
