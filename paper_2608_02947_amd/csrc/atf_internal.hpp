@@ -137,7 +137,10 @@ struct AppendNormedParams {
     int32_t cache_tokens;        // capacity of the contiguous caches
     int32_t scale_tokens;        // cache_tokens rounded up to 16, or page_tokens
     int32_t max_pages, num_pages, page_tokens;
-    int32_t heads_per_wave;      // set by the launcher
+    // set by the launcher: heads of a wave, whether values go with them one token at a time (in
+    // 16-token blocks otherwise), and the waves before those of the blocks
+    int32_t heads_per_wave, value_rows;
+    uint32_t row_waves;
     uint32_t rope_rho_hi[kMaxPairs];
     uint32_t rope_rho_lo[kMaxPairs];
 };
