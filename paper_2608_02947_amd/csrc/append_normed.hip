@@ -249,11 +249,14 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     constexpr int kChunks = D / 16;
     constexpr int kAhead = 4;              // heads loaded before the first is used
     const int lane = threadIdx.x & 63;
-    const uint32_t wave = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (wave >= p.row_waves) {
-        value_blocks<D, kQ8>(p, wave - p.row_waves);
+    uint32_t wave = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // (the blocks of values first: their waves take longest, and would end the call alone)
+    if (blockIdx.x * 4u < p.block_waves) {
+        value_blocks<D, kQ8>(p, wave);
         return;
     }
+    wave -= p.block_waves;
+    if (wave >= p.row_waves) return;
     // this wave's tokens and its heads, all of one kind: queries, keys, values
     const int hpw = p.heads_per_wave;
     const uint32_t q_parts = uint32_t(p.h_q + hpw - 1) / uint32_t(hpw), k_parts = uint32_t(p.h_kv + hpw - 1) / uint32_t(hpw);
@@ -283,13 +286,24 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     float wc[8], ws[8];  // ws with the half's sign: x'_own = own * wc + other * ws
     const float* weight = kind == 0 ? p.q_weight : p.k_weight;
     if (kind != 2) {
+        // the two lanes of a chunk share its 8 angles: half of them each, then both have all
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
             float cs, sn;
-            cos_sin(uint32_t(at.pos), p.rope_rho_hi[8 * c + e], p.rope_rho_lo[8 * c + e], cs, sn);
-            if (hf == 0) sn = -sn;
-            wc[e] = weight != nullptr ? weight[8 * l + e] * cs : cs;
-            ws[e] = weight != nullptr ? weight[8 * (l ^ kChunks) + e] * sn : sn;
+            cos_sin(uint32_t(at.pos), p.rope_rho_hi[8 * c + 4 * hf + e], p.rope_rho_lo[8 * c + 4 * hf + e], cs, sn);
+            const float co = __uint_as_float(other_lane<kLanes>(__float_as_uint(cs)));
+            const float so = __uint_as_float(other_lane<kLanes>(__float_as_uint(sn)));
+            wc[e] = hf ? co : cs;
+            wc[4 + e] = hf ? cs : co;
+            ws[e] = hf ? so : -sn;
+            ws[4 + e] = hf ? sn : -so;
+        }
+        if (weight != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                wc[e] *= weight[8 * l + e];
+                ws[e] *= weight[8 * (l ^ kChunks) + e];
+            }
         }
     }
     const auto turned = [&](u32x4_t v, float* y) __attribute__((always_inline)) {
@@ -382,16 +396,19 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     const int64_t groups = (int64_t(p.batch) * p.n_new + kTokens - 1) / kTokens;
     // one head a wave until the chip is full of waves, then as many as keep it full, so that a
     // token's angles serve them all
-    const int64_t target = 8192;
+    const int64_t target = 4096;
     p.value_rows = p.n_new < 8;
     const int64_t heads = p.h_q + p.h_kv;
     p.heads_per_wave = int32_t(std::min(heads, std::max<int64_t>(1, groups * heads / target)));
     const auto parts = [&](int64_t h) { return (h + p.heads_per_wave - 1) / p.heads_per_wave; };
     const int64_t row_waves = groups * (parts(p.h_q) + (p.value_rows ? 2 : 1) * parts(p.h_kv));
     const int64_t units = int64_t(p.batch) * ((int64_t(p.n_new) + 14) / 16 + 1) * p.h_kv;
-    const int64_t waves = row_waves + (p.value_rows ? 0 : (units + 256 / D - 1) / (256 / D));
+    // whole workgroups of blocks
+    const int64_t block_waves = p.value_rows ? 0 : ((units + 256 / D - 1) / (256 / D) + 3) / 4 * 4;
+    const int64_t waves = row_waves + block_waves;
     if (waves < 1 || waves > 0x7FFFFFFF || units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     p.row_waves = uint32_t(row_waves);
+    p.block_waves = uint32_t(block_waves);
     const dim3 grid(unsigned((waves + 3) / 4));
     (void)hipGetLastError();
     if (p.k_scale != nullptr)
