@@ -19,6 +19,7 @@ namespace atf {
 namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 template <int kCtrl>
@@ -103,6 +104,19 @@ __device__ __forceinline__ uint32_t finite_max(const float* y) {
     return m;
 }
 
+template <bool kStream, typename T>
+__device__ __forceinline__ T load_from(const void* from) {
+    const T* f = static_cast<const T*>(from);
+    return kStream ? __builtin_nontemporal_load(f) : *f;
+}
+template <bool kStream>
+__device__ __forceinline__ void store16(void* to, u32x4_t x) {
+    if constexpr (kStream)
+        __builtin_nontemporal_store(x, static_cast<u32x4_t*>(to));
+    else
+        *static_cast<u32x4_t*>(to) = x;
+}
+
 // A token of the call: its row of the batch, its position, its place in the caches.
 struct Token {
     int64_t entry;  // row of the contiguous caches, or page
@@ -136,7 +150,7 @@ __device__ __forceinline__ Token locate(const AppendNormedParams& p, int b, int 
 // The values of whole 16-token blocks (and of the parts at a row's ends): D / 4 lanes take a
 // block, 4 dims of its 16 tokens each, so that a block is turned to dim-major in the lane's
 // registers and stored 16 bytes at a time.
-template <int D, bool kQ8>
+template <int D, bool kQ8, bool kStream>
 __device__ __forceinline__ void value_blocks(const AppendNormedParams& p, uint32_t wave) {
     constexpr int kLanes = D / 4;
     const int lane = threadIdx.x & 63;
@@ -161,7 +175,10 @@ __device__ __forceinline__ void value_blocks(const AppendNormedParams& p, uint32
     uint2 v[16];
     if (__all(whole)) {
 #pragma unroll
-        for (int t = 0; t < 16; ++t) v[t] = *reinterpret_cast<const uint2*>(src + t * row);
+        for (int t = 0; t < 16; ++t) {
+            const u32x2_t y = load_from<kStream, u32x2_t>(src + t * row);
+            v[t] = make_uint2(y[0], y[1]);
+        }
     } else {
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
@@ -242,17 +259,19 @@ __device__ __forceinline__ void value_blocks(const AppendNormedParams& p, uint32
     }
 }
 
-template <int D, bool kQ8>
+// kStream: the vectors of the call are read and the queries written past the caches, which they
+// would only sweep.
+template <int D, bool kQ8, bool kStream>
 __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedParams p) {
     constexpr int kLanes = D / 8;          // lanes of a vector
     constexpr int kTokens = 64 / kLanes;   // tokens of a wave
     constexpr int kChunks = D / 16;
-    constexpr int kAhead = 4;              // heads loaded before the first is used
+    constexpr int kAhead = 8;              // heads loaded before the first is used
     const int lane = threadIdx.x & 63;
     uint32_t wave = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (the blocks of values first: their waves take longest, and would end the call alone)
     if (blockIdx.x * 4u < p.block_waves) {
-        value_blocks<D, kQ8>(p, wave);
+        value_blocks<D, kQ8, kStream>(p, wave);
         return;
     }
     wave -= p.block_waves;
@@ -276,7 +295,7 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     const auto load = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            x[i] = *reinterpret_cast<const u32x4_t*>(src + int64_t(min(h + i, to - 1)) * D);
+            x[i] = load_from<kStream, u32x4_t>(src + int64_t(min(h + i, to - 1)) * D);
     };
     load(from);
 
@@ -326,7 +345,7 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     const auto query = [&](int h, u32x4_t v) __attribute__((always_inline)) {
         float y[8];
         turned(v, y);
-        if (at.active) *reinterpret_cast<u32x4_t*>(p.q_out + (int64_t(r) * p.h_q + h) * D + 8 * l) = to_bf16(y);
+        if (at.active) store16<kStream>(p.q_out + (int64_t(r) * p.h_q + h) * D + 8 * l, to_bf16(y));
     };
     const auto key = [&](int g, u32x4_t v) __attribute__((always_inline)) {
         float y[8];
@@ -410,12 +429,16 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     p.row_waves = uint32_t(row_waves);
     p.block_waves = uint32_t(block_waves);
     const dim3 grid(unsigned((waves + 3) / 4));
-    (void)hipGetLastError();
+    // queries that the L2s (8 of 4 MB) cannot hold for their reader
+    const bool past = int64_t(p.batch) * p.n_new * p.h_q * D * 2 > (32 << 20);
+    const auto launch = [&](auto kernel) {
+        (void)hipGetLastError();
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p);
+        return hipGetLastError();
+    };
     if (p.k_scale != nullptr)
-        hipLaunchKernelGGL((append_normed_kernel<D, true>), grid, dim3(256), 0, stream, p);
-    else
-        hipLaunchKernelGGL((append_normed_kernel<D, false>), grid, dim3(256), 0, stream, p);
-    return hipGetLastError();
+        return past ? launch(append_normed_kernel<D, true, true>) : launch(append_normed_kernel<D, true, false>);
+    return past ? launch(append_normed_kernel<D, false, true>) : launch(append_normed_kernel<D, false, false>);
 }
 
 }  // namespace
