@@ -1343,11 +1343,14 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
     // the heads of a KV head in workgroups of up to 16, as even as they come
     p.subgroups = (p.group + 15) / 16;
     p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
+    const int64_t cols = int64_t(h_kv) * p.subgroups, target = 768;
     if (n_k_rows != nullptr) {
-        p.splits = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
+        const int64_t room = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
+        p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, target / cols)));
     } else {
         const int64_t steps = (int64_t(p.n_valid) + atf::kDecodeQ8TokenStep - 1) / atf::kDecodeQ8TokenStep;
-        const int64_t s = std::min<int64_t>(atf::decode_splits(batch, h_kv, n_k), steps);
+        const int64_t room = std::min<int64_t>(atf::decode_splits(batch, h_kv, n_k), steps);
+        const int64_t s = std::min(room, std::max<int64_t>(1, target / (cols * batch)));
         const int64_t per = (steps + s - 1) / s;
         p.splits = static_cast<int32_t>((steps + per - 1) / per);
         if (per * atf::kDecodeQ8TokenStep * p.splits >= kPosLimit)

@@ -38,8 +38,9 @@ constexpr int kWaves = 4;
 constexpr int kBlock = 64;             // tokens of a wave's block
 constexpr float kRescale = 8.0f;       // lazy-rescale threshold, log2 units
 
-// what lanes read whose chunk no token keeps, or whose token is past the row's keys
-__device__ const uint32_t g_zeros[64] __attribute__((aligned(256))) = {};
+// what lanes read whose chunk no token keeps, or whose tokens are past the row's keys: as long
+// as the largest offset between a lane's loads
+__device__ const uint32_t g_zeros[512] __attribute__((aligned(256))) = {};
 
 __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
@@ -68,7 +69,7 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ8Params p) {
+__global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
     constexpr int kHalf = D / 2;
     constexpr int kM = D / 64;   // loads of a token: 4 chunks each
@@ -78,8 +79,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
     __shared__ float red_m[NW][16];
     __shared__ float red_l[NW][16];
     __shared__ int s_w[kHalf];
-    // the queries while the waves stream, then the waves' outputs [wave][head][D + 4]
+    // the queries and each wave's copy of them while the waves stream, then the waves' outputs
+    // [wave][head][D + 4]
     constexpr int kMerge = NW * 16 * kOStride;
+    static_assert(kMerge >= 256 * 2 * kM * (1 + NW), "room for the queries");
     __shared__ __attribute__((aligned(16))) float shared[kMerge];
 
     const int tid = threadIdx.x;
@@ -129,17 +132,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
         *reinterpret_cast<u32x4_t*>(&shared[256 * o + 4 * lane]) = z;
     }
     __syncthreads();
+    // this wave's copy of the queries, with the pairs outside q_keep zeroed
+    uint64_t q_keep = ~0ull;
+    float* const qm = &shared[256 * 2 * kM * (1 + wave) + 4 * lane];
+#pragma unroll
+    for (int o = 0; o < 2 * kM; ++o)
+        *reinterpret_cast<u32x4_t*>(qm + 256 * o) = *reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]);
 
     f32x4_t oacc[kDB];
 #pragma unroll
     for (int i = 0; i < kDB; ++i) oacc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, m_thr = -INFINITY, m_neg = 0.f, l_run = 0.f;
     const float sc = p.scale_log2;
-    uint64_t q_keep = 0;
-    u32x4_t qm[2 * kM];  // queries with the pairs outside q_keep zeroed
-#pragma unroll
-    for (int o = 0; o < 2 * kM; ++o) qm[o] = u32x4_t{0u, 0u, 0u, 0u};
-
     const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
     const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
     const uint8_t* const zeros = reinterpret_cast<const uint8_t*>(g_zeros);
@@ -164,24 +168,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
         const uint64_t full = __ballot(my_w >= q_pos - t0);
         const uint64_t keep = __ballot(my_w >= max(0, q_pos - min(t0 + kBlock - 1, t_end - 1)));
 
-        // K operands
+        // K operands (a token past the split's end is the split's last one again)
         u32x4_t kf[4][kM];
         u32x4_t kscale;
         {
             const bool hi = r16 >= 8;
             const int64_t row = hi ? row_b : row_a;
-            const int at = (hi ? at_b : at_a) + (tk & 31);
+            const int at = hi ? at_b : at_a, last = t_end - 1 - t0 - (hi ? 32 : 0);
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
                 const int c = 4 * m + g4;
-                const bool kept = (keep >> (8 * c)) & 0xFFull;
-                const uint8_t* src = keys + ((row * kChunks + c) * cap + at) * 16;
+                const bool kept = last >= 0 && ((keep >> (8 * c)) & 0xFFull) != 0;
+                const uint8_t* src = kept ? keys + ((row * kChunks + c) * cap + at) * 16 : zeros;
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
-                    kf[s][m] = *reinterpret_cast<const u32x4_t*>(kept && t0 + tk + 4 * s < t_end ? src + 64 * s : zeros);
+                    kf[s][m] = *reinterpret_cast<const u32x4_t*>(src + 16 * uint32_t(max(min((tk & 31) + 4 * s, last), 0)));
             }
-            const uint8_t* src = p.k_scale + row * p.scale_tokens + (at & ~15);
-            kscale = *reinterpret_cast<const u32x4_t*>(t0 + (tk & ~15) < t_end ? src : zeros);
+            const uint8_t* src = p.k_scale + row * p.scale_tokens + at + (tk & 16);
+            kscale = *reinterpret_cast<const u32x4_t*>(last >= (tk & 16) ? src : zeros);
         }
         // V^T operands
         u32x4_t vf[kDB], vscale;
@@ -190,9 +194,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
             const int64_t row = hi ? row_b : row_a;
             const int at = (hi ? at_b : at_a) + 16 * (g4 & 1);
             const bool in = t0 + 16 * g4 < t_end;
-            const uint8_t* src = values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16;
+            const uint8_t* src = in ? values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16 : zeros;
 #pragma unroll
-            for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(in ? src + 256 * i : zeros);
+            for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(src + 256 * i);
             vscale = *reinterpret_cast<const u32x4_t*>(in ? p.v_scale + row * p.scale_tokens + at : zeros);
         }
 
@@ -220,8 +224,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
             q_keep = keep;
 #pragma unroll
             for (int o = 0; o < 2 * kM; ++o)
-                qm[o] = keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
-                                   uint32_t(keep >> (8 * (4 * (o >> 1) + g4))) & 0xFFu);
+                *reinterpret_cast<u32x4_t*>(qm + 256 * o) =
+                    keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
+                               uint32_t(keep >> (8 * (4 * (o >> 1) + g4))) & 0xFFu);
         }
         f32x4_t sacc[4];
 #pragma unroll
@@ -230,8 +235,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_q8_kernel(const DecodeQ
             sacc[s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
-                sacc[s] = mfma16(widen(kf[s][m][0], kf[s][m][1], power), qm[2 * m], sacc[s]);
-                sacc[s] = mfma16(widen(kf[s][m][2], kf[s][m][3], power), qm[2 * m + 1], sacc[s]);
+                const u32x4_t* q = reinterpret_cast<const u32x4_t*>(qm + 512 * m);
+                sacc[s] = mfma16(widen(kf[s][m][0], kf[s][m][1], power), q[0], sacc[s]);
+                sacc[s] = mfma16(widen(kf[s][m][2], kf[s][m][3], power), q[64], sacc[s]);
             }
         }
         // tokens past the split's end: no probability, and no value that is not a number
