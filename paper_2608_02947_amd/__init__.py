@@ -739,61 +739,105 @@ def qscale_shape(batch: int, cache_tokens: int, h_kv: int):
     return (batch, h_kv, (cache_tokens + 15) // 16 * 16)
 
 
-def _opt_ptr(t, dtype, name, shape):
-    if t is None:
-        return None
+class _Types:
+    """torch's types and queries that every call below asks for, looked up once."""
+
+    def __init__(self):
+        torch = _torch()
+        self.bf16, self.f32, self.i32, self.u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        self.e4m3, self.e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+        self.device = torch.cuda.current_device
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+_types: Optional[_Types] = None
+
+
+def _call():
+    """(types, current device, stream handle of it) of a call."""
+    global _types
+    if _types is None:
+        _types = _Types()
+    ty = _types
+    if not _torch().cuda.is_initialized():  # no GPU, or none used yet: the tensors will tell
+        return ty, -1, None
+    dev = ty.device()
+    return ty, dev, ty.raw_stream(dev) if ty.raw_stream is not None else _stream_ptr(None)
+
+
+def _ptr(t, dtype, dev, name):
+    """Device pointer of a contiguous tensor of this type on device `dev`."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev and dev >= 0 and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     p = _dev_ptr(t, dtype, name)
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.get_device() != _torch().cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
     return p
 
 
-def _new_heads(fn, q, k_new, v_new, q_out, window, q_weight, k_weight, pos_rows):
-    """The arguments every append with norms shares: (pointers of q, k_new, v_new, q_out;
-    pointers of pos_rows and the weights; B, n_new, h_q, h_kv, d)."""
-    torch = _torch()
-    bf, f32 = torch.bfloat16, torch.float32
-    B, n_new, h_kv, d = k_new.shape
-    if v_new.shape != k_new.shape or window.head_dim != d:
+def _vector(t, dtype, dev, name, n):
+    """Pointer of an optional tensor [n]."""
+    if t is None:
+        return None
+    if t.shape != (n,):
+        raise ValueError(f"{name} must be [{n}], got {list(t.shape)}")
+    return _ptr(t, dtype, dev, name)
+
+
+def _new_heads(fn, ty, dev, q, k_new, v_new, q_out, window, q_weight, k_weight, pos_rows):
+    """The arguments every append with norms shares: (pointers of q, k_new, v_new, q_out),
+    (pointers of pos_rows and the weights), B, n_new, h_q, h_kv, d."""
+    shape = k_new.shape
+    B, n_new, h_kv, d = shape
+    if v_new.shape != shape or window.head_dim != d:
         raise ValueError(f"{fn}: inconsistent shapes")
     if (q is None) != (q_out is None):
         raise ValueError(f"{fn}: q and q_out must be given together")
-    h_q = 0
+    h_q, qp, qop = 0, None, None
     if q is not None:
-        if q.dim() != 4 or q.shape[:2] != k_new.shape[:2] or q.shape[3] != d or q_out.shape != q.shape:
+        qs = q.shape
+        if len(qs) != 4 or qs[0] != B or qs[1] != n_new or qs[3] != d or q_out.shape != qs:
             raise ValueError(f"{fn}: inconsistent shapes")
-        h_q = q.shape[2]
-    ptrs = (None if q is None else _dev_ptr(q, bf, "q"), _dev_ptr(k_new, bf, "k_new"),
-            _dev_ptr(v_new, bf, "v_new"), None if q is None else _dev_ptr(q_out, bf, "q_out"))
-    return (ptrs, _opt_ptr(pos_rows, torch.int32, "pos_rows", (B,)),
-            _opt_ptr(q_weight, f32, "q_weight", (d,)), _opt_ptr(k_weight, f32, "k_weight", (d,)),
-            B, n_new, h_q, h_kv, d)
+        h_q = qs[2]
+        qp = _ptr(q, ty.bf16, dev, "q")
+        qop = qp if q_out is q else _ptr(q_out, ty.bf16, dev, "q_out")
+    return ((qp, _ptr(k_new, ty.bf16, dev, "k_new"), _ptr(v_new, ty.bf16, dev, "v_new"), qop),
+            (_vector(pos_rows, ty.i32, dev, "pos_rows", B), _vector(q_weight, ty.f32, dev, "q_weight", d),
+             _vector(k_weight, ty.f32, dev, "k_weight", d)), B, n_new, h_q, h_kv, d)
 
 
-def _q8_ptrs(fn, k, k_scale, v, v_scale, scale_shape):
-    torch = _torch()
-    if tuple(k_scale.shape) != scale_shape or tuple(v_scale.shape) != scale_shape:
-        raise ValueError(f"{fn}: scales must be {list(scale_shape)} (see qscale_shape)")
-    e4, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
-    return (_dev_ptr(k, e4, "k"), _dev_ptr(k_scale, e8, "k_scale"), _dev_ptr(v, e4, "v"),
-            _dev_ptr(v_scale, e8, "v_scale"))
+def _q8_ptrs(fn, ty, dev, k, k_scale, v, v_scale, lead, tokens, h_kv):
+    shape = (lead, h_kv, (tokens + 15) // 16 * 16)
+    if k_scale.shape != shape or v_scale.shape != shape:
+        raise ValueError(f"{fn}: scales must be {list(shape)} (see qscale_shape)")
+    return (_ptr(k, ty.e4m3, dev, "k"), _ptr(k_scale, ty.e8m0, dev, "k_scale"), _ptr(v, ty.e4m3, dev, "v"),
+            _ptr(v_scale, ty.e8m0, dev, "v_scale"))
 
 
 def _caches(fn, k_cache, v_cache, B, h_kv, d):
     """Token capacity of a pair of contiguous caches of these sizes."""
-    if k_cache.dim() != 5:
+    ks = k_cache.shape
+    if len(ks) != 5:
         raise ValueError(f"{fn}: the K cache must be [B, h_kv, d/16, C, 16]")
-    cap = k_cache.shape[3]
-    if k_cache.shape != kcache_shape(B, cap, h_kv, d) or v_cache.shape != vcache_shape(B, cap, h_kv, d):
+    cap = ks[3]
+    if ks != (B, h_kv, d // 16, cap, 16) or v_cache.shape != (B, h_kv, (cap + 15) // 16, d, 16):
         raise ValueError(f"{fn}: inconsistent shapes")
     return cap
 
 
-def _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d):
-    num_pages, hk, pt, dd = _pages(k_pages, v_pages, fn)
-    if hk != h_kv or dd != d or block_table.dim() != 2 or block_table.shape[0] != B:
+def _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d):
+    """(table pointer, pages of a row, pages, tokens of a page) of page pools of these sizes."""
+    ks, ts = k_pages.shape, block_table.shape
+    if len(ks) != 5:
+        raise ValueError(f"{fn}: page pools must be 5-d (see kpages_shape, vpages_shape)")
+    pages, tokens = ks[0], ks[3]
+    if ks != (pages, h_kv, d // 16, tokens, 16) or v_pages.shape != (pages, h_kv, tokens // 16, d, 16) or \
+            len(ts) != 2 or ts[0] != B:
         raise ValueError(f"{fn}: inconsistent shapes")
-    return num_pages, pt, _dev_ptr(block_table, _torch().int32, "block_table")
+    return _ptr(block_table, ty.i32, dev, "block_table"), ts[1], pages, tokens
 
 
 def atf_cache_append_normed(q, k_new, v_new, q_out, k_cache, v_cache, pos0: int, window: Window,
@@ -804,16 +848,16 @@ def atf_cache_append_normed(q, k_new, v_new, q_out, k_cache, v_cache, pos0: int,
     of atf_cache_append, at positions pos0 .., or pos_rows[b] .. of each row (int32 device
     tensor [B], negative: an idle row; pos0 is 0 then)."""
     fn = "atf_cache_append_normed"
-    torch = _torch()
-    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
-                                                            k_weight, pos_rows)
+    ty, dev, st = _call()
+    new, rows, B, n_new, h_q, h_kv, d = _new_heads(fn, ty, dev, q, k_new, v_new, q_out, window, q_weight,
+                                                   k_weight, pos_rows)
     cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
     cw, keep = window.as_c()
     fp, keep2 = _rope_freq(rope_inv_freq, d)
     _check(_lib.atf_cache_append_normed(
-        *ptrs, _dev_ptr(k_cache, torch.bfloat16, "k_cache"), _dev_ptr(v_cache, torch.bfloat16, "v_cache"),
-        B, n_new, int(pos0), rows, h_q, h_kv, cap, ctypes.byref(cw), fp, qw, kw, float(eps),
-        _stream_ptr(stream)))
+        *new, _ptr(k_cache, ty.bf16, dev, "k_cache"), _ptr(v_cache, ty.bf16, dev, "v_cache"), B, n_new,
+        int(pos0), rows[0], h_q, h_kv, cap, cw, fp, rows[1], rows[2], eps,
+        st if stream is None else stream.cuda_stream))
 
 
 def atf_cache_append_paged_normed(q, k_new, v_new, q_out, k_pages, v_pages, block_table, pos0: int,
@@ -821,16 +865,16 @@ def atf_cache_append_paged_normed(q, k_new, v_new, q_out, k_pages, v_pages, bloc
                                   pos_rows=None, rope_inv_freq=None, stream=None):
     """atf_cache_append_normed into the pages block_table [B, max_pages] (int32, device) names."""
     fn = "atf_cache_append_paged_normed"
-    torch = _torch()
-    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
-                                                            k_weight, pos_rows)
-    num_pages, pt, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
+    ty, dev, st = _call()
+    new, rows, B, n_new, h_q, h_kv, d = _new_heads(fn, ty, dev, q, k_new, v_new, q_out, window, q_weight,
+                                                   k_weight, pos_rows)
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d)
     cw, keep = window.as_c()
     fp, keep2 = _rope_freq(rope_inv_freq, d)
     _check(_lib.atf_cache_append_paged_normed(
-        *ptrs, _dev_ptr(k_pages, torch.bfloat16, "k_pages"), _dev_ptr(v_pages, torch.bfloat16, "v_pages"),
-        table, block_table.shape[1], num_pages, pt, B, n_new, int(pos0), rows, h_q, h_kv,
-        ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+        *new, _ptr(k_pages, ty.bf16, dev, "k_pages"), _ptr(v_pages, ty.bf16, dev, "v_pages"), *pools, B,
+        n_new, int(pos0), rows[0], h_q, h_kv, cw, fp, rows[1], rows[2], eps,
+        st if stream is None else stream.cuda_stream))
 
 
 def atf_cache_append_q8(q, k_new, v_new, q_out, k_cache, k_scale, v_cache, v_scale, pos0: int,
@@ -839,14 +883,15 @@ def atf_cache_append_q8(q, k_new, v_new, q_out, k_cache, k_scale, v_cache, v_sca
     """atf_cache_append_normed into 8-bit caches: k_cache and v_cache torch.float8_e4m3fn of
     kcache_shape and vcache_shape, k_scale and v_scale torch.float8_e8m0fnu of qscale_shape."""
     fn = "atf_cache_append_q8"
-    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
-                                                            k_weight, pos_rows)
+    ty, dev, st = _call()
+    new, rows, B, n_new, h_q, h_kv, d = _new_heads(fn, ty, dev, q, k_new, v_new, q_out, window, q_weight,
+                                                   k_weight, pos_rows)
     cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
+    cache = _q8_ptrs(fn, ty, dev, k_cache, k_scale, v_cache, v_scale, B, cap, h_kv)
     cw, keep = window.as_c()
     fp, keep2 = _rope_freq(rope_inv_freq, d)
-    _check(_lib.atf_cache_append_q8(*ptrs, *cache, B, n_new, int(pos0), rows, h_q, h_kv, cap,
-                                    ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+    _check(_lib.atf_cache_append_q8(*new, *cache, B, n_new, int(pos0), rows[0], h_q, h_kv, cap, cw, fp,
+                                    rows[1], rows[2], eps, st if stream is None else stream.cuda_stream))
 
 
 def atf_cache_append_paged_q8(q, k_new, v_new, q_out, k_pages, k_scale, v_pages, v_scale, block_table,
@@ -854,15 +899,16 @@ def atf_cache_append_paged_q8(q, k_new, v_new, q_out, k_pages, k_scale, v_pages,
                               eps: float = 1e-6, pos_rows=None, rope_inv_freq=None, stream=None):
     """atf_cache_append_q8 into the pages block_table [B, max_pages] (int32, device) names."""
     fn = "atf_cache_append_paged_q8"
-    ptrs, rows, qw, kw, B, n_new, h_q, h_kv, d = _new_heads(fn, q, k_new, v_new, q_out, window, q_weight,
-                                                            k_weight, pos_rows)
-    num_pages, pt, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
+    ty, dev, st = _call()
+    new, rows, B, n_new, h_q, h_kv, d = _new_heads(fn, ty, dev, q, k_new, v_new, q_out, window, q_weight,
+                                                   k_weight, pos_rows)
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, ty, dev, k_pages, k_scale, v_pages, v_scale, pools[2], pools[3], h_kv)
     cw, keep = window.as_c()
     fp, keep2 = _rope_freq(rope_inv_freq, d)
-    _check(_lib.atf_cache_append_paged_q8(
-        *ptrs, *cache, table, block_table.shape[1], num_pages, pt, B, n_new, int(pos0), rows, h_q, h_kv,
-        ctypes.byref(cw), fp, qw, kw, float(eps), _stream_ptr(stream)))
+    _check(_lib.atf_cache_append_paged_q8(*new, *cache, *pools, B, n_new, int(pos0), rows[0], h_q, h_kv, cw,
+                                          fp, rows[1], rows[2], eps,
+                                          st if stream is None else stream.cuda_stream))
 
 
 def atf_cache_read_q8(k_q8, k_scale, v_q8, v_scale, k_cache, v_cache, n_k: int, pos0: int = 0,
@@ -870,91 +916,95 @@ def atf_cache_read_q8(k_q8, k_scale, v_q8, v_scale, k_cache, v_cache, n_k: int, 
     """Positions pos0 .. pos0 + n_k - 1 of 8-bit caches -> the same positions of bf16 caches (of
     any capacity that holds them), exactly."""
     fn = "atf_cache_read_q8"
-    torch = _torch()
-    B, h_kv = k_q8.shape[:2]
-    d = 16 * k_q8.shape[2]
+    ty, dev, st = _call()
+    B, h_kv, nc = k_q8.shape[:3]
+    d = 16 * nc
     cap = _caches(fn, k_q8, v_q8, B, h_kv, d)
     out = _caches(fn, k_cache, v_cache, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_q8, k_scale, v_q8, v_scale, qscale_shape(B, cap, h_kv))
+    cache = _q8_ptrs(fn, ty, dev, k_q8, k_scale, v_q8, v_scale, B, cap, h_kv)
     _check(_lib.atf_cache_read_q8(
-        *cache, _dev_ptr(k_cache, torch.bfloat16, "k_cache"), _dev_ptr(v_cache, torch.bfloat16, "v_cache"),
-        B, int(n_k), int(pos0), h_kv, d, cap, out, _stream_ptr(stream)))
+        *cache, _ptr(k_cache, ty.bf16, dev, "k_cache"), _ptr(v_cache, ty.bf16, dev, "v_cache"), B, int(n_k),
+        int(pos0), h_kv, d, cap, out, st if stream is None else stream.cuda_stream))
 
 
 def atf_cache_read_paged_q8(k_pages, k_scale, v_pages, v_scale, block_table, k_cache, v_cache, n_k: int,
                             pos0: int = 0, stream=None):
     """atf_cache_read_q8 from the pages block_table [B, max_pages] names, into contiguous caches."""
     fn = "atf_cache_read_paged_q8"
-    torch = _torch()
-    num_pages, h_kv, pt, d = _pages(k_pages, v_pages, fn)
-    B = k_cache.shape[0]
+    ty, dev, st = _call()
+    B, h_kv, nc = k_cache.shape[:3]
+    d = 16 * nc
     out = _caches(fn, k_cache, v_cache, B, h_kv, d)
-    _, _, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, ty, dev, k_pages, k_scale, v_pages, v_scale, pools[2], pools[3], h_kv)
     _check(_lib.atf_cache_read_paged_q8(
-        *cache, table, block_table.shape[1], num_pages, pt, _dev_ptr(k_cache, torch.bfloat16, "k_cache"),
-        _dev_ptr(v_cache, torch.bfloat16, "v_cache"), B, int(n_k), int(pos0), h_kv, d, out,
-        _stream_ptr(stream)))
+        *cache, *pools, _ptr(k_cache, ty.bf16, dev, "k_cache"), _ptr(v_cache, ty.bf16, dev, "v_cache"), B,
+        int(n_k), int(pos0), h_kv, d, out, st if stream is None else stream.cuda_stream))
 
 
-def _decode_out(fn, q, o, lse, workspace):
-    torch = _torch()
-    B, h_q, d = q.shape
-    if o.shape != q.shape or lse.shape != (B, h_q):
+def _decode_shapes(fn, q, o, lse):
+    qs = q.shape
+    B, h_q, d = qs
+    if o.shape != qs or lse.shape != (B, h_q):
         raise ValueError(f"{fn}: inconsistent shapes")
-    return ((_dev_ptr(o, torch.bfloat16, "o"), _dev_ptr(lse, torch.float32, "lse")),
-            (_dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()), B, h_q, d)
+    return B, h_q, d
 
 
-def _decode_rows(fn, n_k_rows, q_pos_rows, B):
-    torch = _torch()
+def _decode_out(ty, dev, o, lse):
+    return _ptr(o, ty.bf16, dev, "o"), _ptr(lse, ty.f32, dev, "lse")
+
+
+def _decode_rows(fn, ty, dev, n_k_rows, q_pos_rows, B):
     if n_k_rows.shape != (B,) or q_pos_rows.shape != (B,):
         raise ValueError(f"{fn}: inconsistent shapes")
-    return _dev_ptr(n_k_rows, torch.int32, "n_k_rows"), _dev_ptr(q_pos_rows, torch.int32, "q_pos_rows")
+    return _ptr(n_k_rows, ty.i32, dev, "n_k_rows"), _ptr(q_pos_rows, ty.i32, dev, "q_pos_rows")
 
 
 def atf_decode_q8(q, k_cache, k_scale, v_cache, v_scale, o, lse, q_pos: int, window: Window, workspace,
                   softmax_scale: float = 0.0, stream=None, n_k: Optional[int] = None):
     """atf_decode over 8-bit caches (atf_cache_append_q8); the other arguments as there."""
     fn = "atf_decode_q8"
-    torch = _torch()
-    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
+    ty, dev, st = _call()
+    B, h_q, d = _decode_shapes(fn, q, o, lse)
     h_kv = k_cache.shape[1]
     cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
+    cache = _q8_ptrs(fn, ty, dev, k_cache, k_scale, v_cache, v_scale, B, cap, h_kv)
     cw, keep = window.as_c()
-    _check(_lib.atf_decode_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B,
-                              cap if n_k is None else int(n_k), int(q_pos), h_q, h_kv, cap,
-                              ctypes.byref(cw), float(softmax_scale), *ws, _stream_ptr(stream)))
+    _check(_lib.atf_decode_q8(_ptr(q, ty.bf16, dev, "q"), *cache, *_decode_out(ty, dev, o, lse), B,
+                              cap if n_k is None else int(n_k), int(q_pos), h_q, h_kv, cap, cw,
+                              softmax_scale, _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
+                              st if stream is None else stream.cuda_stream))
 
 
 def atf_decode_ragged_q8(q, k_cache, k_scale, v_cache, v_scale, o, lse, n_k_rows, q_pos_rows,
                          max_n_k: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
     """atf_decode_ragged over 8-bit caches."""
     fn = "atf_decode_ragged_q8"
-    torch = _torch()
-    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
+    ty, dev, st = _call()
+    B, h_q, d = _decode_shapes(fn, q, o, lse)
     h_kv = k_cache.shape[1]
     cap = _caches(fn, k_cache, v_cache, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_cache, k_scale, v_cache, v_scale, qscale_shape(B, cap, h_kv))
-    rows = _decode_rows(fn, n_k_rows, q_pos_rows, B)
+    cache = _q8_ptrs(fn, ty, dev, k_cache, k_scale, v_cache, v_scale, B, cap, h_kv)
+    rows = _decode_rows(fn, ty, dev, n_k_rows, q_pos_rows, B)
     cw, keep = window.as_c()
-    _check(_lib.atf_decode_ragged_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B, *rows, int(max_n_k),
-                                     h_q, h_kv, cap, ctypes.byref(cw), float(softmax_scale), *ws,
-                                     _stream_ptr(stream)))
+    _check(_lib.atf_decode_ragged_q8(_ptr(q, ty.bf16, dev, "q"), *cache, *_decode_out(ty, dev, o, lse), B,
+                                     *rows, int(max_n_k), h_q, h_kv, cap, cw, softmax_scale,
+                                     _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
+                                     st if stream is None else stream.cuda_stream))
 
 
 def atf_decode_paged_q8(q, k_pages, k_scale, v_pages, v_scale, o, lse, block_table, n_k_rows, q_pos_rows,
                         max_n_k: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
     """atf_decode_paged over 8-bit pages."""
     fn = "atf_decode_paged_q8"
-    torch = _torch()
-    out, ws, B, h_q, d = _decode_out(fn, q, o, lse, workspace)
-    num_pages, h_kv, pt, _ = _pages(k_pages, v_pages, fn)
-    _, _, table = _page_pools(fn, k_pages, v_pages, block_table, B, h_kv, d)
-    cache = _q8_ptrs(fn, k_pages, k_scale, v_pages, v_scale, qscale_shape(num_pages, pt, h_kv))
-    rows = _decode_rows(fn, n_k_rows, q_pos_rows, B)
+    ty, dev, st = _call()
+    B, h_q, d = _decode_shapes(fn, q, o, lse)
+    h_kv = k_pages.shape[1]
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d)
+    cache = _q8_ptrs(fn, ty, dev, k_pages, k_scale, v_pages, v_scale, pools[2], pools[3], h_kv)
+    rows = _decode_rows(fn, ty, dev, n_k_rows, q_pos_rows, B)
     cw, keep = window.as_c()
-    _check(_lib.atf_decode_paged_q8(_dev_ptr(q, torch.bfloat16, "q"), *cache, *out, B, table,
-                                    block_table.shape[1], num_pages, pt, *rows, int(max_n_k), h_q, h_kv,
-                                    ctypes.byref(cw), float(softmax_scale), *ws, _stream_ptr(stream)))
+    _check(_lib.atf_decode_paged_q8(_ptr(q, ty.bf16, dev, "q"), *cache, *_decode_out(ty, dev, o, lse), B,
+                                    *pools, *rows, int(max_n_k), h_q, h_kv, cw, softmax_scale,
+                                    _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
+                                    st if stream is None else stream.cuda_stream))
