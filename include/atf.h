@@ -550,7 +550,7 @@ int atf_cache_read_paged_q8(const void *k_pages, const void *k_scale, const void
  * (atf_decode_workspace_bytes of the same arguments); power bytes must be 1 .. 254.  A row whose
  * scores are NaN (a key that was not finite) gives NaN.
  * Errors: as those, plus ATF_EINVAL for NULL or misaligned scales.  Any group size is built:
- * up to 16 query heads of a KV head share a workgroup.  Deterministic: equal inputs give equal bits. */
+ * up to 32 query heads of a KV head share a workgroup.  Deterministic: equal inputs give equal bits. */
 int atf_decode_q8(const void *q, const void *k_cache, const void *k_scale, const void *v_cache,
                   const void *v_scale, void *o, float *lse, int32_t batch, int64_t n_k,
                   int64_t q_pos, int32_t h_q, int32_t h_kv, int64_t cache_tokens,

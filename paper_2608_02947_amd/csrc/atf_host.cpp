@@ -1340,11 +1340,14 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
     p.k_scale = static_cast<const uint8_t*>(k_scale);
     p.v_scale = static_cast<const uint8_t*>(v_scale);
     p.scale_tokens = pg.block_table != nullptr ? pg.page_tokens : scale_tokens(p.cache_tokens);
-    // the heads of a KV head in workgroups of up to 16, as even as they come
-    p.subgroups = (p.group + 15) / 16;
+    // the heads of a KV head in workgroups of up to 32, as even as they come
+    p.subgroups = (p.group + 31) / 32;
     p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
     const int64_t cols = int64_t(h_kv) * p.subgroups, target = 768;
-    if (n_k_rows != nullptr) {
+    p.direct = 0;
+    if (p.direct) {
+        p.splits = 1;
+    } else if (n_k_rows != nullptr) {
         const int64_t room = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
         p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, target / cols)));
     } else {

@@ -107,7 +107,7 @@ struct AppendRotParams : AppendParams {
 };
 
 // Decode over 8-bit caches (decode_q8.hip): kpcm and vpk hold e4m3 bytes in the layouts of
-// q8.hpp's caches, with a power-of-two byte per token.  heads_per_block is at most 16 and need
+// q8.hpp's caches, with a power-of-two byte per token.  heads_per_block is at most 32 and need
 // not divide the group: the last of the `subgroups` workgroups of a KV head takes what is left.
 struct DecodeQ8Params : DecodeParams {
     const uint8_t* k_scale;   // [B][h_kv][scale_tokens], or pages [num_pages][h_kv][page_tokens]

@@ -7,8 +7,8 @@
 //   V [B][h_kv][ceil(cache_tokens/16)][d][16]: 16-token blocks, dim-major, tokens in order; a
 //     power per token, v_scale
 //
-// The heads of one KV head (up to 16 a workgroup) are the columns of v_mfma_f32_16x16x32_bf16,
-// a wave's block is 64 tokens, and every load of K and V is 16 bytes a lane.  With r = lane % 16,
+// The heads of one KV head (up to 32 a workgroup) are the columns of v_mfma_f32_16x16x32_bf16, in
+// one or two tiles, a wave's block is 64 tokens, and every load of K and V is 16 bytes a lane.  With r = lane % 16,
 // g = lane / 16:
 //   scores, tile s = 0 .. 3: A row r is token 16 (r / 4) + 4 s + r % 4, the lane's 16 bytes chunk
 //     4 m + g of it: its two halves are two operands of 8 dims, for two products.  The result
@@ -35,6 +35,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
+constexpr int kDirectWaves = 8;        // of a workgroup that takes a whole row
 constexpr int kBlock = 64;             // tokens of a wave's block
 constexpr float kRescale = 8.0f;       // lazy-rescale threshold, log2 units
 
@@ -68,22 +69,23 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
     return r;
 }
 
-template <int D>
-__global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kernel(const DecodeQ8Params p) {
+// NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4 where rows are split,
+// kDirectWaves where a workgroup takes a whole row and writes its output (p.direct).
+template <int D, int NT, int NW>
+__global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ? 3 : 4)) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
     constexpr int kHalf = D / 2;
     constexpr int kM = D / 64;   // loads of a token: 4 chunks each
     constexpr int kDB = D / 16;  // 16-dim blocks of the output
+    constexpr int kOps = 2 * kM * NT;  // operands of the queries
     constexpr int kOStride = D + 4;
-    constexpr int NW = kWaves;
-    __shared__ float red_m[NW][16];
-    __shared__ float red_l[NW][16];
+    __shared__ float red_m[NW][16 * NT];
+    __shared__ float red_l[NW][16 * NT];
     __shared__ int s_w[kHalf];
-    // the queries and each wave's copy of them while the waves stream, then the waves' outputs
-    // [wave][head][D + 4]
-    constexpr int kMerge = NW * 16 * kOStride;
-    static_assert(kMerge >= 256 * 2 * kM * (1 + NW), "room for the queries");
-    __shared__ __attribute__((aligned(16))) float shared[kMerge];
+    // the queries and each wave's copy of them while the waves stream, then, a tile at a time, the
+    // waves' outputs [wave][head][D + 4]
+    constexpr int kQueries = 256 * kOps * (1 + NW), kMerge = NW * 16 * kOStride;
+    __shared__ __attribute__((aligned(16))) float shared[kQueries > kMerge ? kQueries : kMerge];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -96,11 +98,19 @@ __global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kerne
     const int sub = blockIdx.y % subgroups;
     const int hq0 = g * p.group + sub * p.heads_per_block;
     const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
-    const bool head_ok = r16 < NH;
 
     int b, n_k = p.n_k, q_pos = p.q_pos, n_valid = p.n_valid, t_begin, t_end;
     int64_t slot0 = 0;
-    if (p.n_k_rows != nullptr) {
+    if (p.direct) {
+        b = blockIdx.x;
+        if (p.n_k_rows != nullptr) {
+            n_k = min(max(p.n_k_rows[b], 0), p.n_k);
+            q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
+            n_valid = min(n_k, q_pos + 1);
+        }
+        t_begin = 0;
+        t_end = n_valid;
+    } else if (p.n_k_rows != nullptr) {
         int64_t span;
         int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
         b = ragged_item(p, split, kDecodeQ8TokenStep, t_begin, span, plan);
@@ -123,26 +133,32 @@ __global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kerne
     const int my_w = lane < kHalf ? p.win.W[lane] : -1;
     if (tid < kHalf) s_w[tid] = p.win.W[tid];
 
-    // queries: operand (m, half) at 256 (2 m + half) + 4 lane
-    for (int o = wave; o < 2 * kM; o += NW) {
+    // queries: operand (tile, m, half) at 256 (2 kM tile + 2 m + half) + 4 lane
+    for (int o = wave; o < kOps; o += NW) {
+        const int h = 16 * (o / (2 * kM)) + r16, m = o / 2 % kM;
         u32x4_t z = {0u, 0u, 0u, 0u};
-        if (head_ok)
-            z = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(b) * p.h_q + hq0 + r16) * D + (o & 1) * kHalf +
-                                                  8 * (4 * (o >> 1) + g4));
+        if (h < NH)
+            z = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(b) * p.h_q + hq0 + h) * D + (o & 1) * kHalf +
+                                                  8 * (4 * m + g4));
         *reinterpret_cast<u32x4_t*>(&shared[256 * o + 4 * lane]) = z;
     }
     __syncthreads();
     // this wave's copy of the queries, with the pairs outside q_keep zeroed
     uint64_t q_keep = ~0ull;
-    float* const qm = &shared[256 * 2 * kM * (1 + wave) + 4 * lane];
+    float* const qm = &shared[256 * kOps * (1 + wave) + 4 * lane];
 #pragma unroll
-    for (int o = 0; o < 2 * kM; ++o)
+    for (int o = 0; o < kOps; ++o)
         *reinterpret_cast<u32x4_t*>(qm + 256 * o) = *reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]);
 
-    f32x4_t oacc[kDB];
+    f32x4_t oacc[NT][kDB];
+    float m_run[NT], m_thr[NT], m_neg[NT], l_run[NT];
 #pragma unroll
-    for (int i = 0; i < kDB; ++i) oacc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, m_thr = -INFINITY, m_neg = 0.f, l_run = 0.f;
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < kDB; ++i) oacc[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m_run[n] = m_thr[n] = -INFINITY;
+        m_neg[n] = l_run[n] = 0.f;
+    }
     const float sc = p.scale_log2;
     const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
     const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
@@ -223,21 +239,24 @@ __global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kerne
         if (keep != q_keep) {
             q_keep = keep;
 #pragma unroll
-            for (int o = 0; o < 2 * kM; ++o)
+            for (int o = 0; o < kOps; ++o)
                 *reinterpret_cast<u32x4_t*>(qm + 256 * o) =
                     keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
-                               uint32_t(keep >> (8 * (4 * (o >> 1) + g4))) & 0xFFu);
+                               uint32_t(keep >> (8 * (4 * (o / 2 % kM) + g4))) & 0xFFu);
         }
-        f32x4_t sacc[4];
+        f32x4_t sacc[NT][4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const float power = q8::power((kscale[s] >> (8 * (r16 & 3))) & 255u);
-            sacc[s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
-                const u32x4_t* q = reinterpret_cast<const u32x4_t*>(qm + 512 * m);
-                sacc[s] = mfma16(widen(kf[s][m][0], kf[s][m][1], power), q[0], sacc[s]);
-                sacc[s] = mfma16(widen(kf[s][m][2], kf[s][m][3], power), q[64], sacc[s]);
+                const u32x4_t k0 = widen(kf[s][m][0], kf[s][m][1], power), k1 = widen(kf[s][m][2], kf[s][m][3], power);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(qm + 256 * (2 * kM * n + 2 * m));
+                    sacc[n][s] = mfma16(k0, q[0], m == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sacc[n][s]);
+                    sacc[n][s] = mfma16(k1, q[64], sacc[n][s]);
+                }
             }
         }
         // tokens past the split's end: no probability, and no value that is not a number
@@ -248,7 +267,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kerne
                 uint32_t msk = 0;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    if (4 * s + v >= bound) sacc[s][v] = -INFINITY;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        if (4 * s + v >= bound) sacc[n][s][v] = -INFINITY;
                     msk |= 4 * s + v < bound ? 0xFFu << (8 * v) : 0u;
                 }
                 vscale[s] &= msk;
@@ -256,106 +277,139 @@ __global__ __launch_bounds__(kWaves * 64, D == 128 ? 3 : 4) void decode_q8_kerne
                 for (int i = 0; i < kDB; ++i) vf[i][s] &= msk;
             }
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sacc[s][v]);
-        if (__any(mx * sc > m_thr)) {
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(m_run, mx * sc);
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float alpha = exp2_fast(m_run - m_use);
-            m_run = m_new;
-            m_thr = m_new + kRescale;
-            m_neg = -m_use;
-            l_run *= alpha;
-#pragma unroll
-            for (int i = 0; i < kDB; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) oacc[i][v] *= alpha;
-        }
         // P times the values' powers as two bf16 numbers, what fits and what is left over: one
         // would round every probability to 2^-9, and the output's own rounding is that size
-        u32x4_t ph[2], pl[2];
+        u32x4_t ph[NT][2], pl[NT][2];
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int n = 0; n < NT; ++n) {
+            float mx = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float x[2];
-                uint32_t h[2];
-                bf16x2_t rest;
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int v = 2 * t + k;
-                    const float e = exp2_fast(__builtin_fmaf(sacc[s][v], sc, m_neg));
-                    l_run += e;
-                    x[k] = e * q8::power((vscale[s] >> (8 * v)) & 255u);
-                    h[k] = __float_as_uint(x[k]) & 0xFFFF0000u;
-                    rest[k] = (__bf16)(x[k] - __uint_as_float(h[k]));
-                }
-                ph[s >> 1][2 * (s & 1) + t] = h[0] >> 16 | h[1];
-                pl[s >> 1][2 * (s & 1) + t] = __builtin_bit_cast(uint32_t, rest);
+                for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sacc[n][s][v]);
+            if (__any(mx * sc > m_thr[n])) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float m_new = fmaxf(m_run[n], mx * sc);
+                const float m_use = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = exp2_fast(m_run[n] - m_use);
+                m_run[n] = m_new;
+                m_thr[n] = m_new + kRescale;
+                m_neg[n] = -m_use;
+                l_run[n] *= alpha;
+#pragma unroll
+                for (int i = 0; i < kDB; ++i)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) oacc[n][i][v] *= alpha;
             }
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    float x[2];
+                    uint32_t h[2];
+                    bf16x2_t rest;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int v = 2 * t + k;
+                        const float e = exp2_fast(__builtin_fmaf(sacc[n][s][v], sc, m_neg[n]));
+                        l_run[n] += e;
+                        x[k] = e * q8::power((vscale[s] >> (8 * v)) & 255u);
+                        h[k] = __float_as_uint(x[k]) & 0xFFFF0000u;
+                        rest[k] = (__bf16)(x[k] - __uint_as_float(h[k]));
+                    }
+                    ph[n][s >> 1][2 * (s & 1) + t] = h[0] >> 16 | h[1];
+                    pl[n][s >> 1][2 * (s & 1) + t] = __builtin_bit_cast(uint32_t, rest);
+                }
+        }
 #pragma unroll
         for (int i = 0; i < kDB; ++i) {
             const u32x4_t v0 = widen(vf[i][0], vf[i][1], 1.f), v1 = widen(vf[i][2], vf[i][3], 1.f);
-            oacc[i] = mfma16(v0, ph[0], oacc[i]);
-            oacc[i] = mfma16(v1, ph[1], oacc[i]);
-            oacc[i] = mfma16(v0, pl[0], oacc[i]);
-            oacc[i] = mfma16(v1, pl[1], oacc[i]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                oacc[n][i] = mfma16(v0, ph[n][0], oacc[n][i]);
+                oacc[n][i] = mfma16(v1, ph[n][1], oacc[n][i]);
+                oacc[n][i] = mfma16(v0, pl[n][0], oacc[n][i]);
+                oacc[n][i] = mfma16(v1, pl[n][1], oacc[n][i]);
+            }
         }
     }
 
-    // ---- combine the waves' states (in wave order) and write the split's partial
-    float l_lane = l_run + __shfl_xor(l_run, 16);
-    l_lane += __shfl_xor(l_lane, 32);
-    // every score NaN: any maximum will do for the normaliser to reach the output
-    if (m_run == -INFINITY && l_lane != l_lane) m_run = 0.f;
-    if (g4 == 0) {
-        red_m[wave][r16] = m_run;
-        red_l[wave][r16] = l_lane;
-    }
-    __syncthreads();
-    float m_all = -INFINITY;
+    // ---- combine the waves' states (in wave order) and write the split's partial, or the output
+    // of a row that is not split
+    float l_lane[NT];
 #pragma unroll
-    for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, red_m[w][r16]);
-    const float f = m_run == -INFINITY ? 0.f : exp2_fast(m_run - m_all);
-    if (head_ok) {
-#pragma unroll
-        for (int i = 0; i < kDB; ++i)
-            *reinterpret_cast<f32x4_t*>(&shared[(16 * wave + r16) * kOStride + 16 * i + 4 * g4]) = oacc[i] * f;
-    }
-    __syncthreads();
-    for (int e = tid; e < NH * (D / 4); e += NW * 64) {
-        const int h = e / (D / 4), x = 4 * (e % (D / 4));
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, red_m[w][h]);
-        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) o += *reinterpret_cast<const f32x4_t*>(&shared[(16 * w + h) * kOStride + x]);
-        float L = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w)
-            if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
-        const int64_t slot = p.n_k_rows != nullptr ? slot0 + h : slot0 + int64_t(h) * p.splits;
-        if (x == 0) {
-            p.ws_m[slot] = M;
-            p.ws_l[slot] = L;
+    for (int n = 0; n < NT; ++n) {
+        l_lane[n] = l_run[n] + __shfl_xor(l_run[n], 16);
+        l_lane[n] += __shfl_xor(l_lane[n], 32);
+        // every score NaN: any maximum will do for the normaliser to reach the output
+        if (m_run[n] == -INFINITY && l_lane[n] != l_lane[n]) m_run[n] = 0.f;
+        if (g4 == 0) {
+            red_m[wave][16 * n + r16] = m_run[n];
+            red_l[wave][16 * n + r16] = l_lane[n];
         }
-        *reinterpret_cast<f32x4_t*>(&p.ws_o[slot * D + x]) = o;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        __syncthreads();  // the states are there; the queries, or the last tile, are done with
+        float m_all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, red_m[w][16 * n + r16]);
+        const float f = m_run[n] == -INFINITY ? 0.f : exp2_fast(m_run[n] - m_all);
+        const int heads = min(NH - 16 * n, 16);
+        if (r16 < heads) {
+#pragma unroll
+            for (int i = 0; i < kDB; ++i)
+                *reinterpret_cast<f32x4_t*>(&shared[(16 * wave + r16) * kOStride + 16 * i + 4 * g4]) = oacc[n][i] * f;
+        }
+        __syncthreads();
+        for (int e = tid; e < heads * (D / 4); e += NW * 64) {
+            const int r = e / (D / 4), x = 4 * (e % (D / 4)), h = 16 * n + r;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) M = fmaxf(M, red_m[w][h]);
+            f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) o += *reinterpret_cast<const f32x4_t*>(&shared[(16 * w + r) * kOStride + x]);
+            float L = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
+            if (p.direct) {
+                const bool empty = L == 0.f;  // (as in the merge: O = 0, LSE = -inf)
+                const float inv = empty ? 0.f : 1.f / L;
+                bf16x2_t lo, hi;
+                lo[0] = (__bf16)(empty ? 0.f : o[0] * inv);
+                lo[1] = (__bf16)(empty ? 0.f : o[1] * inv);
+                hi[0] = (__bf16)(empty ? 0.f : o[2] * inv);
+                hi[1] = (__bf16)(empty ? 0.f : o[3] * inv);
+                const int64_t row = int64_t(b) * p.h_q + hq0 + h;
+                *reinterpret_cast<uint2*>(p.o + row * D + x) =
+                    make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+                if (x == 0) p.lse[row] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
+                continue;
+            }
+            const int64_t slot = p.n_k_rows != nullptr ? slot0 + h : slot0 + int64_t(h) * p.splits;
+            if (x == 0) {
+                p.ws_m[slot] = M;
+                p.ws_l[slot] = L;
+            }
+            *reinterpret_cast<f32x4_t*>(&p.ws_o[slot * D + x]) = o;
+        }
     }
 }
 
-template <int D>
+template <int D, int NT>
 hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     // ragged: one workgroup per possible work item (at most p.splits + batch)
     const bool ragged = p.n_k_rows != nullptr;
-    const dim3 grid(unsigned(ragged ? p.splits + p.batch : p.splits), unsigned(p.h_kv * p.subgroups),
-                    unsigned(ragged ? 1 : p.batch));
-    hipLaunchKernelGGL(decode_q8_kernel<D>, grid, dim3(kWaves * 64), 0, stream, p);
+    const dim3 grid(unsigned(p.direct ? p.batch : ragged ? p.splits + p.batch : p.splits),
+                    unsigned(p.h_kv * p.subgroups), unsigned(p.direct || ragged ? 1 : p.batch));
+    if (p.direct) {
+        hipLaunchKernelGGL((decode_q8_kernel<D, NT, kDirectWaves>), grid, dim3(kDirectWaves * 64), 0, stream, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((decode_q8_kernel<D, NT, kWaves>), grid, dim3(kWaves * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : launch_decode_merge_q8(p, D, stream);
 }
@@ -363,17 +417,19 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t stream) {
-    if (p.splits < 1 || p.splits > kDecodeMaxSplits || p.heads_per_block < 1 || p.heads_per_block > 16 ||
+    if (p.splits < 1 || p.splits > kDecodeMaxSplits || p.heads_per_block < 1 || p.heads_per_block > 32 ||
         p.subgroups < 1 || (p.subgroups - 1) * p.heads_per_block >= p.group ||
         p.subgroups * p.heads_per_block < p.group)
         return hipErrorInvalidValue;
-    if (p.n_k_rows == nullptr &&
+    if (!p.direct && p.n_k_rows == nullptr &&
         (int64_t(p.splits) * p.split_tokens < p.n_valid || p.split_tokens % kDecodeQ8TokenStep != 0))
         return hipErrorInvalidValue;
     if (p.n_k_rows != nullptr && (p.q_pos_rows == nullptr || p.ws_plan == nullptr || p.splits > kDecodeMaxSplits - 1))
         return hipErrorInvalidValue;
     (void)hipGetLastError();
-    return head_dim == 64 ? launch_d<64>(p, stream) : launch_d<128>(p, stream);
+    if (p.heads_per_block > 16)
+        return head_dim == 64 ? launch_d<64, 2>(p, stream) : launch_d<128, 2>(p, stream);
+    return head_dim == 64 ? launch_d<64, 1>(p, stream) : launch_d<128, 1>(p, stream);
 }
 
 }  // namespace atf
