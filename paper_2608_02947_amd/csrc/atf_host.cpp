@@ -1343,7 +1343,7 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
     // the heads of a KV head in workgroups of up to 32, as even as they come
     p.subgroups = (p.group + 31) / 32;
     p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
-    const int64_t cols = int64_t(h_kv) * p.subgroups, target = 768;
+    const int64_t cols = int64_t(h_kv) * p.subgroups, target = p.heads_per_block <= 16 && w->head_dim == 64 ? 768 : 512;
     p.direct = 0;
     if (p.direct) {
         p.splits = 1;

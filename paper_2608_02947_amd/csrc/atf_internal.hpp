@@ -178,8 +178,6 @@ hipError_t launch_prefill_rotating(const PrefillRotParams& p, int head_dim, hipS
 int32_t prefill_waves(int32_t batch, int32_t n_q, int32_t n_k, int32_t q_pos0, int32_t h_kv, int32_t group,
                       int32_t cache_tokens, const int32_t* thresholds, int32_t head_dim, bool rotate);
 hipError_t launch_decode(const DecodeParams& p, int head_dim, hipStream_t stream);
-// The merge of the partial states that decode_q8_kernel wrote (decode.hip).
-hipError_t launch_decode_merge_q8(const DecodeParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t stream);
 hipError_t launch_append_normed(const AppendNormedParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_read_q8(const ReadQ8Params& p, int head_dim, hipStream_t stream);

@@ -41,7 +41,6 @@
 // the query once and to each key chunk it loads, so a pruned pair is neither read nor
 // rotated.
 #include "atf_internal.hpp"
-#include "decode_plan.hpp"
 #include "rope.hpp"
 
 #include <mutex>
@@ -99,6 +98,59 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Keys of ragged row r that its query reaches (the clamps keep every read inside the
+// row's cache): min(n_k_rows[r], q_pos_rows[r] + 1), within [0, n_k].
+__device__ __forceinline__ int ragged_valid(const DecodeParams& p, int r) {
+    const int nk = min(max(p.n_k_rows[r], 0), p.n_k);
+    const int qp = min(max(p.q_pos_rows[r], 0), 0x7FFFFFFD);
+    return min(nk, qp + 1);
+}
+
+// Work plan of a ragged batch, the same in every wave that computes it: the batch's
+// causal keys are cut into spans of `span` tokens (about total / p.splits, a multiple
+// of the workgroup's token step), each row into ceil(n_valid / span) items of its own
+// keys, items numbered row by row.  Returns the row of `item` (or -1 past the last
+// item) and its first token; with `plan` set, also writes the index of each row's
+// first item and the item count at plan[B].
+__device__ int ragged_item(const DecodeParams& p, int item, int& t_first, int64_t& span,
+                           int32_t* plan) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += 64) {
+        int64_t nv = r0 + lane < p.batch ? ragged_valid(p, r0 + lane) : 0;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) nv += __shfl_xor(nv, o);
+        total += nv;
+    }
+    span = (total + p.splits - 1) / p.splits;
+    span = (span + kDecodeTokenStep - 1) / kDecodeTokenStep * kDecodeTokenStep;
+    if (span < kDecodeTokenStep) span = kDecodeTokenStep;
+    int row = -1, first = 0;
+    int before = 0;  // items of the rows below r0
+    for (int r0 = 0; r0 < p.batch; r0 += 64) {
+        const int r = r0 + lane;
+        const int cnt = r < p.batch ? int((ragged_valid(p, r) + span - 1) / span) : 0;
+        int incl = cnt;  // inclusive prefix over the wave's rows
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(incl, o);
+            if (lane >= o) incl += y;
+        }
+        incl += before;
+        if (plan != nullptr && r < p.batch) plan[r] = incl - cnt;
+        const uint64_t hit = __ballot(item < incl);
+        if (row < 0 && hit != 0) {
+            const int l = __builtin_ctzll(hit);
+            row = r0 + l;
+            first = item - __shfl(incl - cnt, l);
+        }
+        before = __shfl(incl, 63);
+    }
+    if (plan != nullptr && lane == 0) plan[p.batch] = before;
+    t_first = int(int64_t(first) * span);
+    return row;
+}
+
 template <int D, bool kRot>
 __global__ __launch_bounds__(kWaves * 64, 2) void decode_split_kernel(const DecodeParams p) {
     constexpr int kChunks = D / 16;
@@ -138,7 +190,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_split_kernel(const Deco
     if (p.n_k_rows != nullptr) {
         int64_t span;
         int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
-        b = ragged_item(p, split, kDecodeTokenStep, t_begin, span, plan);
+        b = ragged_item(p, split, t_begin, span, plan);
         if (b < 0) return;  // past the last item (the whole workgroup: wave-uniform)
         n_k = min(max(p.n_k_rows[b], 0), p.n_k);
         q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
@@ -562,7 +614,7 @@ __global__ __launch_bounds__(NW * 64, (NW > 4 ? 2 : kRot ? (D == 128 ? 2 : 3) : 
     } else if (p.n_k_rows != nullptr) {
         int64_t span;
         int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
-        b = ragged_item(p, split, kDecodeTokenStep, t_begin, span, plan);
+        b = ragged_item(p, split, t_begin, span, plan);
         if (b < 0) return;
         n_k = min(max(p.n_k_rows[b], 0), p.n_k);
         q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
@@ -846,10 +898,7 @@ __global__ __launch_bounds__(NW * 64, (NW > 4 ? 2 : kRot ? (D == 128 ? 2 : 3) : 
 // The weights take one state per thread; the output sums take 8 quads of 4 dims x 32
 // state lanes, each lane reading 16 bytes per state, so that all of a thread's loads
 // can be in flight at once.
-//
-// kNaN: a normaliser that is not a number makes the output NaN, as it does with 8-bit caches
-// (without, such a row counts as empty).
-template <int D, bool kNaN>
+template <int D>
 __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
     __shared__ float s_w[kDecodeMaxSplits];  // split weights exp2(m_s - M)
     __shared__ float s_red[8];     // per-wave max, then per-wave sum
@@ -912,17 +961,10 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int k = 0; k < 32; ++k) acc += s_o[k][x];
         // a ragged row without keys has an empty softmax: O = 0, LSE = -inf
-        const bool empty = kNaN ? L == 0.f : !(L > 0.f);
+        const bool empty = !(L > 0.f);
         p.o[int64_t(bh) * D + d0 + x] = __builtin_bit_cast(uint16_t, (__bf16)(empty ? 0.f : acc / L));
         if (blockIdx.y == 0 && tid == 0) p.lse[bh] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
     }
-}
-
-template <int D, bool kNaN>
-hipError_t launch_merge_d(const DecodeParams& p, hipStream_t stream) {
-    hipLaunchKernelGGL((decode_merge_kernel<D, kNaN>), dim3(unsigned(p.batch * p.h_q), unsigned(D / 32)),
-                       dim3(256), 0, stream, p);
-    return hipGetLastError();
 }
 
 template <int D>
@@ -949,7 +991,9 @@ hipError_t launch_decode_d(const DecodeParams& p, hipStream_t stream) {
         hipLaunchKernelGGL((decode_split_kernel<D, false>), grid, dim3(kWaves * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_merge_d<D, false>(p, stream);
+    hipLaunchKernelGGL(decode_merge_kernel<D>, dim3(unsigned(p.batch * p.h_q), unsigned(D / 32)),
+                       dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -968,10 +1012,6 @@ hipError_t launch_decode(const DecodeParams& p, int head_dim, hipStream_t stream
         return hipErrorInvalidValue;
     (void)hipGetLastError();
     return head_dim == 64 ? launch_decode_d<64>(p, stream) : launch_decode_d<128>(p, stream);
-}
-
-hipError_t launch_decode_merge_q8(const DecodeParams& p, int head_dim, hipStream_t stream) {
-    return head_dim == 64 ? launch_merge_d<64, true>(p, stream) : launch_merge_d<128, true>(p, stream);
 }
 
 // The decode workspace of atf_decode_noalloc: a file-scope device array, so that

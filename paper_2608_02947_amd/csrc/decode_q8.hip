@@ -23,7 +23,6 @@
 // lose the pairs kept nowhere, and where a window ends inside the block the keys' bytes are
 // masked lane by lane.
 #include "atf_internal.hpp"
-#include "decode_plan.hpp"
 #include "q8.hpp"
 
 namespace atf {
@@ -69,10 +68,73 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
     return r;
 }
 
+// The sum over the wave's 64 lanes, and each lane's sum of the lanes up to it, by DPP.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_add(int x) {
+    return x + __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xF, false);
+}
+__device__ __forceinline__ int scan_lanes(int x) {
+    x = dpp_add<0x111, 0xF>(x);  // from the lane 1, 2, 4, 8 below in the row of 16
+    x = dpp_add<0x112, 0xF>(x);
+    x = dpp_add<0x114, 0xF>(x);
+    x = dpp_add<0x118, 0xF>(x);
+    x = dpp_add<0x142, 0xA>(x);  // from the last lane of rows 0 and 2 to the rows after them
+    return dpp_add<0x143, 0xC>(x);  // from that of row 1 to rows 2 and 3
+}
+
+// Keys of ragged row r that its query reaches, within [0, n_k], and their steps.
+__device__ __forceinline__ int row_keys(const DecodeParams& p, int r) {
+    const int nk = min(max(p.n_k_rows[r], 0), p.n_k);
+    const int qp = min(max(p.q_pos_rows[r], 0), 0x7FFFFFFD);
+    return min(nk, qp + 1);
+}
+__device__ __forceinline__ int row_steps(const DecodeParams& p, int r) {
+    return r < p.batch ? (row_keys(p, r) + kDecodeQ8TokenStep - 1) / kDecodeQ8TokenStep : 0;
+}
+
+// The work plan of a ragged batch, the same in every wave that computes it: rows in steps of
+// kDecodeQ8TokenStep tokens, cut into items of equal `tokens`, as short as leaves the batch at most
+// p.splits items (as many as run at once; more, up to p.batch more, where it has nearly that
+// many rows), items numbered row by row.  Returns the row of `item` (-1 past the last) and its
+// first token; with `plan` set, writes the index of each row's first item and, at plan[batch],
+// their number.
+__device__ __forceinline__ int ragged_item(const DecodeParams& p, int item, int& t_first, int64_t& tokens, int32_t* plan) {
+    const int lane = threadIdx.x & 63;
+    const int own = row_steps(p, lane);  // of the first 64 rows: mostly all
+    const auto steps = [&](int r0) __attribute__((always_inline)) { return r0 == 0 ? own : row_steps(p, r0 + lane); };
+    int64_t total = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += 64) total += __builtin_amdgcn_readlane(scan_lanes(steps(r0)), 63);
+    int span = max(1, int((total + p.splits - 1) / p.splits));
+    for (int round = 0; round < 8; ++round) {
+        int items = 0;
+        for (int r0 = 0; r0 < p.batch; r0 += 64)
+            items += __builtin_amdgcn_readlane(scan_lanes((steps(r0) + span - 1) / span), 63);
+        if (items <= p.splits) break;
+        span = max(span + 1, int(int64_t(span) * items / p.splits));
+    }
+    int row = -1, first = 0, before = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += 64) {
+        const int cnt = (steps(r0) + span - 1) / span;
+        const int incl = before + scan_lanes(cnt);
+        if (plan != nullptr && r0 + lane < p.batch) plan[r0 + lane] = incl - cnt;
+        const uint64_t hit = __ballot(item < incl);
+        if (row < 0 && hit != 0) {
+            const int l = __builtin_ctzll(hit);
+            row = r0 + l;
+            first = item - __builtin_amdgcn_readlane(incl - cnt, l);
+        }
+        before = __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (plan != nullptr && lane == 0) plan[p.batch] = before;
+    tokens = int64_t(span) * kDecodeQ8TokenStep;
+    t_first = int(first * tokens);
+    return row;
+}
+
 // NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4 where rows are split,
 // kDirectWaves where a workgroup takes a whole row and writes its output (p.direct).
 template <int D, int NT, int NW>
-__global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ? 3 : 4)) void decode_q8_kernel(const DecodeQ8Params p) {
+__global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
     constexpr int kHalf = D / 2;
     constexpr int kM = D / 64;   // loads of a token: 4 chunks each
@@ -99,31 +161,28 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
     const int hq0 = g * p.group + sub * p.heads_per_block;
     const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
 
-    int b, n_k = p.n_k, q_pos = p.q_pos, n_valid = p.n_valid, t_begin, t_end;
+    int b, q_pos = p.q_pos, t_begin, t_end;
     int64_t slot0 = 0;
     if (p.direct) {
         b = blockIdx.x;
-        if (p.n_k_rows != nullptr) {
-            n_k = min(max(p.n_k_rows[b], 0), p.n_k);
-            q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
-            n_valid = min(n_k, q_pos + 1);
-        }
         t_begin = 0;
-        t_end = n_valid;
+        t_end = p.n_valid;
+        if (p.n_k_rows != nullptr) {
+            q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
+            t_end = row_keys(p, b);
+        }
     } else if (p.n_k_rows != nullptr) {
         int64_t span;
         int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
-        b = ragged_item(p, split, kDecodeQ8TokenStep, t_begin, span, plan);
+        b = ragged_item(p, split, t_begin, span, plan);
         if (b < 0) return;
-        n_k = min(max(p.n_k_rows[b], 0), p.n_k);
         q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
-        n_valid = min(n_k, q_pos + 1);
-        t_end = int(min(int64_t(n_valid), int64_t(t_begin) + span));
+        t_end = int(min(int64_t(row_keys(p, b)), t_begin + span));
         slot0 = int64_t(split) * p.h_q + hq0;
     } else {
         b = blockIdx.z;
         t_begin = split * p.split_tokens;
-        t_end = min(n_valid, t_begin + p.split_tokens);
+        t_end = min(p.n_valid, t_begin + p.split_tokens);
         slot0 = (int64_t(b) * p.h_q + hq0) * p.splits + split;
     }
     b = __builtin_amdgcn_readfirstlane(b);
@@ -133,6 +192,80 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
     const int my_w = lane < kHalf ? p.win.W[lane] : -1;
     if (tid < kHalf) s_w[tid] = p.win.W[tid];
 
+    const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
+    const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
+    const uint8_t* const zeros = reinterpret_cast<const uint8_t*>(g_zeros);
+    const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
+
+    // a block's place in the caches: the entries that hold its two halves of 32 tokens (a page
+    // holds whole halves), as rows of KV head g and the place of the half in them; and its pairs
+    // kept at every token and at some
+    struct Blk {
+        int64_t row_a, row_b;
+        int at_a, at_b;
+        uint64_t full, keep;
+    };
+    const int64_t cap = p.block_table != nullptr ? p.page_tokens : p.cache_tokens;
+    const auto locate = [&](int t0) __attribute__((always_inline)) {
+        Blk B;
+        B.row_a = B.row_b = int64_t(b) * p.h_kv + g;
+        B.at_a = t0;
+        B.at_b = t0 + 32;
+        if (p.block_table != nullptr) {
+            const int pt = p.page_tokens;
+            const int32_t* table = p.block_table + int64_t(b) * p.max_pages;
+            const int ia = t0 / pt;
+            B.row_a = int64_t(min(max(table[ia], 0), p.num_pages - 1)) * p.h_kv + g;
+            B.at_a = t0 - ia * pt;
+            B.row_b = B.row_a;
+            B.at_b = B.at_a + 32;
+            if (B.at_b == pt && t_end - t0 > 32) {  // (a row of the table has an entry for every key)
+                B.row_b = int64_t(min(max(table[ia + 1], 0), p.num_pages - 1)) * p.h_kv + g;
+                B.at_b = 0;
+            }
+        }
+        B.full = __ballot(my_w >= q_pos - t0);
+        B.keep = __ballot(my_w >= max(0, q_pos - t0 - min(kBlock, t_end - t0) + 1));
+        return B;
+    };
+    // K operands (a token past the split's end is the split's last one again)
+    u32x4_t kf[4][kM], kscale;
+    const auto load_k = [&](const Blk& B, int t0) __attribute__((always_inline)) {
+        const bool hi = r16 >= 8;
+        const int64_t row = hi ? B.row_b : B.row_a;
+        const int at = hi ? B.at_b : B.at_a, last = t_end - 1 - t0 - (hi ? 32 : 0);
+#pragma unroll
+        for (int m = 0; m < kM; ++m) {
+            const int c = 4 * m + g4;
+            const bool kept = last >= 0 && ((B.keep >> (8 * c)) & 0xFFull) != 0;
+            const uint8_t* src = kept ? keys + ((row * kChunks + c) * cap + at) * 16 : zeros;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                kf[s][m] = *reinterpret_cast<const u32x4_t*>(src + 16 * uint32_t(max(min((tk & 31) + 4 * s, last), 0)));
+        }
+        const uint8_t* src = p.k_scale + row * p.scale_tokens + at + (tk & 16);
+        kscale = *reinterpret_cast<const u32x4_t*>(last >= (tk & 16) ? src : zeros);
+    };
+    // V^T operands
+    u32x4_t vf[kDB], vscale;
+    const auto load_v = [&](const Blk& B, int t0) __attribute__((always_inline)) {
+        const bool hi = g4 >= 2;
+        const int64_t row = hi ? B.row_b : B.row_a;
+        const int at = (hi ? B.at_b : B.at_a) + 16 * (g4 & 1);
+        const bool in = 16 * g4 < t_end - t0;
+        const uint8_t* src = in ? values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16 : zeros;
+#pragma unroll
+        for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(src + 256 * i);
+        vscale = *reinterpret_cast<const u32x4_t*>(in ? p.v_scale + row * p.scale_tokens + at : zeros);
+    };
+
+    int t0 = t_begin + kBlock * wave;
+    Blk B{};
+    if (t0 < t_end) {
+        B = locate(t0);
+        load_k(B, t0);
+        load_v(B, t0);
+    }
     // queries: operand (tile, m, half) at 256 (2 kM tile + 2 m + half) + 4 lane
     for (int o = wave; o < kOps; o += NW) {
         const int h = 16 * (o / (2 * kM)) + r16, m = o / 2 % kM;
@@ -160,62 +293,9 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
         m_neg[n] = l_run[n] = 0.f;
     }
     const float sc = p.scale_log2;
-    const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
-    const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
-    const uint8_t* const zeros = reinterpret_cast<const uint8_t*>(g_zeros);
-    const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
 
-    for (int t0 = t_begin + kBlock * wave; t0 < t_end; t0 += kBlock * NW) {
-        // the entries of the caches that hold the block's two halves of 32 tokens (a page holds
-        // whole halves): rows of KV head g, and the place of token t0 in them
-        int64_t row_a = int64_t(b) * p.h_kv + g, row_b = row_a;
-        int at_a = t0, at_b = t0 + 32;
-        int64_t cap = p.cache_tokens;
-        if (p.block_table != nullptr) {
-            const int pt = p.page_tokens;
-            const int32_t* table = p.block_table + int64_t(b) * p.max_pages;
-            const int ia = t0 / pt, ib = min((t0 + 32) / pt, p.max_pages - 1);
-            row_a = int64_t(min(max(table[ia], 0), p.num_pages - 1)) * p.h_kv + g;
-            row_b = int64_t(min(max(table[ib], 0), p.num_pages - 1)) * p.h_kv + g;
-            at_a = t0 - ia * pt;
-            at_b = (t0 + 32) % pt;
-            cap = pt;
-        }
-        const uint64_t full = __ballot(my_w >= q_pos - t0);
-        const uint64_t keep = __ballot(my_w >= max(0, q_pos - min(t0 + kBlock - 1, t_end - 1)));
-
-        // K operands (a token past the split's end is the split's last one again)
-        u32x4_t kf[4][kM];
-        u32x4_t kscale;
-        {
-            const bool hi = r16 >= 8;
-            const int64_t row = hi ? row_b : row_a;
-            const int at = hi ? at_b : at_a, last = t_end - 1 - t0 - (hi ? 32 : 0);
-#pragma unroll
-            for (int m = 0; m < kM; ++m) {
-                const int c = 4 * m + g4;
-                const bool kept = last >= 0 && ((keep >> (8 * c)) & 0xFFull) != 0;
-                const uint8_t* src = kept ? keys + ((row * kChunks + c) * cap + at) * 16 : zeros;
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    kf[s][m] = *reinterpret_cast<const u32x4_t*>(src + 16 * uint32_t(max(min((tk & 31) + 4 * s, last), 0)));
-            }
-            const uint8_t* src = p.k_scale + row * p.scale_tokens + at + (tk & 16);
-            kscale = *reinterpret_cast<const u32x4_t*>(last >= (tk & 16) ? src : zeros);
-        }
-        // V^T operands
-        u32x4_t vf[kDB], vscale;
-        {
-            const bool hi = g4 >= 2;
-            const int64_t row = hi ? row_b : row_a;
-            const int at = (hi ? at_b : at_a) + 16 * (g4 & 1);
-            const bool in = t0 + 16 * g4 < t_end;
-            const uint8_t* src = in ? values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16 : zeros;
-#pragma unroll
-            for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(src + 256 * i);
-            vscale = *reinterpret_cast<const u32x4_t*>(in ? p.v_scale + row * p.scale_tokens + at : zeros);
-        }
-
+    while (t0 < t_end) {
+        const uint64_t full = B.full, keep = B.keep;
         // windows that end inside the block: this lane's token and chunk, byte by byte
         if (keep & ~full) {
 #pragma unroll
@@ -225,7 +305,7 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
                 for (int e = 0; e < 8; ++e) w[e] = s_w[8 * (4 * m + g4) + e];
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    const int z = q_pos - (t0 + tk + 4 * s);
+                    const int z = q_pos - t0 - (tk + 4 * s);
                     uint32_t lo = 0, hi = 0;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -259,9 +339,16 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
                 }
             }
         }
+        // the next block's keys, into the registers of this one's; its values follow below
+        const bool more = t_end - t0 > kBlock * NW;  // (positions reach 2^31: no sum past t_end)
+        const int t_next = more ? t0 + kBlock * NW : t_end;
+        if (more) {
+            B = locate(t_next);
+            load_k(B, t_next);
+        }
         // tokens past the split's end: no probability, and no value that is not a number
-        if (t0 + kBlock > t_end) {
-            const int bound = t_end - (t0 + 16 * g4);
+        if (t_end - t0 < kBlock) {
+            const int bound = t_end - t0 - 16 * g4;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 uint32_t msk = 0;
@@ -333,6 +420,8 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
                 oacc[n][i] = mfma16(v1, pl[n][1], oacc[n][i]);
             }
         }
+        if (more) load_v(B, t_next);
+        t0 = t_next;
     }
 
     // ---- combine the waves' states (in wave order) and write the split's partial, or the output
@@ -377,12 +466,11 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
                 if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
             if (p.direct) {
                 const bool empty = L == 0.f;  // (as in the merge: O = 0, LSE = -inf)
-                const float inv = empty ? 0.f : 1.f / L;
                 bf16x2_t lo, hi;
-                lo[0] = (__bf16)(empty ? 0.f : o[0] * inv);
-                lo[1] = (__bf16)(empty ? 0.f : o[1] * inv);
-                hi[0] = (__bf16)(empty ? 0.f : o[2] * inv);
-                hi[1] = (__bf16)(empty ? 0.f : o[3] * inv);
+                lo[0] = (__bf16)(empty ? 0.f : o[0] / L);
+                lo[1] = (__bf16)(empty ? 0.f : o[1] / L);
+                hi[0] = (__bf16)(empty ? 0.f : o[2] / L);
+                hi[1] = (__bf16)(empty ? 0.f : o[3] / L);
                 const int64_t row = int64_t(b) * p.h_q + hq0 + h;
                 *reinterpret_cast<uint2*>(p.o + row * D + x) =
                     make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
@@ -399,6 +487,65 @@ __global__ __launch_bounds__(NW * 64, NT == 2 ? (D == 128 ? 2 : 3) : (D == 128 ?
     }
 }
 
+// Merge of the split partials of one (row, head): NW waves, each over every NW-th state, a lane
+// the same D / 64 dims of all of them, so that a wave's loads are whole states, in flight
+// together.
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8Params p) {
+    constexpr int kN = D / 64;
+    typedef float out_t __attribute__((ext_vector_type(kN)));
+    __shared__ float s_o[NW][D];
+    __shared__ float s_l[NW];
+    const int bh = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t base = int64_t(bh) * p.splits, stride = 1;
+    int count = p.splits;
+    if (p.n_k_rows != nullptr) {
+        // (the clamps only restate what the plan guarantees: at most splits + batch items)
+        const int b = bh / p.h_q, most = p.splits + p.batch;
+        const int first = min(max(p.ws_plan[b], 0), most);
+        count = min(max(p.ws_plan[b + 1] - first, 0), most - first);
+        base = int64_t(first) * p.h_q + bh % p.h_q;
+        stride = p.h_q;
+    }
+    count = __builtin_amdgcn_readfirstlane(count);
+    float M = -INFINITY;
+    for (int s = lane; s < count; s += 64) M = fmaxf(M, p.ws_m[base + s * stride]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    out_t O = {};
+    float L = 0.f;
+#pragma unroll 8
+    for (int s = wave; s < count; s += NW) {
+        const int64_t at = base + s * stride;
+        const float m = p.ws_m[at];
+        const float w = m == -INFINITY ? 0.f : exp2_fast(m - M);  // a split with no causal key
+        O += w * *reinterpret_cast<const out_t*>(p.ws_o + at * D + kN * lane);
+        L += w * p.ws_l[at];
+    }
+    *reinterpret_cast<out_t*>(&s_o[wave][kN * lane]) = O;
+    if (lane == 0) s_l[wave] = L;
+    __syncthreads();
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) L += s_l[w];
+    const bool empty = L == 0.f;  // a row without keys: O = 0, LSE = -inf
+    if (threadIdx.x < D / 2) {
+        float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            o.x += s_o[w][2 * threadIdx.x];
+            o.y += s_o[w][2 * threadIdx.x + 1];
+        }
+        bf16x2_t two;
+        two[0] = (__bf16)(empty ? 0.f : o.x / L);
+        two[1] = (__bf16)(empty ? 0.f : o.y / L);
+        *reinterpret_cast<uint32_t*>(p.o + int64_t(bh) * D + 2 * threadIdx.x) = __builtin_bit_cast(uint32_t, two);
+    }
+    if (threadIdx.x == 0) p.lse[bh] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
+}
+
 template <int D, int NT>
 hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     // ragged: one workgroup per possible work item (at most p.splits + batch)
@@ -411,7 +558,13 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     }
     hipLaunchKernelGGL((decode_q8_kernel<D, NT, kWaves>), grid, dim3(kWaves * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_decode_merge_q8(p, D, stream);
+    if (e != hipSuccess) return e;
+    const dim3 heads(unsigned(p.batch * p.h_q));
+    if (p.splits > 32)
+        hipLaunchKernelGGL((decode_q8_merge_kernel<D, 16>), heads, dim3(1024), 0, stream, p);
+    else
+        hipLaunchKernelGGL((decode_q8_merge_kernel<D, 4>), heads, dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 }  // namespace
