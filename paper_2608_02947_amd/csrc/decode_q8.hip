@@ -47,6 +47,13 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
                                                    __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// 16 bytes of global memory (an address that is either of two would be taken for a flat one), and
+// what a block table holds, which nothing writes while the kernel runs (scalar loads)
+__device__ __forceinline__ u32x4_t load16(uint64_t at, int offset) {
+    return *((const __attribute__((address_space(1))) u32x4_t*)(at) + offset / 16);
+}
+typedef const __attribute__((address_space(4))) int32_t const_i32;
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // 8 e4m3 numbers times a power of two as 8 bf16 numbers, exact
@@ -189,40 +196,46 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     q_pos = __builtin_amdgcn_readfirstlane(q_pos);
     t_begin = __builtin_amdgcn_readfirstlane(t_begin);
     t_end = __builtin_amdgcn_readfirstlane(t_end);
-    const int my_w = lane < kHalf ? p.win.W[lane] : -1;
-    if (tid < kHalf) s_w[tid] = p.win.W[tid];
+    int my_w = lane < kHalf ? p.win.W[lane] : -1;
+    if (tid < kHalf) s_w[tid] = my_w;
+    asm volatile("" : "+v"(my_w));  // (has arrived: the block loop need not wait for it)
 
-    const uint8_t* const keys = reinterpret_cast<const uint8_t*>(p.kpcm);
-    const uint8_t* const values = reinterpret_cast<const uint8_t*>(p.vpk);
-    const uint8_t* const zeros = reinterpret_cast<const uint8_t*>(g_zeros);
+    const uint64_t zeros = reinterpret_cast<uint64_t>(g_zeros);
     const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
 
-    // a block's place in the caches: the entries that hold its two halves of 32 tokens (a page
-    // holds whole halves), as rows of KV head g and the place of the half in them; and its pairs
-    // kept at every token and at some
+    // a block: the addresses of the entries that hold its two halves of 32 tokens (a page holds
+    // whole halves; `a`, and how much further `b` is), and its pairs kept at every token and at some
+    struct Place {
+        uint64_t k, ks, v, vs;  // of the half's first token in K chunk 0, V block, scales
+    };
     struct Blk {
-        int64_t row_a, row_b;
-        int at_a, at_b;
+        Place a, b;
         uint64_t full, keep;
     };
     const int64_t cap = p.block_table != nullptr ? p.page_tokens : p.cache_tokens;
+    const auto place = [&](int64_t row, int at) __attribute__((always_inline)) {
+        Place x;
+        x.k = reinterpret_cast<uint64_t>(p.kpcm) + (row * kChunks * cap + at) * 16;
+        x.v = reinterpret_cast<uint64_t>(p.vpk) + (row * ((cap + 15) / 16) * 16 + at) * D;
+        x.ks = reinterpret_cast<uint64_t>(p.k_scale) + row * p.scale_tokens + at;
+        x.vs = reinterpret_cast<uint64_t>(p.v_scale) + row * p.scale_tokens + at;
+        return x;
+    };
     const auto locate = [&](int t0) __attribute__((always_inline)) {
         Blk B;
-        B.row_a = B.row_b = int64_t(b) * p.h_kv + g;
-        B.at_a = t0;
-        B.at_b = t0 + 32;
+        int64_t row = int64_t(b) * p.h_kv + g;
         if (p.block_table != nullptr) {
-            const int pt = p.page_tokens;
-            const int32_t* table = p.block_table + int64_t(b) * p.max_pages;
-            const int ia = t0 / pt;
-            B.row_a = int64_t(min(max(table[ia], 0), p.num_pages - 1)) * p.h_kv + g;
-            B.at_a = t0 - ia * pt;
-            B.row_b = B.row_a;
-            B.at_b = B.at_a + 32;
-            if (B.at_b == pt && t_end - t0 > 32) {  // (a row of the table has an entry for every key)
-                B.row_b = int64_t(min(max(table[ia + 1], 0), p.num_pages - 1)) * p.h_kv + g;
-                B.at_b = 0;
-            }
+            const int pt = p.page_tokens, ia = t0 / pt, at = t0 - ia * pt;
+            const auto* table = (const_i32*)(p.block_table + int64_t(b) * p.max_pages + ia);
+            row = int64_t(min(max(table[0], 0), p.num_pages - 1)) * p.h_kv + g;
+            B.a = place(row, at);
+            B.b = place(row, at + 32);
+            // (a row of the table has an entry for every key)
+            if (at + 32 == pt && t_end - t0 > 32)
+                B.b = place(int64_t(min(max(table[1], 0), p.num_pages - 1)) * p.h_kv + g, 0);
+        } else {
+            B.a = place(row, t0);
+            B.b = place(row, t0 + 32);
         }
         B.full = __ballot(my_w >= q_pos - t0);
         B.keep = __ballot(my_w >= max(0, q_pos - t0 - min(kBlock, t_end - t0) + 1));
@@ -230,33 +243,35 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     };
     // K operands (a token past the split's end is the split's last one again)
     u32x4_t kf[4][kM], kscale;
+    const int64_t k_lane = g4 * cap * 16;
     const auto load_k = [&](const Blk& B, int t0) __attribute__((always_inline)) {
         const bool hi = r16 >= 8;
-        const int64_t row = hi ? B.row_b : B.row_a;
-        const int at = hi ? B.at_b : B.at_a, last = t_end - 1 - t0 - (hi ? 32 : 0);
+        const int last = t_end - 1 - t0 - (hi ? 32 : 0);  // of the half
+        const bool whole = t_end - t0 >= kBlock;
+        const uint64_t at = (hi ? B.b.k : B.a.k) + k_lane;
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
             const int c = 4 * m + g4;
             const bool kept = last >= 0 && ((B.keep >> (8 * c)) & 0xFFull) != 0;
-            const uint8_t* src = kept ? keys + ((row * kChunks + c) * cap + at) * 16 : zeros;
+            const uint64_t src = kept ? at + 64 * m * cap : zeros;
+            if (whole) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                kf[s][m] = *reinterpret_cast<const u32x4_t*>(src + 16 * uint32_t(max(min((tk & 31) + 4 * s, last), 0)));
+                for (int s = 0; s < 4; ++s) kf[s][m] = load16(src + 16 * uint32_t(tk & 31), 64 * s);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) kf[s][m] = load16(src + 16 * uint32_t(max(min((tk & 31) + 4 * s, last), 0)), 0);
+            }
         }
-        const uint8_t* src = p.k_scale + row * p.scale_tokens + at + (tk & 16);
-        kscale = *reinterpret_cast<const u32x4_t*>(last >= (tk & 16) ? src : zeros);
+        kscale = load16(last >= (tk & 16) ? (hi ? B.b.ks : B.a.ks) + (tk & 16) : zeros, 0);
     };
     // V^T operands
     u32x4_t vf[kDB], vscale;
     const auto load_v = [&](const Blk& B, int t0) __attribute__((always_inline)) {
-        const bool hi = g4 >= 2;
-        const int64_t row = hi ? B.row_b : B.row_a;
-        const int at = (hi ? B.at_b : B.at_a) + 16 * (g4 & 1);
-        const bool in = 16 * g4 < t_end - t0;
-        const uint8_t* src = in ? values + ((row * ((cap + 15) / 16) + at / 16) * D + r16) * 16 : zeros;
+        const bool hi = g4 >= 2, in = 16 * g4 < t_end - t0;
+        const uint64_t src = in ? (hi ? B.b.v : B.a.v) + (16 * D * (g4 & 1) + 16 * r16) : zeros;
 #pragma unroll
-        for (int i = 0; i < kDB; ++i) vf[i] = *reinterpret_cast<const u32x4_t*>(src + 256 * i);
-        vscale = *reinterpret_cast<const u32x4_t*>(in ? p.v_scale + row * p.scale_tokens + at : zeros);
+        for (int i = 0; i < kDB; ++i) vf[i] = load16(src, 256 * i);
+        vscale = load16(in ? (hi ? B.b.vs : B.a.vs) + 16 * (g4 & 1) : zeros, 0);
     };
 
     int t0 = t_begin + kBlock * wave;
@@ -340,12 +355,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
             }
         }
         // the next block's keys, into the registers of this one's; its values follow below
-        const bool more = t_end - t0 > kBlock * NW;  // (positions reach 2^31: no sum past t_end)
+        // (after the last block zeros are read, so that the loads in flight, which the waits count,
+        // are the same on every path; positions reach 2^31: no sum past t_end)
+        const bool more = t_end - t0 > kBlock * NW;
         const int t_next = more ? t0 + kBlock * NW : t_end;
-        if (more) {
-            B = locate(t_next);
-            load_k(B, t_next);
-        }
+        if (more) B = locate(t_next);
+        load_k(B, t_next);
         // tokens past the split's end: no probability, and no value that is not a number
         if (t_end - t0 < kBlock) {
             const int bound = t_end - t0 - 16 * g4;
@@ -420,7 +435,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
                 oacc[n][i] = mfma16(v1, pl[n][1], oacc[n][i]);
             }
         }
-        if (more) load_v(B, t_next);
+        load_v(B, t_next);
         t0 = t_next;
     }
 
@@ -487,15 +502,15 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     }
 }
 
-// Merge of the split partials of one (row, head): NW waves, each over every NW-th state, a lane
-// the same D / 64 dims of all of them, so that a wave's loads are whole states, in flight
-// together.
+// Merge of the split partials of one (row, head): NW waves, each over every NW-th state with a
+// maximum of its own, so that no load waits for another; a lane has the same D / 64 dims of all.
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8Params p) {
     constexpr int kN = D / 64;
+    constexpr int kAhead = 8;  // states in flight
     typedef float out_t __attribute__((ext_vector_type(kN)));
     __shared__ float s_o[NW][D];
-    __shared__ float s_l[NW];
+    __shared__ float s_m[NW], s_l[NW];
     const int bh = blockIdx.x;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -509,40 +524,60 @@ __global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8
         base = int64_t(first) * p.h_q + bh % p.h_q;
         stride = p.h_q;
     }
-    count = __builtin_amdgcn_readfirstlane(count);
-    float M = -INFINITY;
-    for (int s = lane; s < count; s += 64) M = fmaxf(M, p.ws_m[base + s * stride]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    float M = -INFINITY, L = 0.f;
     out_t O = {};
-    float L = 0.f;
-#pragma unroll 8
-    for (int s = wave; s < count; s += NW) {
-        const int64_t at = base + s * stride;
-        const float m = p.ws_m[at];
-        const float w = m == -INFINITY ? 0.f : exp2_fast(m - M);  // a split with no causal key
-        O += w * *reinterpret_cast<const out_t*>(p.ws_o + at * D + kN * lane);
-        L += w * p.ws_l[at];
+    for (int s0 = wave; s0 < count; s0 += NW * kAhead) {
+        float m[kAhead], l[kAhead];
+        out_t o[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t at = base + min(s0 + NW * i, count - 1) * stride;
+            m[i] = p.ws_m[at];
+            l[i] = p.ws_l[at];
+            o[i] = *reinterpret_cast<const out_t*>(p.ws_o + at * D + kN * lane);
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (s0 + NW * i >= count) m[i] = -INFINITY;
+            top = fmaxf(top, m[i]);
+        }
+        if (top == -INFINITY) continue;  // splits without a causal key
+        const float f = exp2_fast(M - top);
+        M = top;
+        L *= f;
+        O *= f;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float w = exp2_fast(m[i] - M);
+            L += m[i] == -INFINITY ? 0.f : w * l[i];
+            O += m[i] == -INFINITY ? out_t{} : w * o[i];
+        }
     }
     *reinterpret_cast<out_t*>(&s_o[wave][kN * lane]) = O;
-    if (lane == 0) s_l[wave] = L;
-    __syncthreads();
-    L = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) L += s_l[w];
-    const bool empty = L == 0.f;  // a row without keys: O = 0, LSE = -inf
-    if (threadIdx.x < D / 2) {
-        float2 o = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            o.x += s_o[w][2 * threadIdx.x];
-            o.y += s_o[w][2 * threadIdx.x + 1];
-        }
-        bf16x2_t two;
-        two[0] = (__bf16)(empty ? 0.f : o.x / L);
-        two[1] = (__bf16)(empty ? 0.f : o.y / L);
-        *reinterpret_cast<uint32_t*>(p.o + int64_t(bh) * D + 2 * threadIdx.x) = __builtin_bit_cast(uint32_t, two);
+    if (lane == 0) {
+        s_m[wave] = M;
+        s_l[wave] = L;
     }
+    __syncthreads();
+    if (threadIdx.x >= D / 2) return;
+    M = s_m[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w]);
+    L = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float f = s_m[w] == -INFINITY ? 0.f : exp2_fast(s_m[w] - M);
+        L += f * s_l[w];
+        o.x += f * s_o[w][2 * threadIdx.x];
+        o.y += f * s_o[w][2 * threadIdx.x + 1];
+    }
+    const bool empty = L == 0.f;  // a row without keys: O = 0, LSE = -inf
+    bf16x2_t two;
+    two[0] = (__bf16)(empty ? 0.f : o.x / L);
+    two[1] = (__bf16)(empty ? 0.f : o.y / L);
+    *reinterpret_cast<uint32_t*>(p.o + int64_t(bh) * D + 2 * threadIdx.x) = __builtin_bit_cast(uint32_t, two);
     if (threadIdx.x == 0) p.lse[bh] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
 }
 
@@ -559,9 +594,14 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     hipLaunchKernelGGL((decode_q8_kernel<D, NT, kWaves>), grid, dim3(kWaves * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    // the merge's waves by the states of a row: a ragged batch's longest rows have some times the
+    // average
+    const int64_t states = ragged ? 3 * int64_t(p.splits) / p.batch : p.splits;
     const dim3 heads(unsigned(p.batch * p.h_q));
-    if (p.splits > 32)
+    if (states > 128)
         hipLaunchKernelGGL((decode_q8_merge_kernel<D, 16>), heads, dim3(1024), 0, stream, p);
+    else if (states > 32)
+        hipLaunchKernelGGL((decode_q8_merge_kernel<D, 8>), heads, dim3(512), 0, stream, p);
     else
         hipLaunchKernelGGL((decode_q8_merge_kernel<D, 4>), heads, dim3(256), 0, stream, p);
     return hipGetLastError();
