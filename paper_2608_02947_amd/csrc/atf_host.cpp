@@ -330,6 +330,43 @@ int32_t decode_plan_items(int32_t cols, bool cols16) {
     return cols16 ? std::min(room, std::max(1, 1536 / cols)) : room;
 }
 
+// ---- Decode over 8-bit caches: `groups` workgroups without splits, (row, KV head) pairs, or
+// parts of them where a KV head has more than 32 heads; `tiles` 1 or 2 of 16 heads.
+
+// Workgroups of 4 waves that run at once: 2 a CU, 3 at d = 64 with one tile.
+int32_t decode_q8_slots(int32_t head_dim, int32_t tiles) { return head_dim == 64 && tiles == 1 ? 768 : 512; }
+
+// Whether a row is one workgroup's, which writes the output: no partial states, no merge (3 to 5
+// us), but a row's keys in a row.  With as many rows as CUs always (uniform batches; us, split ->
+// whole: 32 rows of 1,000 keys 24/8 heads 19.9 -> 17.0, of 8,000 86.6 -> 83.0), but for those
+// just past a whole round of the workgroups that run at once (36 rows of 8,000 keys 105 ->
+// 120); with fewer while a row costs less than the merge, and the more of the chip's time the
+// rows fill, the longer (d = 128: 8 rows of 640 keys 12.4 -> 10.1, of 1,500 14 -> 15; 16 of
+// 1,500 18.6 -> 18.1, of 3,000 24.8 -> 26.3; 20 of 4,000 35.2 -> 34.2; d = 64, 16/16 heads:
+// 1 row of 1,000 8.6 -> 8.5, 8 of 2,000 14.6 -> 14.1; 40/2 heads: 32 rows of 640 15.3 -> 14.2, of
+// 1,000 16.5 -> 17.0, 64 of 2,000 28.1 -> 26.4).  Of a ragged batch only the longest row's bound
+// is known, and a row alone can be that long: the limits are lower (40 rows of 16/16 heads up to
+// 1,000 keys 19.2 -> 16.6, one of 4,000 among rows of 1 13.5 -> 21.5; 256 rows up to 2,000 keys,
+// 24/8 heads, 96 -> 87).
+bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged) {
+    const int64_t keys = tiles == 2 ? 450 : head_dim == 64 ? 1100 : 800;
+    if (ragged) return n_valid <= keys * (groups <= 64 ? 1 : groups < 512 ? 2 : groups < 2048 ? 3 : 6);
+    if (groups > 256 && groups < 512) return n_valid <= 1500;
+    return groups > 176 || n_valid <= keys * (groups <= 64 ? 1 : groups <= 128 ? 2 : 5);
+}
+
+// Splits of a uniform batch's rows, at most `room`: as fill the slots; with more groups than half
+// of them, the few that leave the last round fullest.
+int64_t decode_q8_splits(int64_t groups, int32_t head_dim, int32_t tiles, int64_t room) {
+    const int64_t slots = decode_q8_slots(head_dim, tiles);
+    const auto rounds = [&](int64_t s) { return (s * groups + slots - 1) / slots; };
+    int64_t best = std::max<int64_t>(1, slots / groups);
+    if (best == 1)
+        for (int64_t s = 2; s <= 4; ++s)
+            if (rounds(s) * best < rounds(best) * s) best = s;
+    return std::max<int64_t>(1, std::min(best, room));
+}
+
 }  // namespace atf
 
 extern "C" {
@@ -1329,38 +1366,67 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
                    int64_t q_pos, const int32_t* n_k_rows, const int32_t* q_pos_rows, int32_t h_q,
                    int32_t h_kv, int64_t cache_tokens, const PagedArgs& pg, const atf_window* w,
                    float softmax_scale, void* workspace, size_t workspace_bytes, void* hip_stream) {
-    atf::DecodeQ8Params p{};
+    atf::DecodeParams c{};
     const int rc = decode_setup(fn, q, k_cache, v_cache, o, lse, batch, n_k, q_pos, n_k_rows, q_pos_rows, h_q,
                                 h_kv, cache_tokens, w, softmax_scale, workspace, workspace_bytes, pg,
-                                RopeArgs(), p);
+                                RopeArgs(), c);
     if (rc != ATF_OK) return rc;
     if (!k_scale || !v_scale) return fail(ATF_EINVAL, "%s: NULL scale pointer", fn);
     if (!aligned(k_scale, 16) || !aligned(v_scale, 16))
         return fail(ATF_EINVAL, "%s: scales must be 16-byte aligned", fn);
+    const int d = w->head_dim;
+    atf::DecodeQ8Params p{};
+    p.o = c.o;
+    p.lse = lse;
+    p.ws_m = c.ws_m;
+    p.ws_l = c.ws_l;
+    p.ws_o = c.ws_o;
+    p.ws_plan = c.ws_plan;
+    p.batch = batch;
+    p.h_q = h_q;
+    p.q = c.q;
+    p.k = static_cast<const uint8_t*>(k_cache);
+    p.v = static_cast<const uint8_t*>(v_cache);
     p.k_scale = static_cast<const uint8_t*>(k_scale);
     p.v_scale = static_cast<const uint8_t*>(v_scale);
+    p.n_k_rows = n_k_rows;
+    p.q_pos_rows = q_pos_rows;
+    p.block_table = pg.block_table;
+    p.n_k = c.n_k;
+    p.q_pos = c.q_pos;
+    p.n_valid = c.n_valid;
+    p.h_kv = h_kv;
+    p.group = c.group;
+    p.cache_tokens = c.cache_tokens;
     p.scale_tokens = pg.block_table != nullptr ? pg.page_tokens : scale_tokens(p.cache_tokens);
+    p.max_pages = pg.max_pages;
+    p.num_pages = pg.num_pages;
+    p.page_tokens = pg.page_tokens;
+    p.scale_log2 = c.scale_log2;
+    std::memcpy(p.W, c.win.W, sizeof p.W);
     // the heads of a KV head in workgroups of up to 32, as even as they come
     p.subgroups = (p.group + 31) / 32;
     p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
-    const int64_t cols = int64_t(h_kv) * p.subgroups, target = p.heads_per_block <= 16 && w->head_dim == 64 ? 768 : 512;
-    p.direct = 0;
+    const int64_t cols = int64_t(h_kv) * p.subgroups;
+    const int32_t tiles = (p.heads_per_block + 15) / 16;
+    p.direct = atf::decode_q8_direct(batch * cols, d, tiles, p.n_valid, n_k_rows != nullptr);
     if (p.direct) {
         p.splits = 1;
+        p.ws_plan = nullptr;
     } else if (n_k_rows != nullptr) {
         const int64_t room = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
-        p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, target / cols)));
+        p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, atf::decode_q8_slots(d, tiles) / cols)));
     } else {
         const int64_t steps = (int64_t(p.n_valid) + atf::kDecodeQ8TokenStep - 1) / atf::kDecodeQ8TokenStep;
         const int64_t room = std::min<int64_t>(atf::decode_splits(batch, h_kv, n_k), steps);
-        const int64_t s = std::min(room, std::max<int64_t>(1, target / (cols * batch)));
+        const int64_t s = atf::decode_q8_splits(batch * cols, d, tiles, room);
         const int64_t per = (steps + s - 1) / s;
         p.splits = static_cast<int32_t>((steps + per - 1) / per);
         if (per * atf::kDecodeQ8TokenStep * p.splits >= kPosLimit)
             return fail(ATF_EINVAL, "%s: cache too long for the split plan", fn);
         p.split_tokens = static_cast<int32_t>(per * atf::kDecodeQ8TokenStep);
     }
-    const hipError_t e = atf::launch_decode_q8(p, w->head_dim, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = atf::launch_decode_q8(p, d, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return ATF_OK;
 }

@@ -106,14 +106,36 @@ struct AppendRotParams : AppendParams {
     uint32_t rope_rho_lo[kMaxPairs];
 };
 
-// Decode over 8-bit caches (decode_q8.hip): kpcm and vpk hold e4m3 bytes in the layouts of
-// q8.hpp's caches, with a power-of-two byte per token.  heads_per_block is at most 32 and need
-// not divide the group: the last of the `subgroups` workgroups of a KV head takes what is left.
-struct DecodeQ8Params : DecodeParams {
+// Decode over 8-bit caches (decode_q8.hip).  A type of its own, without what its kernel does not
+// read (the arguments' way to the chip is part of a short call): fields as DecodeParams.
+struct DecodeQ8States {
+    uint16_t* o;
+    float* lse;
+    float* ws_m;
+    float* ws_l;
+    float* ws_o;
+    int32_t* ws_plan;         // ragged batch split over work items, else nullptr: a row has `splits`
+    int32_t batch, h_q, splits;
+};
+struct DecodeQ8Params : DecodeQ8States {
+    const uint16_t* q;
+    const uint8_t* k;         // e4m3 [B][h_kv][d/16][cache_tokens][16], or pages
+    const uint8_t* v;         // e4m3 [B][h_kv][ceil(cache_tokens/16)][d][16], tokens in order
     const uint8_t* k_scale;   // [B][h_kv][scale_tokens], or pages [num_pages][h_kv][page_tokens]
     const uint8_t* v_scale;
+    const int32_t* n_k_rows;
+    const int32_t* q_pos_rows;
+    const int32_t* block_table;
+    int32_t n_k, q_pos, n_valid, h_kv, group;
+    int32_t cache_tokens;
     int32_t scale_tokens;     // cache_tokens rounded up to 16, or page_tokens
-    int32_t subgroups;
+    int32_t max_pages, num_pages, page_tokens;
+    int32_t heads_per_block;  // at most 32; need not divide the group: the last of the
+    int32_t subgroups;        // `subgroups` workgroups of a KV head takes what is left
+    int32_t split_tokens;
+    int32_t direct;
+    float scale_log2;
+    int32_t W[kMaxPairs];
 };
 
 // Append with the heads' norms and the rotation (append_normed.hip), of bf16 caches or, with
@@ -197,6 +219,10 @@ int32_t decode_plan_items(int32_t cols, bool cols16);
 // Whether a batch runs without splits (with cols16 only).
 bool decode_direct(int32_t batch, int32_t h_q, int32_t h_kv, int32_t head_dim, int64_t n_valid,
                    int32_t heads_per_block, bool rotate, bool ragged);
+// The same questions of the decode over 8-bit caches.
+int32_t decode_q8_slots(int32_t head_dim, int32_t tiles);
+bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged);
+int64_t decode_q8_splits(int64_t groups, int32_t head_dim, int32_t tiles, int64_t room);
 // Caches from this many tokens are out of the 32-bit lane offsets of decode_split16_kernel
 // (they reach over one chunk's stream) and take decode_split_kernel.
 constexpr int64_t kDecode16MaxTokens = (int64_t(1) << 27) - 64;

@@ -90,22 +90,23 @@ __device__ __forceinline__ int scan_lanes(int x) {
 }
 
 // Keys of ragged row r that its query reaches, within [0, n_k], and their steps.
-__device__ __forceinline__ int row_keys(const DecodeParams& p, int r) {
+__device__ __forceinline__ int row_keys(const DecodeQ8Params& p, int r) {
     const int nk = min(max(p.n_k_rows[r], 0), p.n_k);
     const int qp = min(max(p.q_pos_rows[r], 0), 0x7FFFFFFD);
     return min(nk, qp + 1);
 }
-__device__ __forceinline__ int row_steps(const DecodeParams& p, int r) {
+__device__ __forceinline__ int row_steps(const DecodeQ8Params& p, int r) {
     return r < p.batch ? (row_keys(p, r) + kDecodeQ8TokenStep - 1) / kDecodeQ8TokenStep : 0;
 }
 
 // The work plan of a ragged batch, the same in every wave that computes it: rows in steps of
-// kDecodeQ8TokenStep tokens, cut into items of equal `tokens`, as short as leaves the batch at most
-// p.splits items (as many as run at once; more, up to p.batch more, where it has nearly that
-// many rows), items numbered row by row.  Returns the row of `item` (-1 past the last) and its
+// kDecodeQ8TokenStep tokens, cut into items of equal `tokens`, about p.splits in all: as many as
+// run at once, so the span grows until they are no more than that, unless the batch has so many
+// rows that their last, shorter items are a large part (p.splits + p.batch bounds them then).
+// Items are numbered row by row.  Returns the row of `item` (-1 past the last) and its
 // first token; with `plan` set, writes the index of each row's first item and, at plan[batch],
 // their number.
-__device__ __forceinline__ int ragged_item(const DecodeParams& p, int item, int& t_first, int64_t& tokens, int32_t* plan) {
+__device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, int& t_first, int64_t& tokens, int32_t* plan) {
     const int lane = threadIdx.x & 63;
     const int own = row_steps(p, lane);  // of the first 64 rows: mostly all
     const auto steps = [&](int r0) __attribute__((always_inline)) { return r0 == 0 ? own : row_steps(p, r0 + lane); };
@@ -116,7 +117,8 @@ __device__ __forceinline__ int ragged_item(const DecodeParams& p, int item, int&
         int items = 0;
         for (int r0 = 0; r0 < p.batch; r0 += 64)
             items += __builtin_amdgcn_readlane(scan_lanes((steps(r0) + span - 1) / span), 63);
-        if (items <= p.splits) break;
+        // (many rows: spans long enough for so few items would leave whole rows to one of them)
+        if (items <= p.splits || (round == 0 && items > p.splits + p.splits / 4)) break;
         span = max(span + 1, int(int64_t(span) * items / p.splits));
     }
     int row = -1, first = 0, before = 0;
@@ -138,8 +140,8 @@ __device__ __forceinline__ int ragged_item(const DecodeParams& p, int item, int&
     return row;
 }
 
-// NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4 where rows are split,
-// kDirectWaves where a workgroup takes a whole row and writes its output (p.direct).
+// NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4, or kDirectWaves; with
+// p.direct a workgroup takes a whole row and writes its output.
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
@@ -168,6 +170,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     const int hq0 = g * p.group + sub * p.heads_per_block;
     const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
 
+    int my_w = lane < kHalf ? p.W[lane] : -1;
     int b, q_pos = p.q_pos, t_begin, t_end;
     int64_t slot0 = 0;
     if (p.direct) {
@@ -196,10 +199,6 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     q_pos = __builtin_amdgcn_readfirstlane(q_pos);
     t_begin = __builtin_amdgcn_readfirstlane(t_begin);
     t_end = __builtin_amdgcn_readfirstlane(t_end);
-    int my_w = lane < kHalf ? p.win.W[lane] : -1;
-    if (tid < kHalf) s_w[tid] = my_w;
-    asm volatile("" : "+v"(my_w));  // (has arrived: the block loop need not wait for it)
-
     const uint64_t zeros = reinterpret_cast<uint64_t>(g_zeros);
     const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
 
@@ -215,8 +214,8 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     const int64_t cap = p.block_table != nullptr ? p.page_tokens : p.cache_tokens;
     const auto place = [&](int64_t row, int at) __attribute__((always_inline)) {
         Place x;
-        x.k = reinterpret_cast<uint64_t>(p.kpcm) + (row * kChunks * cap + at) * 16;
-        x.v = reinterpret_cast<uint64_t>(p.vpk) + (row * ((cap + 15) / 16) * 16 + at) * D;
+        x.k = reinterpret_cast<uint64_t>(p.k) + (row * kChunks * cap + at) * 16;
+        x.v = reinterpret_cast<uint64_t>(p.v) + (row * ((cap + 15) / 16) * 16 + at) * D;
         x.ks = reinterpret_cast<uint64_t>(p.k_scale) + row * p.scale_tokens + at;
         x.vs = reinterpret_cast<uint64_t>(p.v_scale) + row * p.scale_tokens + at;
         return x;
@@ -237,9 +236,11 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
             B.a = place(row, t0);
             B.b = place(row, t0 + 32);
         }
+        return B;
+    };
+    const auto classify = [&](Blk& B, int t0) __attribute__((always_inline)) {
         B.full = __ballot(my_w >= q_pos - t0);
         B.keep = __ballot(my_w >= max(0, q_pos - t0 - min(kBlock, t_end - t0) + 1));
-        return B;
     };
     // K operands (a token past the split's end is the split's last one again)
     u32x4_t kf[4][kM], kscale;
@@ -277,9 +278,15 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     int t0 = t_begin + kBlock * wave;
     Blk B{};
     if (t0 < t_end) {
+        // (the values first: they need no window, whose table is on its way)
         B = locate(t0);
-        load_k(B, t0);
         load_v(B, t0);
+    }
+    if (tid < kHalf) s_w[tid] = my_w;
+    asm volatile("" : "+v"(my_w));  // it has arrived: the loop need not wait for it
+    if (t0 < t_end) {
+        classify(B, t0);
+        load_k(B, t0);
     }
     // queries: operand (tile, m, half) at 256 (2 kM tile + 2 m + half) + 4 lane
     for (int o = wave; o < kOps; o += NW) {
@@ -309,6 +316,12 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     }
     const float sc = p.scale_log2;
 
+    // (nothing in flight: the loop's waits count its own loads alone)
+    asm volatile("" : "+v"(kscale), "+v"(vscale));
+#pragma unroll
+    for (int i = 0; i < kDB; ++i) asm volatile("" : "+v"(vf[i]));
+#pragma unroll
+    for (int m = 0; m < kM; ++m) asm volatile("" : "+v"(kf[0][m]), "+v"(kf[1][m]), "+v"(kf[2][m]), "+v"(kf[3][m]));
     while (t0 < t_end) {
         const uint64_t full = B.full, keep = B.keep;
         // windows that end inside the block: this lane's token and chunk, byte by byte
@@ -359,7 +372,10 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
         // are the same on every path; positions reach 2^31: no sum past t_end)
         const bool more = t_end - t0 > kBlock * NW;
         const int t_next = more ? t0 + kBlock * NW : t_end;
-        if (more) B = locate(t_next);
+        if (more) {
+            B = locate(t_next);
+            classify(B, t_next);
+        }
         load_k(B, t_next);
         // tokens past the split's end: no probability, and no value that is not a number
         if (t_end - t0 < kBlock) {
@@ -505,7 +521,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
 // Merge of the split partials of one (row, head): NW waves, each over every NW-th state with a
 // maximum of its own, so that no load waits for another; a lane has the same D / 64 dims of all.
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8Params p) {
+__global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8States p) {
     constexpr int kN = D / 64;
     constexpr int kAhead = 8;  // states in flight
     typedef float out_t __attribute__((ext_vector_type(kN)));
@@ -516,7 +532,7 @@ __global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t base = int64_t(bh) * p.splits, stride = 1;
     int count = p.splits;
-    if (p.n_k_rows != nullptr) {
+    if (p.ws_plan != nullptr) {
         // (the clamps only restate what the plan guarantees: at most splits + batch items)
         const int b = bh / p.h_q, most = p.splits + p.batch;
         const int first = min(max(p.ws_plan[b], 0), most);
@@ -587,13 +603,14 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     const bool ragged = p.n_k_rows != nullptr;
     const dim3 grid(unsigned(p.direct ? p.batch : ragged ? p.splits + p.batch : p.splits),
                     unsigned(p.h_kv * p.subgroups), unsigned(p.direct || ragged ? 1 : p.batch));
-    if (p.direct) {
+    // whole rows: eight waves while every CU has one, four where the rows are more
+    if (p.direct && int64_t(grid.x) * grid.y <= 256) {
         hipLaunchKernelGGL((decode_q8_kernel<D, NT, kDirectWaves>), grid, dim3(kDirectWaves * 64), 0, stream, p);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((decode_q8_kernel<D, NT, kWaves>), grid, dim3(kWaves * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || p.direct) return e;
     // the merge's waves by the states of a row: a ragged batch's longest rows have some times the
     // average
     const int64_t states = ragged ? 3 * int64_t(p.splits) / p.batch : p.splits;
@@ -617,7 +634,7 @@ hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t s
     if (!p.direct && p.n_k_rows == nullptr &&
         (int64_t(p.splits) * p.split_tokens < p.n_valid || p.split_tokens % kDecodeQ8TokenStep != 0))
         return hipErrorInvalidValue;
-    if (p.n_k_rows != nullptr && (p.q_pos_rows == nullptr || p.ws_plan == nullptr || p.splits > kDecodeMaxSplits - 1))
+    if (p.n_k_rows != nullptr && (p.q_pos_rows == nullptr || (!p.direct && (p.ws_plan == nullptr || p.splits > kDecodeMaxSplits - 1))))
         return hipErrorInvalidValue;
     (void)hipGetLastError();
     if (p.heads_per_block > 16)

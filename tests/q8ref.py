@@ -63,7 +63,8 @@ def norm_rotate(x, weight, eps, pos, theta):
     y = x * w * rs
     a = pos.astype(np.float64)[:, None, None] * theta
     lo, hi = y[..., : d // 2], y[..., d // 2:]
-    r = np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], axis=-1)
+    with np.errstate(invalid="ignore"):  # (an infinity times 0)
+        r = np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], axis=-1)
     m = np.abs(lo) + np.abs(hi)
     return r, 2.0 ** -17 * np.concatenate([m, m], axis=-1)
 
