@@ -1232,8 +1232,8 @@ int append_normed_impl(const char* fn, const void* q, const void* k_new, const v
                     ? "%s: pos0 %lld with pos_rows (the rows' positions are theirs: pass 0), %lld new tokens"
                     : "%s: %lld tokens at position %lld do not fit the cache", fn,
                     (long long)(pos_rows != nullptr ? pos0 : n_new), (long long)(pos_rows != nullptr ? n_new : pos0));
-    if (n_new > kPosLimit || int64_t(batch) * n_new > kPosLimit)
-        return fail(ATF_EINVAL, "%s: too many tokens for one call", fn);
+    if (n_new > kPosLimit || int64_t(batch) * n_new > (int64_t(1) << 26))
+        return fail(ATF_EINVAL, "%s: more than 2^26 tokens in one call", fn);
     if (int64_t(h_q) + 2 * int64_t(h_kv) > 65535)
         return fail(ATF_EUNSUPPORTED, "%s: more than 65535 heads", fn);
     atf::AppendNormedParams p{};

@@ -180,6 +180,7 @@ struct ReadQ8Params {
     int32_t batch, n_k, pos0, h_kv;
     int32_t src_tokens, scale_tokens, dst_tokens;
     int32_t max_pages, num_pages, page_tokens;
+    uint32_t key_blocks;         // set by the launcher
 };
 
 // One pass of RoPE over a pair-chunk-major K cache (rotate.hip): key t of every (batch,
