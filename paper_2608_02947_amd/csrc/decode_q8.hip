@@ -89,41 +89,67 @@ __device__ __forceinline__ int scan_lanes(int x) {
     return dpp_add<0x143, 0xC>(x);  // from that of row 1 to rows 2 and 3
 }
 
-// Keys of ragged row r that its query reaches, within [0, n_k], and their steps.
-__device__ __forceinline__ int row_keys(const DecodeQ8Params& p, int r) {
-    const int nk = min(max(p.n_k_rows[r], 0), p.n_k);
-    const int qp = min(max(p.q_pos_rows[r], 0), 0x7FFFFFFD);
-    return min(nk, qp + 1);
+// A row of a ragged batch: the position of its query, and the keys that it reaches, in [0, n_k].
+struct Row {
+    int q_pos, keys;
+};
+__device__ __forceinline__ Row row_of(const DecodeQ8Params& p, int r) {
+    Row x = {0, 0};
+    if (r < p.batch) {
+        x.q_pos = min(max(p.q_pos_rows[r], 0), 0x7FFFFFFD);
+        x.keys = min(min(max(p.n_k_rows[r], 0), p.n_k), x.q_pos + 1);
+    }
+    return x;
 }
-__device__ __forceinline__ int row_steps(const DecodeQ8Params& p, int r) {
-    return r < p.batch ? (row_keys(p, r) + kDecodeQ8TokenStep - 1) / kDecodeQ8TokenStep : 0;
+
+// ceil(n / span) for n and span up to 2^23, with inv near 1 / span
+__device__ __forceinline__ int pieces(int n, int span, float inv) {
+    const int up = n + span - 1;
+    int q = int(float(up) * inv);
+    const int rest = up - q * span;
+    return q + (rest >= span ? 1 : 0) - (rest < 0 ? 1 : 0);
 }
 
 // The work plan of a ragged batch, the same in every wave that computes it: rows in steps of
 // kDecodeQ8TokenStep tokens, cut into items of equal `tokens`, about p.splits in all: as many as
 // run at once, so the span grows until they are no more than that, unless the batch has so many
 // rows that their last, shorter items are a large part (p.splits + p.batch bounds them then).
-// Items are numbered row by row.  Returns the row of `item` (-1 past the last) and its
+// Items are numbered row by row.  Returns the row of `item` (-1 past the last), its Row and its
 // first token; with `plan` set, writes the index of each row's first item and, at plan[batch],
 // their number.
-__device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, int& t_first, int64_t& tokens, int32_t* plan) {
+__device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, Row& out, int& t_first, int64_t& tokens,
+                                           int32_t* plan) {
     const int lane = threadIdx.x & 63;
-    const int own = row_steps(p, lane);  // of the first 64 rows: mostly all
-    const auto steps = [&](int r0) __attribute__((always_inline)) { return r0 == 0 ? own : row_steps(p, r0 + lane); };
-    int64_t total = 0;
-    for (int r0 = 0; r0 < p.batch; r0 += 64) total += __builtin_amdgcn_readlane(scan_lanes(steps(r0)), 63);
-    int span = max(1, int((total + p.splits - 1) / p.splits));
-    for (int round = 0; round < 8; ++round) {
+    const auto steps_of = [](const Row& x) __attribute__((always_inline)) {
+        return int((uint32_t(x.keys) + kDecodeQ8TokenStep - 1) / kDecodeQ8TokenStep);
+    };
+    const Row own = row_of(p, lane);  // of the first 64 rows: mostly all
+    const int own_steps = steps_of(own);
+    const auto steps = [&](int r0) __attribute__((always_inline)) {
+        return r0 == 0 ? own_steps : steps_of(row_of(p, r0 + lane));
+    };
+    float total = 0.f;  // (a guess of the span is all it is for)
+    int alive = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += 64) {
+        const int n = steps(r0);
+        total += float(__builtin_amdgcn_readlane(scan_lanes(n), 63));
+        alive += __builtin_popcountll(__ballot(n > 0));
+    }
+    const bool many = 4 * alive > 3 * p.splits;
+    // (a row's last item is half a span on average)
+    int span = max(1, int(__builtin_ceilf(total / float(many ? p.splits : p.splits - alive / 2))));
+    float inv = 1.f / float(span);
+    for (int round = 0; round < 8 && !many; ++round) {
         int items = 0;
         for (int r0 = 0; r0 < p.batch; r0 += 64)
-            items += __builtin_amdgcn_readlane(scan_lanes((steps(r0) + span - 1) / span), 63);
-        // (many rows: spans long enough for so few items would leave whole rows to one of them)
-        if (items <= p.splits || (round == 0 && items > p.splits + p.splits / 4)) break;
-        span = max(span + 1, int(int64_t(span) * items / p.splits));
+            items += __builtin_amdgcn_readlane(scan_lanes(pieces(steps(r0), span, inv)), 63);
+        if (items <= p.splits) break;
+        span = max(span + 1, int(float(span) * float(items) / float(p.splits)));
+        inv = 1.f / float(span);
     }
     int row = -1, first = 0, before = 0;
     for (int r0 = 0; r0 < p.batch; r0 += 64) {
-        const int cnt = (steps(r0) + span - 1) / span;
+        const int cnt = pieces(steps(r0), span, inv);
         const int incl = before + scan_lanes(cnt);
         if (plan != nullptr && r0 + lane < p.batch) plan[r0 + lane] = incl - cnt;
         const uint64_t hit = __ballot(item < incl);
@@ -131,6 +157,8 @@ __device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, in
             const int l = __builtin_ctzll(hit);
             row = r0 + l;
             first = item - __builtin_amdgcn_readlane(incl - cnt, l);
+            out = r0 == 0 ? Row{__builtin_amdgcn_readlane(own.q_pos, l), __builtin_amdgcn_readlane(own.keys, l)}
+                          : row_of(p, row);
         }
         before = __builtin_amdgcn_readlane(incl, 63);
     }
@@ -178,16 +206,18 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
         t_begin = 0;
         t_end = p.n_valid;
         if (p.n_k_rows != nullptr) {
-            q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
-            t_end = row_keys(p, b);
+            const Row r = row_of(p, b);
+            q_pos = r.q_pos;
+            t_end = r.keys;
         }
     } else if (p.n_k_rows != nullptr) {
         int64_t span;
         int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
-        b = ragged_item(p, split, t_begin, span, plan);
+        Row r = {0, 0};
+        b = ragged_item(p, split, r, t_begin, span, plan);
         if (b < 0) return;
-        q_pos = min(max(p.q_pos_rows[b], 0), 0x7FFFFFFD);
-        t_end = int(min(int64_t(row_keys(p, b)), t_begin + span));
+        q_pos = r.q_pos;
+        t_end = int(min(int64_t(r.keys), t_begin + span));
         slot0 = int64_t(split) * p.h_q + hq0;
     } else {
         b = blockIdx.z;
@@ -535,8 +565,9 @@ __global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8
     if (p.ws_plan != nullptr) {
         // (the clamps only restate what the plan guarantees: at most splits + batch items)
         const int b = bh / p.h_q, most = p.splits + p.batch;
-        const int first = min(max(p.ws_plan[b], 0), most);
-        count = min(max(p.ws_plan[b + 1] - first, 0), most - first);
+        const auto* plan = (const_i32*)(p.ws_plan + b);
+        const int first = min(max(plan[0], 0), most);
+        count = min(max(plan[1] - first, 0), most - first);
         base = int64_t(first) * p.h_q + bh % p.h_q;
         stride = p.h_q;
     }
