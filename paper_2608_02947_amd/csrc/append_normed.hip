@@ -147,114 +147,90 @@ __device__ __forceinline__ Token locate(const AppendNormedParams& p, int b, int 
     return k;
 }
 
-// The values of whole 16-token blocks (and of the parts at a row's ends): D / 4 lanes take a
-// block, 4 dims of its 16 tokens each, so that a block is turned to dim-major in the lane's
-// registers and stored 16 bytes at a time.
+// The tokens of row b that its caches have room for: [0, n), and those of them at its ends that
+// do not fill a 16-token block of the V cache: [0, head) and [tail, n).
+struct Ends {
+    int first, n, head, tail;
+};
+__device__ __forceinline__ Ends ends_of(const AppendNormedParams& p, int b) {
+    Ends e;
+    e.first = p.pos_rows != nullptr ? p.pos_rows[b] : p.pos0;
+    const int64_t room = p.block_table != nullptr ? int64_t(p.max_pages) * p.page_tokens : p.cache_tokens;
+    e.n = e.first < 0 ? 0 : int(max(int64_t(0), min(int64_t(p.n_new), room - e.first)));
+    e.head = min(e.n, (16 - (e.first & 15)) & 15);
+    e.tail = max(e.head, e.n - ((e.first + e.n) & 15));
+    return e;
+}
+
+// The values of whole 16-token blocks: D / 2 lanes take a block, 2 dims of its 16 tokens each, so
+// that a block is turned to dim-major in the lane's registers and stored 16 bytes at a time.
 template <int D, bool kQ8, bool kStream>
 __device__ __forceinline__ void value_blocks(const AppendNormedParams& p, uint32_t wave) {
-    constexpr int kLanes = D / 4;
+    constexpr int kLanes = D / 2;
     const int lane = threadIdx.x & 63;
-    const int x = lane % kLanes;  // dims 4x .. 4x + 3
+    const int x = lane % kLanes;  // dims 2x, 2x + 1
     const uint32_t nblk = (uint32_t(p.n_new) + 14u) / 16u + 1u;
     const uint32_t units = uint32_t(p.batch) * nblk * uint32_t(p.h_kv);
     const uint32_t unit = wave * (64 / kLanes) + lane / kLanes, u = min(unit, units - 1);
     const int g = int(u % uint32_t(p.h_kv));
     const uint32_t rest = u / uint32_t(p.h_kv);
     const int b = int(rest / nblk), k = int(rest % nblk);
-    const int first = p.pos_rows != nullptr ? p.pos_rows[b] : p.pos0;
-    // the block's first token in the call, and those of its tokens that are in the call
-    const int t0 = 16 * k - (first & 15);
-    int lo = max(0, -t0), hi = min(16, p.n_new - t0);
-    const Token at = locate(p, b, max(t0, 0), unit < units && hi > lo);
-    if (!at.stored) hi = lo;
-    hi = min(hi, at.cap - (at.tok & ~15));  // (a contiguous cache may end inside the block)
-    if (__all(hi <= lo)) return;
+    const Ends e = ends_of(p, b);
+    const int t0 = 16 * k - (e.first & 15);  // the block's first token in the call
+    const Token at = locate(p, b, max(t0, 0), unit < units && t0 >= e.head && t0 + 16 <= e.tail);
+    if (!__any(at.stored)) return;
     const int64_t row = int64_t(p.h_kv) * D;
-    const uint16_t* src = p.v_src + ((int64_t(b) * p.n_new + t0) * p.h_kv + g) * D + 4 * x;
-    const bool whole = lo == 0 && hi == 16;
-    uint2 v[16];
-    if (__all(whole)) {
+    const uint16_t* src = p.v_src + ((int64_t(b) * p.n_new + (at.stored ? t0 : 0)) * p.h_kv + g) * D + 2 * x;
+    uint32_t v[16];
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            const u32x2_t y = load_from<kStream, u32x2_t>(src + t * row);
-            v[t] = make_uint2(y[0], y[1]);
-        }
-    } else {
-#pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            v[t] = make_uint2(0u, 0u);
-            if (t >= lo && t < hi) v[t] = *reinterpret_cast<const uint2*>(src + t * row);
-        }
-    }
+    for (int t = 0; t < 16; ++t) v[t] = load_from<kStream, uint32_t>(src + (at.stored ? t * row : 0));
     const int64_t eg = at.entry * p.h_kv + g;
-    const int64_t block = (eg * ((at.cap + 15) / 16) + at.tok / 16) * D + 4 * x;  // row of dim 4x
+    const int64_t block = (eg * ((int64_t(at.cap) + 15) / 16) + at.tok / 16) * D + 2 * x;  // row of dim 2x
+    u32x4_t out[2][kQ8 ? 1 : 2];
     if constexpr (kQ8) {
-        uint32_t byte[16], w[16];
+        uint32_t byte[16];
+        u32x4_t bytes;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            const float y[4] = {bf_lo(v[t].x), bf_hi(v[t].x), bf_lo(v[t].y), bf_hi(v[t].y)};
-            uint32_t m = max_lanes<16>(finite_max<4>(y));
-            if constexpr (kLanes == 32) {
-                const auto both = __builtin_amdgcn_permlane16_swap(m, m, false, false);
-                m = max(both[0], both[1]);
-            }
-            byte[t] = q8::scale_byte(m);
-            const float inv = q8::inverse_power(byte[t]);
-            w[t] = q8::pack4(q8::scaled(y[0], inv), q8::scaled(y[1], inv), q8::scaled(y[2], inv), q8::scaled(y[3], inv));
-        }
-        uint8_t* dst = static_cast<uint8_t*>(p.v_dst) + block * 16;
-        uint8_t* scale = p.v_scale + eg * p.scale_tokens + (at.tok & ~15);
-        if (whole) {
-            u32x4_t out[4], bytes;  // out[dim][4 tokens]
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[2];  // two tokens of two dims each
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t* q = &w[4 * i];
-                const uint32_t ab = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), cd = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
-                const uint32_t AB = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), CD = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
-                out[0][i] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
-                out[1][i] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
-                out[2][i] = __builtin_amdgcn_perm(CD, AB, 0x05040100u);
-                out[3][i] = __builtin_amdgcn_perm(CD, AB, 0x07060302u);
-                bytes[i] = byte[4 * i] | byte[4 * i + 1] << 8 | byte[4 * i + 2] << 16 | byte[4 * i + 3] << 24;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4_t*>(dst + 16 * j) = out[j];
-            if (x == 0) *reinterpret_cast<u32x4_t*>(scale) = bytes;
-        } else {
-#pragma unroll
-            for (int t = 0; t < 16; ++t)
-                if (t >= lo && t < hi) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) dst[16 * j + t] = uint8_t(w[t] >> (8 * j));
-                    if (x == 0) scale[t] = uint8_t(byte[t]);
+            for (int j = 0; j < 4; ++j) {
+                const int t = 4 * i + j;
+                const float y[2] = {bf_lo(v[t]), bf_hi(v[t])};
+                uint32_t m = max_lanes<16>(finite_max<2>(y));
+                const auto m16 = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+                m = max(m16[0], m16[1]);
+                if constexpr (kLanes == 64) {
+                    const auto m32 = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+                    m = max(m32[0], m32[1]);
                 }
+                byte[t] = q8::scale_byte(m);
+                const float inv = q8::inverse_power(byte[t]);
+                const float z0 = q8::scaled(y[0], inv), z1 = q8::scaled(y[1], inv);
+                w[j / 2] = j % 2 ? q8::pack2<1>(z0, z1, w[j / 2]) : q8::pack2<0>(z0, z1, 0u);
+            }
+            out[0][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
+            out[1][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
+            bytes[i] = byte[4 * i] | byte[4 * i + 1] << 8 | byte[4 * i + 2] << 16 | byte[4 * i + 3] << 24;
+        }
+        if (at.stored) {
+            uint8_t* dst = static_cast<uint8_t*>(p.v_dst) + block * 16;
+            *reinterpret_cast<u32x4_t*>(dst) = out[0][0];
+            *reinterpret_cast<u32x4_t*>(dst + 16) = out[1][0];
+            if (x == 0) *reinterpret_cast<u32x4_t*>(p.v_scale + eg * p.scale_tokens + at.tok) = bytes;
         }
     } else {
         // slot 8h + 4a + b of a dim's row holds token 8a + 4h + b
-        uint16_t* dst = static_cast<uint16_t*>(p.v_dst) + block * 16;
-        if (whole) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32x4_t out[2];
+        for (int i = 0; i < 8; ++i) {
+            const int t = 8 * (i / 2 % 2) + 4 * (i / 4) + 2 * (i % 2);
+            out[0][i / 4][i % 4] = __builtin_amdgcn_perm(v[t + 1], v[t], 0x05040100u);
+            out[1][i / 4][i % 4] = __builtin_amdgcn_perm(v[t + 1], v[t], 0x07060302u);
+        }
+        if (at.stored) {
+            uint16_t* dst = static_cast<uint16_t*>(p.v_dst) + block * 16;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = 8 * (i / 2 % 2) + 4 * (i / 4) + 2 * (i % 2);
-                    out[i / 4][i % 4] = __builtin_amdgcn_perm(j / 2 ? v[t + 1].y : v[t + 1].x, j / 2 ? v[t].y : v[t].x,
-                                                              j % 2 ? 0x07060302u : 0x05040100u);
-                }
-                *reinterpret_cast<u32x4_t*>(dst + 16 * j) = out[0];
-                *reinterpret_cast<u32x4_t*>(dst + 16 * j + 8) = out[1];
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 16; ++t)
-                if (t >= lo && t < hi) {
-                    uint16_t* to = dst + 8 * (t / 4 % 2) + 4 * (t / 8) + t % 4;
-                    to[0] = uint16_t(v[t].x);
-                    to[16] = uint16_t(v[t].x >> 16);
-                    to[32] = uint16_t(v[t].y);
-                    to[48] = uint16_t(v[t].y >> 16);
-                }
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4_t*>(dst + 8 * j) = out[j / 2][j % 2];
         }
     }
 }
@@ -275,19 +251,35 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
         return;
     }
     wave -= p.block_waves;
-    if (wave >= p.row_waves) return;
-    // this wave's tokens and its heads, all of one kind: queries, keys, values
+    // this wave's tokens and its heads, all of one kind: values by themselves, queries, keys
     const int hpw = p.heads_per_wave;
     const uint32_t q_parts = uint32_t(p.h_q + hpw - 1) / uint32_t(hpw), k_parts = uint32_t(p.h_kv + hpw - 1) / uint32_t(hpw);
-    const uint32_t parts = q_parts + k_parts + (p.value_rows ? k_parts : 0u);
+    const bool alone = wave < p.value_waves;
+    const uint32_t parts = alone ? k_parts : q_parts + k_parts;
+    if (!alone) wave -= p.value_waves;
     uint32_t part = wave % parts;
-    const int kind = part < q_parts ? 0 : part < q_parts + k_parts ? 1 : 2;
-    part -= kind == 0 ? 0u : kind == 1 ? q_parts : q_parts + k_parts;
+    const int kind = alone ? 2 : part < q_parts ? 0 : 1;
+    if (kind == 1) part -= q_parts;
     const int n_heads = kind == 0 ? p.h_q : p.h_kv;
     const int from = int(part) * hpw, to = min(from + hpw, n_heads);
-    const uint32_t rows = uint32_t(p.batch) * uint32_t(p.n_new);
+    const uint32_t rows = uint32_t(p.batch) * (alone && p.value_ends ? 32u : uint32_t(p.n_new));
     const uint32_t row = wave / parts * uint32_t(kTokens) + uint32_t(lane / kLanes);
-    const uint32_t r = min(row, rows - 1);
+    if (wave / parts * uint32_t(kTokens) >= rows) return;
+    uint32_t b, t;
+    bool given = row < rows;
+    if (alone && p.value_ends) {
+        // 32 places a row of the batch: the tokens before its first whole block, and after the last
+        b = min(row / 32u, uint32_t(p.batch) - 1u);
+        const uint32_t j = row % 32u;
+        const Ends e = ends_of(p, int(b));
+        t = j < 16u ? j : uint32_t(e.tail) + j - 16u;
+        given = given && (j < 16u ? int(t) < e.head : int(t) < e.n);
+        if (!given) t = 0;
+    } else {
+        b = min(row, rows - 1) / uint32_t(p.n_new);
+        t = min(row, rows - 1) - b * uint32_t(p.n_new);
+    }
+    const uint32_t r = b * uint32_t(p.n_new) + t;
     const int l = lane % kLanes;
     const int c = l % kChunks, hf = l / kChunks;  // pair-chunk, half of the pairs
     const uint16_t* src = (kind == 0 ? p.q : kind == 1 ? p.k_src : p.v_src) + int64_t(r) * n_heads * D + 8 * l;
@@ -299,8 +291,7 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     };
     load(from);
 
-    const uint32_t b = r / uint32_t(p.n_new);
-    const Token at = locate(p, int(b), int(r - b * uint32_t(p.n_new)), row < rows);
+    const Token at = locate(p, int(b), int(t), given);
     const int64_t eg0 = at.entry * p.h_kv;
     float wc[8], ws[8];  // ws with the half's sign: x'_own = own * wc + other * ws
     const float* weight = kind == 0 ? p.q_weight : p.k_weight;
@@ -416,18 +407,22 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     // one head a wave until the chip is full of waves, then as many as keep it full, so that a
     // token's angles serve them all
     const int64_t target = 4096;
-    p.value_rows = p.n_new < 8;
     const int64_t heads = p.h_q + p.h_kv;
     p.heads_per_wave = int32_t(std::min(heads, std::max<int64_t>(1, groups * heads / target)));
     const auto parts = [&](int64_t h) { return (h + p.heads_per_wave - 1) / p.heads_per_wave; };
-    const int64_t row_waves = groups * (parts(p.h_q) + (p.value_rows ? 2 : 1) * parts(p.h_kv));
+    const int64_t row_waves = groups * (parts(p.h_q) + parts(p.h_kv));
+    // values: token by token in a short call, else whole 16-token blocks (in whole workgroups) and
+    // the tokens at the rows' ends by themselves
+    const bool blocks = p.n_new >= 16;
     const int64_t units = int64_t(p.batch) * ((int64_t(p.n_new) + 14) / 16 + 1) * p.h_kv;
-    // whole workgroups of blocks
-    const int64_t block_waves = p.value_rows ? 0 : ((units + 256 / D - 1) / (256 / D) + 3) / 4 * 4;
-    const int64_t waves = row_waves + block_waves;
-    if (waves < 1 || waves > 0x7FFFFFFF || units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    p.row_waves = uint32_t(row_waves);
+    const int64_t block_waves = blocks ? ((units + 128 / D - 1) / (128 / D) + 3) / 4 * 4 : 0;
+    const bool aligned = p.pos_rows == nullptr && p.pos0 % 16 == 0 && p.n_new % 16 == 0;
+    p.value_ends = blocks;
+    const int64_t alone = blocks ? (aligned ? 0 : (int64_t(p.batch) * 32 + kTokens - 1) / kTokens) : groups;
+    const int64_t waves = block_waves + alone * parts(p.h_kv) + row_waves;
+    if (waves < 1 || waves >= (int64_t(1) << 26) || units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     p.block_waves = uint32_t(block_waves);
+    p.value_waves = uint32_t(alone * parts(p.h_kv));
     const dim3 grid(unsigned((waves + 3) / 4));
     // queries that the L2s (8 of 4 MB) cannot hold for their reader
     const bool past = int64_t(p.batch) * p.n_new * p.h_q * D * 2 > (32 << 20);

@@ -159,10 +159,10 @@ struct AppendNormedParams {
     int32_t cache_tokens;        // capacity of the contiguous caches
     int32_t scale_tokens;        // cache_tokens rounded up to 16, or page_tokens
     int32_t max_pages, num_pages, page_tokens;
-    // set by the launcher: heads of a wave, whether values go with them one token at a time (in
-    // 16-token blocks otherwise), the waves of the blocks, which come first, and of the rows
-    int32_t heads_per_wave, value_rows;
-    uint32_t block_waves, row_waves;
+    // set by the launcher: heads of a wave; waves of whole value blocks, which come first; waves
+    // of values by themselves, and whether those are only the tokens at the rows' ends
+    int32_t heads_per_wave, value_ends;
+    uint32_t block_waves, value_waves;
     uint32_t rope_rho_hi[kMaxPairs];
     uint32_t rope_rho_lo[kMaxPairs];
 };

@@ -41,5 +41,11 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
 }
 
+// two of them into the low (0) or the high half of a word
+template <int kHigh>
+__device__ __forceinline__ uint32_t pack2(float a, float b, uint32_t word) {
+    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(a, b, int(word), kHigh != 0));
+}
+
 }  // namespace q8
 }  // namespace atf
