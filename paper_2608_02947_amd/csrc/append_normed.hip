@@ -14,6 +14,7 @@
 #include "q8.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace atf {
 namespace {
@@ -92,16 +93,28 @@ __device__ __forceinline__ u32x4_t to_bf16(const float* y) {
     return r;
 }
 
-// The largest finite magnitude of n numbers, as bits (0 if there is none).
-template <int n>
-__device__ __forceinline__ uint32_t finite_max(const float* y) {
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// The largest magnitude of n numbers, as bits: of all of them (above the finite ones' bits if one
+// is not finite), or of the finite ones (0 if there is none).
+template <int n, bool kFinite>
+__device__ __forceinline__ uint32_t largest(const float* y) {
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < n; ++e) {
-        const uint32_t a = __float_as_uint(y[e]) & 0x7FFFFFFFu;
-        m = max(m, a < q8::kInfBits ? a : 0u);
+        const uint32_t a = magnitude(y[e]);
+        m = max(m, kFinite && a >= q8::kInfBits ? 0u : a);
     }
     return m;
+}
+
+// Calls f with whether every lane's numbers, whose largest magnitude is m, are plain ones.
+template <typename F>
+__device__ __forceinline__ void by_kind(uint32_t m, F f) {
+    if (__any(m > q8::kPlainBits))
+        f(std::false_type{});
+    else
+        f(std::true_type{});
 }
 
 template <bool kStream, typename T>
@@ -188,31 +201,39 @@ __device__ __forceinline__ void value_blocks(const AppendNormedParams& p, uint32
     const int64_t block = (eg * ((int64_t(at.cap) + 15) / 16) + at.tok / 16) * D + 2 * x;  // row of dim 2x
     u32x4_t out[2][kQ8 ? 1 : 2];
     if constexpr (kQ8) {
-        uint32_t byte[16];
-        u32x4_t bytes;
+        uint32_t all = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w[2];  // two tokens of two dims each
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int t = 4 * i + j;
-                const float y[2] = {bf_lo(v[t]), bf_hi(v[t])};
-                uint32_t m = max_lanes<16>(finite_max<2>(y));
-                const auto m16 = __builtin_amdgcn_permlane16_swap(m, m, false, false);
-                m = max(m16[0], m16[1]);
-                if constexpr (kLanes == 64) {
-                    const auto m32 = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-                    m = max(m32[0], m32[1]);
-                }
-                byte[t] = q8::scale_byte(m);
-                const float inv = q8::inverse_power(byte[t]);
-                const float z0 = q8::scaled(y[0], inv), z1 = q8::scaled(y[1], inv);
-                w[j / 2] = j % 2 ? q8::pack2<1>(z0, z1, w[j / 2]) : q8::pack2<0>(z0, z1, 0u);
-            }
-            out[0][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
-            out[1][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
-            bytes[i] = byte[4 * i] | byte[4 * i + 1] << 8 | byte[4 * i + 2] << 16 | byte[4 * i + 3] << 24;
+        for (int t = 0; t < 16; ++t) {
+            const float y[2] = {bf_lo(v[t]), bf_hi(v[t])};
+            all = max(all, largest<2, false>(y));
         }
+        u32x4_t bytes;
+        by_kind(all, [&](auto plain) __attribute__((always_inline)) {
+            constexpr bool kPlain = decltype(plain)::value;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w[2];  // two tokens of two dims each
+                bytes[i] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float y[2] = {bf_lo(v[4 * i + j]), bf_hi(v[4 * i + j])};
+                    uint32_t m = max_lanes<16>(largest<2, !kPlain>(y));
+                    const auto m16 = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+                    m = max(m16[0], m16[1]);
+                    if constexpr (kLanes == 64) {
+                        const auto m32 = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+                        m = max(m32[0], m32[1]);
+                    }
+                    const uint32_t byte = q8::scale_byte(m);
+                    const float inv = q8::inverse_power(byte);
+                    const float z0 = q8::scaled<kPlain>(y[0], inv), z1 = q8::scaled<kPlain>(y[1], inv);
+                    w[j / 2] = j % 2 ? q8::pack2<1>(z0, z1, w[j / 2]) : q8::pack2<0>(z0, z1, 0u);
+                    bytes[i] |= byte << (8 * j);
+                }
+                out[0][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
+                out[1][0][i] = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
+            }
+        });
         if (at.stored) {
             uint8_t* dst = static_cast<uint8_t*>(p.v_dst) + block * 16;
             *reinterpret_cast<u32x4_t*>(dst) = out[0][0];
@@ -333,6 +354,21 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
             for (int e = 0; e < 8; ++e) y[e] *= rs;
         }
     };
+    // a row's 8 numbers of this lane as e4m3, and the row's power
+    [[maybe_unused]] const auto quantised = [&](const float* y, uint32_t& byte) __attribute__((always_inline)) {
+        uint2 w;
+        const uint32_t m = max_lanes<kLanes>(largest<8, false>(y));
+        by_kind(m, [&](auto plain) __attribute__((always_inline)) {
+            constexpr bool kPlain = decltype(plain)::value;
+            byte = q8::scale_byte(kPlain ? m : max_lanes<kLanes>(largest<8, true>(y)));
+            const float inv = q8::inverse_power(byte);
+            float z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = q8::scaled<kPlain>(y[e], inv);
+            w = make_uint2(q8::pack4(z[0], z[1], z[2], z[3]), q8::pack4(z[4], z[5], z[6], z[7]));
+        });
+        return w;
+    };
     const auto query = [&](int h, u32x4_t v) __attribute__((always_inline)) {
         float y[8];
         turned(v, y);
@@ -343,14 +379,10 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
         turned(v, y);
         const int64_t to_k = (((eg0 + g) * kChunks + c) * at.cap + at.tok) * 16 + 8 * hf;
         if constexpr (kQ8) {
-            const uint32_t byte = q8::scale_byte(max_lanes<kLanes>(finite_max<8>(y)));
-            const float inv = q8::inverse_power(byte);
-            float z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = q8::scaled(y[e], inv);
+            uint32_t byte;
+            const uint2 w = quantised(y, byte);
             if (at.stored) {
-                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.k_dst) + to_k) =
-                    make_uint2(q8::pack4(z[0], z[1], z[2], z[3]), q8::pack4(z[4], z[5], z[6], z[7]));
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.k_dst) + to_k) = w;
                 if (l == 0) p.k_scale[(eg0 + g) * p.scale_tokens + at.tok] = uint8_t(byte);
             }
         } else if (at.stored) {
@@ -364,14 +396,10 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
             float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = e & 1 ? bf_hi(v[e / 2]) : bf_lo(v[e / 2]);
-            const uint32_t byte = q8::scale_byte(max_lanes<kLanes>(finite_max<8>(y)));
-            const float inv = q8::inverse_power(byte);
             uint8_t* dst = static_cast<uint8_t*>(p.v_dst) + to_v + at.tok % 16;
-            uint32_t w[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                w[i] = q8::pack4(q8::scaled(y[4 * i], inv), q8::scaled(y[4 * i + 1], inv),
-                                 q8::scaled(y[4 * i + 2], inv), q8::scaled(y[4 * i + 3], inv));
+            uint32_t byte;
+            const uint2 x2 = quantised(y, byte);
+            const uint32_t w[2] = {x2.x, x2.y};
             if (at.stored) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dst[16 * e] = uint8_t(w[e / 4] >> (8 * (e % 4)));

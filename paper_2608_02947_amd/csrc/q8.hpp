@@ -28,9 +28,15 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
 __device__ __forceinline__ float inverse_power(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Magnitudes whose largest has bits up to here are finite and meet 448 or less: nearly all
+// rows, whose numbers need no more than the product (kPlain below).
+constexpr uint32_t kPlainBits = (kMaxByte + 8) << 23 | 0x600000u;  // 448 * 2^119
+
 // x scaled by 2^-e, ready to be rounded: in range (the clamp binds at the largest power only),
 // and NaN where x is not finite
+template <bool kPlain>
 __device__ __forceinline__ float scaled(float x, float inv) {
+    if constexpr (kPlain) return x * inv;
     const float y = __builtin_amdgcn_fmed3f(x * inv, -448.f, 448.f);
     return fabsf(x) < INFINITY ? y : __uint_as_float(0x7FC00000u);
 }
