@@ -181,9 +181,10 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     __shared__ float red_m[NW][16 * NT];
     __shared__ float red_l[NW][16 * NT];
     __shared__ int s_w[kHalf];
-    // the queries and each wave's copy of them while the waves stream, then, a tile at a time, the
-    // waves' outputs [wave][head][D + 4]
-    constexpr int kQueries = 256 * kOps * (1 + NW), kMerge = NW * 16 * kOStride;
+    // the queries (and each wave's copy of them, where it is not in registers) while the waves
+    // stream, then, a tile at a time, the waves' outputs [wave][head][D + 4]
+    constexpr bool kQueryRegs = NT == 1 || D == 64;  // (the queries' registers: 2 tiles at d = 128 have none left)
+    constexpr int kQueries = 256 * kOps * (kQueryRegs ? 1 : 1 + NW), kMerge = NW * 16 * kOStride;
     __shared__ __attribute__((aligned(16))) float shared[kQueries > kMerge ? kQueries : kMerge];
 
     const int tid = threadIdx.x;
@@ -328,12 +329,24 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
         *reinterpret_cast<u32x4_t*>(&shared[256 * o + 4 * lane]) = z;
     }
     __syncthreads();
-    // this wave's copy of the queries, with the pairs outside q_keep zeroed
+    // the queries, with the pairs outside q_keep zeroed
     uint64_t q_keep = ~0ull;
-    float* const qm = &shared[256 * kOps * (1 + wave) + 4 * lane];
+    [[maybe_unused]] u32x4_t q_regs[kQueryRegs ? kOps : 1];
+    [[maybe_unused]] float* const q_lds = &shared[256 * kOps * (1 + wave) + 4 * lane];
+    const auto set_query = [&](int o, u32x4_t x) __attribute__((always_inline)) {
+        if constexpr (kQueryRegs)
+            q_regs[o] = x;
+        else
+            *reinterpret_cast<u32x4_t*>(q_lds + 256 * o) = x;
+    };
+    const auto query = [&](int o) __attribute__((always_inline)) {
+        if constexpr (kQueryRegs)
+            return q_regs[o];
+        else
+            return *reinterpret_cast<const u32x4_t*>(q_lds + 256 * o);
+    };
 #pragma unroll
-    for (int o = 0; o < kOps; ++o)
-        *reinterpret_cast<u32x4_t*>(qm + 256 * o) = *reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]);
+    for (int o = 0; o < kOps; ++o) set_query(o, *reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]));
 
     f32x4_t oacc[NT][kDB];
     float m_run[NT], m_thr[NT], m_neg[NT], l_run[NT];
@@ -378,9 +391,8 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
             q_keep = keep;
 #pragma unroll
             for (int o = 0; o < kOps; ++o)
-                *reinterpret_cast<u32x4_t*>(qm + 256 * o) =
-                    keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
-                               uint32_t(keep >> (8 * (4 * (o / 2 % kM) + g4))) & 0xFFu);
+                set_query(o, keep_pairs(*reinterpret_cast<const u32x4_t*>(&shared[256 * o + 4 * lane]),
+                                        uint32_t(keep >> (8 * (4 * (o / 2 % kM) + g4))) & 0xFFu));
         }
         f32x4_t sacc[NT][4];
 #pragma unroll
@@ -391,9 +403,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
                 const u32x4_t k0 = widen(kf[s][m][0], kf[s][m][1], power), k1 = widen(kf[s][m][2], kf[s][m][3], power);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(qm + 256 * (2 * kM * n + 2 * m));
-                    sacc[n][s] = mfma16(k0, q[0], m == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sacc[n][s]);
-                    sacc[n][s] = mfma16(k1, q[64], sacc[n][s]);
+                    const int o = 2 * kM * n + 2 * m;
+                    sacc[n][s] = mfma16(k0, query(o), m == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sacc[n][s]);
+                    sacc[n][s] = mfma16(k1, query(o + 1), sacc[n][s]);
                 }
             }
         }
