@@ -56,22 +56,28 @@ __device__ __forceinline__ uint32_t other_lane(uint32_t x) {
 
 // cos and sin of the angle of pair rho (0.64 fixed point, revolutions) at position pos.  The
 // nearest quarter turn is taken off the 32-bit fraction in integers; what is left, at most
-// pi/4, goes through the Taylor series to x^9 and x^10 (truncation below 2^-28), so both are
-// within about an ulp: 8-bit keys round on from here, and the hardware's own sine is 2^-20 off.
+// pi/4, is turned to radians in two floats, whose first goes through the Taylor series to x^9 and
+// x^10 (truncation below 2^-28) and whose second is added to first order.  Both are within about
+// 0.7 ulp: 8-bit keys round on from here, where every error that could be 2^-24 shows as numbers
+// rounded to the other side (the hardware's own sine is 2^-20 off).
 __device__ __forceinline__ void cos_sin(uint32_t pos, uint32_t rho_hi, uint32_t rho_lo, float& cs, float& sn) {
     const uint32_t f = pos * rho_hi + __umulhi(pos, rho_lo);
     const uint32_t quarter = (f + 0x20000000u) >> 30;
-    const float x = float(int32_t(f - (quarter << 30))) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+    const int32_t r = int32_t(f - (quarter << 30));
+    const float rh = float(r), rl = float(r - int32_t(rh));
+    constexpr float kUnit = 1.4629180792671596e-9f, kUnitLow = float(1.4629180792671596e-9 - double(kUnit));  // 2 pi / 2^32
+    const float x = rh * kUnit;
+    const float low = __builtin_fmaf(rh, kUnit, -x) + __builtin_fmaf(rh, kUnitLow, rl * kUnit);
     const float y = x * x;
     float s = __builtin_fmaf(y, 2.7557319e-6f, -1.9841270e-4f);
     s = __builtin_fmaf(y, s, 8.3333333e-3f);
     s = __builtin_fmaf(y, s, -1.6666667e-1f);
-    s = __builtin_fmaf(x * y, s, x);
+    s = __builtin_fmaf(x * y, s, low) + x;
     float c = __builtin_fmaf(y, -2.7557319e-7f, 2.4801587e-5f);
     c = __builtin_fmaf(y, c, -1.3888889e-3f);
     c = __builtin_fmaf(y, c, 4.1666667e-2f);
     c = __builtin_fmaf(y, c, -0.5f);
-    c = __builtin_fmaf(y, c, 1.f);
+    c = __builtin_fmaf(y, c, -x * low) + 1.f;
     const bool swap = quarter & 1;
     const float a = swap ? s : c, b = swap ? c : s;
     cs = (quarter + 1) & 2 ? -a : a;
@@ -349,7 +355,11 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
             y[2 * i + 1] = __builtin_fmaf(a1, wc[2 * i + 1], bf_hi(o) * ws[2 * i + 1]);
         }
         if (weight != nullptr) {
-            const float rs = rsqrtf(__builtin_fmaf(sum_lanes<kLanes>(ss), 1.f / D, p.eps));
+            // (one Newton step on the hardware's root, which is an ulp off)
+            const float mean = __builtin_fmaf(sum_lanes<kLanes>(ss), 1.f / D, p.eps);
+            float rs = rsqrtf(mean);
+            const float off = __builtin_fmaf(-mean * rs, rs, 1.f);
+            if (fabsf(off) < 0.5f) rs = __builtin_fmaf(0.5f * rs, off, rs);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= rs;
         }
