@@ -485,7 +485,8 @@ int atf_cache_append_normed(const void *q, const void *k_new, const void *v_new,
                             void *hip_stream);
 
 /* atf_cache_append_normed into pages (layouts and tables as atf_cache_append_paged; tokens whose
- * table entry is outside [0, num_pages) or past the table are not stored). */
+ * table entry is outside [0, num_pages) or past the table are not stored).  Pages that a call
+ * writes must be one row's: where two rows write the same slot, it may hold some of either. */
 int atf_cache_append_paged_normed(const void *q, const void *k_new, const void *v_new, void *q_out,
                                   void *k_pages, void *v_pages, const int32_t *block_table,
                                   int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,

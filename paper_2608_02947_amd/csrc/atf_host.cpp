@@ -1186,7 +1186,8 @@ PagedArgs paged_args(const int32_t* block_table, int32_t max_pages, int32_t num_
     return pg;
 }
 
-int32_t scale_tokens(int64_t cache_tokens) { return static_cast<int32_t>((cache_tokens + 15) / 16 * 16); }
+// (2^31 at most)
+uint32_t scale_tokens(int64_t cache_tokens) { return static_cast<uint32_t>((cache_tokens + 15) / 16 * 16); }
 
 struct HeadNorms {
     const float* q_weight;
@@ -1398,7 +1399,7 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
     p.h_kv = h_kv;
     p.group = c.group;
     p.cache_tokens = c.cache_tokens;
-    p.scale_tokens = pg.block_table != nullptr ? pg.page_tokens : scale_tokens(p.cache_tokens);
+    p.scale_tokens = scale_tokens(pg.block_table != nullptr ? pg.page_tokens : p.cache_tokens);
     p.max_pages = pg.max_pages;
     p.num_pages = pg.num_pages;
     p.page_tokens = pg.page_tokens;

@@ -128,7 +128,7 @@ struct DecodeQ8Params : DecodeQ8States {
     const int32_t* block_table;
     int32_t n_k, q_pos, n_valid, h_kv, group;
     int32_t cache_tokens;
-    int32_t scale_tokens;     // cache_tokens rounded up to 16, or page_tokens
+    uint32_t scale_tokens;    // cache_tokens rounded up to 16 (2^31 at most), or page_tokens
     int32_t max_pages, num_pages, page_tokens;
     int32_t heads_per_block;  // at most 32; need not divide the group: the last of the
     int32_t subgroups;        // `subgroups` workgroups of a KV head takes what is left
@@ -157,7 +157,7 @@ struct AppendNormedParams {
     const int32_t* block_table;  // [B][max_pages], or nullptr: contiguous caches
     int32_t batch, n_new, h_q, h_kv, pos0;
     int32_t cache_tokens;        // capacity of the contiguous caches
-    int32_t scale_tokens;        // cache_tokens rounded up to 16, or page_tokens
+    uint32_t scale_tokens;       // cache_tokens rounded up to 16 (2^31 at most), or page_tokens
     int32_t max_pages, num_pages, page_tokens;
     // set by the launcher: heads of a wave; waves of whole value blocks, which come first; waves
     // of values by themselves, and whether those are only the tokens at the rows' ends
@@ -178,7 +178,8 @@ struct ReadQ8Params {
     uint16_t* v_dst;             // [B][h_kv][ceil(dst_tokens/16)][d][16]
     const int32_t* block_table;  // [B][max_pages], or nullptr: contiguous source
     int32_t batch, n_k, pos0, h_kv;
-    int32_t src_tokens, scale_tokens, dst_tokens;
+    int32_t src_tokens, dst_tokens;
+    uint32_t scale_tokens;
     int32_t max_pages, num_pages, page_tokens;
     uint32_t key_blocks;         // set by the launcher
 };

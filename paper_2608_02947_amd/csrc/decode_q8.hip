@@ -128,7 +128,7 @@ __device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, Ro
     const auto steps = [&](int r0) __attribute__((always_inline)) {
         return r0 == 0 ? own_steps : steps_of(row_of(p, r0 + lane));
     };
-    float total = 0.f;  // (a guess of the span is all it is for)
+    float total = 0.f;
     int alive = 0;
     for (int r0 = 0; r0 < p.batch; r0 += 64) {
         const int n = steps(r0);
@@ -136,8 +136,9 @@ __device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, Ro
         alive += __builtin_popcountll(__ballot(n > 0));
     }
     const bool many = 4 * alive > 3 * p.splits;
-    // (a row's last item is half a span on average)
-    int span = max(1, int(__builtin_ceilf(total / float(many ? p.splits : p.splits - alive / 2))));
+    if (total >= 16777216.f) total *= 1.0002f;  // above what it is rounded by, so that the bound holds
+    // (a row's last item is half a span on average; no row has more than 2^23 steps)
+    int span = max(1, int(fminf(__builtin_ceilf(total / float(many ? p.splits : p.splits - alive / 2)), 8388608.f)));
     float inv = 1.f / float(span);
     for (int round = 0; round < 8 && !many; ++round) {
         int items = 0;
@@ -233,8 +234,8 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     const uint64_t zeros = reinterpret_cast<uint64_t>(g_zeros);
     const int tk = 16 * (r16 >> 2) + (r16 & 3);  // this lane's token of tile 0 (tile s adds 4 s)
 
-    // a block: the addresses of the entries that hold its two halves of 32 tokens (a page holds
-    // whole halves; `a`, and how much further `b` is), and its pairs kept at every token and at some
+    // a block: where its two halves of 32 tokens are (a page holds whole halves), and its pairs
+    // kept at every token and at some
     struct Place {
         uint64_t k, ks, v, vs;  // of the half's first token in K chunk 0, V block, scales
     };

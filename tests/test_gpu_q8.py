@@ -471,6 +471,70 @@ def test_decode_nan_rows():
         assert torch.isnan(lse[1]).all() and torch.isfinite(lse[[0, 2]]).all()
 
 
+def test_decodes_at_once_and_one_after_another():
+    """Two decodes at once on two streams, each with a workspace of its own, and decodes of
+    different sizes one after another in one workspace: the bits of each alone."""
+    import paper_2608_02947_amd as atf
+    note("decodes at once")
+    d, T = 128, 3000
+    win, _ = window("exact", d)
+    calls, spaces, outs = [], [], []
+    for i, (B, h_q, h_kv, ragged) in enumerate([(2, 8, 2, False), (3, 20, 1, True), (1, 4, 4, True)]):
+        k, ke, v, ve = q8_caches(6, h_kv, 544, d, 70 + i)
+        (kc, ks), (vc, vs) = to_layout(k, ke, False), to_layout(v, ve, True)
+        if ragged:  # 544-token pages, the first of them in every row
+            table = torch.tensor([[0, 1 + b, 2, 5, 3, 4] for b in range(B)], dtype=torch.int32, device=DEV)
+            rows = [torch.tensor([T - 700 * b - x for b in range(B)], dtype=torch.int32, device=DEV) for x in (0, 1)]
+        else:
+            k, ke, v, ve = q8_caches(B, h_kv, T, d, 80 + i)
+            (kc, ks), (vc, vs) = to_layout(k, ke, False), to_layout(v, ve, True)
+        q = randn((B, h_q, d), 60 + i).to(DEV)
+
+        def call(out, ws, stream=None, q=q, c=(kc, ks, vc, vs), more=(table, *rows) if ragged else None):
+            o, lse = out
+            if more is None:
+                atf.atf_decode_q8(q, *c, o, lse, T - 1, win, ws, stream=stream)
+            else:
+                atf.atf_decode_paged_q8(q, *c, o, lse, *more, T, win, ws, stream=stream)
+        calls.append(call)
+        spaces.append(workspace(B, h_q, h_kv, T, d))
+        outs.append((torch.zeros_like(q), torch.zeros((B, h_q), device=DEV)))
+
+    def run(spaces, streams=(None,) * 3):
+        for o, lse in outs:
+            o.zero_(), lse.zero_()
+        torch.cuda.synchronize()
+        for call, out, ws, s in zip(calls, outs, spaces, streams):
+            call(out, ws, s)
+        torch.cuda.synchronize()
+        return [x.clone() for out in outs for x in out]
+
+    alone = run(spaces)
+    streams = [torch.cuda.Stream() for _ in calls]
+    for how in [(spaces, streams)] * 3 + [([max(spaces, key=torch.Tensor.numel)] * 3,)]:
+        assert all(torch.equal(a, b) for a, b in zip(alone, run(*how)))
+
+
+def test_binding_refuses_views_and_types():
+    import paper_2608_02947_amd as atf
+    note("views and types")
+    d = 64
+    win, _ = window("exact", d)
+    c = Case(d, 4, 2, 2, 3, True, [0, 5], 40)
+    q, k = c.q.to(DEV), c.k.to(DEV)
+    good = [q, k, k.clone(), q.clone(), c.kc, c.ks, c.vc, c.vs]
+    atf.atf_cache_append_q8(*good, 0, win)
+    for i, bad in ((0, q.transpose(0, 1).contiguous().transpose(0, 1)), (1, k.float()), (3, q.to(torch.float16)),
+                   (4, c.kc.view(torch.uint8)), (5, c.ks.view(torch.uint8)), (6, c.vc.cpu())):
+        with pytest.raises((TypeError, ValueError)):
+            atf.atf_cache_append_q8(*[bad if j == i else x for j, x in enumerate(good)], 0, win)
+    with pytest.raises((TypeError, ValueError)):
+        atf.atf_cache_append_q8(*good, 0, win, q_weight=torch.ones(d, dtype=BF, device=DEV))
+    with pytest.raises((TypeError, ValueError)):
+        atf.atf_cache_append_q8(*good, 0, win, pos_rows=torch.zeros(2, dtype=torch.int64, device=DEV))
+    torch.cuda.synchronize()
+
+
 # ---- together, as a server uses them
 
 def test_prompt_then_steps_captured():

@@ -98,6 +98,18 @@ def test_append_refusals(scaled, pages):
         assert call(cap=0) == EINVAL and call(cap=2 ** 31) == EINVAL
 
 
+def test_largest_capacity():
+    """Scales of the longest caches, 2^31 a head, are counted as such: buffers apart are accepted."""
+    lib, far = atf.library(), 1 << 44
+    (w, keep), cap = _window(64), 2 ** 31 - 1
+    at = [None] + [far * i for i in (1, 2)] + [None] + [far * i for i in (3, 4, 5, 6)]
+    assert lib.atf_cache_append_q8(*at, 1, 0, 0, None, 0, 1, cap, ctypes.byref(w), None, None, None, 1e-6, None) == OK
+    assert lib.atf_cache_read_q8(*[far * i for i in range(1, 7)], 1, 0, cap, 1, 64, cap, cap, None) == OK
+    # the same buffers nearer than a head's 2^31 scales
+    at[5], at[7] = far, far + 2 ** 31 - 16
+    assert lib.atf_cache_append_q8(*at, 1, 0, 0, None, 0, 1, cap, ctypes.byref(w), None, None, None, 1e-6, None) == EINVAL
+
+
 @pytest.mark.parametrize("pages", [False, True], ids=["contiguous", "paged"])
 def test_read_refusals(pages):
     lib = atf.library()
