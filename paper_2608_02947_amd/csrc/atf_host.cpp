@@ -333,9 +333,6 @@ int32_t decode_plan_items(int32_t cols, bool cols16) {
 // ---- Decode over 8-bit caches: `groups` workgroups without splits, (row, KV head) pairs, or
 // parts of them where a KV head has more than 32 heads; `tiles` 1 or 2 of 16 heads.
 
-// Workgroups of 4 waves that run at once: 2 a CU, 3 at d = 64 with one tile.
-int32_t decode_q8_slots(int32_t head_dim, int32_t tiles) { return head_dim == 64 && tiles == 1 ? 768 : 512; }
-
 // Whether a row is one workgroup's, which writes the output: no partial states, no merge (3 to 5
 // us), but a row's keys in a row.  With as many rows as CUs always (uniform batches; us, split ->
 // whole: 32 rows of 1,000 keys 24/8 heads 19.9 -> 17.0, of 8,000 86.6 -> 83.0), but for those
@@ -343,22 +340,47 @@ int32_t decode_q8_slots(int32_t head_dim, int32_t tiles) { return head_dim == 64
 // 120); with fewer while a row costs less than the merge, and the more of the chip's time the
 // rows fill, the longer (d = 128: 8 rows of 640 keys 12.4 -> 10.1, of 1,500 14 -> 15; 16 of
 // 1,500 18.6 -> 18.1, of 3,000 24.8 -> 26.3; 20 of 4,000 35.2 -> 34.2; d = 64, 16/16 heads:
-// 1 row of 1,000 8.6 -> 8.5, 8 of 2,000 14.6 -> 14.1; 40/2 heads: 32 rows of 640 15.3 -> 14.2, of
-// 1,000 16.5 -> 17.0, 64 of 2,000 28.1 -> 26.4).  Of a ragged batch only the longest row's bound
-// is known, and a row alone can be that long: the limits are lower (40 rows of 16/16 heads up to
-// 1,000 keys 19.2 -> 16.6, one of 4,000 among rows of 1 13.5 -> 21.5; 256 rows up to 2,000 keys,
-// 24/8 heads, 96 -> 87).
+// 1 row of 1,000 8.6 -> 8.5, 8 of 2,000 14.6 -> 14.1; two tiles, 40/2 heads, d = 128: 8 rows of
+// 500 keys 13.0 -> 12.6, of 800 13.7 -> 16.7; 48 of 1,700 23.2 -> 22.9, of 2,200 25.4 -> 27.7; 80
+// of 3,000 44 -> 35).  Of a ragged batch only the longest row's bound is known, and a row alone
+// can be that long: the limits are lower for many rows (40 rows of 16/16 heads up to 1,000 keys
+// 19.2 -> 16.6, one of 4,000 among rows of 1 13.5 -> 21.5; 256 rows up to 2,000 keys, 24/8 heads,
+// 96 -> 87; 40/2 heads: 32 rows up to 640 15.1 -> 14.0, up to 800 15.4 -> 16.4, d = 64 up to
+// 1,000 12.6 -> 11.7; 64 rows up to 1,000 19.6 -> 17.2, 120 up to 2,000 29.2 -> 25.4).
 bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged) {
-    const int64_t keys = tiles == 2 ? 450 : head_dim == 64 ? 1100 : 800;
-    if (ragged) return n_valid <= keys * (groups <= 64 ? 1 : groups < 512 ? 2 : groups < 2048 ? 3 : 6);
+    if (ragged) {
+        const int64_t keys = head_dim == 64 ? (tiles == 2 ? 1000 : 1100) : tiles == 2 ? 640 : 800;
+        return n_valid <= keys * (groups <= 64 ? 1 : groups <= 160 ? 2 : groups < 512 ? tiles + 1 : groups < 2048 ? 3 : 6);
+    }
+    const int64_t keys = tiles == 2 ? 600 : head_dim == 64 ? 1100 : 800;
     if (groups > 256 && groups < 512) return n_valid <= 1500;
-    return groups > 176 || n_valid <= keys * (groups <= 64 ? 1 : groups <= 128 ? 2 : 5);
+    return groups > 176 || n_valid <= keys * (groups <= 64 ? 1 : groups <= 128 ? tiles + 1 : 5);
+}
+
+// Waves of a workgroup, 4 or 8.  Whole rows have 8 while every CU has one, so that a row is read
+// faster.  Of split rows, 8 halve the partial states and their merge, 4 begin and end sooner and
+// balance better: 8 for few rows with many keys (1 row of 131,072 keys, 8/1 heads, d = 128: 20.1 ->
+// 17.1 us; 14/2 heads 20.6 -> 19.8, 1,048,576 keys, 28/4 heads, 138 -> 136; of 30,000 keys 11.7 ->
+// 12.1; 1 to 12 rows of 24/8 heads 1 to 8 % either way), and for two tiles, whose states are
+// more, from as many keys on (3 rows of 16,000 keys 40/2 heads 18.7 -> 17.9, of 4,000 13.5 -> 13.7)
+// and for ragged batches of fewer rows than half the work items, which halve with them (3 rows up
+// to 1,000 keys 15.3 -> 13.4, 16 up to 16,000 24.1 -> 21.7, 24 up to 30,011 33.4 -> 33.5, 80 up
+// to 16,000 48.7 -> 53.8).  Other ragged batches: 4 rows up to 100,000 keys 8/1 heads 19.4 ->
+// 17.6 (d = 64 18.4 -> 14.7), up to 30,000 13.5 -> 13.8.
+int32_t decode_q8_waves(int32_t tiles, int64_t groups, int64_t n_valid, bool ragged, bool direct) {
+    if (direct) return groups <= 256 ? 8 : 4;
+    if (tiles == 2 && ragged) return groups <= 128 ? 8 : 4;
+    return (tiles == 2 || groups <= 4) && groups * n_valid >= (ragged ? 192000 : 96000) ? 8 : 4;
+}
+
+// Workgroups that run at once: 2 of 4 waves a CU, 3 at d = 64 with one tile; 1 of 8 waves.
+int32_t decode_q8_slots(int32_t head_dim, int32_t tiles, int32_t waves) {
+    return waves == 8 ? 256 : head_dim == 64 && tiles == 1 ? 768 : 512;
 }
 
 // Splits of a uniform batch's rows, at most `room`: as fill the slots; with more groups than half
 // of them, the few that leave the last round fullest.
-int64_t decode_q8_splits(int64_t groups, int32_t head_dim, int32_t tiles, int64_t room) {
-    const int64_t slots = decode_q8_slots(head_dim, tiles);
+int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room) {
     const auto rounds = [&](int64_t s) { return (s * groups + slots - 1) / slots; };
     int64_t best = std::max<int64_t>(1, slots / groups);
     if (best == 1)
@@ -1411,16 +1433,18 @@ int decode_q8_impl(const char* fn, const void* q, const void* k_cache, const voi
     const int64_t cols = int64_t(h_kv) * p.subgroups;
     const int32_t tiles = (p.heads_per_block + 15) / 16;
     p.direct = atf::decode_q8_direct(batch * cols, d, tiles, p.n_valid, n_k_rows != nullptr);
+    p.waves = atf::decode_q8_waves(tiles, batch * cols, p.n_valid, n_k_rows != nullptr, p.direct != 0);
+    const int64_t slots = atf::decode_q8_slots(d, tiles, p.waves);
     if (p.direct) {
         p.splits = 1;
         p.ws_plan = nullptr;
     } else if (n_k_rows != nullptr) {
         const int64_t room = atf::decode_ragged_items(h_kv * (p.group / decode_heads_per_block(p.group)));
-        p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, atf::decode_q8_slots(d, tiles) / cols)));
+        p.splits = static_cast<int32_t>(std::min(room, std::max<int64_t>(1, slots / cols)));
     } else {
         const int64_t steps = (int64_t(p.n_valid) + atf::kDecodeQ8TokenStep - 1) / atf::kDecodeQ8TokenStep;
         const int64_t room = std::min<int64_t>(atf::decode_splits(batch, h_kv, n_k), steps);
-        const int64_t s = atf::decode_q8_splits(batch * cols, d, tiles, room);
+        const int64_t s = atf::decode_q8_splits(batch * cols, slots, room);
         const int64_t per = (steps + s - 1) / s;
         p.splits = static_cast<int32_t>((steps + per - 1) / per);
         if (per * atf::kDecodeQ8TokenStep * p.splits >= kPosLimit)

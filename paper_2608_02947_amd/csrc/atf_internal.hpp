@@ -134,6 +134,7 @@ struct DecodeQ8Params : DecodeQ8States {
     int32_t subgroups;        // `subgroups` workgroups of a KV head takes what is left
     int32_t split_tokens;
     int32_t direct;
+    int32_t waves;            // of a workgroup: 4 or 8
     float scale_log2;
     int32_t W[kMaxPairs];
 };
@@ -222,15 +223,16 @@ int32_t decode_plan_items(int32_t cols, bool cols16);
 bool decode_direct(int32_t batch, int32_t h_q, int32_t h_kv, int32_t head_dim, int64_t n_valid,
                    int32_t heads_per_block, bool rotate, bool ragged);
 // The same questions of the decode over 8-bit caches.
-int32_t decode_q8_slots(int32_t head_dim, int32_t tiles);
+int32_t decode_q8_waves(int32_t tiles, int64_t groups, int64_t n_valid, bool ragged, bool direct);
+int32_t decode_q8_slots(int32_t head_dim, int32_t tiles, int32_t waves);
 bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged);
-int64_t decode_q8_splits(int64_t groups, int32_t head_dim, int32_t tiles, int64_t room);
+int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room);
 // Caches from this many tokens are out of the 32-bit lane offsets of decode_split16_kernel
 // (they reach over one chunk's stream) and take decode_split_kernel.
 constexpr int64_t kDecode16MaxTokens = (int64_t(1) << 27) - 64;
 // Tokens handled per decode workgroup iteration (the split granularity).
 constexpr int32_t kDecodeTokenStep = 128;
-// The same of the 8-bit caches' decode: four waves, 64 tokens each.
+// The same of the 8-bit caches' decode: 64 tokens a wave, of four waves or of half of eight.
 constexpr int32_t kDecodeQ8TokenStep = 256;
 // Largest split count the merge kernel accepts.
 constexpr int32_t kDecodeMaxSplits = 4096;

@@ -33,8 +33,6 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kDirectWaves = 8;        // of a workgroup that takes a whole row
 constexpr int kBlock = 64;             // tokens of a wave's block
 constexpr float kRescale = 8.0f;       // lazy-rescale threshold, log2 units
 
@@ -169,8 +167,8 @@ __device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, Ro
     return row;
 }
 
-// NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4, or kDirectWaves; with
-// p.direct a workgroup takes a whole row and writes its output.
+// NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4 or 8; with p.direct a
+// workgroup takes a whole row and writes its output.
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
@@ -647,12 +645,10 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
     const bool ragged = p.n_k_rows != nullptr;
     const dim3 grid(unsigned(p.direct ? p.batch : ragged ? p.splits + p.batch : p.splits),
                     unsigned(p.h_kv * p.subgroups), unsigned(p.direct || ragged ? 1 : p.batch));
-    // whole rows: eight waves while every CU has one, four where the rows are more
-    if (p.direct && int64_t(grid.x) * grid.y <= 256) {
-        hipLaunchKernelGGL((decode_q8_kernel<D, NT, kDirectWaves>), grid, dim3(kDirectWaves * 64), 0, stream, p);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL((decode_q8_kernel<D, NT, kWaves>), grid, dim3(kWaves * 64), 0, stream, p);
+    if (p.waves == 8)
+        hipLaunchKernelGGL((decode_q8_kernel<D, NT, 8>), grid, dim3(512), 0, stream, p);
+    else
+        hipLaunchKernelGGL((decode_q8_kernel<D, NT, 4>), grid, dim3(256), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.direct) return e;
     // the merge's waves by the states of a row: a ragged batch's longest rows have some times the
@@ -673,7 +669,7 @@ hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
 hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t stream) {
     if (p.splits < 1 || p.splits > kDecodeMaxSplits || p.heads_per_block < 1 || p.heads_per_block > 32 ||
         p.subgroups < 1 || (p.subgroups - 1) * p.heads_per_block >= p.group ||
-        p.subgroups * p.heads_per_block < p.group)
+        p.subgroups * p.heads_per_block < p.group || (p.waves != 4 && p.waves != 8))
         return hipErrorInvalidValue;
     if (!p.direct && p.n_k_rows == nullptr &&
         (int64_t(p.splits) * p.split_tokens < p.n_valid || p.split_tokens % kDecodeQ8TokenStep != 0))

@@ -331,6 +331,8 @@ DECODES = [  # d, h_q, h_kv, B, n_k, q_pos, cap
     (64, 4, 4, 80, 70, 69, 70), (128, 2, 2, 150, 33, 40, 48),   # more rows than a round of workgroups
     (64, 1, 1, 1, 40000, 39999, 40000), (128, 40, 1, 1, 20000, 20010, 20001),  # merges of 8 and 16 waves
     (64, 3, 1, 260, 1530, 1529, 1530),                          # few splits of many rows
+    # split over workgroups of 8 waves
+    (128, 4, 2, 1, 50011, 50010, 50020), (64, 2, 1, 1, 96005, 97000, 96010), (128, 20, 1, 1, 97000, 96999, 97000),
 ]
 
 
@@ -370,6 +372,7 @@ RAGGED = [  # d, h_q, h_kv, lengths, query positions less lengths, pages
     (64, 16, 16, [65, 129, 1, 1000], 96), (128, 32, 4, [1, 2048, 33], 64), (64, 2, 1, [5] * 70, 32),
     (64, 3, 1, [(37 * i) % 2300 for i in range(130)], 0), (128, 2, 1, [4000 - 900 * i for i in range(5)] + [3] * 90, 32),
     (64, 20, 2, [3000, 0, 1, 2999], 0),
+    (64, 4, 1, [96001, 700], 0), (64, 17, 1, [(53 * i) % 2500 for i in range(132)], 0),
 ]
 
 
