@@ -191,10 +191,15 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15;
     const int g4 = lane >> 4;
-    const int split = blockIdx.x;
+    // of a ragged batch's work items the ones past the last come last, whatever the heads: they
+    // would take the place of others where the chip has just one for each
     const int subgroups = p.subgroups;
-    const int g = blockIdx.y / subgroups;
-    const int sub = blockIdx.y % subgroups;
+    const bool items = !p.direct && p.n_k_rows != nullptr;
+    const uint32_t cols = uint32_t(p.h_kv * subgroups);
+    const int split = int(items ? blockIdx.x / cols : blockIdx.x);
+    const int col = int(items ? blockIdx.x - split * cols : blockIdx.y);
+    const int g = col / subgroups;
+    const int sub = col % subgroups;
     const int hq0 = g * p.group + sub * p.heads_per_block;
     const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
 
@@ -210,9 +215,9 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
             q_pos = r.q_pos;
             t_end = r.keys;
         }
-    } else if (p.n_k_rows != nullptr) {
+    } else if (items) {
         int64_t span;
-        int32_t* plan = (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) ? p.ws_plan : nullptr;
+        int32_t* plan = (blockIdx.x == 0 && wave == 0) ? p.ws_plan : nullptr;
         Row r = {0, 0};
         b = ragged_item(p, split, r, t_begin, span, plan);
         if (b < 0) return;
@@ -549,7 +554,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
                 if (x == 0) p.lse[row] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
                 continue;
             }
-            const int64_t slot = p.n_k_rows != nullptr ? slot0 + h : slot0 + int64_t(h) * p.splits;
+            const int64_t slot = items ? slot0 + h : slot0 + int64_t(h) * p.splits;
             if (x == 0) {
                 p.ws_m[slot] = M;
                 p.ws_l[slot] = L;
@@ -641,10 +646,12 @@ __global__ __launch_bounds__(NW * 64) void decode_q8_merge_kernel(const DecodeQ8
 
 template <int D, int NT>
 hipError_t launch_d(const DecodeQ8Params& p, hipStream_t stream) {
-    // ragged: one workgroup per possible work item (at most p.splits + batch)
-    const bool ragged = p.n_k_rows != nullptr;
-    const dim3 grid(unsigned(p.direct ? p.batch : ragged ? p.splits + p.batch : p.splits),
-                    unsigned(p.h_kv * p.subgroups), unsigned(p.direct || ragged ? 1 : p.batch));
+    // ragged: a workgroup per possible work item (at most p.splits + batch) and KV head, or part
+    const bool ragged = p.n_k_rows != nullptr, items = ragged && !p.direct;
+    const int64_t cols = int64_t(p.h_kv) * p.subgroups;
+    const int64_t x = p.direct ? p.batch : items ? (int64_t(p.splits) + p.batch) * cols : p.splits;
+    if (x * p.waves * 64 > 0xFFFFFFFF) return hipErrorInvalidConfiguration;  // (the threads of a grid)
+    const dim3 grid(unsigned(x), unsigned(items ? 1 : cols), unsigned(p.direct || ragged ? 1 : p.batch));
     if (p.waves == 8)
         hipLaunchKernelGGL((decode_q8_kernel<D, NT, 8>), grid, dim3(512), 0, stream, p);
     else
