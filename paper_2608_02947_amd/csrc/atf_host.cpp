@@ -342,17 +342,25 @@ int32_t decode_plan_items(int32_t cols, bool cols16) {
 // 1,500 18.6 -> 18.1, of 3,000 24.8 -> 26.3; 20 of 4,000 35.2 -> 34.2; d = 64, 16/16 heads:
 // 1 row of 1,000 8.6 -> 8.5, 8 of 2,000 14.6 -> 14.1; two tiles, 40/2 heads, d = 128: 8 rows of
 // 500 keys 13.0 -> 12.6, of 800 13.7 -> 16.7; 48 of 1,700 23.2 -> 22.9, of 2,200 25.4 -> 27.7; 80
-// of 3,000 44 -> 35).  Of a ragged batch only the longest row's bound is known, and a row alone
-// can be that long: the limits are lower for many rows (40 rows of 16/16 heads up to 1,000 keys
-// 19.2 -> 16.6, one of 4,000 among rows of 1 13.5 -> 21.5; 256 rows up to 2,000 keys, 24/8 heads,
-// 96 -> 87; 40/2 heads: 32 rows up to 640 15.1 -> 14.0, up to 800 15.4 -> 16.4, d = 64 up to
-// 1,000 12.6 -> 11.7; 64 rows up to 1,000 19.6 -> 17.2, 120 up to 2,000 29.2 -> 25.4).
+// of 3,000 44 -> 35).  Of a ragged batch only the longest row's bound is known; the others are
+// shorter, so that most of a split batch's work is its merge, but a row alone can be that long
+// (rows of up to n keys, a third of it on average: 24/8 heads of 128, 8 rows up to 640 11.5 -> 9.5,
+// up to 1,300 11.9 -> 13.4; 40 up to 1,000 17.5 -> 17.3, up to 1,300 18.0 -> 19.9; 128 up to 2,000
+// 48 -> 43; 16/16 heads of 64, 16 rows up to 2,000 13.8 -> 13.1, 64 up to 1,300 22.0 -> 22.8; 40/2
+// heads of 128, 32 rows up to 640 15.1 -> 13.9, up to 800 15.4 -> 16.4, 128 up to 2,000 29.5 ->
+// 25.3, 300 up to 3,200 67 -> 55; one row of 4,000 among 39 of 1, 16/16 heads, 13.5 -> 21.5).
 bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged) {
+    const bool small = head_dim == 64;
     if (ragged) {
-        const int64_t keys = head_dim == 64 ? (tiles == 2 ? 1000 : 1100) : tiles == 2 ? 640 : 800;
-        return n_valid <= keys * (groups <= 64 ? 1 : groups <= 160 ? 2 : groups < 512 ? tiles + 1 : groups < 2048 ? 3 : 6);
+        const int64_t keys = small ? (tiles == 2 ? 500 : 550) : tiles == 2 ? 320 : 400;
+        const int64_t times = groups <= 64    ? 2
+                              : tiles == 2    ? (groups <= 160 ? 4 : groups < 512 ? 6 : 10)
+                              : groups < 512  ? (small ? 4 : 3)
+                              : groups < 2048 ? (small ? 3 : 6)
+                                              : (small ? 6 : 12);
+        return n_valid <= keys * times;
     }
-    const int64_t keys = tiles == 2 ? 600 : head_dim == 64 ? 1100 : 800;
+    const int64_t keys = tiles == 2 ? 600 : small ? 1100 : 800;
     if (groups > 256 && groups < 512) return n_valid <= 1500;
     return groups > 176 || n_valid <= keys * (groups <= 64 ? 1 : groups <= 128 ? tiles + 1 : 5);
 }
