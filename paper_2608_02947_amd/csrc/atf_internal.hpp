@@ -195,7 +195,8 @@ struct RotateParams {
     uint32_t rope_rho_lo[kMaxPairs];
 };
 
-// Kernel launchers (prefill.hip, decode.hip, rotate.hip and the files named).  Return the HIP error of the launch.
+// Kernel launchers (one in each .hip file, two in prefill.hip and rotate.hip).  Return the HIP error
+// of the launch.
 hipError_t launch_prefill(const PrefillParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_prefill_rotating(const PrefillRotParams& p, int head_dim, hipStream_t stream);
 // The kernel a prefill takes: 4 or 8 waves per row block of prefill_short_kernel, 0 for

@@ -1,15 +1,15 @@
 // Windowed single-token decode over 8-bit caches (q8.hpp), gfx950: decode.hip's split-KV decode
 // with the keys and values read as e4m3 numbers and widened to bf16 in registers.
 //
-// Caches (written by append_normed.hip):
+// Caches (append_normed.hip writes them):
 //   K [B][h_kv][d/16][cache_tokens][16]: chunk c of a token is 16 bytes, pairs 8c .. 8c + 7,
 //     first components then second; a power per token, k_scale [B][h_kv][ceil16(cache_tokens)]
 //   V [B][h_kv][ceil(cache_tokens/16)][d][16]: 16-token blocks, dim-major, tokens in order; a
 //     power per token, v_scale
 //
 // The heads of one KV head (up to 32 a workgroup) are the columns of v_mfma_f32_16x16x32_bf16, in
-// one or two tiles, a wave's block is 64 tokens, and every load of K and V is 16 bytes a lane.  With r = lane % 16,
-// g = lane / 16:
+// one or two tiles, a wave's block is 64 tokens, and every load of K and V is 16 bytes a lane.
+// With r = lane % 16, g = lane / 16:
 //   scores, tile s = 0 .. 3: A row r is token 16 (r / 4) + 4 s + r % 4, the lane's 16 bytes chunk
 //     4 m + g of it: its two halves are two operands of 8 dims, for two products.  The result
 //     gives the lane, for head r, tokens 16 g + 4 s + v.
@@ -22,6 +22,13 @@
 // token and at every token: chunks without a kept pair are read from a line of zeros, queries
 // lose the pairs kept nowhere, and where a window ends inside the block the keys' bytes are
 // masked lane by lane.
+//
+// Bound by HBM reads where rows are long or many: one row of 1,048,576 keys, 28/4 heads of 128 (734 MB
+// of kept pairs and values) 138 us, 5.3 TB/s; 8 rows of 32,768, 24/8 heads, 433 MB in 84 (a streaming
+// read reaches 5.57).  24 rows up to 30,011 of 40/2 heads, 97 MB, take 33: the first loads arrive
+// after 8 us and the merge ends 8 after the last.  64 tokens a wave make the values' 16 tokens of a
+// lane a block of the cache and the keys' powers 16 bytes a lane.  2 waves a SIMD: a block's
+// operands, the next ones in flight, and the outputs take 208 (d = 128, one tile) to 240 registers.
 #include "atf_internal.hpp"
 #include "q8.hpp"
 
