@@ -207,3 +207,51 @@ def test_binding_refuses_shapes_types_and_host_tensors():
     with pytest.raises(ValueError):
         atf.atf_decode_paged_q8(o, k8[0], sc, v8, sc, o, lse, torch.zeros(B, 2, dtype=torch.int32),
                                 torch.zeros(B, dtype=torch.int32), torch.zeros(B, dtype=torch.int32), 5, win, ws)
+
+
+def _rule(name, restype, *argtypes):
+    f = getattr(ctypes.CDLL(atf.LIB_PATH), name)
+    f.restype, f.argtypes = restype, argtypes
+    return f
+
+
+_i32, _i64, _bool = ctypes.c_int32, ctypes.c_int64, ctypes.c_bool
+_direct = _rule("_ZN3atf16decode_q8_directEliilb", _bool, _i64, _i32, _i32, _i64, _bool)
+_waves = _rule("_ZN3atf15decode_q8_wavesEillbb", _i32, _i32, _i64, _i64, _bool, _bool)
+_slots = _rule("_ZN3atf15decode_q8_slotsEiii", _i32, _i32, _i32, _i32)
+_splits = _rule("_ZN3atf16decode_q8_splitsElll", _i64, _i64, _i64, _i64)
+_room = _rule("_ZN3atf13decode_splitsEiil", _i32, _i32, _i32, _i64)
+
+
+def test_decode_plan_rules():
+    """Whole rows or splits, 4 or 8 waves: both sides of the rules' borders."""
+    assert _direct(8, 128, 1, 800, False) and not _direct(8, 128, 1, 801, False)
+    assert _direct(200, 128, 1, 10 ** 6, False) and not _direct(300, 128, 1, 1501, False)
+    assert _direct(512, 128, 2, 10 ** 6, False) and not _direct(128, 64, 2, 1801, False)
+    assert _direct(64, 64, 1, 1100, True) and not _direct(64, 64, 1, 1101, True)
+    assert _direct(100, 128, 1, 1200, True) and not _direct(100, 128, 1, 1201, True)
+    assert _direct(200, 128, 2, 1920, True) and not _direct(160, 128, 2, 1281, True)
+    assert _direct(4096, 128, 1, 4800, True) and not _direct(4096, 128, 1, 4801, True)
+    assert _waves(1, 256, 1000, False, True) == 8 and _waves(1, 257, 1000, False, True) == 4
+    assert _waves(1, 4, 24000, False, False) == 8 and _waves(1, 4, 23999, False, False) == 4
+    assert _waves(1, 5, 10 ** 6, False, False) == 4 and _waves(2, 5, 10 ** 6, False, False) == 8
+    assert _waves(2, 128, 500, True, False) == 8 and _waves(2, 129, 500, True, False) == 4
+    assert _waves(1, 2, 96000, True, False) == 8 and _waves(1, 2, 95999, True, False) == 4
+
+
+def test_decode_splits_fit_the_workspace():
+    """Splits and the states they write: within the workspace's room, none without keys."""
+    for d in (64, 128):
+        for tiles in (1, 2):
+            for waves in (4, 8):
+                slots = _slots(d, tiles, waves)
+                for batch in (1, 2, 3, 7, 16, 36, 100, 400, 5000):
+                    for h_kv in (1, 2, 5, 8, 64):
+                        for n in (1, 255, 256, 257, 5000, 131072, 10 ** 6, 2 ** 31 - 2):
+                            steps = -(-n // 256)
+                            room = min(_room(batch, h_kv, n), steps)
+                            s = _splits(batch * h_kv, slots, room)
+                            assert 1 <= s <= room
+                            per = -(-steps // s)
+                            used = -(-steps // per)
+                            assert used <= s and (used - 1) * per * 256 < n <= used * per * 256
