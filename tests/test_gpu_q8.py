@@ -149,6 +149,9 @@ APPENDS = [  # d, h_q, h_kv, B, n, positions, cap, pages
     (64, 1, 3, 2, 67, [2, 5], 77, 0),
     (128, 6, 2, 1, 100, [0], 100, 32),
     (128, 28, 4, 2, 131, [16, 3], 150, 0),
+    (64, 14, 2, 3, 48, [17, -1, 63], 120, 32),
+    (64, 16, 16, 3, 4001, [-1, 5, 300], 4200, 0),    # more heads of a wave than it loads at once
+    (128, 40, 2, 2, 1701, [9, 100], 1790, 64),       # queries past the L2s
 ]
 
 
@@ -516,6 +519,71 @@ def test_decodes_at_once_and_one_after_another():
     streams = [torch.cuda.Stream() for _ in calls]
     for how in [(spaces, streams)] * 3 + [([max(spaces, key=torch.Tensor.numel)] * 3,)]:
         assert all(torch.equal(a, b) for a, b in zip(alone, run(*how)))
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of pools of 4.5 GiB, appended to, read back and decoded over: the bytes and
+    bits of the same pages in small pools; and the end of one cache of 2^26 tokens and more."""
+    import paper_2608_02947_amd as atf
+    note("pools past 4 GiB")
+    d, h_q, h_kv, pt, B, n = 128, 4, 2, 64, 2, 150
+    win, _ = window("exact", d)
+    small, large = 8, 9 * 2 ** 15
+    q, k, v = (randn((B, n, h, d), 31 + h).to(DEV) for h in (h_q, h_kv, h_kv))
+    got = []
+    for pages in (small, large):
+        table = torch.tensor([[pages - 1, pages - 4, pages - 2], [pages - 6, pages - 3, pages - 5]], dtype=torch.int32, device=DEV)
+        kc = torch.zeros(atf.kpages_shape(pages, pt, h_kv, d), dtype=torch.uint8, device=DEV).view(E4)
+        vc = torch.zeros(atf.vpages_shape(pages, pt, h_kv, d), dtype=torch.uint8, device=DEV).view(E4)
+        ks, vs = (torch.zeros(atf.qscale_shape(pages, pt, h_kv), dtype=torch.uint8, device=DEV).view(E8) for _ in "kv")
+        qo = torch.empty_like(q)
+        atf.atf_cache_append_paged_q8(q, k, v, qo, kc, ks, vc, vs, table, 0, win)
+        kb = torch.zeros(atf.kcache_shape(B, n, h_kv, d), dtype=BF, device=DEV)
+        vb = torch.zeros(atf.vcache_shape(B, n, h_kv, d), dtype=BF, device=DEV)
+        atf.atf_cache_read_paged_q8(kc, ks, vc, vs, table, kb, vb, n)
+        rows = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([n, n - 1], [n - 1, n - 2])]
+        o, lse = torch.empty((B, h_q, d), dtype=BF, device=DEV), torch.empty((B, h_q), device=DEV)
+        atf.atf_decode_paged_q8(qo[:, -1].contiguous(), kc, ks, vc, vs, o, lse, table, *rows, n, win, workspace(B, h_q, h_kv, n, d))
+        torch.cuda.synchronize()
+        got.append([x[-8:].view(torch.uint8).cpu() for x in (kc, vc, ks, vs)] + [x.cpu() for x in (qo, kb, vb, o, lse)])
+        assert not kc[0].view(torch.uint8).any()  # a page of no row
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    del kc, vc, ks, vs
+
+    note("cache past 4 GiB")
+    d, cap, n, pos0 = 64, 2 ** 26 + 1000, 101, 2 ** 26 + 77
+    win, W = window("exact", d)
+    k, v = (randn((1, n, 1, d), 41 + i).to(DEV) for i in range(2))
+    kc = torch.zeros(atf.kcache_shape(1, cap, 1, d), dtype=torch.uint8, device=DEV).view(E4)
+    vc = torch.zeros(atf.vcache_shape(1, cap, 1, d), dtype=torch.uint8, device=DEV).view(E4)
+    ks, vs = (torch.full(atf.qscale_shape(1, cap, 1), 127, dtype=torch.uint8, device=DEV).view(E8) for _ in "kv")
+    atf.atf_cache_append_q8(None, k, v, None, kc, ks, vc, vs, pos0, win)
+    kb = torch.zeros(atf.kcache_shape(1, cap, 1, d), dtype=BF, device=DEV)
+    vb = torch.zeros(atf.vcache_shape(1, cap, 1, d), dtype=BF, device=DEV)
+    atf.atf_cache_read_q8(kc, ks, vc, vs, kb, vb, n, pos0)
+    torch.cuda.synchronize()
+    got = R.v_tokens(R.f64(vb[:, :, pos0 // 16 : (pos0 + n) // 16 + 1]), True)[0, 0, pos0 % 16 : pos0 % 16 + n]
+    assert np.array_equal(got, value(*R.quantise(R.f64(v[0, :, 0]))))
+    pos = pos0 + np.arange(n, dtype=np.int64)
+    want, err = R.norm_rotate(R.f64(k[0]), None, 0.0, pos, R.theta(d, 1e4))
+    got = R.k_tokens(R.f64(kb[:, :, :, pos0 : pos0 + n]))[0, 0]
+    power = 2.0 ** (ks.view(torch.uint8)[0, 0, pos0 : pos0 + n].cpu().numpy().astype(np.float64) - 127)[:, None]
+    assert (np.abs(got - want[:, 0]) <= np.maximum(R.E4M3_HALF * np.abs(want[:, 0]), R.E4M3_TINY * power) * (1 + 2.0 ** -10) + err[:, 0]).all()
+    # nothing else is written
+    assert not kc[0, 0, :, :pos0].view(torch.uint8).any()
+    assert all((x.view(torch.uint8)[0, 0, :pos0] == 127).all() for x in (ks, vs))
+    # decode over all of it: pos0 keys of score 0 with values 0, then the new ones.  The zeros' weights
+    # are of one size and sum to whole multiples of it, exact below 2^24; at most 2^11 such sums are
+    # joined, each with a rounding
+    q = randn((1, 3, d), 43)
+    o, lse = torch.empty((1, 3, d), dtype=BF, device=DEV), torch.empty((1, 3), device=DEV)
+    atf.atf_decode_q8(q.to(DEV), kc, ks, vc, vs, o, lse, pos0 + n - 1, win, workspace(1, 3, 1, pos0 + n, d), n_k=pos0 + n)
+    torch.cuda.synchronize()
+    wo, wl, oe, le = R.decode(R.f64(q[0]), got[None], value(*R.quantise(R.f64(v[0, :, 0])))[None], n - 1, W, d ** -0.5)
+    share = np.exp(wl) / (pos0 + np.exp(wl))
+    off = 2.0 ** -13  # of the sum, relative
+    assert (np.abs(R.f64(o[0]) - wo * share[:, None]) <= (oe + off * np.abs(wo)) * share[:, None]).all()
+    assert (np.abs(lse[0].cpu().numpy() - np.log(pos0 + np.exp(wl))) <= le + off + 2.0 ** -19).all()
 
 
 def test_binding_refuses_views_and_types():
