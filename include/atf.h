@@ -471,7 +471,7 @@ int atf_decode_paged_unrotated(const void *q, const void *k_pages, const void *v
  *   eps      finite, >= 0
  *   w, rope_inv_freq  the rotation, as atf_cache_append_rotated; a frequency of 0 leaves its
  *            pair as it is (all of them 0: no rotation)
- * n_new == 0 is a no-op.
+ * n_new == 0 is a no-op (k_new and v_new may be NULL then).
  * Errors: ATF_EINVAL (NULL window, pointer or only one of q and q_out, misaligned pointer,
  * written buffers that overlap another one (q_out == q aside), batch < 1, heads < 1, n_new < 0,
  * pos0 < 0, pos0 != 0 with pos_rows, pos0 + n_new > cache_tokens, cache_tokens < 1 or

@@ -1270,8 +1270,8 @@ int append_normed_impl(const char* fn, const void* q, const void* k_new, const v
     atf::AppendNormedParams p{};
     const int rc = rope_fractions(fn, w, rope_inv_freq, p.rope_rho_hi, p.rope_rho_lo);
     if (rc != ATF_OK) return rc;
-    if (!k_new || !v_new || !cache.k || !cache.v || (scaled && (!cache.k_scale || !cache.v_scale)))
-        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    if ((n_new > 0 && (!k_new || !v_new)) || !cache.k || !cache.v || (scaled && (!cache.k_scale || !cache.v_scale)))
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);  // (tensors without elements have none)
     for (const void* x : {q, k_new, v_new, static_cast<const void*>(q_out), static_cast<const void*>(cache.k),
                           static_cast<const void*>(cache.k_scale), static_cast<const void*>(cache.v),
                           static_cast<const void*>(cache.v_scale)})

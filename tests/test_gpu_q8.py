@@ -595,6 +595,7 @@ def test_binding_refuses_views_and_types():
     q, k = c.q.to(DEV), c.k.to(DEV)
     good = [q, k, k.clone(), q.clone(), c.kc, c.ks, c.vc, c.vs]
     atf.atf_cache_append_q8(*good, 0, win)
+    atf.atf_cache_append_q8(*[x[:, :0] for x in good[:4]], *good[4:], 40, win)  # no tokens: nothing
     for i, bad in ((0, q.transpose(0, 1).contiguous().transpose(0, 1)), (1, k.float()), (3, q.to(torch.float16)),
                    (4, c.kc.view(torch.uint8)), (5, c.ks.view(torch.uint8)), (6, c.vc.cpu())):
         with pytest.raises((TypeError, ValueError)):

@@ -77,6 +77,7 @@ def test_append_refusals(scaled, pages):
 
     assert call(n=0) == OK and call(n=0, q=None, qo=None, h_q=0) == OK
     assert call(n=0, qo=BIG) == OK                       # in place
+    assert call(n=0, q=None, qo=None, k=None, v=None) == OK  # tensors without elements
     for bad in (dict(window=False), dict(batch=0), dict(h_kv=0), dict(h_q=0), dict(n=-1), dict(pos0=-1),
                 dict(q=None), dict(qo=None), dict(k=None), dict(v=None), dict(kc=None), dict(vc=None),
                 dict(k=2 * BIG + 8), dict(qo=4 * BIG + 2), dict(kc=5 * BIG + 4), dict(eps=-1.0),
