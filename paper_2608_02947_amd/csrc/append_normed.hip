@@ -287,15 +287,13 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     }
     wave -= p.block_waves;
     // this wave's tokens and its heads, all of one kind: values by themselves, queries, keys
-    const int hpw = p.heads_per_wave;
-    const uint32_t q_parts = uint32_t(p.h_q + hpw - 1) / uint32_t(hpw), k_parts = uint32_t(p.h_kv + hpw - 1) / uint32_t(hpw);
     const bool alone = wave < p.value_waves;
-    const uint32_t parts = alone ? k_parts : q_parts + k_parts;
+    const uint32_t parts = alone ? p.kv_parts : p.q_parts + p.kv_parts;
     if (!alone) wave -= p.value_waves;
     uint32_t part = wave % parts;
-    const int kind = alone ? 2 : part < q_parts ? 0 : 1;
-    if (kind == 1) part -= q_parts;
-    const int n_heads = kind == 0 ? p.h_q : p.h_kv;
+    const int kind = alone ? 2 : part < p.q_parts ? 0 : 1;
+    if (kind == 1) part -= p.q_parts;
+    const int n_heads = kind == 0 ? p.h_q : p.h_kv, hpw = kind == 0 ? p.q_heads_per_wave : p.kv_heads_per_wave;
     const int from = int(part) * hpw, to = min(from + hpw, n_heads);
     const uint32_t rows = uint32_t(p.batch) * (alone && p.value_ends ? 32u : uint32_t(p.n_new));
     const uint32_t row = wave / parts * uint32_t(kTokens) + uint32_t(lane / kLanes);
@@ -450,13 +448,21 @@ template <int D>
 hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     constexpr int kTokens = 64 / (D / 8);
     const int64_t groups = (int64_t(p.batch) * p.n_new + kTokens - 1) / kTokens;
-    // one head a wave until the chip is full of waves, then as many as keep it full, so that a
-    // token's angles serve them all
-    const int64_t target = 4096;
+    // one head a wave until the chip is full of waves (3 run on a SIMD), then as many as keep it full,
+    // so that a token's angles serve them all, in equal parts.  As many as leave at most 3400 waves,
+    // against at least 4096: 1,000 tokens of 28/4 heads of 128 into 8-bit caches 11.5 -> 8.2 us,
+    // 4,000 of 14/2 heads of 64 11.6 -> 8.4, 3,885 of 16/16 13.5 -> 12.7; 900 of 40/2 11.3 -> 12.0;
+    // 16,384 and more the same
+    const int64_t target = 3400;
     const int64_t heads = p.h_q + p.h_kv;
-    p.heads_per_wave = int32_t(std::min(heads, std::max<int64_t>(1, groups * heads / target)));
-    const auto parts = [&](int64_t h) { return (h + p.heads_per_wave - 1) / p.heads_per_wave; };
-    const int64_t row_waves = groups * (parts(p.h_q) + parts(p.h_kv));
+    const int64_t most = std::max<int64_t>(1, (groups * heads + target - 1) / target);
+    const auto part = [&](int32_t h, int32_t& per_wave, uint32_t& parts) {
+        parts = uint32_t((h + most - 1) / most);
+        per_wave = h > 0 ? int32_t((h + parts - 1) / parts) : 1;
+    };
+    part(p.h_q, p.q_heads_per_wave, p.q_parts);
+    part(p.h_kv, p.kv_heads_per_wave, p.kv_parts);
+    const int64_t row_waves = groups * (int64_t(p.q_parts) + p.kv_parts);
     // values: token by token in a short call, else whole 16-token blocks (in whole workgroups) and
     // the tokens at the rows' ends by themselves
     const bool blocks = p.n_new >= 16;
@@ -465,11 +471,11 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     const bool aligned = p.pos_rows == nullptr && p.pos0 % 16 == 0 && p.n_new % 16 == 0;
     p.value_ends = blocks;
     const int64_t alone = blocks ? (aligned ? 0 : (int64_t(p.batch) * 32 + kTokens - 1) / kTokens) : groups;
-    const int64_t waves = block_waves + alone * parts(p.h_kv) + row_waves;
+    const int64_t waves = block_waves + alone * p.kv_parts + row_waves;
     // (a grid has less than 2^32 threads)
     if (waves < 1 || waves > (int64_t(1) << 26) - 4 || units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     p.block_waves = uint32_t(block_waves);
-    p.value_waves = uint32_t(alone * parts(p.h_kv));
+    p.value_waves = uint32_t(alone * p.kv_parts);
     const dim3 grid(unsigned((waves + 3) / 4));
     // queries that the L2s (8 of 4 MB) cannot hold for their reader
     const bool past = int64_t(p.batch) * p.n_new * p.h_q * D * 2 > (32 << 20);
