@@ -501,8 +501,8 @@ int atf_cache_append_paged_normed(const void *q, const void *k_new, const void *
  * no infinities) and one power of two that they are multiplied by, as an e8m0 byte (exponent +
  * 127): the smallest 2^e, e in [-60, 119], with max |x| <= 448 * 2^e (the maximum over the
  * row's finite numbers, 2^-60 if they are all 0 or none is).  Numbers are x / 2^e rounded to
- * nearest even, from fp32 and once (keys after norm and rotation); what is not finite is
- * stored as NaN.
+ * nearest even, once (keys after norm and rotation in fp32, or in 64 bits where fp32 leaves open to
+ * which of two numbers); what is not finite is stored as NaN.
  *   k_cache  e4m3 [batch][h_kv][d/16][cache_tokens][16]   pair-chunk-major as the bf16 K cache
  *   v_cache  e4m3 [batch][h_kv][ceil(cache_tokens/16)][d][16]  16-token blocks stored d-major,
  *            a block's tokens IN ORDER (unlike the bf16 V cache's)

@@ -65,9 +65,7 @@ __device__ __forceinline__ uint32_t other_lane(uint32_t x) {
 // nearest quarter turn is taken off the 32-bit fraction in integers; what is left, at most
 // pi/4, is turned to radians in two floats, whose first goes through the Taylor series to x^9 and
 // x^10 (truncation below 2^-28) and whose second is added to first order.  Both are within about
-// 1.1 ulp, 0.3 in the mean square: 8-bit keys round on from here, and each error shows as numbers
-// that round to the other side (with one float of radians 1.5 times as many; the hardware's own
-// sine is 2^-20 off).
+// 1.1 ulp, 0.3 in the mean square (the hardware's own sine is 2^-20 off).
 __device__ __forceinline__ void cos_sin(uint32_t pos, uint32_t rho_hi, uint32_t rho_lo, float& cs, float& sn) {
     const uint32_t f = pos * rho_hi + __umulhi(pos, rho_lo);
     const uint32_t quarter = (f + 0x20000000u) >> 30;
@@ -90,6 +88,61 @@ __device__ __forceinline__ void cos_sin(uint32_t pos, uint32_t rho_hi, uint32_t 
     const float a = swap ? s : c, b = swap ? c : s;
     cs = (quarter + 1) & 2 ? -a : a;
     sn = quarter & 2 ? -b : b;
+}
+
+// The same in 64 bits, from 64 bits of the fraction: Taylor series to x^13 and x^14 (truncation below
+// 2^-41).
+__device__ __forceinline__ void cos_sin64(uint32_t pos, uint32_t rho_hi, uint32_t rho_lo, double& cs, double& sn) {
+    const uint64_t f = uint64_t(pos) * (uint64_t(rho_hi) << 32 | rho_lo);
+    const uint32_t quarter = uint32_t((f + (uint64_t(1) << 61)) >> 62);
+    const double x = double(int64_t(f - (uint64_t(quarter) << 62))) * 3.4061215800304553e-19;  // 2 pi / 2^64
+    const double y = x * x;
+    double s = __builtin_fma(y, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+    s = __builtin_fma(y, s, 1.0 / 362880.0);
+    s = __builtin_fma(y, s, -1.0 / 5040.0);
+    s = __builtin_fma(y, s, 1.0 / 120.0);
+    s = __builtin_fma(y, s, -1.0 / 6.0);
+    s = __builtin_fma(x * y, s, x);
+    double c = __builtin_fma(y, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+    c = __builtin_fma(y, c, -1.0 / 3628800.0);
+    c = __builtin_fma(y, c, 1.0 / 40320.0);
+    c = __builtin_fma(y, c, -1.0 / 720.0);
+    c = __builtin_fma(y, c, 1.0 / 24.0);
+    c = __builtin_fma(y, c, -0.5);
+    c = __builtin_fma(y, c, 1.0);
+    const bool swap = quarter & 1;
+    const double a = swap ? s : c, b = swap ? c : s;
+    cs = (quarter + 1) & 2 ? -a : a;
+    sn = quarter & 2 ? -b : b;
+}
+
+// x as fp32, and where it is none, the odd one of its two neighbours: what rounds it on rounds as if
+// from x itself.
+__device__ __forceinline__ float to_odd(double x) {
+    const float f = float(x);
+    const double rest = x - double(f);
+    uint32_t bits = __float_as_uint(f);
+    if (fabsf(f) < INFINITY && rest != 0. && (bits & 1u) == 0u) bits += (rest > 0.) == (x > 0.) ? 1u : ~0u;
+    return __uint_as_float(bits);
+}
+
+template <int kCtrl>
+__device__ __forceinline__ double dpp64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, uint64_t(dpp<kCtrl>(uint32_t(u >> 32))) << 32 | dpp<kCtrl>(uint32_t(u)));
+}
+template <int kLanes>
+__device__ __forceinline__ double other_lane64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, uint64_t(other_lane<kLanes>(uint32_t(u >> 32))) << 32 | other_lane<kLanes>(uint32_t(u)));
+}
+template <int kLanes>
+__device__ __forceinline__ double sum_lanes64(double x) {
+    x += dpp64<kXor1>(x);
+    x += dpp64<kXor2>(x);
+    x += dpp64<kMirror8>(x);
+    if constexpr (kLanes == 16) x += dpp64<kMirror16>(x);
+    return x;
 }
 
 __device__ __forceinline__ float bf_lo(uint32_t x) { return __uint_as_float(x << 16); }
@@ -286,13 +339,27 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
         return;
     }
     wave -= p.block_waves;
-    // this wave's tokens and its heads, all of one kind: values by themselves, queries, keys
+    // this wave's tokens and its heads, all of one kind: values by themselves, keys, queries
     const bool alone = wave < p.value_waves;
-    const uint32_t parts = alone ? p.kv_parts : p.q_parts + p.kv_parts;
     if (!alone) wave -= p.value_waves;
-    uint32_t part = wave % parts;
-    const int kind = alone ? 2 : part < p.q_parts ? 0 : 1;
-    if (kind == 1) part -= p.q_parts;
+    // (in a long call a token's queries and keys side by side, which HBM reads 2 to 5 % faster, else
+    // the keys first, which take longest)
+    int kind = 2;
+    uint32_t parts = p.kv_parts, part;
+    if (kStream && !alone) {
+        parts += p.q_parts;
+        part = wave % parts;
+        kind = part < p.q_parts ? 0 : 1;
+        if (kind == 1) part -= p.q_parts;
+    } else {
+        if (!alone) kind = wave < p.key_waves ? 1 : 0;
+        if (kind == 0) {
+            wave -= p.key_waves;
+            parts = p.q_parts;
+            if (parts == 0) return;  // a wave past the last one's work, of a call without queries
+        }
+        part = wave % parts;
+    }
     const int n_heads = kind == 0 ? p.h_q : p.h_kv, hpw = kind == 0 ? p.q_heads_per_wave : p.kv_heads_per_wave;
     const int from = int(part) * hpw, to = min(from + hpw, n_heads);
     const uint32_t rows = uint32_t(p.batch) * (alone && p.value_ends ? 32u : uint32_t(p.n_new));
@@ -370,10 +437,77 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
             for (int e = 0; e < 8; ++e) y[e] *= rs;
         }
     };
-    // a row's 8 numbers of this lane as e4m3, and the row's power
-    [[maybe_unused]] const auto quantised = [&](const float* y, uint32_t& byte) __attribute__((always_inline)) {
+    // Numbers of a key so near to the middle of two e4m3 numbers (their lower 20 bits near half a
+    // step), or whose largest is so near to 448 powers, that fp32's own error may decide: within kNear
+    // ulps, twice that error's size.  One head of a wave in 500 has one; it is formed again in 64 bits
+    // once the wave is through, so that keys round as the formula's do: of 4 million without norm
+    // 3 round to the other side, small ones nearly all (those below 2^-6 of the power,
+    // whose steps are others, and those that are what is left of a much larger difference), at 0.04
+    // to 0.09 of plain fp32's error.  The heads met again cost the calls where a wave's time counts:
+    // 64 rows of one token 5.0 -> 5.6 us, 3,885 tokens of 16/16 heads of 64 12.7 -> 12.9, 32,768 of 28/4
+    // 110.8 -> 111.3.  Without norm and angle fp32 is exact.
+    constexpr uint32_t kNear = 2;
+    [[maybe_unused]] bool exact = weight == nullptr;
+    if constexpr (kQ8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) exact = exact && (kind == 2 || ws[e] == 0.f);
+    }
+    [[maybe_unused]] const auto doubtful = [&](const float* y, uint32_t m) __attribute__((always_inline)) {
+        uint32_t near = (m << 9) + ((kNear << 9) - 0xC0000000u);  // (up to 16 times as far above it)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) near = min(near, (__float_as_uint(y[e]) << 12) + ((kNear << 12) - 0x80000000u));
+        return __any(near < (kNear << 13) && !exact) != 0;
+    };
+    [[maybe_unused]] const auto refined = [&](u32x4_t v, float* y) __attribute__((always_inline)) {
+        double rs = 1.;
+        if (weight != nullptr) {
+            double ss = 0.;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double a0 = bf_lo(v[i]), a1 = bf_hi(v[i]);
+                ss = __builtin_fma(a0, a0, ss);
+                ss = __builtin_fma(a1, a1, ss);
+            }
+            rs = 1. / __builtin_sqrt(sum_lanes64<kLanes>(ss) / D + double(p.eps));
+        }
+        // as above, 4 angles a lane: elements i and 4 + i a turn of the loop, which is short code (it is
+        // met cold) and moves what is used or made to where the next turn has it
+        u32x4_t rh, rl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            rh[i] = p.rope_rho_hi[8 * c + 4 * hf + i];
+            rl[i] = p.rope_rho_lo[8 * c + 4 * hf + i];
+        }
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < 4; ++i) {
+            float w[4] = {1.f, 1.f, 1.f, 1.f};
+            if (weight != nullptr) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = weight[8 * (k & 1 ? l ^ kChunks : l) + 4 * (k / 2) + i];
+            }
+            double cs, sn;
+            cos_sin64(uint32_t(at.pos), rh[0], rl[0], cs, sn);
+            const double co = other_lane64<kLanes>(cs), so = other_lane64<kLanes>(sn);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const double a = double(bf_lo(v[2 * k])) * w[2 * k];
+                const double o = double(bf_lo(other_lane<kLanes>(v[2 * k]))) * w[2 * k + 1];
+                const double x = __builtin_fma(a, k == hf ? cs : co, (hf ? o : -o) * (k == hf ? sn : so)) * rs;
+#pragma unroll
+                for (int e = 0; e < 3; ++e) y[4 * k + e] = y[4 * k + e + 1];
+                y[4 * k + 3] = to_odd(x);
+                v[2 * k] = i & 1 ? v[2 * k + 1] : v[2 * k] >> 16;
+            }
+#pragma unroll
+            for (int e = 0; e < 3; ++e) {
+                rh[e] = rh[e + 1];
+                rl[e] = rl[e + 1];
+            }
+        }
+    };
+    // a row's 8 numbers of this lane as e4m3, and the row's power; m is its largest magnitude
+    [[maybe_unused]] const auto quantised = [&](const float* y, uint32_t m, uint32_t& byte) __attribute__((always_inline)) {
         uint2 w;
-        const uint32_t m = max_lanes<kLanes>(largest<8, false>(y));
         by_kind(m, [&](auto plain) __attribute__((always_inline)) {
             constexpr bool kPlain = decltype(plain)::value;
             byte = q8::scale_byte(kPlain ? m : max_lanes<kLanes>(largest<8, true>(y)));
@@ -390,18 +524,27 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
         turned(v, y);
         if (at.active) store16<kStream>(p.q_out + (int64_t(r) * p.h_q + h) * D + 8 * l, to_bf16(y));
     };
+    [[maybe_unused]] const auto store_q8 = [&](int g, const float* y, uint32_t m) __attribute__((always_inline)) {
+        const int64_t to_k = (((eg0 + g) * kChunks + c) * at.cap + at.tok) * 16 + 8 * hf;
+        uint32_t byte;
+        const uint2 w = quantised(y, m, byte);
+        if (at.stored) {
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.k_dst) + to_k) = w;
+            if (l == 0) p.k_scale[(eg0 + g) * p.scale_tokens + at.tok] = uint8_t(byte);
+        }
+    };
+    [[maybe_unused]] uint64_t again = 0;  // the heads, counted from the wave's first, that are formed in 64 bits
     const auto key = [&](int g, u32x4_t v) __attribute__((always_inline)) {
         float y[8];
         turned(v, y);
-        const int64_t to_k = (((eg0 + g) * kChunks + c) * at.cap + at.tok) * 16 + 8 * hf;
         if constexpr (kQ8) {
-            uint32_t byte;
-            const uint2 w = quantised(y, byte);
-            if (at.stored) {
-                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.k_dst) + to_k) = w;
-                if (l == 0) p.k_scale[(eg0 + g) * p.scale_tokens + at.tok] = uint8_t(byte);
-            }
+            const uint32_t m = max_lanes<kLanes>(largest<8, false>(y));
+            if (doubtful(y, m))
+                again |= uint64_t(1) << (g - from);
+            else
+                store_q8(g, y, m);
         } else if (at.stored) {
+            const int64_t to_k = (((eg0 + g) * kChunks + c) * at.cap + at.tok) * 16 + 8 * hf;
             *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.k_dst) + to_k) = to_bf16(y);
         }
     };
@@ -414,7 +557,7 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
             for (int e = 0; e < 8; ++e) y[e] = e & 1 ? bf_hi(v[e / 2]) : bf_lo(v[e / 2]);
             uint8_t* dst = static_cast<uint8_t*>(p.v_dst) + to_v + at.tok % 16;
             uint32_t byte;
-            const uint2 x2 = quantised(y, byte);
+            const uint2 x2 = quantised(y, max_lanes<kLanes>(largest<8, false>(y)), byte);
             const uint32_t w[2] = {x2.x, x2.y};
             if (at.stored) {
 #pragma unroll
@@ -442,6 +585,14 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
         heads(key);
     else
         heads(value);
+    if constexpr (kQ8) {
+        for (; again != 0; again &= again - 1) {
+            const int g = from + __builtin_ctzll(again);
+            float y[8];
+            refined(*reinterpret_cast<const u32x4_t*>(src + int64_t(g) * D), y);
+            store_q8(g, y, max_lanes<kLanes>(largest<8, false>(y)));
+        }
+    }
 }
 
 template <int D>
@@ -456,12 +607,12 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     const int64_t target = 3400;
     const int64_t heads = p.h_q + p.h_kv;
     const int64_t most = std::max<int64_t>(1, (groups * heads + target - 1) / target);
-    const auto part = [&](int32_t h, int32_t& per_wave, uint32_t& parts) {
+    const auto part = [&](int32_t h, int64_t most, int32_t& per_wave, uint32_t& parts) {
         parts = uint32_t((h + most - 1) / most);
         per_wave = h > 0 ? int32_t((h + parts - 1) / parts) : 1;
     };
-    part(p.h_q, p.q_heads_per_wave, p.q_parts);
-    part(p.h_kv, p.kv_heads_per_wave, p.kv_parts);
+    part(p.h_q, most, p.q_heads_per_wave, p.q_parts);
+    part(p.h_kv, std::min<int64_t>(most, 64), p.kv_heads_per_wave, p.kv_parts);  // (of the keys at most 64: a wave counts them in bits)
     const int64_t row_waves = groups * (int64_t(p.q_parts) + p.kv_parts);
     // values: token by token in a short call, else whole 16-token blocks (in whole workgroups) and
     // the tokens at the rows' ends by themselves
@@ -476,6 +627,7 @@ hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     if (waves < 1 || waves > (int64_t(1) << 26) - 4 || units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     p.block_waves = uint32_t(block_waves);
     p.value_waves = uint32_t(alone * p.kv_parts);
+    p.key_waves = uint32_t(groups * p.kv_parts);
     const dim3 grid(unsigned((waves + 3) / 4));
     // queries that the L2s (8 of 4 MB) cannot hold for their reader
     const bool past = int64_t(p.batch) * p.n_new * p.h_q * D * 2 > (32 << 20);

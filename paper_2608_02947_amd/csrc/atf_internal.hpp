@@ -162,11 +162,11 @@ struct AppendNormedParams {
     int32_t max_pages, num_pages, page_tokens;
     // set by the launcher: heads of a wave, and waves of a token's heads; waves of whole value
     // blocks, which come first; waves of values by themselves, and whether those are only the
-    // tokens at the rows' ends
+    // tokens at the rows' ends; waves of keys
     int32_t q_heads_per_wave, kv_heads_per_wave;
     uint32_t q_parts, kv_parts;
     int32_t value_ends;
-    uint32_t block_waves, value_waves;
+    uint32_t block_waves, value_waves, key_waves;
     uint32_t rope_rho_hi[kMaxPairs];
     uint32_t rope_rho_lo[kMaxPairs];
 };

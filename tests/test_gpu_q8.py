@@ -173,6 +173,14 @@ def test_append_one_position_for_all_rows(d, q8):
 
 
 @pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+@pytest.mark.parametrize("d,h_kv,B,n", [(64, 1, 1, 1), (128, 3, 2, 50), (64, 5, 3, 17), (128, 1, 1, 7)])
+def test_append_without_queries(d, h_kv, B, n, q8):
+    """Waves of the last workgroup without work, and no queries that they could take."""
+    note(f"append no queries {d} {h_kv} {B} {n} {q8}")
+    Case(d, 1, h_kv, B, n, q8, None, 60, 0, pos0=5, q=False).run().check()
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
 def test_append_in_place_far_positions_and_streams(q8):
     """Queries far past the cache (their keys are not stored) and written over themselves, on
     another stream."""
