@@ -231,6 +231,9 @@ int32_t decode_q8_waves(int32_t tiles, int64_t groups, int64_t n_valid, bool rag
 int32_t decode_q8_slots(int32_t head_dim, int32_t tiles, int32_t waves);
 bool decode_q8_direct(int64_t groups, int32_t head_dim, int32_t tiles, int64_t n_valid, bool ragged);
 int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room);
+// The first token of a wave's 64-token blocks in a workgroup's tokens [t_begin, t_end), t_end if it has
+// none (the end may be 2^31 - 1: no sum is formed past it).
+__host__ __device__ int32_t decode_q8_first(int32_t t_begin, int32_t t_end, int32_t wave);
 // Caches from this many tokens are out of the 32-bit lane offsets of decode_split16_kernel
 // (they reach over one chunk's stream) and take decode_split_kernel.
 constexpr int64_t kDecode16MaxTokens = (int64_t(1) << 27) - 64;

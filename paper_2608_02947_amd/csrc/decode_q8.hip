@@ -33,6 +33,11 @@
 #include "q8.hpp"
 
 namespace atf {
+
+__host__ __device__ int32_t decode_q8_first(int32_t t_begin, int32_t t_end, int32_t wave) {
+    return t_end - t_begin > 64 * wave ? t_begin + 64 * wave : t_end;
+}
+
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -317,7 +322,7 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
         vscale = load16(in ? (hi ? B.b.vs : B.a.vs) + 16 * (g4 & 1) : zeros, 0);
     };
 
-    int t0 = t_begin + kBlock * wave;
+    int t0 = decode_q8_first(t_begin, t_end, wave);
     Blk B{};
     if (t0 < t_end) {
         // (the values first: they need no window, whose table is on its way)
