@@ -548,8 +548,9 @@ int atf_cache_read_paged_q8(const void *k_pages, const void *k_scale, const void
 /* Decode over 8-bit caches: atf_decode, atf_decode_ragged and atf_decode_paged with the keys and
  * values read as number * power (widened exactly; scores, softmax and the products with the
  * values as there).  Keys are the rotated ones.  Same windows, clamping, empty rows and workspace
- * (atf_decode_workspace_bytes of the same arguments); power bytes must be 1 .. 254.  A row whose
- * scores are NaN (a key that was not finite) gives NaN.
+ * (atf_decode_workspace_bytes of the same arguments); power bytes must be 1 .. 254.  A row gives NaN
+ * where a number of a key is NaN (one that was not finite) in a pair that the window keeps; past its
+ * pair's window such a number does not count.
  * Errors: as those, plus ATF_EINVAL for NULL or misaligned scales.  Any group size is built:
  * up to 32 query heads of a KV head share a workgroup.  Deterministic: equal inputs give equal bits. */
 int atf_decode_q8(const void *q, const void *k_cache, const void *k_scale, const void *v_cache,

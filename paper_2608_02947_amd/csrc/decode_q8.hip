@@ -20,8 +20,9 @@
 //
 // A pair is kept at distance z iff z <= W_r.  Per block, two ballots give the pairs kept at some
 // token and at every token: chunks without a kept pair are read from a line of zeros, queries
-// lose the pairs kept nowhere, and where a window ends inside the block the keys' bytes are
-// masked lane by lane.
+// lose the pairs kept nowhere, and so do the keys in chunks that hold others (a number that is none
+// must not count there: 0.5 to 1 % of long rows' time); where a window ends inside the block the
+// keys' bytes are masked lane by lane.
 //
 // Bound by HBM reads where rows are long or many: one row of 1,048,576 keys, 28/4 heads of 128 (734 MB
 // of kept pairs and values) 138 us, 5.3 TB/s; 8 rows of 32,768, 24/8 heads, 433 MB in 84 (a streaming
@@ -84,6 +85,9 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t mask) {
         r[t] = x[t] & (((mask >> (2 * t)) & 1u ? 0x0000FFFFu : 0u) | ((mask >> (2 * t + 1)) & 1u ? 0xFFFF0000u : 0u));
     return r;
 }
+
+// 4 bits as bytes of ones
+__device__ __forceinline__ uint32_t byte_mask(uint32_t bits) { return (__umul24(bits, 0x204081u) & 0x01010101u) * 255u; }
 
 // The sum over the wave's 64 lanes, and each lane's sum of the lanes up to it, by DPP.
 template <int kCtrl, int kRows>
@@ -400,6 +404,19 @@ __global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8
                         hi |= w[4 + e] >= z ? 0xFFu << (8 * e) : 0u;
                     }
                     kf[s][m] &= u32x4_t{lo, hi, lo, hi};
+                }
+            }
+        } else {
+            // chunks that hold pairs kept and pruned at all of the block's tokens: the pruned ones'
+            // numbers must not count even where they are none, and 0 times NaN is NaN
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                const uint32_t four = uint32_t(keep >> (32 * m));  // chunks 4 m .. 4 m + 3
+                if ((four ^ (four >> 1)) & 0x7F7F7F7Fu) {
+                    const uint32_t pairs = four >> (8 * g4);
+                    const uint32_t lo = byte_mask(pairs & 15u), hi = byte_mask((pairs >> 4) & 15u);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) kf[s][m] &= u32x4_t{lo, hi, lo, hi};
                 }
             }
         }
