@@ -473,10 +473,10 @@ int atf_decode_paged_unrotated(const void *q, const void *k_pages, const void *v
  *            pair as it is (all of them 0: no rotation)
  * n_new == 0 is a no-op (k_new and v_new may be NULL then).
  * Errors: ATF_EINVAL (NULL window, pointer or only one of q and q_out, misaligned pointer,
- * written buffers that overlap another one (q_out == q aside), batch < 1, heads < 1, n_new < 0,
- * pos0 < 0, pos0 != 0 with pos_rows, pos0 + n_new > cache_tokens, cache_tokens < 1 or
- * > 2^31 - 1, batch * n_new > 2^26, a bad eps or rotation frequency); ATF_EUNSUPPORTED
- * (d not 64 or 128, h_q + 2 h_kv above 65535); ATF_EHIP. */
+ * written buffers that overlap another one or an array that the call reads (q_out == q aside),
+ * batch < 1, heads < 1, n_new < 0, pos0 < 0, pos0 != 0 with pos_rows, pos0 + n_new > cache_tokens,
+ * cache_tokens < 1 or > 2^31 - 1, batch * n_new > 2^26, a bad eps or rotation frequency);
+ * ATF_EUNSUPPORTED (d not 64 or 128, h_q + 2 h_kv above 65535); ATF_EHIP. */
 int atf_cache_append_normed(const void *q, const void *k_new, const void *v_new, void *q_out,
                             void *k_cache, void *v_cache, int32_t batch, int64_t n_new,
                             int64_t pos0, const int32_t *pos_rows, int32_t h_q, int32_t h_kv,

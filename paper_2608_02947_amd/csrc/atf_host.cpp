@@ -1216,6 +1216,8 @@ PagedArgs paged_args(const int32_t* block_table, int32_t max_pages, int32_t num_
     return pg;
 }
 
+size_t table_bytes(const PagedArgs& pg, int32_t batch) { return size_t(batch) * size_t(pg.max_pages) * 4; }
+
 // (2^31 at most)
 uint32_t scale_tokens(int64_t cache_tokens) { return static_cast<uint32_t>((cache_tokens + 15) / 16 * 16); }
 
@@ -1292,6 +1294,10 @@ int append_normed_impl(const char* fn, const void* q, const void* k_new, const v
         {"the V cache", cache.v, v_bytes, true},
         {"k_scale", cache.k_scale, s_bytes, true},
         {"v_scale", cache.v_scale, s_bytes, true},
+        {"q_weight", norms.q_weight, size_t(d) * 4, false},
+        {"k_weight", norms.k_weight, size_t(d) * 4, false},
+        {"pos_rows", pos_rows, size_t(batch) * 4, false},
+        {"the block table", pg != nullptr ? pg->block_table : nullptr, pg != nullptr ? table_bytes(*pg, batch) : 0, false},
     };
     const int apart = check_apart(fn, spans);
     if (apart != ATF_OK) return apart;
@@ -1362,6 +1368,7 @@ int read_q8_impl(const char* fn, const void* k_src, const void* k_scale, const v
         {"v_scale", v_scale, src * padded, false},
         {"the K cache", k_dst, dst * size_t(cache_tokens) * d * 2, true},
         {"the V cache", v_dst, dst * size_t(scale_tokens(cache_tokens)) * d * 2, true},
+        {"the block table", pg != nullptr ? pg->block_table : nullptr, pg != nullptr ? table_bytes(*pg, batch) : 0, false},
     };
     const int apart = check_apart(fn, spans);
     if (apart != ATF_OK) return apart;
