@@ -226,6 +226,9 @@ int32_t decode_plan_items(int32_t cols, bool cols16);
 // Whether a batch runs without splits (with cols16 only).
 bool decode_direct(int32_t batch, int32_t h_q, int32_t h_kv, int32_t head_dim, int64_t n_valid,
                    int32_t heads_per_block, bool rotate, bool ragged);
+// The token of a wave's next block, `step` past t0 in [0, t_end), or t_end if that is none (the end may be
+// 2^31 - 1: no sum is formed past it).
+__host__ __device__ int32_t decode_next(int32_t t0, int32_t t_end, int32_t step);
 // The same questions of the decode over 8-bit caches.
 int32_t decode_q8_waves(int32_t tiles, int64_t groups, int64_t n_valid, bool ragged, bool direct);
 int32_t decode_q8_slots(int32_t head_dim, int32_t tiles, int32_t waves);

@@ -46,6 +46,11 @@
 #include <mutex>
 
 namespace atf {
+
+__host__ __device__ int32_t decode_next(int32_t t0, int32_t t_end, int32_t step) {
+    return t_end - t0 > step ? t0 + step : t_end;
+}
+
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -323,7 +328,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_split_kernel(const Deco
             load_k(B, t0);
         }
     }
-    for (; t0 < t_end; t0 += 32 * kWaves) {
+    for (; t0 < t_end; t0 = decode_next(t0, t_end, 32 * kWaves)) {
         if constexpr (!kRot) {
             B = locate(t0);
             load_k(B, t0);
@@ -429,7 +434,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_split_kernel(const Deco
         if constexpr (kRot) {
             // the next block's K (past the split's last block the current block is loaded
             // again, so that the loads in flight do not depend on the path)
-            const int tn = t0 + 32 * kWaves < t_end ? t0 + 32 * kWaves : t0;
+            const int tn = t_end - t0 > 32 * kWaves ? t0 + 32 * kWaves : t0;
             B = locate(tn);
             load_k(B, tn);
         }
