@@ -186,7 +186,7 @@ __device__ __forceinline__ int ragged_item(const DecodeQ8Params& p, int item, Ro
 // NT tiles of 16 heads share what a wave loads and widens.  NW waves: 4 or 8; with p.direct a
 // workgroup takes a whole row and writes its output.
 template <int D, int NT, int NW>
-__global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 3 : 2) void decode_q8_kernel(const DecodeQ8Params p) {
+__global__ __launch_bounds__(NW * 64, NT == 1 && D == 64 ? 4 : 2) void decode_q8_kernel(const DecodeQ8Params p) {
     constexpr int kChunks = D / 16;
     constexpr int kHalf = D / 2;
     constexpr int kM = D / 64;   // loads of a token: 4 chunks each
