@@ -470,7 +470,7 @@ int atf_decode_paged_unrotated(const void *q, const void *k_pages, const void *v
  *   q_weight, k_weight  fp32 [d], DEVICE, or NULL: those heads are turned but not normed
  *   eps      finite, >= 0
  *   w, rope_inv_freq  the rotation, as atf_cache_append_rotated; a frequency of 0 leaves its
- *            pair as it is (all of them 0: no rotation)
+ *            pair's numbers, where they are finite, as they are (all of them 0: no rotation)
  * n_new == 0 is a no-op (k_new and v_new may be NULL then).
  * Errors: ATF_EINVAL (NULL window, pointer or only one of q and q_out, misaligned pointer,
  * written buffers that overlap another one or an array that the call reads (q_out == q aside),
@@ -501,8 +501,11 @@ int atf_cache_append_paged_normed(const void *q, const void *k_new, const void *
  * no infinities) and one power of two that they are multiplied by, as an e8m0 byte (exponent +
  * 127): the smallest 2^e, e in [-60, 119], with max |x| <= 448 * 2^e (the maximum over the
  * row's finite numbers, 2^-60 if they are all 0 or none is).  Numbers are x / 2^e rounded to
- * nearest even, once (keys after norm and rotation in fp32, or in 64 bits where fp32 leaves open to
- * which of two numbers); what is not finite is stored as NaN.
+ * nearest even, once; what is not finite is stored as NaN.  Values are rounded exactly.  Keys are normed
+ * and turned in fp32, whose error may decide where a number or the row's largest lies next to a
+ * border.  Rows where a number of at least 2^-6 of the power comes within 2 ulps of one, or the
+ * largest within 2 of 448 powers, are formed again in 64 bits; smaller numbers, and small differences
+ * of large ones, may still be the neighbour of the nearest.
  *   k_cache  e4m3 [batch][h_kv][d/16][cache_tokens][16]   pair-chunk-major as the bf16 K cache
  *   v_cache  e4m3 [batch][h_kv][ceil(cache_tokens/16)][d][16]  16-token blocks stored d-major,
  *            a block's tokens IN ORDER (unlike the bf16 V cache's)

@@ -443,11 +443,11 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     };
     // Numbers of a key so near to the middle of two e4m3 numbers (their lower 20 bits near half a
     // step), or whose largest is so near to 448 powers, that fp32's own error may decide: within kNear
-    // ulps, twice that error's size.  One head of a wave in 500 has one; it is formed again in 64 bits
-    // once the wave is through, so that keys round as the formula's do: of 4 million without norm
-    // 3 round to the other side, small ones nearly all (those below 2^-6 of the power,
-    // whose steps are others, and those that are what is left of a much larger difference), at 0.04
-    // to 0.09 of plain fp32's error.  The heads met again cost the calls where a wave's time counts:
+    // ulps (that error's mean square is 0.4 ulps, with norm 0.75).  One head of a wave in 500 has one; it is formed
+    // again in 64 bits once the wave is through.  Of 537 million random numbers 350 to 440 round to the
+    // other side (plain fp32: 780 to 960), at 0.04 to 0.09 of plain fp32's error: none that the test looks
+    // for (plain fp32: 35 to 41), but small ones, below 2^-6 of the power, whose steps are others, and
+    // those that are what is left of a larger difference.  The heads met again cost the calls where a wave's time counts:
     // 64 rows of one token 5.0 -> 5.6 us, 3,885 tokens of 16/16 heads of 64 12.7 -> 12.9, 32,768 of 28/4
     // 110.8 -> 111.3.  Without norm and angle fp32 is exact.
     constexpr uint32_t kNear = 2;
@@ -603,9 +603,11 @@ template <int D>
 hipError_t launch_d(AppendNormedParams p, hipStream_t stream) {
     constexpr int kTokens = 64 / (D / 8);
     const int64_t groups = (int64_t(p.batch) * p.n_new + kTokens - 1) / kTokens;
-    // one head a wave until the chip is full of waves (3 run on a SIMD), then as many as keep it full,
-    // so that a token's angles serve them all, in equal parts.  As many as leave at most 3400 waves,
-    // against at least 4096: 1,000 tokens of 28/4 heads of 128 into 8-bit caches 11.5 -> 8.2 us,
+    // one head a wave until the chip is about full of waves (4 run on a SIMD), then as many as keep it
+    // full, so that a token's angles serve them all, in equal parts.  As many as would leave 3400 waves
+    // if all of a token's heads could be shared out evenly; queries and keys are by themselves, so that
+    // there are more (16,384 for 32,768 tokens of 28/4 heads of 128, 3,888 for 3,885 of 16/16 of 64).
+    // Against enough to leave 4096: 1,000 tokens of 28/4 heads of 128 into 8-bit caches 11.5 -> 8.2 us,
     // 4,000 of 14/2 heads of 64 11.6 -> 8.4, 3,885 of 16/16 13.5 -> 12.7; 900 of 40/2 11.3 -> 12.0;
     // 16,384 and more the same
     const int64_t target = 3400;

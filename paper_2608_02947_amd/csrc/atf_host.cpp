@@ -334,10 +334,15 @@ int32_t decode_plan_items(int32_t cols, bool cols16) {
 // parts of them where a KV head has more than 32 heads; `tiles` 1 or 2 of 16 heads.
 
 // Whether a row is one workgroup's, which writes the output: no partial states, no merge (3 to 5
-// us), but a row's keys in a row.  With as many rows as CUs always (uniform batches; us, split ->
-// whole: 32 rows of 1,000 keys 24/8 heads 19.9 -> 17.0, of 8,000 86.6 -> 83.0), but for those
-// just past a whole round of the workgroups that run at once (36 rows of 8,000 keys 105 ->
-// 120); with fewer while a row costs less than the merge, and the more of the chip's time the
+// us), but a row's keys in a row.  Uniform batches (us, split -> whole): from 177 to 256 groups, where
+// they nearly fill the CUs once, at any length (24/8 heads, 23 rows of 8,000 keys 72 -> 63, of 32,768
+// 242 -> 220; 28 of 32,768 and of 100,000 the same; 32 of 1,000 19.9 -> 17.0, of 8,000 86 -> 82, of 32,768
+// 292 -> 298; 14 of 8,000 16/16 heads of 64 46 -> 42; 92 of 8,000 40/2 heads 88 -> 73).  From 257 to 511
+// up to 1,500 keys only (36 rows of 8,000 105 -> 120, 60 of 2,000 45 -> 49; but 33 of 2,000 37 -> 34
+// would gain, and with two tiles 130 of 2,000 76 -> 42).  From 512 on at any length: most batches are as
+// fast either way (84 rows of 32,768 782 -> 768), those just past a whole round of workgroups lose (65 rows
+// of 8,000 178 -> 194, of 32,768 637 -> 723, 97 913 -> 990; 33 of 32,768 16/16 heads of 64 335 -> 393).
+// With fewer than 177 while a row costs less than the merge, and the more of the chip's time the
 // rows fill, the longer (d = 128: 8 rows of 640 keys 12.4 -> 10.1, of 1,500 14 -> 15; 16 of
 // 1,500 18.6 -> 18.1, of 3,000 24.8 -> 26.3; 20 of 4,000 35.2 -> 34.2; d = 64, 16/16 heads:
 // 1 row of 1,000 8.6 -> 8.5, 8 of 2,000 14.6 -> 14.1; two tiles, 40/2 heads, d = 128: 8 rows of
@@ -381,7 +386,9 @@ int32_t decode_q8_waves(int32_t tiles, int64_t groups, int64_t n_valid, bool rag
     return (tiles == 2 || groups <= 4) && groups * n_valid >= (ragged ? 192000 : 96000) ? 8 : 4;
 }
 
-// Workgroups that run at once: 2 of 4 waves a CU, 3 at d = 64 with one tile; 1 of 8 waves.
+// Workgroups that a plan counts on at once: 2 of 4 waves a CU, 3 at d = 64 with one tile; 1 of 8 waves.
+// Those of two tiles or d = 128 fill a CU; at d = 64 with one tile 4 of 4 waves or 2 of 8 run, but plans
+// of 4 were no faster (ragged batches 10 % either way, a long uniform one 139 -> 147 us).
 int32_t decode_q8_slots(int32_t head_dim, int32_t tiles, int32_t waves) {
     return waves == 8 ? 256 : head_dim == 64 && tiles == 1 ? 768 : 512;
 }
