@@ -13,8 +13,8 @@
 //
 // Bound by HBM where the call is long: 32,768 tokens of 28/4 heads of 128 into 8-bit caches move
 // 571 MB in 110 us (5.2 TB/s, a device copy reaches 5.4), 16,384 of 24/8 heads into bf16 ones 336 MB
-// in 66 us; 3,885 tokens of 16/16 heads of 64 40 MB in 13 us, where vector work (busy 0.63) and a
-// launch's start and end count; one token of each of 16 rows takes 4.3 us.  8 dims a lane make
+// in 67 us; 3,885 tokens of 16/16 heads of 64 40 MB in 13 us, where vector work (busy 0.63) and a
+// launch's start and end count; one token of each of 16 rows takes 3.9 us.  8 dims a lane make
 // every access of a vector 16 bytes; with fewer lanes a vector the keys' 16-byte chunks would be
 // gathered, with more the row's sum would cross more lanes.
 #include "atf_internal.hpp"

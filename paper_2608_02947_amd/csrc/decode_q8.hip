@@ -25,7 +25,7 @@
 // keys' bytes are masked lane by lane.
 //
 // Bound by HBM reads where rows are long or many: one row of 1,048,576 keys, 28/4 heads of 128 (734 MB
-// of kept pairs and values) 138 us, 5.3 TB/s; 8 rows of 32,768, 24/8 heads, 433 MB in 84 (a streaming
+// of kept pairs and values) 142 us, 5.2 TB/s; 8 rows of 32,768, 24/8 heads, 433 MB in 85 (a streaming
 // read reaches 5.57).  24 rows up to 30,011 of 40/2 heads, 97 MB, take 33: the first block is there
 // after 10.6 us and the merge ends 7 after the last.  64 tokens a wave make the values' 16 tokens of a
 // lane a block of the cache and the keys' powers 16 bytes a lane.  2 waves a SIMD: a block's
