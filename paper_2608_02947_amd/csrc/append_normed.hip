@@ -66,8 +66,9 @@ __device__ __forceinline__ uint32_t other_lane(uint32_t x) {
 // pi/4, is turned to radians in two floats, whose first goes through the Taylor series to x^9 and
 // x^10 (truncation below 2^-28) and whose second is added to first order.  The fraction's low word
 // (rounded to it, so that the two do not cancel) is part of the second: next to a quarter turn the
-// smaller of the two is little more.  Both are within about 1.2 ulp, 0.3 in the mean square, of those of
-// the angle as it is held, pos times 2^-64 of a turn off (the hardware's own sine is 2^-20 off).
+// smaller of sine and cosine is little more.  Both are within about 1.2 ulp, 0.3 in the root mean
+// square, of those of the angle as it is held, pos times 2^-64 of a turn off (the hardware's own
+// sine is 2^-20 off).
 __device__ __forceinline__ void cos_sin(uint32_t pos, uint32_t rho_hi, uint32_t rho_lo, float& cs, float& sn) {
     const uint32_t rest = pos * rho_lo;
     const uint32_t f = pos * rho_hi + __umulhi(pos, rho_lo) + (rest >> 31);
@@ -443,13 +444,14 @@ __global__ __launch_bounds__(256) void append_normed_kernel(const AppendNormedPa
     };
     // Numbers of a key so near to the middle of two e4m3 numbers (their lower 20 bits near half a
     // step), or whose largest is so near to 448 powers, that fp32's own error may decide: within kNear
-    // ulps (that error's mean square is 0.4 ulps, with norm 0.75).  One head of a wave in 500 has one; it is formed
-    // again in 64 bits once the wave is through.  Of 537 million random numbers 350 to 440 round to the
-    // other side (plain fp32: 780 to 960), at 0.04 to 0.09 of plain fp32's error: none that the test looks
-    // for (plain fp32: 35 to 41), but small ones, below 2^-6 of the power, whose steps are others, and
-    // those that are what is left of a larger difference.  The heads met again cost the calls where a wave's time counts:
-    // 64 rows of one token 5.0 -> 5.6 us, 3,885 tokens of 16/16 heads of 64 12.7 -> 12.9, 32,768 of 28/4
-    // 110.8 -> 111.3.  Without norm and angle fp32 is exact.
+    // ulps (that error is 0.4 ulps in the root mean square, with norm 0.75).  One head of a wave in 500
+    // has one; it is formed again in 64 bits once the wave is through.  Of 537 million random numbers
+    // 350 to 440 round to the other side (plain fp32: 780 to 960), at 0.04 to 0.09 of plain fp32's
+    // error: none of those next to a border that are no small difference (plain fp32: 35 to 41), but
+    // small ones, below 2^-6 of the power, whose steps are others, and what is left of a larger
+    // difference.  The heads met again cost the calls where a wave's time counts: 64 rows of one token
+    // 5.0 -> 5.6 us, 3,885 tokens of 16/16 heads of 64 12.7 -> 12.9, 32,768 of 28/4 110.8 -> 111.3.
+    // Without norm and angle fp32 is exact.
     constexpr uint32_t kNear = 2;
     [[maybe_unused]] bool exact = weight == nullptr;
     if constexpr (kQ8) {
