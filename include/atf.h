@@ -575,6 +575,141 @@ int atf_decode_paged_q8(const void *q, const void *k_pages, const void *k_scale,
                         const atf_window *w, float softmax_scale, void *workspace,
                         size_t workspace_bytes, void *hip_stream);
 
+/* ---- Sparse attention over pages ------------------------------------------------------
+ *
+ * A serving step whose queries attend some blocks of their row's keys: pages and slots for the new
+ * tokens (atf_plan_pages), the tokens appended through their slots (atf_cache_append_slots), bounds
+ * of the keys of the blocks they touched (atf_block_bounds), the blocks that each query takes by
+ * them (atf_select_blocks), and attention over those (atf_attend_blocks).  Pages as in
+ * atf_cache_append_paged.  A block is block_tokens tokens of a row, a multiple of 32 that divides
+ * page_tokens: token t is in block t / block_tokens.
+ *
+ * Tokens of all rows are PACKED one behind the other.  Each has a row (token_rows) and a position;
+ * a token whose row is outside [0, batch) is padding: nothing of it is read into an output, and its
+ * outputs keep what they hold.  All arrays are on the DEVICE, so that a captured step can be
+ * replayed with other lengths.
+ *
+ * Pages and slots.  Row b holds n_k_rows[b] tokens (clamped to what max_pages_per_row pages hold) and
+ * gets n_new_rows[b].  A negative entry ends the row: its pages go back on the stack of free pages,
+ * rows and pages in order, and it holds nothing.  Then the rows that grow take the pages that they lack
+ * from the stack's top, rows and pages in order, until one finds too few: it and all after it
+ * that would grow get nothing, as do a row that would outgrow its table and, with the rows after it, a
+ * row whose tokens would end past max_tokens.
+ *   block_table  int32 [batch][max_pages_per_row]  entries of the pages taken are written, no others
+ *   free_pages   int32 [free_capacity]: the first *free_count are free, the last of them taken first;
+ *                pages that come back are written behind them (those past the capacity are lost)
+ *   free_count   int32 [1], clamped to [0, free_capacity]
+ *   n_k_out      int32 [batch]: tokens that each row holds after the step; may be n_k_rows itself
+ *   row_starts   int32 [batch + 1]: first packed token of each row (max(n_new_rows[b], 0) tokens a
+ *                row, rows that get nothing too; at most max_tokens)
+ *   slots        int64 [max_tokens]: page * page_tokens + token of the page, or -1: tokens of rows that
+ *                get nothing, tokens past the last row's, tokens whose table entry is negative
+ *   token_rows, positions  int32 [max_tokens]: row and position, or -1 for the first two of those
+ *   counts       int32 [3]: free pages left, packed tokens, rows that should grow and got nothing;
+ *                may be free_count itself (with room for three)
+ * Called again with the same inputs (n_k_out and counts apart from them) it gives the same outputs.
+ * Whole numbers: the same in every run.
+ * Errors: ATF_EINVAL (NULL or misaligned pointer; buffers that overlap, the two named aside; batch < 1
+ * or > 2^20; page_tokens not a positive multiple of 32; max_pages_per_row < 1 or more tokens in a row's
+ * pages than 2^31 - 1; free_capacity < 0; max_tokens < 0 or > 2^30); ATF_EHIP. */
+int atf_plan_pages(int32_t *block_table, int32_t max_pages_per_row, int32_t page_tokens,
+                   int32_t *free_pages, int32_t free_capacity, const int32_t *free_count,
+                   int32_t batch, const int32_t *n_k_rows, const int32_t *n_new_rows,
+                   int32_t *n_k_out, int32_t *row_starts, int64_t max_tokens, int64_t *slots,
+                   int32_t *token_rows, int32_t *positions, int32_t *counts, void *hip_stream);
+
+/* Write packed tokens into pages, each at its slot; tokens whose slot is outside [0, num_pages *
+ * page_tokens) are not stored.  Where two tokens have the same slot it may hold some of either.
+ * Pure data movement (bit-exact); _rotated turns key t to positions[t] on the way in (rotation as
+ * atf_cache_append_rotated; the position of a token that is stored is >= 0).
+ *   k_new, v_new  bf16 [n_tokens][h_kv][d]                    (device, read)
+ *   slots         int64 [n_tokens], DEVICE, 8-byte aligned;  positions  int32 [n_tokens], DEVICE
+ * n_tokens == 0 is a no-op.
+ * Errors: ATF_EINVAL (NULL window or pointer, misaligned pointer, pages that overlap each other or an
+ * input, n_tokens < 0, h_kv < 1, n_tokens * h_kv > 2^29, bad page arguments, a bad rotation
+ * frequency); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
+int atf_cache_append_slots(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
+                           const int64_t *slots, int64_t n_tokens, int32_t num_pages,
+                           int32_t page_tokens, int32_t h_kv, int32_t head_dim, void *hip_stream);
+int atf_cache_append_slots_rotated(const void *k_new, const void *v_new, void *k_pages,
+                                   void *v_pages, const int64_t *slots, const int32_t *positions,
+                                   int64_t n_tokens, int32_t num_pages, int32_t page_tokens,
+                                   int32_t h_kv, const atf_window *w, const double *rope_inv_freq,
+                                   void *hip_stream);
+
+/* Bounds of the keys of blocks: per KV head and dim the largest and the smallest of the block's
+ * keys (rotated ones, as atf_decode_paged reads them), exactly; NaN in both where a key's number is
+ * NaN.  Written for the blocks that hold the last n_new_rows[b] of row b's n_k_rows[b] tokens
+ * (n_new_rows clamped to [0, max_new], n_k_rows to what the row's pages hold), over the tokens that
+ * the row holds; no other block's change.
+ *   bounds  bf16 [num_pages][h_kv][page_tokens/block_tokens][d/16][2][16]: per chunk of 8 pairs the
+ *           16 largest, then the 16 smallest, dims as in the K cache    (device, written)
+ * Table entries are clamped to [0, num_pages).  Blocks that a call writes must be one row's.
+ * Errors: ATF_EINVAL (NULL or misaligned pointer, bounds that overlap an input, batch < 1, h_kv < 1,
+ * max_new < 0, bad page or block arguments); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
+int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_table,
+                     int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                     int32_t block_tokens, int32_t batch, const int32_t *n_k_rows,
+                     const int32_t *n_new_rows, int64_t max_new, int32_t h_kv, int32_t head_dim,
+                     void *hip_stream);
+
+/* The blocks that query tokens take.  Token t, at position p of row b, reaches keys 0 .. last =
+ * min(p, n_k_rows[b] - 1) and the blocks 0 .. last / block_tokens.  With hi and lo a block's bounds, z0 and
+ * z1 the distances of its last reached and of its first key, the score of a block for a query head is
+ *   sum over pairs r with z0 <= W_r of u_r,   u_r = sum over the pair's two dims of
+ *                                                   max(q, 0) hi + min(q, 0) lo,
+ * with max(u_r, 0) for u_r where z1 > W_r: no key of the block has a larger windowed score (unscaled).
+ * The query heads of one KV head take the same blocks: a block counts by its largest score of them.
+ * Taken are, top_blocks in all: the first first_blocks blocks and the last last_blocks; blocks
+ * with a score that is NaN; then those with the largest scores; of equal ones the lower block.  Scores
+ * are compared as exact sums would be: summed in 64 bits wherever fp32 cannot tell.
+ *   q       bf16 [n_tokens][h_q][d], rotated                       (device, read)
+ *   bounds  as atf_block_bounds                                    (device, read)
+ *   blocks  int32 [n_tokens][h_kv][top_blocks], ascending, then -1 where the row has fewer (device, written)
+ *   token_rows, positions  int32 [n_tokens];  n_k_rows  int32 [batch], clamped to [0, max_n_k]
+ *   workspace: device, >= atf_select_workspace_bytes(n_tokens, h_q, h_kv, max_n_k, block_tokens, d)
+ *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each
+ * Table entries are clamped to [0, num_pages).  n_tokens == 0 is a no-op.  Deterministic.
+ * Errors: ATF_EINVAL (NULL window or pointer, misaligned pointer, written buffers that overlap another
+ * one, batch < 1, n_tokens < 0, n_tokens * h_q > 2^23, heads < 1, h_q % h_kv != 0, max_n_k < 1 or more than a
+ * row's pages hold, top_blocks < 1 or > 4096, first_blocks or last_blocks < 0 or their sum above top_blocks,
+ * bad page or block arguments, bad window); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EWORKSPACE; ATF_EHIP.
+ * The size function returns 0 for invalid sizes. */
+size_t atf_select_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int64_t max_n_k,
+                                  int32_t block_tokens, int32_t head_dim);
+int atf_select_blocks(const void *q, const void *bounds, int32_t *blocks, int64_t n_tokens,
+                      const int32_t *block_table, int32_t max_pages_per_row, int32_t num_pages,
+                      int32_t page_tokens, int32_t block_tokens, int32_t batch,
+                      const int32_t *token_rows, const int32_t *positions, const int32_t *n_k_rows,
+                      int64_t max_n_k, int32_t top_blocks, int32_t first_blocks,
+                      int32_t last_blocks, int32_t h_q, int32_t h_kv, const atf_window *w,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Windowed attention of query tokens over the blocks that a list names for each token and KV head:
+ * atf_decode_paged's scores, softmax and sums over the keys of those blocks that the token reaches
+ * (keys 0 .. min(p, n_k_rows[b] - 1) of its row).  Entries of the list that are negative or past the
+ * last reached block are skipped, the others may come in any order; a block named twice counts
+ * twice.  A token with no key gets 0 and an LSE of -INFINITY.
+ *   q, o     bf16 [n_tokens][h_q][d];  lse  fp32 [n_tokens][h_q]
+ *   blocks   int32 [n_tokens][h_kv][top_blocks], as atf_select_blocks writes it   (device, read)
+ *   n_k_rows int32 [batch], clamped to what a row's pages hold
+ *   workspace: device, >= atf_attend_workspace_bytes(n_tokens, h_q, h_kv, top_blocks, block_tokens, d)
+ *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each
+ * A row gives NaN where a number of a key is NaN in a pair that the window keeps; past its pair's
+ * window such a number does not count.  softmax_scale <= 0 selects 1/sqrt(d).  Any group size is
+ * built: up to 32 query heads of a KV head share a workgroup.  Table entries are clamped to [0, num_pages).
+ * n_tokens == 0 is a no-op.  Deterministic.
+ * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite. */
+size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int32_t top_blocks,
+                                  int32_t block_tokens, int32_t head_dim);
+int atf_attend_blocks(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,
+                      int64_t n_tokens, const int32_t *block_table, int32_t max_pages_per_row,
+                      int32_t num_pages, int32_t page_tokens, int32_t block_tokens, int32_t batch,
+                      const int32_t *token_rows, const int32_t *positions, const int32_t *n_k_rows,
+                      const int32_t *blocks, int32_t top_blocks, int32_t h_q, int32_t h_kv,
+                      const atf_window *w, float softmax_scale, void *workspace,
+                      size_t workspace_bytes, void *hip_stream);
+
 /* Message of the most recent failed call on this thread ("" if none). */
 const char *atf_last_error(void);
 

@@ -30,6 +30,11 @@ The functions carry the C names of ``include/atf.h``:
   (e4m3 numbers and a power of two per row); :func:`atf_cache_read_q8`,
   :func:`atf_cache_read_paged_q8` -- those read back into bf16 caches; :func:`atf_decode_q8`,
   :func:`atf_decode_ragged_q8`, :func:`atf_decode_paged_q8` -- decode over them.
+- :func:`atf_plan_pages`, :func:`atf_cache_append_slots`, :func:`atf_cache_append_slots_rotated`
+  -- pages and slots of packed tokens from the rows' lengths, on the GPU, and appends through
+  them; :func:`atf_block_bounds`, :func:`atf_select_blocks`, :func:`atf_attend_blocks` (with
+  :func:`atf_select_workspace_bytes`, :func:`atf_attend_workspace_bytes`) -- bounds of the keys of
+  blocks, the blocks a query takes by them, attention over those.
 """
 from __future__ import annotations
 
@@ -127,6 +132,16 @@ def _load():
                                                 f32, P, ctypes.c_size_t, P]),
         "atf_decode_paged_q8": (ctypes.c_int, [P, P, P, P, P, P, P, i32, P, i32, i32, i32, P, P, i64,
                                                i32, i32, W, f32, P, ctypes.c_size_t, P]),
+        "atf_plan_pages": (ctypes.c_int, [P, i32, i32, P, i32, P, i32, P, P, P, P, i64, P, P, P, P, P]),
+        "atf_cache_append_slots": (ctypes.c_int, [P, P, P, P, P, i64, i32, i32, i32, i32, P]),
+        "atf_cache_append_slots_rotated": (ctypes.c_int, [P, P, P, P, P, P, i64, i32, i32, i32, W, P, P]),
+        "atf_block_bounds": (ctypes.c_int, [P, P, P, i32, i32, i32, i32, i32, P, P, i64, i32, i32, P]),
+        "atf_select_workspace_bytes": (ctypes.c_size_t, [i64, i32, i32, i64, i32, i32]),
+        "atf_select_blocks": (ctypes.c_int, [P, P, P, i64, P, i32, i32, i32, i32, i32, P, P, P, i64, i32, i32,
+                                             i32, i32, i32, W, P, ctypes.c_size_t, P]),
+        "atf_attend_workspace_bytes": (ctypes.c_size_t, [i64, i32, i32, i32, i32, i32]),
+        "atf_attend_blocks": (ctypes.c_int, [P, P, P, P, P, i64, P, i32, i32, i32, i32, i32, P, P, P, P, i32,
+                                             i32, i32, W, f32, P, ctypes.c_size_t, P]),
         "atf_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -147,7 +162,9 @@ EXPORTED = ("atf_window_table", "atf_retention_profile", "atf_count_terms", "atf
             "atf_decode_paged_unrotated", "atf_cache_append_normed", "atf_cache_append_paged_normed",
             "atf_cache_append_q8", "atf_cache_append_paged_q8", "atf_cache_read_q8",
             "atf_cache_read_paged_q8", "atf_decode_q8", "atf_decode_ragged_q8",
-            "atf_decode_paged_q8", "atf_last_error")
+            "atf_decode_paged_q8", "atf_plan_pages", "atf_cache_append_slots",
+            "atf_cache_append_slots_rotated", "atf_block_bounds", "atf_select_workspace_bytes",
+            "atf_select_blocks", "atf_attend_workspace_bytes", "atf_attend_blocks", "atf_last_error")
 
 
 def library():
@@ -745,7 +762,7 @@ class _Types:
     def __init__(self):
         torch = _torch()
         self.bf16, self.f32, self.i32, self.u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
-        self.e4m3, self.e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+        self.e4m3, self.e8m0, self.i64 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.int64
         self.device = torch.cuda.current_device
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -1008,3 +1025,166 @@ def atf_decode_paged_q8(q, k_pages, k_scale, v_pages, v_scale, o, lse, block_tab
                                     *pools, *rows, int(max_n_k), h_q, h_kv, cw, softmax_scale,
                                     _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
                                     st if stream is None else stream.cuda_stream))
+
+
+# ---------------------------------------------------------------------------
+# pages and slots, and attention over the blocks of a row that a query takes
+# ---------------------------------------------------------------------------
+def bounds_shape(num_pages: int, page_tokens: int, block_tokens: int, h_kv: int, head_dim: int):
+    """Shape of the bounds beside K pages, bf16: [num_pages, h_kv, page_tokens/block_tokens,
+    d/16, 2, 16], per chunk the largest numbers, then the smallest."""
+    return (num_pages, h_kv, page_tokens // block_tokens, head_dim // 16, 2, 16)
+
+
+def atf_plan_pages(block_table, page_tokens: int, free_pages, free_count, n_k_rows, n_new_rows, n_k_out,
+                   row_starts, slots, token_rows, positions, counts, stream=None):
+    """Rows that end give back their pages, rows that grow take new ones, and every new token gets
+    its slot, row and position.  block_table [B, max_pages], free_pages [F], free_count [1],
+    n_k_rows and n_new_rows [B] (negative: the row ends) -> block_table, free_pages, n_k_out [B] (may
+    be n_k_rows), row_starts [B + 1], slots [T] (int64), token_rows and positions [T], counts
+    [3] (free pages left, packed tokens, rows refused).  All on the device, int32 but slots."""
+    fn = "atf_plan_pages"
+    ty, dev, st = _call()
+    if len(block_table.shape) != 2 or len(free_pages.shape) != 1 or len(slots.shape) != 1:
+        raise ValueError(f"{fn}: block_table must be [B, max_pages], free_pages [F], slots [T]")
+    B, width = block_table.shape
+    F, T = free_pages.shape[0], slots.shape[0]
+    if free_count.numel() < 1 or counts.shape != (3,):
+        raise ValueError(f"{fn}: free_count must hold a number, counts three")
+    _check(_lib.atf_plan_pages(
+        _ptr(block_table, ty.i32, dev, "block_table"), width, int(page_tokens),
+        _ptr(free_pages, ty.i32, dev, "free_pages"), F, _ptr(free_count, ty.i32, dev, "free_count"), B,
+        _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), _vector(n_new_rows, ty.i32, dev, "n_new_rows", B),
+        _vector(n_k_out, ty.i32, dev, "n_k_out", B), _vector(row_starts, ty.i32, dev, "row_starts", B + 1), T,
+        _ptr(slots, ty.i64, dev, "slots"), _vector(token_rows, ty.i32, dev, "token_rows", T),
+        _vector(positions, ty.i32, dev, "positions", T), _ptr(counts, ty.i32, dev, "counts"),
+        st if stream is None else stream.cuda_stream))
+
+
+def _slot_args(fn, ty, dev, k_new, v_new, k_pages, v_pages, slots):
+    """(pointers of k_new, v_new, k_pages, v_pages, slots), T, pages, tokens of a page, h_kv, d."""
+    T, h_kv, d = k_new.shape
+    ks = k_pages.shape
+    if len(ks) != 5:
+        raise ValueError(f"{fn}: page pools must be 5-d (see kpages_shape, vpages_shape)")
+    pages, tokens = ks[0], ks[3]
+    if v_new.shape != k_new.shape or ks != (pages, h_kv, d // 16, tokens, 16) or \
+            v_pages.shape != (pages, h_kv, tokens // 16, d, 16) or slots.shape != (T,):
+        raise ValueError(f"{fn}: inconsistent shapes")
+    return ((_ptr(k_new, ty.bf16, dev, "k_new"), _ptr(v_new, ty.bf16, dev, "v_new"),
+             _ptr(k_pages, ty.bf16, dev, "k_pages"), _ptr(v_pages, ty.bf16, dev, "v_pages"),
+             _ptr(slots, ty.i64, dev, "slots")), T, pages, tokens, h_kv, d)
+
+
+def atf_cache_append_slots(k_new, v_new, k_pages, v_pages, slots, stream=None):
+    """Packed tokens k_new, v_new [T, h_kv, d] into pages, token t at slots[t] (int64 [T], device;
+    negative: not stored), as atf_plan_pages gives them."""
+    fn = "atf_cache_append_slots"
+    ty, dev, st = _call()
+    ptrs, T, pages, tokens, h_kv, d = _slot_args(fn, ty, dev, k_new, v_new, k_pages, v_pages, slots)
+    _check(_lib.atf_cache_append_slots(*ptrs, T, pages, tokens, h_kv, d, st if stream is None else stream.cuda_stream))
+
+
+def atf_cache_append_slots_rotated(k_new, v_new, k_pages, v_pages, slots, positions, window: Window,
+                                   rope_inv_freq=None, stream=None):
+    """atf_cache_append_slots with the keys given unrotated: key t is turned to positions[t]
+    (int32 [T], device)."""
+    fn = "atf_cache_append_slots_rotated"
+    ty, dev, st = _call()
+    ptrs, T, pages, tokens, h_kv, d = _slot_args(fn, ty, dev, k_new, v_new, k_pages, v_pages, slots)
+    if window.head_dim != d:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    cw, keep = window.as_c()
+    fp, keep2 = _rope_freq(rope_inv_freq, d)
+    _check(_lib.atf_cache_append_slots_rotated(*ptrs, _vector(positions, ty.i32, dev, "positions", T), T, pages,
+                                               tokens, h_kv, cw, fp, st if stream is None else stream.cuda_stream))
+
+
+def _bounds(fn, ty, dev, bounds, page_tokens, h_kv, d):
+    """(pointer of the bounds, tokens of a block) of pages of page_tokens tokens."""
+    bs = bounds.shape
+    if len(bs) != 6 or bs != (bs[0], h_kv, bs[2], d // 16, 2, 16) or bs[2] < 1 or page_tokens % bs[2]:
+        raise ValueError(f"{fn}: bounds must be [pages, h_kv, blocks of a page, d/16, 2, 16] (see bounds_shape)")
+    return _ptr(bounds, ty.bf16, dev, "bounds"), page_tokens // bs[2]
+
+
+def _rows_table(fn, ty, dev, block_table):
+    """(table pointer, rows, pages of a row)."""
+    if len(block_table.shape) != 2:
+        raise ValueError(f"{fn}: block_table must be [B, max_pages]")
+    return _ptr(block_table, ty.i32, dev, "block_table"), block_table.shape[0], block_table.shape[1]
+
+
+def atf_block_bounds(k_pages, bounds, block_table, n_k_rows, n_new_rows, max_new: int, stream=None):
+    """Largest and smallest number of each dim of the keys of the blocks that hold the last
+    n_new_rows[b] (at most max_new) of row b's n_k_rows[b] tokens (int32 [B], device), into bounds
+    of bounds_shape."""
+    fn = "atf_block_bounds"
+    ty, dev, st = _call()
+    if len(k_pages.shape) != 5 or k_pages.shape[4] != 16 or bounds.shape[0] != k_pages.shape[0]:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    pages, h_kv, nc, pt, _ = k_pages.shape
+    bp, bt = _bounds(fn, ty, dev, bounds, pt, h_kv, 16 * nc)
+    tp, B, width = _rows_table(fn, ty, dev, block_table)
+    _check(_lib.atf_block_bounds(_ptr(k_pages, ty.bf16, dev, "k_pages"), bp, tp, width, pages, pt, bt, B,
+                                 _vector(n_k_rows, ty.i32, dev, "n_k_rows", B),
+                                 _vector(n_new_rows, ty.i32, dev, "n_new_rows", B), int(max_new), h_kv, 16 * nc,
+                                 st if stream is None else stream.cuda_stream))
+
+
+def atf_select_workspace_bytes(n_tokens: int, h_q: int, h_kv: int, max_n_k: int, block_tokens: int,
+                               head_dim: int) -> int:
+    return int(_lib.atf_select_workspace_bytes(n_tokens, h_q, h_kv, max_n_k, block_tokens, head_dim))
+
+
+def atf_select_blocks(q, bounds, blocks, block_table, page_tokens: int, token_rows, positions, n_k_rows,
+                      max_n_k: int, window: Window, workspace, first_blocks: int = 1, last_blocks: int = 1,
+                      stream=None):
+    """The blocks that each query token takes: q [T, h_q, d] bf16, rotated; bounds of bounds_shape;
+    token_rows and positions [T], n_k_rows [B] (int32, device) -> blocks [T, h_kv, N] int32, ascending,
+    -1 where a row has fewer: the first and the last ones, then those whose bounds allow the largest
+    scores; workspace: uint8 of atf_select_workspace_bytes()."""
+    fn = "atf_select_blocks"
+    ty, dev, st = _call()
+    T, h_q, d = q.shape
+    if len(blocks.shape) != 3 or blocks.shape[0] != T or window.head_dim != d:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    h_kv, top = blocks.shape[1], blocks.shape[2]
+    bp, bt = _bounds(fn, ty, dev, bounds, int(page_tokens), h_kv, d)
+    tp, B, width = _rows_table(fn, ty, dev, block_table)
+    cw, keep = window.as_c()
+    _check(_lib.atf_select_blocks(
+        _ptr(q, ty.bf16, dev, "q"), bp, _ptr(blocks, ty.i32, dev, "blocks"), T, tp, width, bounds.shape[0],
+        int(page_tokens), bt, B, _vector(token_rows, ty.i32, dev, "token_rows", T),
+        _vector(positions, ty.i32, dev, "positions", T), _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), int(max_n_k),
+        top, int(first_blocks), int(last_blocks), h_q, h_kv, cw, _ptr(workspace, ty.u8, dev, "workspace"),
+        workspace.numel(), st if stream is None else stream.cuda_stream))
+
+
+def atf_attend_workspace_bytes(n_tokens: int, h_q: int, h_kv: int, top_blocks: int, block_tokens: int,
+                               head_dim: int) -> int:
+    return int(_lib.atf_attend_workspace_bytes(n_tokens, h_q, h_kv, top_blocks, block_tokens, head_dim))
+
+
+def atf_attend_blocks(q, k_pages, v_pages, o, lse, block_table, token_rows, positions, n_k_rows, blocks,
+                      block_tokens: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
+    """Windowed attention of query tokens q [T, h_q, d] over the blocks [T, h_kv, N] of their rows
+    (int32; negative: none) -> o like q, lse [T, h_q] fp32; workspace: uint8 of
+    atf_attend_workspace_bytes()."""
+    fn = "atf_attend_blocks"
+    ty, dev, st = _call()
+    T, h_q, d = q.shape
+    h_kv = k_pages.shape[1]
+    if o.shape != q.shape or lse.shape != (T, h_q) or len(blocks.shape) != 3 or blocks.shape[:2] != (T, h_kv) or \
+            window.head_dim != d:
+        raise ValueError(f"{fn}: inconsistent shapes")
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, block_table.shape[0], h_kv, d)
+    B = block_table.shape[0]
+    cw, keep = window.as_c()
+    _check(_lib.atf_attend_blocks(
+        _ptr(q, ty.bf16, dev, "q"), _ptr(k_pages, ty.bf16, dev, "k_pages"), _ptr(v_pages, ty.bf16, dev, "v_pages"),
+        *_decode_out(ty, dev, o, lse), T, *pools, int(block_tokens), B,
+        _vector(token_rows, ty.i32, dev, "token_rows", T), _vector(positions, ty.i32, dev, "positions", T),
+        _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), _ptr(blocks, ty.i32, dev, "blocks"), blocks.shape[2], h_q,
+        h_kv, cw, softmax_scale, _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
+        st if stream is None else stream.cuda_stream))

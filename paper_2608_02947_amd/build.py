@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libatf.so")
 SOURCES = ["atf_host.cpp", "prefill.hip", "decode.hip", "rotate.hip", "append_normed.hip",
-           "cache_q8.hip", "decode_q8.hip"]
+           "cache_q8.hip", "decode_q8.hip", "pages.hip", "blocks.hip", "attend_blocks.hip"]
 # device-limit microbenchmarks timed by bench.py --peaks (not part of the attention ABI)
 PROBE_SOURCES = ["peaks.hip"]
 PROBE_LIB = os.path.join(PKG, "libatf_peaks.so")

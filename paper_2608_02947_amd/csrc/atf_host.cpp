@@ -1586,3 +1586,416 @@ int atf_decode_paged_q8(const void* q, const void* k_pages, const void* k_scale,
 }
 
 }  // extern "C"
+
+namespace {
+
+// ---- pages and slots, and attention over the blocks of a row that a query takes
+
+// Page pools of block_tokens-token blocks.
+int check_blocks(const char* fn, const PagedArgs& pg, int32_t block_tokens, int64_t* row_cap) {
+    const int rc = check_pages(fn, pg, row_cap);
+    if (rc != ATF_OK) return rc;
+    if (block_tokens < 32 || block_tokens % 32 != 0 || pg.page_tokens % block_tokens != 0)
+        return fail(ATF_EINVAL, "%s: block_tokens %d must be a positive multiple of 32 that divides page_tokens %d",
+                    fn, block_tokens, pg.page_tokens);
+    return ATF_OK;
+}
+
+int check_head_dim(const char* fn, int32_t d) {
+    if (d != 64 && d != 128) return fail(ATF_EUNSUPPORTED, "%s: head_dim %d not built (64 or 128)", fn, d);
+    return ATF_OK;
+}
+
+// Bytes of a pool whose tokens take row_bytes a head: 2^46 at most, more than a device holds (the
+// factors may be any int32s).
+size_t pool_bytes(const PagedArgs& pg, int32_t h_kv, int64_t row_bytes) {
+    const u128 n = u128(pg.num_pages) * u128(pg.page_tokens) * u128(h_kv) * u128(row_bytes);
+    return size_t(std::min(n, u128(1) << 46));
+}
+
+int append_slots_impl(const char* fn, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                      const int64_t* slots, const int32_t* positions, int64_t n_tokens, int32_t num_pages,
+                      int32_t page_tokens, int32_t h_kv, int32_t d, bool turn, atf::AppendSlotsParams& p,
+                      void* hip_stream) {
+    if (n_tokens < 0 || h_kv < 1) return fail(ATF_EINVAL, "%s: need n_tokens >= 0 and h_kv >= 1", fn);
+    if (page_tokens < 32 || page_tokens % 32 != 0 || num_pages < 1)
+        return fail(ATF_EINVAL, "%s: page_tokens %d must be a positive multiple of 32, num_pages >= 1", fn, page_tokens);
+    if (n_tokens > (int64_t(1) << 29) / h_kv)
+        return fail(ATF_EINVAL, "%s: n_tokens * h_kv above 2^29", fn);
+    if (!k_pages || !v_pages || (n_tokens > 0 && (!k_new || !v_new || !slots || (turn && !positions))))
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
+        !aligned(slots, 8) || !aligned(positions, 4))
+        return fail(ATF_EINVAL, "%s: tensors must be 16-byte, slots 8-byte, positions 4-byte aligned", fn);
+    const PagedArgs pg = paged_args(nullptr, 1, num_pages, page_tokens);
+    const size_t pool = pool_bytes(pg, h_kv, 2 * int64_t(d)), rows = size_t(n_tokens) * size_t(h_kv) * size_t(d) * 2;
+    const Span spans[] = {{"k_pages", k_pages, pool, true},
+                          {"v_pages", v_pages, pool, true},
+                          {"k_new", k_new, rows, false},
+                          {"v_new", v_new, rows, false},
+                          {"slots", slots, size_t(n_tokens) * 8, false},
+                          {"positions", positions, size_t(n_tokens) * 4, false}};
+    const int rc = check_apart(fn, spans);
+    if (rc != ATF_OK) return rc;
+    if (n_tokens == 0) return ATF_OK;
+    p.k_new = static_cast<const uint16_t*>(k_new);
+    p.v_new = static_cast<const uint16_t*>(v_new);
+    p.k_pages = static_cast<uint16_t*>(k_pages);
+    p.v_pages = static_cast<uint16_t*>(v_pages);
+    p.slots = slots;
+    p.positions = positions;
+    p.pool_tokens = int64_t(num_pages) * page_tokens;
+    p.n_tokens = static_cast<int32_t>(n_tokens);
+    p.h_kv = h_kv;
+    p.page_tokens = page_tokens;
+    const hipError_t e = atf::launch_append_slots(p, turn, d, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+// What a selection and the attention over it share: the query tokens and where their rows are.
+struct QueryTokens {
+    int64_t n_tokens;
+    int32_t batch;
+    const int32_t* token_rows;
+    const int32_t* positions;
+    const int32_t* n_k_rows;
+    int32_t h_q, h_kv;
+};
+int check_tokens(const char* fn, const QueryTokens& q) {
+    if (q.batch < 1 || q.n_tokens < 0 || q.h_q < 1 || q.h_kv < 1)
+        return fail(ATF_EINVAL, "%s: need batch >= 1, n_tokens >= 0, heads >= 1", fn);
+    if (q.h_q % q.h_kv != 0) return fail(ATF_EINVAL, "%s: h_q %d not a multiple of h_kv %d", fn, q.h_q, q.h_kv);
+    if (q.n_tokens > atf::kMaxTokenHeads / q.h_q)
+        return fail(ATF_EINVAL, "%s: n_tokens * h_q above 2^23", fn);
+    if (!q.n_k_rows || (q.n_tokens > 0 && (!q.token_rows || !q.positions)))
+        return fail(ATF_EINVAL, "%s: NULL rows, positions or row lengths", fn);
+    if (!aligned(q.token_rows, 4) || !aligned(q.positions, 4) || !aligned(q.n_k_rows, 4))
+        return fail(ATF_EINVAL, "%s: rows, positions and row lengths must be 4-byte aligned", fn);
+    return ATF_OK;
+}
+
+struct SelectLayout {
+    int32_t slab;
+    size_t total;
+};
+SelectLayout select_layout(int64_t n_tokens, int32_t h_kv, int64_t row_blocks) {
+    const u128 each = u128(h_kv) * u128(row_blocks) * 8;
+    int64_t slab = int64_t(std::min<u128>(u128(atf::kSelectSlabBytes) / each, u128(std::max<int64_t>(n_tokens, 1))));
+    slab = std::max<int64_t>(1, std::min<int64_t>(slab, 65535 / h_kv));
+    SelectLayout L;
+    L.slab = static_cast<int32_t>(slab);
+    const u128 total = u128(slab) * each;
+    L.total = total > u128(INT64_MAX) ? 0 : align_up(size_t(total), 256);
+    return L;
+}
+
+}  // namespace
+
+extern "C" {
+
+int atf_plan_pages(int32_t* block_table, int32_t max_pages_per_row, int32_t page_tokens, int32_t* free_pages,
+                   int32_t free_capacity, const int32_t* free_count, int32_t batch, const int32_t* n_k_rows,
+                   const int32_t* n_new_rows, int32_t* n_k_out, int32_t* row_starts, int64_t max_tokens,
+                   int64_t* slots, int32_t* token_rows, int32_t* positions, int32_t* counts, void* hip_stream) {
+    const char* fn = "plan_pages";
+    int64_t cap;
+    // (the pool's size is not known here, nor needed)
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, 1, page_tokens);
+    int rc = check_pages(fn, pg, &cap);
+    if (rc != ATF_OK) return rc;
+    if (batch < 1 || batch > (1 << 20) || free_capacity < 0 || max_tokens < 0 || max_tokens > (int64_t(1) << 30))
+        return fail(ATF_EINVAL, "%s: need 1 <= batch <= 2^20, free_capacity >= 0, 0 <= max_tokens <= 2^30", fn);
+    if ((free_capacity > 0 && !free_pages) || !free_count || !n_k_rows || !n_new_rows || !n_k_out || !row_starts ||
+        !counts || (max_tokens > 0 && (!slots || !token_rows || !positions)))
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    const void* ints[] = {free_pages, free_count, n_k_rows, n_new_rows, n_k_out, row_starts, token_rows, positions, counts};
+    for (const void* x : ints)
+        if (!aligned(x, 4)) return fail(ATF_EINVAL, "%s: arrays must be 4-byte aligned", fn);
+    if (!aligned(slots, 8)) return fail(ATF_EINVAL, "%s: slots must be 8-byte aligned", fn);
+    const size_t rows = size_t(batch) * 4, tokens = size_t(max_tokens) * 4;
+    const Span spans[] = {{"block_table", block_table, table_bytes(pg, batch), true},
+                          {"free_pages", free_pages, size_t(free_capacity) * 4, true},
+                          {"free_count", counts == free_count ? nullptr : free_count, 4, false},
+                          {"n_k_rows", n_k_out == n_k_rows ? nullptr : n_k_rows, rows, false},
+                          {"n_new_rows", n_new_rows, rows, false},
+                          {"n_k_out", n_k_out, rows, true},
+                          {"row_starts", row_starts, rows + 4, true},
+                          {"slots", slots, 2 * tokens, true},
+                          {"token_rows", token_rows, tokens, true},
+                          {"positions", positions, tokens, true},
+                          {"counts", counts, 12, true}};
+    rc = check_apart(fn, spans);
+    if (rc != ATF_OK) return rc;
+    atf::PlanParams p{};
+    p.block_table = block_table;
+    p.free_pages = free_pages;
+    p.free_count = free_count;
+    p.n_k_rows = n_k_rows;
+    p.n_new_rows = n_new_rows;
+    p.n_k_out = n_k_out;
+    p.row_starts = row_starts;
+    p.slots = slots;
+    p.token_rows = token_rows;
+    p.positions = positions;
+    p.counts = counts;
+    p.batch = batch;
+    p.max_pages = max_pages_per_row;
+    p.page_tokens = page_tokens;
+    p.free_capacity = free_capacity;
+    p.max_tokens = static_cast<int32_t>(max_tokens);
+    const hipError_t e = atf::launch_plan_pages(p, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+int atf_cache_append_slots(const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int64_t* slots,
+                           int64_t n_tokens, int32_t num_pages, int32_t page_tokens, int32_t h_kv, int32_t head_dim,
+                           void* hip_stream) {
+    const char* fn = "cache_append_slots";
+    const int rc = check_head_dim(fn, head_dim);
+    if (rc != ATF_OK) return rc;
+    atf::AppendSlotsParams p{};
+    return append_slots_impl(fn, k_new, v_new, k_pages, v_pages, slots, nullptr, n_tokens, num_pages, page_tokens,
+                             h_kv, head_dim, false, p, hip_stream);
+}
+
+int atf_cache_append_slots_rotated(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                   const int64_t* slots, const int32_t* positions, int64_t n_tokens,
+                                   int32_t num_pages, int32_t page_tokens, int32_t h_kv, const atf_window* w,
+                                   const double* rope_inv_freq, void* hip_stream) {
+    const char* fn = "cache_append_slots_rotated";
+    if (w == nullptr) return fail(ATF_EINVAL, "%s: NULL window", fn);
+    int rc = check_head_dim(fn, w->head_dim);
+    if (rc != ATF_OK) return rc;
+    atf::AppendSlotsParams p{};
+    rc = rope_fractions(fn, w, rope_inv_freq, p.rope_rho_hi, p.rope_rho_lo);
+    if (rc != ATF_OK) return rc;
+    return append_slots_impl(fn, k_new, v_new, k_pages, v_pages, slots, positions, n_tokens, num_pages, page_tokens,
+                             h_kv, w->head_dim, true, p, hip_stream);
+}
+
+int atf_block_bounds(const void* k_pages, void* bounds, const int32_t* block_table, int32_t max_pages_per_row,
+                     int32_t num_pages, int32_t page_tokens, int32_t block_tokens, int32_t batch,
+                     const int32_t* n_k_rows, const int32_t* n_new_rows, int64_t max_new, int32_t h_kv,
+                     int32_t head_dim, void* hip_stream) {
+    const char* fn = "block_bounds";
+    int rc = check_head_dim(fn, head_dim);
+    if (rc != ATF_OK) return rc;
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    int64_t cap;
+    rc = check_blocks(fn, pg, block_tokens, &cap);
+    if (rc != ATF_OK) return rc;
+    if (batch < 1 || h_kv < 1 || max_new < 0)
+        return fail(ATF_EINVAL, "%s: need batch >= 1, h_kv >= 1, max_new >= 0", fn);
+    if (!k_pages || !bounds || !n_k_rows || !n_new_rows) return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    if (!aligned(k_pages, 16) || !aligned(bounds, 16) || !aligned(n_k_rows, 4) || !aligned(n_new_rows, 4))
+        return fail(ATF_EINVAL, "%s: tensors must be 16-byte, row arrays 4-byte aligned", fn);
+    const size_t rows = size_t(batch) * 4;
+    const Span spans[] = {{"bounds", bounds, pool_bytes(pg, h_kv, 4 * int64_t(head_dim)) / size_t(block_tokens), true},
+                          {"k_pages", k_pages, pool_bytes(pg, h_kv, 2 * int64_t(head_dim)), false},
+                          {"block_table", block_table, table_bytes(pg, batch), false},
+                          {"n_k_rows", n_k_rows, rows, false},
+                          {"n_new_rows", n_new_rows, rows, false}};
+    rc = check_apart(fn, spans);
+    if (rc != ATF_OK) return rc;
+    max_new = std::min(max_new, cap);
+    if (max_new == 0) return ATF_OK;
+    atf::BoundsParams p{};
+    p.k_pages = static_cast<const uint16_t*>(k_pages);
+    p.bounds = static_cast<uint16_t*>(bounds);
+    p.block_table = block_table;
+    p.n_k_rows = n_k_rows;
+    p.n_new_rows = n_new_rows;
+    p.batch = batch;
+    p.max_pages = max_pages_per_row;
+    p.num_pages = num_pages;
+    p.page_tokens = page_tokens;
+    p.block_tokens = block_tokens;
+    p.h_kv = h_kv;
+    p.chunks = static_cast<uint32_t>(head_dim / 16);
+    p.max_new = static_cast<int32_t>(max_new);
+    p.row_blocks = static_cast<uint32_t>(std::min(cap / block_tokens, (max_new + block_tokens - 2) / block_tokens + 1));
+    const hipError_t e = atf::launch_block_bounds(p, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+size_t atf_select_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int64_t max_n_k, int32_t block_tokens,
+                                  int32_t head_dim) {
+    if (n_tokens < 0 || h_q < 1 || h_kv < 1 || h_q % h_kv || max_n_k < 1 || max_n_k > kPosLimit ||
+        block_tokens < 32 || block_tokens % 32 != 0 || (head_dim != 64 && head_dim != 128) ||
+        n_tokens > atf::kMaxTokenHeads / h_q)
+        return 0;
+    return select_layout(n_tokens, h_kv, (max_n_k + block_tokens - 1) / block_tokens).total;
+}
+
+int atf_select_blocks(const void* q, const void* bounds, int32_t* blocks, int64_t n_tokens, const int32_t* block_table,
+                      int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens, int32_t block_tokens,
+                      int32_t batch, const int32_t* token_rows, const int32_t* positions, const int32_t* n_k_rows,
+                      int64_t max_n_k, int32_t top_blocks, int32_t first_blocks, int32_t last_blocks, int32_t h_q,
+                      int32_t h_kv, const atf_window* w, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const char* fn = "select_blocks";
+    if (w == nullptr) return fail(ATF_EINVAL, "%s: NULL window", fn);
+    const int d = w->head_dim;
+    int rc = check_head_dim(fn, d);
+    if (rc != ATF_OK) return rc;
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    int64_t cap;
+    rc = check_blocks(fn, pg, block_tokens, &cap);
+    if (rc != ATF_OK) return rc;
+    rc = check_tokens(fn, {n_tokens, batch, token_rows, positions, n_k_rows, h_q, h_kv});
+    if (rc != ATF_OK) return rc;
+    if (max_n_k < 1 || max_n_k > cap)
+        return fail(ATF_EINVAL, "%s: max_n_k %lld must be in [1, %lld], what a row's pages hold", fn,
+                    (long long)max_n_k, (long long)cap);
+    if (top_blocks < 1 || top_blocks > atf::kMaxTopBlocks || first_blocks < 0 || last_blocks < 0 ||
+        first_blocks > top_blocks || last_blocks > top_blocks - first_blocks)
+        return fail(ATF_EINVAL, "%s: need 1 <= top_blocks <= %d, first_blocks and last_blocks >= 0, their sum at most "
+                    "top_blocks", fn, atf::kMaxTopBlocks);
+    atf::WindowTable win;
+    rc = build_table(w, &win);
+    if (rc != ATF_OK) return rc;
+    if (!bounds || (n_tokens > 0 && (!q || !blocks))) return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    if (!aligned(q, 16) || !aligned(bounds, 16) || !aligned(blocks, 4))
+        return fail(ATF_EINVAL, "%s: q and bounds must be 16-byte, blocks 4-byte aligned", fn);
+    const int64_t row_blocks = (max_n_k + block_tokens - 1) / block_tokens;
+    const SelectLayout L = select_layout(n_tokens, h_kv, row_blocks);
+    if (workspace == nullptr || L.total == 0 || workspace_bytes < L.total)
+        return fail(ATF_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, L.total,
+                    workspace == nullptr ? size_t(0) : workspace_bytes);
+    if (!aligned(workspace, 16)) return fail(ATF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+    const size_t tokens = size_t(n_tokens) * 4;
+    const Span spans[] = {{"blocks", blocks, tokens * size_t(h_kv) * size_t(top_blocks), true},
+                          {"workspace", workspace, L.total, true},
+                          {"q", q, tokens / 2 * size_t(h_q) * size_t(d), false},
+                          {"bounds", bounds, pool_bytes(pg, h_kv, 4 * int64_t(d)) / size_t(block_tokens), false},
+                          {"block_table", block_table, table_bytes(pg, batch), false},
+                          {"token_rows", token_rows, tokens, false},
+                          {"positions", positions, tokens, false},
+                          {"n_k_rows", n_k_rows, size_t(batch) * 4, false}};
+    rc = check_apart(fn, spans);
+    if (rc != ATF_OK) return rc;
+    if (n_tokens == 0) return ATF_OK;
+    atf::SelectParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.bounds = static_cast<const uint16_t*>(bounds);
+    p.blocks = blocks;
+    p.block_table = block_table;
+    p.token_rows = token_rows;
+    p.positions = positions;
+    p.n_k_rows = n_k_rows;
+    p.keys = static_cast<uint64_t*>(workspace);
+    p.batch = batch;
+    p.max_pages = max_pages_per_row;
+    p.num_pages = num_pages;
+    p.page_tokens = page_tokens;
+    p.block_tokens = block_tokens;
+    p.n_tokens = static_cast<int32_t>(n_tokens);
+    p.max_n_k = static_cast<int32_t>(max_n_k);
+    p.row_blocks = static_cast<int32_t>(row_blocks);
+    p.top = top_blocks;
+    p.first_blocks = first_blocks;
+    p.last_blocks = last_blocks;
+    p.h_q = h_q;
+    p.h_kv = h_kv;
+    p.group = h_q / h_kv;
+    p.chunks = d / 16;
+    p.slab = L.slab;
+    std::memcpy(p.W, win.W, sizeof p.W);
+    const hipError_t e = atf::launch_select_blocks(p, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int32_t top_blocks,
+                                  int32_t block_tokens, int32_t head_dim) {
+    if (n_tokens < 0 || h_q < 1 || h_kv < 1 || h_q % h_kv || top_blocks < 1 || top_blocks > atf::kMaxTopBlocks ||
+        block_tokens < 32 || block_tokens % 32 != 0 || (head_dim != 64 && head_dim != 128) ||
+        n_tokens > atf::kMaxTokenHeads / h_q)
+        return 0;
+    return 256;
+}
+
+int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, void* o, float* lse, int64_t n_tokens,
+                      const int32_t* block_table, int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
+                      int32_t block_tokens, int32_t batch, const int32_t* token_rows, const int32_t* positions,
+                      const int32_t* n_k_rows, const int32_t* blocks, int32_t top_blocks, int32_t h_q, int32_t h_kv,
+                      const atf_window* w, float softmax_scale, void* workspace, size_t workspace_bytes,
+                      void* hip_stream) {
+    const char* fn = "attend_blocks";
+    if (w == nullptr) return fail(ATF_EINVAL, "%s: NULL window", fn);
+    const int d = w->head_dim;
+    int rc = check_head_dim(fn, d);
+    if (rc != ATF_OK) return rc;
+    const PagedArgs pg = paged_args(block_table, max_pages_per_row, num_pages, page_tokens);
+    int64_t cap;
+    rc = check_blocks(fn, pg, block_tokens, &cap);
+    if (rc != ATF_OK) return rc;
+    rc = check_tokens(fn, {n_tokens, batch, token_rows, positions, n_k_rows, h_q, h_kv});
+    if (rc != ATF_OK) return rc;
+    if (top_blocks < 1 || top_blocks > atf::kMaxTopBlocks)
+        return fail(ATF_EINVAL, "%s: need 1 <= top_blocks <= %d", fn, atf::kMaxTopBlocks);
+    if (!std::isfinite(softmax_scale)) return fail(ATF_EINVAL, "%s: softmax_scale must be finite", fn);
+    atf::WindowTable win;
+    rc = build_table(w, &win);
+    if (rc != ATF_OK) return rc;
+    if (!k_pages || !v_pages || (n_tokens > 0 && (!q || !o || !lse || !blocks)))
+        return fail(ATF_EINVAL, "%s: NULL pointer", fn);
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(o, 16) || !aligned(lse, 4) ||
+        !aligned(blocks, 4))
+        return fail(ATF_EINVAL, "%s: q/k/v/o must be 16-byte, lse and blocks 4-byte aligned", fn);
+    const size_t need = atf_attend_workspace_bytes(n_tokens, h_q, h_kv, top_blocks, block_tokens, d);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(ATF_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                    workspace == nullptr ? size_t(0) : workspace_bytes);
+    if (!aligned(workspace, 16)) return fail(ATF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+    const size_t tokens = size_t(n_tokens) * 4, rows = tokens / 2 * size_t(h_q) * size_t(d);
+    const size_t pool = pool_bytes(pg, h_kv, 2 * int64_t(d));
+    const Span spans[] = {{"o", o, rows, true},
+                          {"lse", lse, tokens * size_t(h_q), true},
+                          {"workspace", workspace, need, true},
+                          {"q", q, rows, false},
+                          {"k_pages", k_pages, pool, false},
+                          {"v_pages", v_pages, pool, false},
+                          {"blocks", blocks, tokens * size_t(h_kv) * size_t(top_blocks), false},
+                          {"block_table", block_table, table_bytes(pg, batch), false},
+                          {"token_rows", token_rows, tokens, false},
+                          {"positions", positions, tokens, false},
+                          {"n_k_rows", n_k_rows, size_t(batch) * 4, false}};
+    rc = check_apart(fn, spans);
+    if (rc != ATF_OK) return rc;
+    if (n_tokens == 0) return ATF_OK;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(float(d));
+    atf::AttendParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.k_pages = static_cast<const uint16_t*>(k_pages);
+    p.v_pages = static_cast<const uint16_t*>(v_pages);
+    p.o = static_cast<uint16_t*>(o);
+    p.lse = lse;
+    p.block_table = block_table;
+    p.token_rows = token_rows;
+    p.positions = positions;
+    p.n_k_rows = n_k_rows;
+    p.blocks = blocks;
+    p.batch = batch;
+    p.max_pages = max_pages_per_row;
+    p.num_pages = num_pages;
+    p.page_tokens = page_tokens;
+    p.block_tokens = block_tokens;
+    p.n_tokens = static_cast<int32_t>(n_tokens);
+    p.max_n_k = static_cast<int32_t>(cap);
+    p.top = top_blocks;
+    p.h_q = h_q;
+    p.h_kv = h_kv;
+    p.group = h_q / h_kv;
+    p.subgroups = (p.group + 31) / 32;
+    p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    std::memcpy(p.W, win.W, sizeof p.W);
+    const hipError_t e = atf::launch_attend_blocks(p, d, static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return ATF_OK;
+}
+
+}  // extern "C"

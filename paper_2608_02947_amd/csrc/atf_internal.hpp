@@ -198,6 +198,92 @@ struct RotateParams {
     uint32_t rope_rho_lo[kMaxPairs];
 };
 
+// Pages handed out and slots found from the rows' lengths (pages.hip).
+struct PlanParams {
+    int32_t* block_table;        // [B][max_pages]
+    int32_t* free_pages;         // [free_capacity], the first *free_count of them free
+    const int32_t* free_count;
+    const int32_t* n_k_rows;     // [B] tokens each row holds
+    const int32_t* n_new_rows;   // [B] tokens it gets; negative: the row ends
+    int32_t* n_k_out;            // [B], may be n_k_rows
+    int32_t* row_starts;         // [B + 1]
+    int64_t* slots;              // [max_tokens], as the two below
+    int32_t* token_rows;
+    int32_t* positions;
+    int32_t* counts;             // [3], may begin at free_count
+    int32_t batch, max_pages, page_tokens, free_capacity, max_tokens;
+};
+
+// Tokens appended through their slots (pages.hip).
+struct AppendSlotsParams {
+    const uint16_t* k_new;       // [n_tokens][h_kv][d]
+    const uint16_t* v_new;
+    uint16_t* k_pages;           // [num_pages][h_kv][d/16][page_tokens][16]
+    uint16_t* v_pages;           // [num_pages][h_kv][page_tokens/16][d][16]
+    const int64_t* slots;        // [n_tokens]; outside [0, pool_tokens): not stored
+    const int32_t* positions;    // [n_tokens], keys turned; else nullptr
+    int64_t pool_tokens;         // num_pages * page_tokens
+    int32_t n_tokens, h_kv, page_tokens;
+    uint32_t rope_rho_hi[kMaxPairs];
+    uint32_t rope_rho_lo[kMaxPairs];
+};
+
+// Bounds of the keys of the blocks that hold the rows' newest tokens (blocks.hip).
+struct BoundsParams {
+    const uint16_t* k_pages;
+    uint16_t* bounds;            // [num_pages][h_kv][page_tokens/block_tokens][d/16][2][16]
+    const int32_t* block_table;
+    const int32_t* n_k_rows;
+    const int32_t* n_new_rows;
+    int32_t batch, max_pages, num_pages, page_tokens, block_tokens, h_kv;
+    uint32_t chunks;             // d/16
+    int32_t max_new;
+    uint32_t row_blocks;         // most blocks of a row that max_new tokens lie in
+};
+
+// The blocks that query tokens take (blocks.hip).
+struct SelectParams {
+    const uint16_t* q;           // [n_tokens][h_q][d]
+    const uint16_t* bounds;      // as BoundsParams
+    int32_t* blocks;             // [n_tokens][h_kv][top]
+    const int32_t* block_table;
+    const int32_t* token_rows;   // [n_tokens]; outside [0, batch): nothing is written
+    const int32_t* positions;    // [n_tokens]
+    const int32_t* n_k_rows;     // [batch], clamped to [0, max_n_k]
+    uint64_t* keys;              // [slab][h_kv][row_blocks], workspace
+    int32_t batch, max_pages, num_pages, page_tokens, block_tokens;
+    int32_t n_tokens, max_n_k, row_blocks, top, first_blocks, last_blocks;
+    int32_t h_q, h_kv, group, chunks;
+    int32_t slab, first_token;   // tokens of a launch, the first of them
+    int32_t W[kMaxPairs];
+};
+
+// Attention over listed blocks (attend_blocks.hip).
+struct AttendParams {
+    const uint16_t* q;           // [n_tokens][h_q][d]
+    const uint16_t* k_pages;
+    const uint16_t* v_pages;
+    uint16_t* o;                 // like q
+    float* lse;                  // [n_tokens][h_q]
+    const int32_t* block_table;
+    const int32_t* token_rows;
+    const int32_t* positions;
+    const int32_t* n_k_rows;     // clamped to [0, max_n_k]
+    const int32_t* blocks;       // [n_tokens][h_kv][top]
+    int32_t batch, max_pages, num_pages, page_tokens, block_tokens;
+    int32_t n_tokens, max_n_k, top, h_q, h_kv, group;
+    int32_t heads_per_block, subgroups;  // as DecodeQ8Params
+    float scale_log2;
+    int32_t W[kMaxPairs];
+};
+
+// Most (token, query head)s of a selection or of the attention over it, and blocks of a list.
+constexpr int64_t kMaxTokenHeads = int64_t(1) << 23;
+constexpr int32_t kMaxTopBlocks = 4096;
+// Workspace that a selection takes for the scores of the tokens of one launch, at most (more where
+// a single token needs it).
+constexpr int64_t kSelectSlabBytes = int64_t(256) << 20;
+
 // Kernel launchers (one in each .hip file, two in prefill.hip and rotate.hip).  Return the HIP error
 // of the launch.
 hipError_t launch_prefill(const PrefillParams& p, int head_dim, hipStream_t stream);
@@ -211,6 +297,11 @@ hipError_t launch_decode_q8(const DecodeQ8Params& p, int head_dim, hipStream_t s
 hipError_t launch_append_normed(const AppendNormedParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_read_q8(const ReadQ8Params& p, int head_dim, hipStream_t stream);
 hipError_t launch_append(const AppendRotParams& p, bool turn, int head_dim, hipStream_t stream);
+hipError_t launch_plan_pages(const PlanParams& p, hipStream_t stream);
+hipError_t launch_append_slots(const AppendSlotsParams& p, bool turn, int head_dim, hipStream_t stream);
+hipError_t launch_block_bounds(const BoundsParams& p, hipStream_t stream);
+hipError_t launch_select_blocks(const SelectParams& p, hipStream_t stream);
+hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_rotate_kcache(const RotateParams& p, int head_dim, hipStream_t stream);
 
 // Most splits per (batch, kv head) of a uniform batch, and most work items per column of
