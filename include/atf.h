@@ -626,8 +626,8 @@ int atf_plan_pages(int32_t *block_table, int32_t max_pages_per_row, int32_t page
  *   slots         int64 [n_tokens], DEVICE, 8-byte aligned;  positions  int32 [n_tokens], DEVICE
  * n_tokens == 0 is a no-op.
  * Errors: ATF_EINVAL (NULL window or pointer, misaligned pointer, pages that overlap each other or an
- * input, n_tokens < 0, h_kv < 1, n_tokens * h_kv > 2^29, bad page arguments, a bad rotation
- * frequency); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
+ * input, n_tokens < 0, h_kv < 1, n_tokens * h_kv > 2^29, bad page arguments, pages of more than
+ * 2^35 tokens, a bad rotation frequency); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
 int atf_cache_append_slots(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
                            const int64_t *slots, int64_t n_tokens, int32_t num_pages,
                            int32_t page_tokens, int32_t h_kv, int32_t head_dim, void *hip_stream);
@@ -646,7 +646,8 @@ int atf_cache_append_slots_rotated(const void *k_new, const void *v_new, void *k
  *           16 largest, then the 16 smallest, dims as in the K cache    (device, written)
  * Table entries are clamped to [0, num_pages).  Blocks that a call writes must be one row's.
  * Errors: ATF_EINVAL (NULL or misaligned pointer, bounds that overlap an input, batch < 1, h_kv < 1,
- * max_new < 0, bad page or block arguments); ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
+ * max_new < 0, more than 2^30 blocks times h_kv in a row's pages, bad page or block arguments);
+ * ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
 int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_table,
                      int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
                      int32_t block_tokens, int32_t batch, const int32_t *n_k_rows,

@@ -1622,6 +1622,8 @@ int append_slots_impl(const char* fn, const void* k_new, const void* v_new, void
         return fail(ATF_EINVAL, "%s: page_tokens %d must be a positive multiple of 32, num_pages >= 1", fn, page_tokens);
     if (n_tokens > (int64_t(1) << 29) / h_kv)
         return fail(ATF_EINVAL, "%s: n_tokens * h_kv above 2^29", fn);
+    if (int64_t(num_pages) * page_tokens > int64_t(1) << 35)
+        return fail(ATF_EINVAL, "%s: pages of more than 2^35 tokens", fn);
     if (!k_pages || !v_pages || (n_tokens > 0 && (!k_new || !v_new || !slots || (turn && !positions))))
         return fail(ATF_EINVAL, "%s: NULL pointer", fn);
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
@@ -1788,6 +1790,8 @@ int atf_block_bounds(const void* k_pages, void* bounds, const int32_t* block_tab
     if (rc != ATF_OK) return rc;
     if (batch < 1 || h_kv < 1 || max_new < 0)
         return fail(ATF_EINVAL, "%s: need batch >= 1, h_kv >= 1, max_new >= 0", fn);
+    if (cap / block_tokens > (int64_t(1) << 30) / h_kv)
+        return fail(ATF_EINVAL, "%s: more than 2^30 blocks times h_kv in a row's pages", fn);
     if (!k_pages || !bounds || !n_k_rows || !n_new_rows) return fail(ATF_EINVAL, "%s: NULL pointer", fn);
     if (!aligned(k_pages, 16) || !aligned(bounds, 16) || !aligned(n_k_rows, 4) || !aligned(n_new_rows, 4))
         return fail(ATF_EINVAL, "%s: tensors must be 16-byte, row arrays 4-byte aligned", fn);
@@ -1813,10 +1817,9 @@ int atf_block_bounds(const void* k_pages, void* bounds, const int32_t* block_tab
     p.page_tokens = page_tokens;
     p.block_tokens = block_tokens;
     p.h_kv = h_kv;
-    p.chunks = static_cast<uint32_t>(head_dim / 16);
     p.max_new = static_cast<int32_t>(max_new);
     p.row_blocks = static_cast<uint32_t>(std::min(cap / block_tokens, (max_new + block_tokens - 2) / block_tokens + 1));
-    const hipError_t e = atf::launch_block_bounds(p, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = atf::launch_block_bounds(p, head_dim, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return fail(ATF_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return ATF_OK;
 }

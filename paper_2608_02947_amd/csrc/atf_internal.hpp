@@ -236,7 +236,6 @@ struct BoundsParams {
     const int32_t* n_k_rows;
     const int32_t* n_new_rows;
     int32_t batch, max_pages, num_pages, page_tokens, block_tokens, h_kv;
-    uint32_t chunks;             // d/16
     int32_t max_new;
     uint32_t row_blocks;         // most blocks of a row that max_new tokens lie in
 };
@@ -299,7 +298,7 @@ hipError_t launch_read_q8(const ReadQ8Params& p, int head_dim, hipStream_t strea
 hipError_t launch_append(const AppendRotParams& p, bool turn, int head_dim, hipStream_t stream);
 hipError_t launch_plan_pages(const PlanParams& p, hipStream_t stream);
 hipError_t launch_append_slots(const AppendSlotsParams& p, bool turn, int head_dim, hipStream_t stream);
-hipError_t launch_block_bounds(const BoundsParams& p, hipStream_t stream);
+hipError_t launch_block_bounds(const BoundsParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_select_blocks(const SelectParams& p, hipStream_t stream);
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_rotate_kcache(const RotateParams& p, int head_dim, hipStream_t stream);

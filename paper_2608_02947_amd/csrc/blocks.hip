@@ -18,70 +18,105 @@ __device__ __forceinline__ s16x2_t ordered(uint32_t x) {
 }
 
 // Bounds: per dim the largest and the smallest of the block's keys (those of its row), a wave per
-// (row, block, KV head, chunk of 8 pairs).  A lane reads 16 bytes: one half (first or second
-// components) of a token's chunk; lanes of equal parity then share their extremes.
+// (row, block, KV head, 4 chunks of 8 pairs).  A lane reads 16 bytes: one half (first or second
+// components) of a token's chunk, 8 loads in flight; a token past the last is the last one again.
+// Lanes of equal parity then share their extremes: the smallest as the largest complement, so that
+// after the first step, which leaves one in the lower lanes and the other in the upper ones, both
+// go on together.
 // Bound by HBM reads.
+constexpr int kBoundChunks = 4;
+
+template <int kCtrl>
+__device__ __forceinline__ s16x2_t larger_dpp(s16x2_t x) {
+    return __builtin_elementwise_max(
+        x, __builtin_bit_cast(s16x2_t, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), kCtrl, 0xF, 0xF, true)));
+}
+
+template <int D>
 __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p) {
+    constexpr int kChunks = D / 16, kParts = kChunks / kBoundChunks;
     const int lane = threadIdx.x & 63;
-    const uint64_t units = uint64_t(p.batch) * p.row_blocks * p.h_kv * p.chunks;
-    for (uint64_t unit = uint64_t(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += uint64_t(gridDim.x) * 4) {
-        const int c = int(unit % p.chunks);
-        uint64_t rest = unit / p.chunks;
-        const int g = int(rest % p.h_kv);
-        rest /= p.h_kv;
-        const int b = int(rest / p.row_blocks);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const uint32_t units = p.row_blocks * uint32_t(p.h_kv) * kParts;
+    for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
         const int64_t cap = int64_t(p.max_pages) * p.page_tokens;
         const int n = int(min(int64_t(max(p.n_k_rows[b], 0)), cap));
         const int fresh = min(min(max(p.n_new_rows[b], 0), p.max_new), n);
         if (fresh == 0) continue;
-        const int j = (n - fresh) / p.block_tokens + int(rest % p.row_blocks);
-        const int first = j * p.block_tokens;  // (of a block below the row's end: no overflow)
-        if (j > (n - 1) / p.block_tokens) continue;
-        const int count = min(p.block_tokens, n - first);
-        const int page = min(max(p.block_table[int64_t(b) * p.max_pages + first / p.page_tokens], 0), p.num_pages - 1);
-        const int at = first % p.page_tokens;
-        const uint16_t* src = p.k_pages + ((int64_t(page) * p.h_kv + g) * p.chunks + c) * p.page_tokens * 16 +
-                              int64_t(at) * 16 + (lane & 1) * 8;
-        s16x2_t hi[4], lo[4];
+        const int j0 = (n - fresh) / p.block_tokens, j1 = (n - 1) / p.block_tokens;
+        for (uint32_t unit = wave; unit < units; unit += gridDim.x * 4) {
+            const int c0 = int(unit % kParts) * kBoundChunks;
+            const uint32_t rest = unit / kParts;
+            const uint32_t k = rest / uint32_t(p.h_kv);
+            const int g = int(rest - k * uint32_t(p.h_kv));
+            if (k > uint32_t(j1 - j0)) break;
+            const int first = (j0 + int(k)) * p.block_tokens;
+            const int last = min(p.block_tokens, n - first) - 1;
+            const int page = min(max(p.block_table[int64_t(b) * p.max_pages + first / p.page_tokens], 0), p.num_pages - 1);
+            const int at = first % p.page_tokens;
+            const int64_t pc = (int64_t(page) * p.h_kv + g) * kChunks + c0;
+            const uint16_t* src = p.k_pages + (pc * p.page_tokens + at) * 16 + (lane & 1) * 8;
+            s16x2_t hi[kBoundChunks][4], lo[kBoundChunks][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = s16x2_t{-32768, -32768};
-            lo[e] = s16x2_t{32767, 32767};
-        }
-        for (int t = lane >> 1; t < count; t += 32) {
-            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(src + t * 16);
+            for (int c = 0; c < kBoundChunks; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const s16x2_t v = ordered(x[e]);
-                hi[e] = __builtin_elementwise_max(hi[e], v);
-                lo[e] = __builtin_elementwise_min(lo[e], v);
+                for (int e = 0; e < 4; ++e) {
+                    hi[c][e] = s16x2_t{-32768, -32768};
+                    lo[c][e] = s16x2_t{32767, 32767};
+                }
+            for (int t0 = 0; t0 <= last; t0 += 64) {
+                u32x4_t x[kBoundChunks][2];
+#pragma unroll
+                for (int c = 0; c < kBoundChunks; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        x[c][h] = *reinterpret_cast<const u32x4_t*>(
+                            src + (int64_t(c) * p.page_tokens + min(t0 + 32 * h + (lane >> 1), last)) * 16);
+#pragma unroll
+                for (int c = 0; c < kBoundChunks; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const s16x2_t v = ordered(x[c][h][e]);
+                            hi[c][e] = __builtin_elementwise_max(hi[c][e], v);
+                            lo[c][e] = __builtin_elementwise_min(lo[c][e], v);
+                        }
             }
-        }
 #pragma unroll
-        for (int o = 2; o < 64; o <<= 1)
+            for (int c = 0; c < kBoundChunks; ++c) {
+                u32x4_t out, none;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                hi[e] = __builtin_elementwise_max(
-                    hi[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, hi[e]), o)));
-                lo[e] = __builtin_elementwise_min(
-                    lo[e], __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, lo[e]), o)));
-            }
-        if (lane < 2) {
-            u32x4_t h, l;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t x = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, hi[e])));
-                uint32_t y = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, lo[e])));
+                for (int e = 0; e < 4; ++e) {
+                    // lanes 32..63 of the largest trade places with lanes 0..31 of the complements
+                    const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, hi[c][e]),
+                                                                     ~__builtin_bit_cast(uint32_t, lo[c][e]), false, false);
+                    s16x2_t v = __builtin_elementwise_max(__builtin_bit_cast(s16x2_t, uint32_t(sw[0])),
+                                                          __builtin_bit_cast(s16x2_t, uint32_t(sw[1])));
+                    v = larger_dpp<0x4E>(v);   // lane ^ 2
+                    v = larger_dpp<0x124>(v);  // 4 and 8 on in the row of 16
+                    v = larger_dpp<0x128>(v);
+                    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+                    const auto rows = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+                    v = __builtin_elementwise_max(__builtin_bit_cast(s16x2_t, uint32_t(rows[0])),
+                                                  __builtin_bit_cast(s16x2_t, uint32_t(rows[1])));
+                    // (a positive NaN shows in the largest, a negative one in the largest complement)
+                    none[e] = (v[0] > 0x7F80 ? 0x7FC0u : 0u) | (v[1] > 0x7F80 ? 0x7FC00000u : 0u);
+                    const uint32_t y = __builtin_bit_cast(uint32_t, v);
+                    out[e] = __builtin_bit_cast(uint32_t, ordered(lane < 32 ? y : ~y));
+                }
                 // a key that is none: no bound either
-                const uint32_t none = (hi[e][0] > 0x7F80 || lo[e][0] < short(~0x7F80) ? 0x7FC0u : 0u) |
-                                      (hi[e][1] > 0x7F80 || lo[e][1] < short(~0x7F80) ? 0x7FC00000u : 0u);
-                h[e] = x | none;
-                l[e] = y | none;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const auto sw = __builtin_amdgcn_permlane32_swap(none[e], none[e], false, false);
+                    out[e] |= sw[0] | sw[1];
+                }
+                if ((lane & 31) < 2) {
+                    const int64_t bc = ((int64_t(page) * p.h_kv + g) * (p.page_tokens / p.block_tokens) +
+                                        at / p.block_tokens) * kChunks + c0 + c;
+                    *reinterpret_cast<u32x4_t*>(p.bounds + bc * 32 + (lane >> 5) * 16 + (lane & 1) * 8) = out;
+                }
             }
-            uint16_t* dst = p.bounds + (((int64_t(page) * p.h_kv + g) * (p.page_tokens / p.block_tokens) +
-                                         at / p.block_tokens) * p.chunks + c) * 32 + lane * 8;
-            *reinterpret_cast<u32x4_t*>(dst) = h;
-            *reinterpret_cast<u32x4_t*>(dst + 16) = l;
         }
     }
 }
@@ -229,11 +264,16 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(const SelectParams p
 
 }  // namespace
 
-hipError_t launch_block_bounds(const BoundsParams& p, hipStream_t stream) {
+hipError_t launch_block_bounds(const BoundsParams& p, int head_dim, hipStream_t stream) {
     (void)hipGetLastError();
-    const uint64_t units = uint64_t(p.batch) * uint64_t(p.row_blocks) * uint64_t(p.h_kv) * uint64_t(p.chunks);
-    const dim3 grid(unsigned(std::min<uint64_t>((units + 3) / 4, 1u << 20)));
-    hipLaunchKernelGGL(block_bounds_kernel, grid, dim3(256), 0, stream, p);
+    const uint64_t units = uint64_t(p.row_blocks) * uint64_t(p.h_kv) * uint64_t(head_dim / 16 / kBoundChunks);
+    if (units > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    // (a grid has fewer than 2^32 threads)
+    const dim3 grid(unsigned(std::min<uint64_t>((units + 3) / 4, 1u << 13)), unsigned(std::min(p.batch, 1 << 10)));
+    if (head_dim == 64)
+        hipLaunchKernelGGL(block_bounds_kernel<64>, grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL(block_bounds_kernel<128>, grid, dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 

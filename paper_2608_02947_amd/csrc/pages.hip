@@ -7,13 +7,13 @@
 //   a row that grows needs p(n_b + m_b) - p(n_b) pages; with E_b the sum of the needs up to and with
 //     row b it gets them if E_b <= f: page i of it is entry f - 1 - (E_b - need_b) - i
 //   token i of it is at position n_b + i: slot = page of the position * page_tokens + the rest
-// So it takes two sums over the rows: of the pages given back, then, row by row, of the needs and of
-// the tokens.  1,024 rows at a time, a thread each; the pages of a row move by pieces of 256, a
-// wave each, in turn.  Tokens are found from their number by a search in the rows' first tokens:
-// in the same workgroup if they are few, else by slots_kernel, which finds a row's first position,
-// or -1 if the row got nothing, where the plan left it: at the row's first token.
+// So it takes sums over the rows, of the pages given back, of the needs and of the tokens: a pass for
+// 1,024 rows, a thread each.  Up to 2 pages or tokens of a row are its thread's work, more go by
+// pieces of 256, a wave each in turn.  Where tokens are many slots_kernel writes them: it finds a
+// token's row by a search in the rows' first tokens, and the row's first position, or -1 if the row got
+// nothing, where the plan left it: at the row's first token.
 //
-// Bound by latency: a launch, and a few loads that wait for one another.
+// Bound by latency: a launch, and loads that wait for one another.
 #include "atf_internal.hpp"
 #include "rope.hpp"
 
@@ -28,31 +28,55 @@ constexpr int kPiece = 256;        // pages that a wave moves at once
 constexpr int kSlotThreads = 256;
 constexpr int kSlotRows = 2048;    // rows whose first tokens slots_kernel holds in LDS
 
-__device__ __forceinline__ int64_t scan_wave(int64_t x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+// Sum of each lane's and the lanes below it, by DPP: over rows of 16 lanes, then over the wave.
+template <int kCtrl, int kRows, typename Int>
+__device__ __forceinline__ Int dpp_add(Int x) {
+    if constexpr (sizeof(Int) == 4) {
+        return x + __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xF, false);
+    } else {
+        const int lo = __builtin_amdgcn_update_dpp(0, int(x), kCtrl, kRows, 0xF, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, int(x >> 32), kCtrl, kRows, 0xF, false);
+        return x + (Int(hi) << 32 | uint32_t(lo));
     }
-    return x;
+}
+template <typename Int>
+__device__ __forceinline__ Int scan_row16(Int x) {
+    x = dpp_add<0x111, 0xF>(x);  // from the lane 1, 2, 4, 8 below in the row of 16
+    x = dpp_add<0x112, 0xF>(x);
+    x = dpp_add<0x114, 0xF>(x);
+    return dpp_add<0x118, 0xF>(x);
+}
+template <typename Int>
+__device__ __forceinline__ Int scan_wave(Int x) {
+    x = scan_row16(x);
+    x = dpp_add<0x142, 0xA>(x);  // from the last lane of rows 0 and 2 to the rows after them
+    return dpp_add<0x143, 0xC>(x);  // from that of row 1 to rows 2 and 3
+}
+template <typename Int>
+__device__ __forceinline__ Int lane_of(Int x, int lane) {
+    if constexpr (sizeof(Int) == 4)
+        return __builtin_amdgcn_readlane(x, lane);
+    else
+        return Int(__builtin_amdgcn_readlane(int(x >> 32), lane)) << 32 | uint32_t(__builtin_amdgcn_readlane(int(x), lane));
 }
 
-// Each thread's sum of the threads up to it, and the sum of all.  `part` is free again after the
-// next barrier.
-__device__ __forceinline__ int64_t scan_block(int64_t x, int64_t* part, int64_t* all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    x = scan_wave(x, lane);
-    if (lane == 63) part[wave] = x;
-    __syncthreads();
-    int64_t before = 0, sum = 0;
+// x: each thread's sums of the threads up to it; all: the sums of all.  `part` is free again after
+// the next barrier.
+template <int N, typename Int>
+__device__ __forceinline__ void scan_block(Int (&x)[N], Int (&all)[N], Int (*part)[kPlanWaves]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
-        const int64_t y = part[w];
-        before += w < wave ? y : 0;
-        sum += y;
+    for (int i = 0; i < N; ++i) {
+        x[i] = scan_wave(x[i]);
+        if (lane == 63) part[i][wave] = x[i];
     }
-    *all = sum;
-    return x + before;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const Int sums = scan_row16(part[i][lane & (kPlanWaves - 1)]);
+        all[i] = lane_of(sums, kPlanWaves - 1);
+        if (wave > 0) x[i] += lane_of(sums, wave - 1);
+    }
 }
 
 struct PlanRow {
@@ -100,129 +124,196 @@ __device__ __forceinline__ void write_token(const PlanParams& p, int t, int row,
     p.positions[t] = pos;
 }
 
-// kTokens: the tokens too (rows fit one pass then)
-template <bool kTokens>
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanParams p) {
-    __shared__ int64_t s_part[3][kPlanWaves];
-    __shared__ int s_start[kTokens ? kPlanThreads + 1 : 1];
-    __shared__ int s_first[kTokens ? kPlanThreads : 1];
-    // rows whose pages move by pieces: pages, the first entry of the row, of the stack
-    __shared__ int s_rows;
-    __shared__ int s_count[kPlanThreads], s_entry[kPlanThreads], s_stack[kPlanThreads];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int max_tokens = p.max_tokens;
+// Rows of one pass whose pages or tokens move by pieces, and what each row needs for that.
+struct PlanPass {
+    int count[3];                 // rows listed: pages given back, pages taken, tokens written
+    int rows[3][kPlanThreads];
+    int n[kPlanThreads], grow[kPlanThreads], start[kPlanThreads], have[kPlanThreads], need[kPlanThreads];
+    int64_t stack[kPlanThreads];  // the stack's entry of the row's first page
+};
+constexpr int kGive = 0, kTake = 1, kWrite = 2;
 
-    // a row's pages to (given) or from the stack; few at once by the row's own thread
-    const auto move = [&](int rows0, int b, int count, int entry, int64_t stack, bool given) {
-        int slot = -1;
-        if (count > 0 && count <= 2) {
-            int32_t* at = p.block_table + int64_t(b) * p.max_pages + entry;
-            for (int i = 0; i < count; ++i) {
-                if (given) {
-                    if (stack + i < p.free_capacity) p.free_pages[stack + i] = at[i];
-                } else {
-                    at[i] = p.free_pages[stack - i];
-                }
-            }
-        } else if (count > 2) {
-            slot = tid;
+// body(row of the pass, first) for each piece of the listed rows, a wave each in turn
+template <typename Size, typename Body>
+__device__ __forceinline__ void by_pieces(const PlanPass& s, int list, Size size, Body body) {
+    int turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = s.count[list];
+    for (int k = 0; k < rows; ++k) {
+        const int r = __builtin_amdgcn_readfirstlane(s.rows[list][k]);
+        const int pieces = (__builtin_amdgcn_readfirstlane(size(r)) + kPiece - 1) / kPiece;
+        for (; turn < pieces; turn += kPlanWaves) body(r, turn * kPiece);
+        turn -= pieces;  // the next row's go on with the next wave
+    }
+}
+
+// Int holds the sums of all rows' pages and tokens; kOne: the rows are one pass (their numbers stay
+// in registers), and kTokens: their tokens are written here.
+template <typename Int, bool kOne, bool kTokens>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanParams p) {
+    __shared__ Int s_part[2][3][kPlanWaves];
+    __shared__ PlanPass s;
+    __shared__ int s_refused;
+    __shared__ int64_t s_taken;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t f0 = min(max(*p.free_count, 0), p.free_capacity);
+    if (tid < 3) s.count[tid] = 0;
+    if (tid == 0) s_refused = 0, s_taken = 0;
+
+    const auto table = [&](int b) { return p.block_table + int64_t(b) * p.max_pages; };
+    const auto give = [&](int r0, const PlanRow& r, int64_t stack) {
+        // (past the capacity: nothing)
+        stack = min(stack, int64_t(p.free_capacity));
+        if (r.ends && r.have <= 2) {
+            for (int i = 0; i < r.have; ++i)
+                if (stack + i < p.free_capacity) p.free_pages[stack + i] = table(r0 + tid)[i];
+        } else if (r.ends) {
+            s.rows[kGive][atomicAdd(&s.count[kGive], 1)] = tid;
+            s.have[tid] = r.have;
+            s.stack[tid] = stack;
         }
-        s_count[tid] = slot >= 0 ? count : 0;
-        s_entry[tid] = entry;
-        s_stack[tid] = int(stack);
-        if (tid == 0) s_rows = 0;
-        __syncthreads();
-        if (slot >= 0) atomicMax(&s_rows, tid + 1);
-        __syncthreads();
-        const int rows = s_rows;
-        for (int r = 0, turn = wave; r < rows; ++r) {
-            const int n = s_count[r];
-            if (n == 0) continue;
-            int32_t* at = p.block_table + int64_t(rows0 + r) * p.max_pages + s_entry[r];
-            const int64_t from = s_stack[r];
-            for (; turn * kPiece < n; turn += kPlanWaves) {
+    };
+    const auto give_pieces = [&](int r0) {
+        by_pieces(s, kGive, [&](int r) { return s.have[r]; }, [&](int r, int first) {
+            const int32_t* from = table(r0 + r);
+            int32_t page[kPiece / 64];
 #pragma unroll
-                for (int k = 0; k < kPiece / 64; ++k) {
-                    const int i = turn * kPiece + 64 * k + lane;
-                    if (i >= n) continue;
-                    if (given) {
-                        if (from + i < p.free_capacity) p.free_pages[from + i] = at[i];
-                    } else {
-                        at[i] = p.free_pages[from - i];
-                    }
-                }
+            for (int k = 0; k < kPiece / 64; ++k) page[k] = from[min(first + 64 * k + lane, s.have[r] - 1)];
+#pragma unroll
+            for (int k = 0; k < kPiece / 64; ++k) {
+                const int i = first + 64 * k + lane;
+                if (i < s.have[r] && s.stack[r] + i < p.free_capacity) p.free_pages[s.stack[r] + i] = page[k];
             }
-            turn -= (n + kPiece - 1) / kPiece;  // the next row's pieces go on with the next wave
-        }
-        __syncthreads();
+        });
+    };
+    const auto write = [&](int t, int b, int pos, int page) {
+        const bool is = pos >= 0;
+        p.slots[t] = is && page >= 0 ? int64_t(page) * p.page_tokens + pos % p.page_tokens : -1;
+        p.token_rows[t] = is ? b : -1;
+        p.positions[t] = pos;
     };
 
-    // pages given back
-    const int64_t f0 = min(max(*p.free_count, 0), p.free_capacity);
-    int64_t given = 0;
-    for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
-        const PlanRow r = plan_row(p, r0 + tid);
-        int64_t all;
-        const int64_t mine = r.ends ? r.have : 0;
-        const int64_t end = scan_block(mine, s_part[0], &all);
-        if (all == 0) {
+    PlanRow r = plan_row(p, tid);
+    Int all[3], x[3] = {Int(r.ends ? r.have : 0), Int(r.need), Int(min(r.grow, p.max_tokens + 1))};
+    int64_t f;
+    if constexpr (kOne) {
+        const Int back = x[0];
+        scan_block(x, all, s_part[0]);
+        f = min(f0 + all[0], int64_t(p.free_capacity));
+        if (all[0] > 0) {
+            give(0, r, f0 + x[0] - back);
             __syncthreads();
-            continue;
+            give_pieces(0);
+            __syncthreads();
         }
-        move(r0, r0 + tid, int(mine), 0, min(f0 + given + end - mine, int64_t(p.free_capacity)), true);
-        given += all;
+    } else {
+        int64_t given = 0;
+        for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
+            r = plan_row(p, r0 + tid);
+            Int y[1] = {Int(r.ends ? r.have : 0)}, sum[1];
+            const Int back = y[0];
+            scan_block(y, sum, s_part[0]);
+            give(r0, r, f0 + given + y[0] - back);
+            __syncthreads();
+            give_pieces(r0);
+            __syncthreads();
+            if (tid == 0) s.count[kGive] = 0;
+            given += sum[0];
+            __syncthreads();
+        }
+        f = min(f0 + given, int64_t(p.free_capacity));
     }
-    const int64_t f = min(f0 + given, int64_t(p.free_capacity));
 
-    // pages taken
-    int64_t needed = 0, tokens = 0, taken = 0, refused = 0;
-    for (int r0 = 0; r0 < p.batch; r0 += kPlanThreads) {
+    int64_t needed = 0, tokens = 0;
+    for (int r0 = 0; r0 < (kOne ? 1 : p.batch); r0 += kPlanThreads) {
         const int b = r0 + tid;
-        const PlanRow r = plan_row(p, b);
-        int64_t all_need, all_grow, all_taken;
-        const int64_t need_end = needed + scan_block(r.need, s_part[0], &all_need);
-        const int64_t end = tokens + scan_block(r.grow, s_part[1], &all_grow);
-        const bool ok = r.grow > 0 && r.fits && need_end <= f && end <= max_tokens;
-        const int64_t start = end - r.grow;
-        // (one sum for both: the pages of 1,024 rows are fewer than 2^40)
-        scan_block((int64_t(r.grow > 0 && !ok) << 40) + (ok ? r.need : 0), s_part[2], &all_taken);
-        const int64_t all_refused = all_taken >> 40;
-        all_taken &= (int64_t(1) << 40) - 1;
-        const int first = ok ? r.n : -1;
+        if constexpr (!kOne) {
+            r = plan_row(p, b);
+            x[0] = 0;
+            x[1] = Int(r.need);
+            x[2] = Int(min(r.grow, p.max_tokens + 1));
+            scan_block(x, all, s_part[1]);
+        }
+        const int64_t need_end = needed + x[1], end = tokens + x[2];
+        const bool ok = r.grow > 0 && r.fits && need_end <= f && end <= p.max_tokens;
+        const int start = int(min(end - min(r.grow, p.max_tokens + 1), int64_t(p.max_tokens)));
+        const int64_t stack = f - 1 - (need_end - r.need);
         if (b < p.batch) {
-            p.row_starts[b + 1] = int(min(end, int64_t(max_tokens)));
+            p.row_starts[b + 1] = int(min(end, int64_t(p.max_tokens)));
             p.n_k_out[b] = r.ends ? 0 : ok ? r.n + r.grow : r.n;
-            if (!kTokens && r.grow > 0 && start < max_tokens) p.positions[start] = first;
+            if (!kTokens && r.grow > 0 && start < p.max_tokens) p.positions[start] = ok ? r.n : -1;
         }
-        if (kTokens) {
-            s_start[tid + 1] = int(min(end, int64_t(max_tokens)));
-            s_first[tid] = first;
+        // the rows that get pages come before all others that want some
+        if (ok && r.need > 0) atomicMax(reinterpret_cast<unsigned long long*>(&s_taken), (unsigned long long)(need_end));
+        const uint64_t no = __ballot(r.grow > 0 && !ok);
+        if (lane == 0 && no != 0) atomicAdd(&s_refused, __builtin_popcountll(no));
+        const int count = kTokens ? min(r.grow, p.max_tokens - start) : 0;
+        bool info = false;
+        if (ok && r.need <= 2) {
+            for (int i = 0; i < r.need; ++i) table(b)[r.have + i] = p.free_pages[stack - i];
+        } else if (ok) {
+            s.rows[kTake][atomicAdd(&s.count[kTake], 1)] = tid;
+            info = true;
         }
-        move(r0, b, ok ? r.need : 0, r.have, f - 1 - (need_end - r.need), false);
-        needed += all_need;
-        tokens += all_grow;
-        taken += all_taken;
-        refused += all_refused;
+        if (kTokens && count > 2) {
+            s.rows[kWrite][atomicAdd(&s.count[kWrite], 1)] = tid;
+            info = true;
+        } else if (kTokens) {
+            for (int i = 0; i < count; ++i) {
+                const int pos = ok ? r.n + i : -1, at = pos / p.page_tokens;
+                write(start + i, b, pos, !ok ? -1 : at < r.have ? table(b)[at] : p.free_pages[stack - (at - r.have)]);
+            }
+        }
+        if (info) {
+            s.n[tid] = ok ? r.n : -1;
+            s.grow[tid] = count;
+            s.start[tid] = start;
+            s.have[tid] = r.have;
+            s.need[tid] = ok ? r.need : 0;
+            s.stack[tid] = stack;
+        }
+        __syncthreads();
+        by_pieces(s, kTake, [&](int q) { return s.need[q]; }, [&](int q, int first) {
+            int32_t page[kPiece / 64];
+            int32_t* to = table(r0 + q) + s.have[q];
+#pragma unroll
+            for (int k = 0; k < kPiece / 64; ++k) page[k] = p.free_pages[s.stack[q] - min(first + 64 * k + lane, s.need[q] - 1)];
+#pragma unroll
+            for (int k = 0; k < kPiece / 64; ++k)
+                if (first + 64 * k + lane < s.need[q]) to[first + 64 * k + lane] = page[k];
+        });
+        if constexpr (kTokens)
+            by_pieces(s, kWrite, [&](int q) { return s.grow[q]; }, [&](int q, int first) {
+                const int n = s.n[q], have = s.have[q];
+                int32_t page[kPiece / 64];
+#pragma unroll
+                for (int k = 0; k < kPiece / 64; ++k) {
+                    const int at = n < 0 ? 0 : (n + min(first + 64 * k + lane, s.grow[q] - 1)) / p.page_tokens;
+                    page[k] = -1;
+                    if (n >= 0) page[k] = at < have ? table(r0 + q)[at] : p.free_pages[s.stack[q] - (at - have)];
+                }
+#pragma unroll
+                for (int k = 0; k < kPiece / 64; ++k) {
+                    const int i = first + 64 * k + lane;
+                    if (i < s.grow[q]) write(s.start[q] + i, r0 + q, n < 0 ? -1 : n + i, page[k]);
+                }
+            });
+        needed += all[1];
+        tokens = min(tokens + all[2], int64_t(p.max_tokens) + 1);
+        if constexpr (!kOne) {
+            __syncthreads();
+            if (tid == 0) s.count[kTake] = 0;
+            __syncthreads();
+        }
     }
+    const int packed = int(min(tokens, int64_t(p.max_tokens)));
     if (tid == 0) {
         p.row_starts[0] = 0;
-        p.counts[0] = int(f - taken);
-        p.counts[1] = int(min(tokens, int64_t(max_tokens)));
-        p.counts[2] = int(refused);
-        if (kTokens) s_start[0] = 0;
+        p.counts[0] = int(f - s_taken);
+        p.counts[1] = packed;
+        p.counts[2] = s_refused;
     }
-    if constexpr (kTokens) {
-        __syncthreads();
-        const int n = int(min(tokens, int64_t(max_tokens)));
-        for (int t = tid; t < max_tokens; t += kPlanThreads) {
-            int row = -1, pos = -1;
-            if (t < n) {
-                row = row_of_token(s_start, p.batch, t);
-                pos = s_first[row] < 0 ? -1 : s_first[row] + t - s_start[row];
-            }
-            write_token(p, t, row, pos);
-        }
-    }
+    if constexpr (kTokens)
+        for (int t = packed + tid; t < p.max_tokens; t += kPlanThreads) write(t, -1, -1, -1);
 }
 
 __global__ __launch_bounds__(kSlotThreads) void slots_kernel(const PlanParams p) {
@@ -249,52 +340,52 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(const PlanParams p)
 
 // Appends through slots.  A run is tokens, one behind the other in the call, whose slots follow each
 // other inside a 16-token block of a page: a wave writes one head of a run.  Token t leads a run if
-// its slot starts a block or does not follow the slot of t - 1.  kWindow tokens a wave: 1 where
-// tokens are few (most waves of a prompt have no leader then), else 16, where prompts have one or two.
-//   keys: lanes along a token's row, 16 bytes each of both halves of a chunk, 32 bytes stored
-//   values: a lane takes 2 dims; a whole block's 16 tokens by two 16-byte stores a dim, others by
-//     2 bytes a token
+// its slot starts a block or does not follow the slot of t - 1.  A wave looks for the leaders of
+// kWindow tokens: 1 where tokens are few (most waves of a prompt have no leader then), else 16, where
+// prompts have one or two.
+//   keys: a lane takes one chunk of one token, 16 bytes of each half, and stores 32 bytes
+//   values: a whole block's as rotate.hip's appends take them: 2 dims x the 8 tokens of one half of the
+//     slots (slot 8h + e holds token 8(e/4) + 4h + e%4) a lane, two 16-byte stores; of others 2 dims a
+//     lane, 8 tokens loaded before the first is stored, 2 bytes a store
+// Bound by HBM where tokens are many.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 template <int D, bool kTurn, int kWindow>
 __global__ __launch_bounds__(256) void append_slots_kernel(const AppendSlotsParams p) {
     constexpr int kChunks = D / 16;
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kSteps = D / 64;
     const int lane = threadIdx.x & 63;
-    const int64_t windows = (int64_t(p.n_tokens) + kWindow - 1) / kWindow;
-    const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int g = int(unit % p.h_kv);
-    const int64_t win = unit / p.h_kv;
-    if (win >= windows) return;
-    const int t0 = int(win) * kWindow;
+    const uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int g = int(unit % uint32_t(p.h_kv));
+    const int64_t t0 = int64_t(unit / uint32_t(p.h_kv)) * kWindow;
+    if (t0 >= p.n_tokens) return;
     // slots of the tokens t0 - 1 .. t0 + kWindow + 14
     int64_t slot = -1;
-    {
-        const int64_t t = int64_t(t0) - 1 + lane;
-        if (lane <= kWindow + 15 && t >= 0 && t < p.n_tokens) slot = p.slots[t];
-        if (slot < 0 || slot >= p.pool_tokens) slot = -1;
-    }
+    if (lane <= kWindow + 15 && t0 - 1 + lane >= 0 && t0 - 1 + lane < p.n_tokens) slot = p.slots[t0 - 1 + lane];
+    if (slot >= p.pool_tokens) slot = -1;
     const int64_t before = __shfl_up(slot, 1);
     const uint64_t valid = __ballot(slot >= 0);
     const uint64_t leads = __ballot(lane > 0 && slot >= 0 && (slot % 16 == 0 || slot != before + 1));
     uint64_t todo = leads & (((uint64_t(1) << kWindow) - 1) << 1);
+    const int64_t row = int64_t(p.h_kv) * D;
     while (todo) {
         const int l = __builtin_ctzll(todo);
         todo &= todo - 1;
-        // the run: up to the next leader, the next token that is not stored, or 16
+        // the run: up to the next leader or the next token that is not stored
         const uint64_t stops = (leads | ~valid) >> (l + 1);
         const int n = min(16, __builtin_ctzll(stops) + 1);  // (lanes past the window's end stop it)
-        const int t = t0 - 1 + l;
-        const int64_t first = __shfl(slot, l);
-        const int64_t page = first / p.page_tokens;
-        const int at = int(first % p.page_tokens);
-        const int64_t ph = page * p.h_kv + g;
-        uint16_t* kd = p.k_pages + (ph * kChunks * p.page_tokens + at) * 16;
-        uint16_t* vd = p.v_pages + (ph * (p.page_tokens / 16) + at / 16) * int64_t(D) * 16;
-        const int64_t row = int64_t(p.h_kv) * D, src0 = (int64_t(t) * p.h_kv + g) * D;
-        // keys: record i = (token i / chunks, chunk i % chunks)
-        for (int i = lane; i < n * kChunks; i += 64) {
-            const int x = i / kChunks, c = i % kChunks;
-            const uint16_t* src = p.k_new + src0 + x * row + 8 * c;
-            u32x4 lo = *reinterpret_cast<const u32x4*>(src), hi = *reinterpret_cast<const u32x4*>(src + D / 2);
+        const int64_t t = t0 - 1 + l;
+        // its 16-token block of the pool (the pool has fewer than 2^31 of them)
+        const uint32_t blk = uint32_t(__builtin_amdgcn_readlane(int(slot >> 4), l));
+        const int at = __builtin_amdgcn_readlane(int(slot), l) & 15;
+        const uint32_t per = uint32_t(p.page_tokens) / 16, page = blk / per, in = blk - page * per;
+        const int64_t ph = int64_t(page) * p.h_kv + g;
+        uint16_t* kd = p.k_pages + (ph * kChunks * p.page_tokens + in * 16) * 16;
+        uint16_t* vd = p.v_pages + (ph * per + in) * int64_t(D) * 16;
+        const uint16_t* ks = p.k_new + (t * p.h_kv + g) * D;
+        const uint16_t* vs = p.v_new + (t * p.h_kv + g) * D;
+
+        const auto key = [&](int x, int c, u32x4 lo, u32x4 hi) __attribute__((always_inline)) {
             if constexpr (kTurn) {
                 const uint32_t pos = uint32_t(p.positions[t + x]);
                 float cs8[8], sn8[8];
@@ -308,19 +399,58 @@ __global__ __launch_bounds__(256) void append_slots_kernel(const AppendSlotsPara
                 lo = rope::rotate_cs(a, b, 0, cs8, sn8);
                 hi = rope::rotate_cs(b, a, 1, cs8, sn8);
             }
-            u32x4* dst = reinterpret_cast<u32x4*>(kd + (int64_t(c) * p.page_tokens + x) * 16);
+            u32x4* dst = reinterpret_cast<u32x4*>(kd + (int64_t(c) * p.page_tokens + at + x) * 16);
             dst[0] = lo;
             dst[1] = hi;
-        }
-        // values: slot 8h + 4a + b of a dim's 16 holds token 8a + 4h + b
-        if (2 * lane < D) {
-            const int b0 = at % 16;
-            for (int x = 0; x < n; ++x) {
-                const uint32_t two = *reinterpret_cast<const uint32_t*>(p.v_new + src0 + x * row + 2 * lane);
-                const int k = b0 + x, s = 8 * ((k >> 2) & 1) + 4 * (k >> 3) + (k & 3);
-                vd[(2 * lane) * 16 + s] = uint16_t(two);
-                vd[(2 * lane + 1) * 16 + s] = uint16_t(two >> 16);
+        };
+        if (n == 16) {
+            u32x4 kx[kSteps], ky[kSteps];
+            uint32_t vx[kSteps][8];
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                const int x = (lane + 64 * j) / kChunks, c = lane % kChunks;
+                kx[j] = *reinterpret_cast<const u32x4*>(ks + x * row + 8 * c);
+                ky[j] = *reinterpret_cast<const u32x4*>(ks + x * row + 8 * c + D / 2);
             }
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                const int i = lane + 64 * j, two = i % (D / 2), h = i / (D / 2);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    vx[j][e] = *reinterpret_cast<const uint32_t*>(vs + (8 * (e / 4) + 4 * h + e % 4) * row + 2 * two);
+            }
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) key((lane + 64 * j) / kChunks, lane % kChunks, kx[j], ky[j]);
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                const int i = lane + 64 * j, two = i % (D / 2), h = i / (D / 2);
+                u32x4 a, b;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    a[e] = (vx[j][2 * e] & 0xFFFFu) | vx[j][2 * e + 1] << 16;
+                    b[e] = vx[j][2 * e] >> 16 | (vx[j][2 * e + 1] & 0xFFFF0000u);
+                }
+                *reinterpret_cast<u32x4*>(vd + (2 * two) * 16 + 8 * h) = a;
+                *reinterpret_cast<u32x4*>(vd + (2 * two + 1) * 16 + 8 * h) = b;
+            }
+        } else {
+            for (int i = lane; i < n * kChunks; i += 64) {
+                const uint16_t* src = ks + (i / kChunks) * row + 8 * (i % kChunks);
+                key(i / kChunks, i % kChunks, *reinterpret_cast<const u32x4*>(src), *reinterpret_cast<const u32x4*>(src + D / 2));
+            }
+            if (2 * lane < D)
+                for (int x0 = 0; x0 < n; x0 += 8) {
+                    uint32_t vx[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) vx[e] = *reinterpret_cast<const uint32_t*>(vs + min(x0 + e, n - 1) * row + 2 * lane);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (x0 + e >= n) continue;
+                        const int x = at + x0 + e, to = 8 * ((x >> 2) & 1) + 4 * (x >> 3) + (x & 3);
+                        vd[(2 * lane) * 16 + to] = uint16_t(vx[e]);
+                        vd[(2 * lane + 1) * 16 + to] = uint16_t(vx[e] >> 16);
+                    }
+                }
         }
     }
 }
@@ -343,11 +473,17 @@ hipError_t launch_append_slots_d(const AppendSlotsParams& p, hipStream_t stream)
 
 hipError_t launch_plan_pages(const PlanParams& p, hipStream_t stream) {
     (void)hipGetLastError();
-    if (p.batch <= kPlanThreads && p.max_tokens <= 8192) {
-        hipLaunchKernelGGL(plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, stream, p);
+    // sums of the pages and of the tokens (at most max_tokens + 1 a row) in 32 bits
+    const bool one = p.batch <= kPlanThreads && int64_t(p.batch) * p.max_pages <= INT32_MAX &&
+                     p.batch * (int64_t(p.max_tokens) + 1) <= INT32_MAX;
+    if (one && p.max_tokens <= 8192) {
+        hipLaunchKernelGGL((plan_kernel<int32_t, true, true>), dim3(1), dim3(kPlanThreads), 0, stream, p);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, p);
+    if (one)
+        hipLaunchKernelGGL((plan_kernel<int32_t, true, false>), dim3(1), dim3(kPlanThreads), 0, stream, p);
+    else
+        hipLaunchKernelGGL((plan_kernel<int64_t, false, false>), dim3(1), dim3(kPlanThreads), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.max_tokens == 0) return e;
     const unsigned blocks = unsigned(std::min<int64_t>(2048, (int64_t(p.max_tokens) + kSlotThreads - 1) / kSlotThreads));
