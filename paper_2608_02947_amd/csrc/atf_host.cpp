@@ -1678,17 +1678,35 @@ int check_tokens(const char* fn, const QueryTokens& q) {
 }
 
 struct SelectLayout {
-    int32_t slab;
-    size_t total;
+    int32_t slab, pack, ranges, range_tiles, key_stride;
+    size_t off_exact, off_sizes, total;  // total 0: too large
 };
-SelectLayout select_layout(int64_t n_tokens, int32_t h_kv, int64_t row_blocks) {
-    const u128 each = u128(h_kv) * u128(row_blocks) * 8;
-    int64_t slab = int64_t(std::min<u128>(u128(atf::kSelectSlabBytes) / each, u128(std::max<int64_t>(n_tokens, 1))));
+// Tokens of a row one behind the other share the columns of the matrix products: where there are more
+// than two a row they are taken to.  A wave has a tile of 16 blocks at least, and waves are 4,096 in all
+// at least, where there are tiles for them (four for every SIMD).
+SelectLayout select_layout(int64_t n_tokens, int32_t batch, int32_t h_q, int32_t h_kv, int64_t row_blocks) {
+    SelectLayout L{};
+    const int32_t group = h_q / h_kv;
+    const int64_t stride = (row_blocks + 15) / 16 * 16, tiles = stride / 16;
+    n_tokens = std::max<int64_t>(n_tokens, 1);
+    // (workspaces are sized without the rows: for one token of each)
+    L.pack = group < 16 && n_tokens > 2 * int64_t(batch) ? 16 / group : 1;
+    const int64_t most_ranges = std::min<int64_t>(tiles, (4096 + h_kv - 1) / h_kv);
+    const u128 each = u128(h_kv) * (u128(stride) * 12 + u128(most_ranges) * 4);
+    int64_t slab = int64_t(std::min<u128>(u128(atf::kSelectSlabBytes) / each, u128(n_tokens)));
     slab = std::max<int64_t>(1, std::min<int64_t>(slab, 65535 / h_kv));
-    SelectLayout L;
+    if (slab * h_kv > 65535) return L;
+    const int64_t groups = (slab + L.pack - 1) / L.pack * h_kv;
+    const int64_t ranges = std::min<int64_t>(tiles, (4096 + groups - 1) / groups);
+    L.range_tiles = static_cast<int32_t>((tiles + ranges - 1) / ranges);
+    L.ranges = static_cast<int32_t>((tiles + L.range_tiles - 1) / L.range_tiles);
     L.slab = static_cast<int32_t>(slab);
-    const u128 total = u128(slab) * each;
-    L.total = total > u128(INT64_MAX) ? 0 : align_up(size_t(total), 256);
+    L.key_stride = static_cast<int32_t>(stride);
+    const u128 keys = u128(slab) * u128(h_kv) * u128(stride);
+    if (keys * 16 > u128(1) << 46) return L;
+    L.off_exact = align_up(size_t(keys) * 4, 256);
+    L.off_sizes = L.off_exact + align_up(size_t(keys) * 8, 256);
+    L.total = L.off_sizes + align_up(size_t(slab) * size_t(h_kv) * size_t(most_ranges) * 4, 256);
     return L;
 }
 
@@ -1830,7 +1848,7 @@ size_t atf_select_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, i
         block_tokens < 32 || block_tokens % 32 != 0 || (head_dim != 64 && head_dim != 128) ||
         n_tokens > atf::kMaxTokenHeads / h_q)
         return 0;
-    return select_layout(n_tokens, h_kv, (max_n_k + block_tokens - 1) / block_tokens).total;
+    return select_layout(n_tokens, 1, h_q, h_kv, (max_n_k + block_tokens - 1) / block_tokens).total;
 }
 
 int atf_select_blocks(const void* q, const void* bounds, int32_t* blocks, int64_t n_tokens, const int32_t* block_table,
@@ -1863,8 +1881,9 @@ int atf_select_blocks(const void* q, const void* bounds, int32_t* blocks, int64_
     if (!aligned(q, 16) || !aligned(bounds, 16) || !aligned(blocks, 4))
         return fail(ATF_EINVAL, "%s: q and bounds must be 16-byte, blocks 4-byte aligned", fn);
     const int64_t row_blocks = (max_n_k + block_tokens - 1) / block_tokens;
-    const SelectLayout L = select_layout(n_tokens, h_kv, row_blocks);
-    if (workspace == nullptr || L.total == 0 || workspace_bytes < L.total)
+    const SelectLayout L = select_layout(n_tokens, batch, h_q, h_kv, row_blocks);
+    if (L.total == 0) return fail(ATF_EINVAL, "%s: more heads or blocks than a call takes", fn);
+    if (workspace == nullptr || workspace_bytes < L.total)
         return fail(ATF_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, L.total,
                     workspace == nullptr ? size_t(0) : workspace_bytes);
     if (!aligned(workspace, 16)) return fail(ATF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
@@ -1888,11 +1907,17 @@ int atf_select_blocks(const void* q, const void* bounds, int32_t* blocks, int64_
     p.token_rows = token_rows;
     p.positions = positions;
     p.n_k_rows = n_k_rows;
-    p.keys = static_cast<uint64_t*>(workspace);
+    p.keys = static_cast<int32_t*>(workspace);
+    p.exact_keys = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + L.off_exact);
+    p.sizes = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.off_sizes);
+    p.key_stride = L.key_stride;
+    p.pack = L.pack;
+    p.ranges = L.ranges;
+    p.range_tiles = L.range_tiles;
     p.batch = batch;
     p.max_pages = max_pages_per_row;
     p.num_pages = num_pages;
-    p.page_tokens = page_tokens;
+    p.page_blocks = page_tokens / block_tokens;
     p.block_tokens = block_tokens;
     p.n_tokens = static_cast<int32_t>(n_tokens);
     p.max_n_k = static_cast<int32_t>(max_n_k);

@@ -249,11 +249,19 @@ struct SelectParams {
     const int32_t* token_rows;   // [n_tokens]; outside [0, batch): nothing is written
     const int32_t* positions;    // [n_tokens]
     const int32_t* n_k_rows;     // [batch], clamped to [0, max_n_k]
-    uint64_t* keys;              // [slab][h_kv][row_blocks], workspace
-    int32_t batch, max_pages, num_pages, page_tokens, block_tokens;
+    // workspace: scores as integers of their order [slab][h_kv][key_stride], the same in 64 bits
+    // where fp32 does not do, and the largest sum of magnitudes of each range of tiles
+    int32_t* keys;
+    uint64_t* exact_keys;
+    float* sizes;                // [slab][h_kv][ranges]
+    int32_t batch, max_pages, num_pages, page_blocks, block_tokens;
     int32_t n_tokens, max_n_k, row_blocks, top, first_blocks, last_blocks;
     int32_t h_q, h_kv, group, chunks;
-    int32_t slab, first_token;   // tokens of a launch, the first of them
+    int32_t key_stride;          // row_blocks rounded up to 16
+    int32_t pack;                // tokens whose heads share the columns of a product
+    int32_t ranges, range_tiles; // waves of a (token, KV head), tiles of 16 blocks of each
+    int32_t slab, first_token, tokens;  // tokens of a launch at most; set by the launcher: the
+                                 // first of this one, and their number
     int32_t W[kMaxPairs];
 };
 

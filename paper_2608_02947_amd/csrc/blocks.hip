@@ -1,5 +1,6 @@
 // Bounds of the keys of each block of a row, and the blocks that a query takes by them, gfx950.
 #include "atf_internal.hpp"
+#include "scan.hpp"
 
 #include <algorithm>
 
@@ -122,8 +123,40 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
 }
 
 // ---- selection
+//
+// A block's score for a query head is a sum over pairs of 2 products (positive parts of the query
+// with the largest, negative ones with the smallest numbers), so the scores of 16 blocks and 16 columns
+// (heads of one or more tokens of a row) are products of v_mfma_f32_16x16x32_bf16, one a chunk: its 32
+// numbers of a block's record are the 32 of the sum.  With r = lane % 16, g = lane / 16: A row r is block
+// r of the tile, the lane's 16 bytes its largest first, largest second, smallest first, smallest second
+// components (g = 0 .. 3); the result gives the lane, for column r, blocks 4 g + v.
+// Pairs kept at the whole of a tile's 16 blocks go in so; a pair whose window ends in the tile (each does in one
+// tile of a row) has a product of its own, of which every block and column takes what its distance
+// allows; chunks without a kept pair are not read.
+//
+// These sums are in fp32, off by no more than their error bound: n additions, each at most 2^-23 of the
+// sum of magnitudes, which a second product has.  pick_kernel finds the border of the blocks taken
+// among them; blocks as near to it as the bound allows, mostly the one that is the border, are summed
+// again in 64 bits unless all or none of them are taken.
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// What a query token sees: its row, its position, and the last key that it reaches (-1: none).
+__device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                   __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// pairs of a chunk that bits of `bits` keep
+__device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t bits) {
+    u32x4_t r;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+        r[t] = x[t] & (((bits >> (2 * t)) & 1u ? 0x0000FFFFu : 0u) | ((bits >> (2 * t + 1)) & 1u ? 0xFFFF0000u : 0u));
+    return r;
+}
+__device__ __forceinline__ u32x4_t magnitudes(u32x4_t x) { return x & 0x7FFF7FFFu; }
+
+// What a query token sees: its row (-1: padding), its position, and the last key that it reaches (below
+// 0: none).
 struct Token {
     int row, pos, last;
 };
@@ -140,125 +173,492 @@ __device__ __forceinline__ Token token_of(const SelectParams& p, int t) {
 
 // The bounds of block j of a row, for KV head g.
 __device__ __forceinline__ const uint16_t* bounds_of(const SelectParams& p, int row, int g, int j) {
-    const int per = p.page_tokens / p.block_tokens;
-    const int page = min(max(p.block_table[int64_t(row) * p.max_pages + j / per], 0), p.num_pages - 1);
-    return p.bounds + ((int64_t(page) * p.h_kv + g) * per + j % per) * p.chunks * 32;
+    const uint32_t per = uint32_t(p.page_blocks), i = uint32_t(j) / per;
+    const int page = min(max(p.block_table[int64_t(row) * p.max_pages + i], 0), p.num_pages - 1);
+    return p.bounds + ((int64_t(page) * p.h_kv + g) * per + (uint32_t(j) - i * per)) * p.chunks * 32;
+}
+
+// fp32 numbers as integers of the same order and back; what is not finite above all
+__device__ __forceinline__ int key_of(float x) {
+    const int v = __float_as_int(x);
+    return (v & 0x7F800000) == 0x7F800000 ? 0x7FFFFFFF : v ^ ((v >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7FFFFFFF)); }
+
+template <int kCtrl>
+__device__ __forceinline__ int max_dpp(int x, int none, bool take) {
+    const int y = __builtin_amdgcn_update_dpp(none, x, kCtrl, 0xF, 0xF, false);
+    return take ? max(x, y) : x;
+}
+// The largest of a lane and the G - 1 after it in the row of 16 (for the first of them, column h = 0).
+__device__ __forceinline__ int max_columns(int x, int h, int G) {
+    if (G > 1) x = max_dpp<0x101>(x, INT32_MIN, h + 1 < G);
+    if (G > 2) x = max_dpp<0x102>(x, INT32_MIN, h + 2 < G);
+    if (G > 4) x = max_dpp<0x104>(x, INT32_MIN, h + 4 < G);
+    if (G > 8) x = max_dpp<0x108>(x, INT32_MIN, h + 8 < G);
+    return x;
+}
+
+// A wave: some tiles of 16 blocks, for the columns of `pack` tokens (of one row each time it goes
+// through the tiles) or one token's heads, 16 at a time.
+template <int D>
+__global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
+    constexpr int kChunks = D / 16, kHalf = D / 2;
+    __shared__ u32x4_t s_tile[4][kChunks][64];
+    const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int range = blockIdx.x * 4 + wave;
+    if (range >= p.ranges) return;
+    const int g = int(blockIdx.y) % p.h_kv, t0 = int(blockIdx.y) / p.h_kv * p.pack;  // (of the slab)
+    const int G = p.group, width = min(G, 16);
+    const int my_w = lane < kHalf ? p.W[lane] : -1;
+    // this lane's column: head h (and 16 more of its token's each time) of token t
+    const int at = r16 / width, h = r16 - at * width;
+    const int t = t0 + at;
+    const bool is = at < p.pack && t < p.tokens;
+    Token tok = {-1, 0, -1};
+    if (is) tok = token_of(p, p.first_token + t);
+    bool todo = is && tok.row >= 0 && tok.last >= 0;
+    float worst = 0.f;  // largest sum of magnitudes
+    const int tile0 = range * p.range_tiles;
+
+    // the positive or the negative numbers of a column's query
+    const uint16_t* q = p.q + (int64_t(p.first_token + (is ? t : t0)) * p.h_q + g * G) * D + (g4 & 1) * kHalf;
+    const uint32_t sign = g4 >= 2 ? 0u : ~0u;
+    const auto part_of = [&](u32x4_t x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] &= (((x[e] >> 15) & 0x00010001u) * 0xFFFFu) ^ sign;
+        return x;
+    };
+    u32x4_t b[kChunks];
+    const auto load_q = [&](int h0) __attribute__((always_inline)) {
+        const uint16_t* from = q + (h0 + h < G ? h0 + h : 0) * D;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) b[c] = *reinterpret_cast<const u32x4_t*>(from + 8 * c);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) b[c] = part_of(b[c]);
+    };
+    load_q(0);
+
+    for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
+        const int row = __builtin_amdgcn_readlane(tok.row, __builtin_ctzll(rest));
+        const bool mine = todo && tok.row == row;
+        todo = todo && !mine;
+        int first_pos = 0x7FFFFFFF, last_pos = 0, last_key = -1;
+        for (uint64_t m = __ballot(mine) & 0xFFFF; m != 0; m &= m - 1) {  // (16 columns, alike in the rows of lanes)
+            const int l = __builtin_ctzll(m), pos = __builtin_amdgcn_readlane(tok.pos, l);
+            first_pos = min(first_pos, pos);
+            last_pos = max(last_pos, pos);
+            last_key = max(last_key, __builtin_amdgcn_readlane(tok.last, l));
+        }
+        const int n = last_key / p.block_tokens + 1, tiles = (n + 15) / 16;
+        for (int tile = tile0; tile < min(tiles, tile0 + p.range_tiles); ++tile) {
+            const int j0 = 16 * tile, j15 = min(j0 + 15, n - 1);
+            const int far = last_pos - j0 * p.block_tokens;
+            const int near = max(0, first_pos - min(last_key, j15 * p.block_tokens + (p.block_tokens - 1)));
+            const uint64_t full = __ballot(my_w >= far), keep = __ballot(my_w >= near);
+            const uint16_t* src = bounds_of(p, row, g, min(j0 + r16, n - 1)) + 8 * g4;
+            u32x4_t a[kChunks];
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                a[c] = u32x4_t{0u, 0u, 0u, 0u};
+                if ((keep >> (8 * c)) & 0xFFull) a[c] = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
+            }
+            const uint64_t some = keep & ~full;  // pairs whose windows end in the tile
+            if (some != 0) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) s_tile[wave][c][lane] = a[c];
+            }
+            int best[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
+            for (int h0 = 0; h0 < G; h0 += 16) {
+                const bool live = mine && h0 + h < G;
+                if (G > 16) load_q(h0);
+                f32x4_t sum = {0.f, 0.f, 0.f, 0.f}, size = sum;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const uint32_t whole = uint32_t(full >> (8 * c)) & 0xFFu;
+                    if (whole == 0xFFu) {
+                        sum = mfma16(a[c], b[c], sum);
+                        size = mfma16(magnitudes(a[c]), magnitudes(b[c]), size);
+                    } else if (whole != 0) {
+                        const u32x4_t x = keep_pairs(a[c], whole), y = keep_pairs(b[c], whole);
+                        sum = mfma16(x, y, sum);
+                        size = mfma16(magnitudes(x), magnitudes(y), size);
+                    }
+                }
+                for (uint64_t m = some; m != 0; m &= m - 1) {
+                    const int r = __builtin_ctzll(m), c = r / 8, w = __builtin_amdgcn_readlane(my_w, r);
+                    const u32x4_t x = keep_pairs(s_tile[wave][c][lane], 1u << (r % 8));
+                    const u32x4_t y = keep_pairs(
+                        part_of(*reinterpret_cast<const u32x4_t*>(q + (h0 + h < G ? h0 + h : 0) * D + 8 * c)), 1u << (r % 8));
+                    const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                    const f32x4_t v = mfma16(magnitudes(x), magnitudes(y), f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // (a tile past the row's end may reach past 2^31: wrapped, and not written)
+                        const int first = int(uint32_t(j0 + 4 * g4 + i) * uint32_t(p.block_tokens));
+                        const bool kept = w >= tok.pos - min(int(uint32_t(first) + uint32_t(p.block_tokens - 1)), tok.last);
+                        // (a window that ends inside the block: no less than 0)
+                        const float x0 = w < tok.pos - first && u[i] < 0.f ? 0.f : u[i];
+                        if (kept) sum[i] += x0;
+                        if (kept) size[i] += v[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (live) best[i] = max(best[i], key_of(sum[i]));
+                    if (live) worst = fmaxf(worst, size[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) best[i] = max_columns(best[i], h, width);
+            if (mine && h == 0)
+                *reinterpret_cast<int4*>(p.keys + (int64_t(t) * p.h_kv + g) * p.key_stride + j0 + 4 * g4) =
+                    make_int4(best[0], best[1], best[2], best[3]);
+        }
+    }
+    // (not less than 0: its bits are in order)
+    int bound = max_columns(__float_as_int(worst), h, width);
+    bound = max(bound, __shfl_xor(bound, 16));
+    bound = max(bound, __shfl_xor(bound, 32));
+    if (is && h == 0 && g4 == 0) p.sizes[(int64_t(t) * p.h_kv + g) * p.ranges + range] = __int_as_float(bound);
 }
 
 __device__ __forceinline__ double widen(uint16_t x) { return double(__uint_as_float(uint32_t(x) << 16)); }
 
-// A score as an integer of the same order: NaN above all, forced blocks above that; 0 is none.
-constexpr uint64_t kForced = ~0ull, kNaN = ~0ull - 1;
-__device__ __forceinline__ uint64_t key_of(double x) {
-    if (x != x) return kNaN;
-    const int64_t v = __double_as_longlong(x + 0.0);
-    return uint64_t(v ^ ((v >> 63) & 0x7FFFFFFFFFFFFFFFll)) ^ 0x8000000000000000ull;
+__device__ __forceinline__ double add_lanes(double x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
 }
 
-// Scores of one query token's blocks for one KV head, a block a thread, in 64 bits.
-__global__ __launch_bounds__(256) void scores_kernel(const SelectParams p) {
-    extern __shared__ double s_q[];  // [head][d]
-    __shared__ int s_w[kMaxPairs];
-    const int d = p.chunks * 16, half = d / 2;
-    const int t = p.first_token + int(blockIdx.y) / p.h_kv, g = int(blockIdx.y) % p.h_kv;
-    const Token tok = token_of(p, t);
-    if (tok.row < 0 || tok.last < 0) return;
-    const int n = tok.last / p.block_tokens + 1;
-    if (int64_t(blockIdx.x) * 256 >= n) return;
-    for (int i = threadIdx.x; i < p.group * d; i += 256)
-        s_q[i] = widen(p.q[(int64_t(t) * p.h_q + g * p.group) * d + i]);
-    if (threadIdx.x < half) s_w[threadIdx.x] = p.W[threadIdx.x];
-    __syncthreads();
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= n) return;
-    const uint16_t* bounds = bounds_of(p, tok.row, g, j);
-    const int near = tok.pos - min(j * p.block_tokens + (p.block_tokens - 1), tok.last);
-    const int far = tok.pos - j * p.block_tokens;
+// The score of block j in 64 bits, as an integer of the same order, NaN above all; a pair a lane.
+constexpr uint64_t kNaN = ~0ull;
+__device__ __forceinline__ uint64_t exact_key(const SelectParams& p, const Token& tok, int t, int g, int j) {
+    const int lane = threadIdx.x & 63, d = p.chunks * 16, half = d / 2;
+    const int first = j * p.block_tokens;
+    const int far = tok.pos - first, near = tok.pos - min(first + (p.block_tokens - 1), tok.last);
+    const int w = lane < half ? p.W[lane] : -1;
+    const bool kept = lane < half && w >= near;
+    const uint16_t* at = bounds_of(p, tok.row, g, j) + lane / 8 * 32 + lane % 8;
+    double hi0 = 0, hi1 = 0, lo0 = 0, lo1 = 0;
+    if (kept) hi0 = widen(at[0]), hi1 = widen(at[8]), lo0 = widen(at[16]), lo1 = widen(at[24]);
     double best = 0;
     bool none = false;
     for (int h = 0; h < p.group; ++h) {
-        double sum = 0;
-        for (int r = 0; r < half; ++r) {
-            if (s_w[r] < near) continue;
-            const uint16_t* at = bounds + (r / 8) * 32 + r % 8;
-            const double q0 = s_q[h * d + r], q1 = s_q[h * d + half + r];
-            double u = fmax(q0, 0.0) * widen(at[0]) + fmin(q0, 0.0) * widen(at[16]);
-            u += fmax(q1, 0.0) * widen(at[8]) + fmin(q1, 0.0) * widen(at[24]);
-            if (s_w[r] < far && u < 0) u = 0;  // some of the block's keys are past the pair's window
-            sum += u;
+        const uint16_t* q = p.q + (int64_t(t) * p.h_q + g * p.group + h) * d;
+        double u = 0;
+        if (kept) {
+            const double q0 = widen(q[lane]), q1 = widen(q[lane + half]);
+            // (a query that is none stays so)
+            u = (q0 < 0 ? 0 : q0) * hi0 + (q0 > 0 ? 0 : q0) * lo0;
+            u += (q1 < 0 ? 0 : q1) * hi1 + (q1 > 0 ? 0 : q1) * lo1;
+            if (w < far && u < 0) u = 0;
         }
-        none = none || sum != sum;
-        best = h == 0 ? sum : fmax(best, sum);
+        u = add_lanes(u);
+        none = none || u != u;
+        best = h == 0 || u > best ? u : best;
     }
-    uint64_t key = none ? kNaN : key_of(best);
-    if (j < p.first_blocks || j >= n - p.last_blocks) key = kForced;
-    p.keys[(int64_t(blockIdx.y)) * p.row_blocks + j] = key;
+    if (none) return kNaN;
+    const int64_t v = __double_as_longlong(best + 0.0);
+    return uint64_t(v ^ ((v >> 63) & 0x7FFFFFFFFFFFFFFFll)) ^ 0x8000000000000000ull;
 }
 
-// The largest keys of a token's blocks for one KV head, in the order of the blocks; equal ones from
-// the first.  The smallest key taken is found 8 bits at a time.
-constexpr int kPickThreads = 256;
-__global__ __launch_bounds__(kPickThreads) void pick_kernel(const SelectParams p) {
-    __shared__ int s_hist[256];
-    __shared__ int s_part[2][kPickThreads / 64];
-    __shared__ uint64_t s_prefix;
-    __shared__ int s_left;
+// The blocks of one token for one KV head.  kPer keys of a thread stay in registers; 0: they are read
+// again each time.
+constexpr int kBins = 2048;
+constexpr int kListed = 256;  // blocks that are ranked, or summed again, one against another
+
+template <int kThreads>
+struct PickShared {
+    int hist[kBins];
+    int part[2][kThreads / 64];
+    int low[kThreads / 64], high[kThreads / 64];
+    float size[kThreads / 64];
+    int bin, above, inside;
+    int listed, sure;
+    int border;
+    int list[kListed];
+    uint64_t exact[kListed];
+    uint8_t win[kListed];
+};
+
+// Blocks j where take(j), in order, behind each other: a step of kThreads blocks at a time.
+template <int kThreads, typename Take>
+__device__ __forceinline__ void write_taken(int32_t* out, int n, PickShared<kThreads>& s, Take take) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int t = p.first_token + int(blockIdx.x) / p.h_kv, g = int(blockIdx.x) % p.h_kv;
+    int taken = 0;
+    for (int i = 0; i * kThreads < n; ++i) {
+        const int j = i * kThreads + tid;
+        const bool yes = j < n && take(i, j);
+        const uint64_t m = __ballot(yes);
+        if (lane == 0) s.part[i & 1][wave] = __builtin_popcountll(m);
+        __syncthreads();
+        int at = taken + __builtin_popcountll(m & ((1ull << lane) - 1));
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) {
+            at += w < wave ? s.part[i & 1][w] : 0;
+            taken += s.part[i & 1][w];
+        }
+        if (yes) out[at] = j;
+    }
+}
+
+// Every block's score in 64 bits, the border found 8 bits at a time: where fp32 tells nothing (numbers
+// that are not finite, many equal blocks).
+template <int kThreads>
+__device__ __forceinline__ void pick_exact(const SelectParams& p, const Token& tok, int t, int g, int n, int want,
+                                                     uint64_t* keys, int32_t* out, PickShared<kThreads>& s) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const auto forced = [&](int j) { return j < p.first_blocks || j >= n - p.last_blocks; };
+    __syncthreads();
+    for (int j = __builtin_amdgcn_readfirstlane(tid >> 6); j < n; j += kThreads / 64) {
+        if (forced(j)) continue;
+        const uint64_t k = exact_key(p, tok, t, g, j);
+        if (lane == 0) keys[j] = k;
+    }
+    uint64_t prefix = 0;
+    int left = want;  // of the keys that begin with the prefix
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += kThreads) s.hist[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += kThreads)
+            if (!forced(j) && (shift == 56 || (keys[j] >> (shift + 8)) == (prefix >> (shift + 8))))
+                atomicAdd(&s.hist[(keys[j] >> shift) & 255], 1);
+        __syncthreads();
+        if (tid == 0) {
+            int rest = left, v = 255;
+            while (rest > s.hist[v]) rest -= s.hist[v--];
+            s.bin = v;
+            s.above = rest;
+        }
+        __syncthreads();
+        prefix |= uint64_t(s.bin) << shift;
+        left = s.above;
+        __syncthreads();
+    }
+    // the equal ones from the first: their number before block j counts as it goes
+    int equal = 0;
+    const int wave = tid >> 6;
+    int taken = 0;
+    for (int j0 = 0; j0 < n; j0 += kThreads) {
+        const int j = j0 + tid;
+        const bool free = j < n && !forced(j), is = free && keys[j] == prefix;
+        const uint64_t eq = __ballot(is);
+        if (lane == 0) s.part[0][wave] = __builtin_popcountll(eq);
+        __syncthreads();
+        int before = equal + __builtin_popcountll(eq & ((1ull << lane) - 1));
+        for (int w = 0; w < kThreads / 64; ++w) {
+            before += w < wave ? s.part[0][w] : 0;
+            equal += s.part[0][w];
+        }
+        const bool yes = j < n && (!free || keys[j] > prefix || (is && before < left));
+        const uint64_t m = __ballot(yes);
+        if (lane == 0) s.part[1][wave] = __builtin_popcountll(m);
+        __syncthreads();
+        int at = taken + __builtin_popcountll(m & ((1ull << lane) - 1));
+        for (int w = 0; w < kThreads / 64; ++w) {
+            at += w < wave ? s.part[1][w] : 0;
+            taken += s.part[1][w];
+        }
+        if (yes) out[at] = j;
+        __syncthreads();
+    }
+}
+
+template <int kThreads, int kPer>
+__global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
+    constexpr int kWaves = kThreads / 64;
+    __shared__ PickShared<kThreads> s;
+    __shared__ int s_scan[1][kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int slab_t = int(blockIdx.x) / p.h_kv, g = int(blockIdx.x) % p.h_kv, t = p.first_token + slab_t;
     const Token tok = token_of(p, t);
     if (tok.row < 0) return;
     int32_t* out = p.blocks + (int64_t(t) * p.h_kv + g) * p.top;
     const int n = tok.last < 0 ? 0 : tok.last / p.block_tokens + 1;
     if (n <= p.top) {
-        for (int i = tid; i < p.top; i += kPickThreads) out[i] = i < n ? i : -1;
+        for (int i = tid; i < p.top; i += kThreads) out[i] = i < n ? i : -1;
         return;
     }
-    const uint64_t* keys = p.keys + int64_t(blockIdx.x) * p.row_blocks;
-    uint64_t prefix = 0;
-    int left = p.top;  // of the keys that begin with the prefix
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        s_hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < n; j += kPickThreads) {
-            const uint64_t k = keys[j];
-            if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            int rest = left, v = 255;
-            while (rest > s_hist[v]) rest -= s_hist[v--];
-            s_prefix = prefix | uint64_t(v) << shift;
-            s_left = rest;
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
+    const int64_t at = int64_t(slab_t) * p.h_kv + g;
+    const int* keys = p.keys + at * p.key_stride;
+    const int want = p.top - p.first_blocks - p.last_blocks;
+    // blocks that are taken anyway have the lowest key, which no score has
+    const auto load = [&](int j) { return j >= p.first_blocks && j < n - p.last_blocks ? keys[j] : INT32_MIN; };
+    [[maybe_unused]] int kept[kPer > 0 ? kPer : 1];
+    if constexpr (kPer > 0) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) kept[i] = load(i * kThreads + tid);
     }
-    // above the border all, at the border the first `left`
-    int taken = 0, equal = 0;
-    for (int j0 = 0; j0 < n; j0 += kPickThreads) {
-        const int j = j0 + tid;
-        const uint64_t k = j < n ? keys[j] : 0;
-        const bool is = j < n && k == prefix;
-        const uint64_t eq = __ballot(is);
-        __syncthreads();
-        if (lane == 0) s_part[0][wave] = __builtin_popcountll(eq);
-        __syncthreads();
-        int before = equal + __builtin_popcountll(eq & ((1ull << lane) - 1));
-        for (int w = 0; w < kPickThreads / 64; ++w) {
-            before += w < wave ? s_part[0][w] : 0;
-            equal += s_part[0][w];
+    const auto each = [&](auto body) __attribute__((always_inline)) {
+        if constexpr (kPer > 0) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (kept[i] != INT32_MIN) body(i * kThreads + tid, kept[i]);
+        } else {
+            for (int j = tid; j < n; j += kThreads) {
+                const int k = load(j);
+                if (k != INT32_MIN) body(j, k);
+            }
         }
-        const bool take = (j < n && k > prefix) || (is && before < left);
-        const uint64_t tk = __ballot(take);
-        if (lane == 0) s_part[1][wave] = __builtin_popcountll(tk);
-        __syncthreads();
-        int at = taken + __builtin_popcountll(tk & ((1ull << lane) - 1));
-        for (int w = 0; w < kPickThreads / 64; ++w) {
-            at += w < wave ? s_part[1][w] : 0;
-            taken += s_part[1][w];
+    };
+    // extremes, and the error bound
+    int low = INT32_MAX, high = INT32_MIN;
+    each([&](int, int k) __attribute__((always_inline)) {
+        low = min(low, k);
+        high = max(high, k);
+    });
+    float size = 0.f;
+    for (int i = tid; i < p.ranges; i += kThreads) size = fmaxf(size, p.sizes[at * p.ranges + i]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        low = min(low, __shfl_xor(low, o));
+        high = max(high, __shfl_xor(high, o));
+        size = fmaxf(size, __shfl_xor(size, o));
+    }
+    if (lane == 0) s.low[wave] = low, s.high[wave] = high, s.size[wave] = size;
+    if (tid == 0) s.listed = s.sure = 0;
+    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+        low = min(low, s.low[w]);
+        high = max(high, s.high[w]);
+        size = fmaxf(size, s.size[w]);
+    }
+    // each of at most 2 d + 64 additions is off by 2^-23 of the magnitudes' sum, itself no further off
+    const double error = double(size) * (p.chunks * 32 + 128) * 0x1p-23;
+    bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
+
+    double above = INFINITY, from = INFINITY;  // blocks over `above` are taken, those from `from` on maybe
+    bool all = true;                           // the latter all are
+    if (want > 0 && !exact) {
+        int left = want;
+        int border = low;
+        for (;;) {
+            const uint32_t reach = uint32_t(high) - uint32_t(low);
+            const int shift = max(0, 21 - __builtin_clz(reach | 1));  // bins are 11 bits
+            each([&](int, int k) __attribute__((always_inline)) {
+                if (k >= low && k <= high) atomicAdd(&s.hist[(uint32_t(k) - uint32_t(low)) >> shift], 1);
+            });
+            __syncthreads();
+            // the bin where `left` is reached, from the highest
+            constexpr int kOwn = kBins / kThreads;
+            int own[kOwn], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) sum += own[i] = s.hist[kBins - 1 - (tid * kOwn + i)];
+            int upto[1] = {sum}, total[1];
+            scan::block<kWaves>(upto, total, s_scan);
+            int before = upto[0] - sum;
+            if (before < left && left <= upto[0]) {
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    if (before < left && left <= before + own[i]) {
+                        s.bin = kBins - 1 - (tid * kOwn + i);
+                        s.above = before;
+                        s.inside = own[i];
+                    }
+                    before += own[i];
+                }
+            }
+            __syncthreads();
+            left -= s.above;
+            low = int(uint32_t(low) + (uint32_t(s.bin) << shift));
+            high = min(high, int(uint32_t(low) + ((1u << shift) - 1)));
+            border = low;
+            if (shift == 0) break;
+            if (s.inside <= kListed) {
+                each([&](int, int k) __attribute__((always_inline)) {
+                    if (k >= low && k <= high) s.list[atomicAdd(&s.listed, 1)] = k;
+                });
+                __syncthreads();
+                if (tid < s.inside) {
+                    const int k = s.list[tid];
+                    int over = 0, same = 0;
+                    for (int i = 0; i < s.inside; ++i) {
+                        over += s.list[i] > k;
+                        same += s.list[i] == k;
+                    }
+                    if (over < left && left <= over + same) s.border = k;
+                }
+                __syncthreads();
+                border = s.border;
+                if (tid == 0) s.listed = 0;
+                break;
+            }
+            for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+            __syncthreads();
         }
-        if (take) out[at] = j;
+        above = double(value_of(border)) + 2 * error;
+        from = double(value_of(border)) - 2 * error;
+        __syncthreads();
+        int sure = 0;
+        each([&](int j, int k) __attribute__((always_inline)) {
+            const double x = double(value_of(k));
+            if (x > above)
+                ++sure;
+            else if (x >= from) {
+                const int i = atomicAdd(&s.listed, 1);
+                if (i < kListed) s.list[i] = j;
+            }
+        });
+        sure = scan::lane_of(scan::wave(sure), 63);
+        if (lane == 0 && sure > 0) atomicAdd(&s.sure, sure);
+        __syncthreads();
+        const int listed = s.listed, rest = want - s.sure;
+        all = listed == rest;
+        exact = !all && listed > kListed;
+        if (!all && !exact) {
+            for (int i = wave; i < listed; i += kWaves) {
+                const uint64_t k = exact_key(p, tok, t, g, __builtin_amdgcn_readfirstlane(s.list[i]));
+                if (lane == 0) s.exact[i] = k;
+            }
+            __syncthreads();
+            if (tid < listed) {
+                int over = 0;
+                for (int i = 0; i < listed; ++i)
+                    over += s.exact[i] > s.exact[tid] || (s.exact[i] == s.exact[tid] && s.list[i] < s.list[tid]);
+                s.win[tid] = over < rest;
+            }
+            __syncthreads();
+        }
+    }
+    if (exact) {
+        pick_exact<kThreads>(p, tok, t, g, n, want, p.exact_keys + at * p.key_stride, out, s);
+        return;
+    }
+    const auto take = [&](int k, int j) __attribute__((always_inline)) {
+        if (k == INT32_MIN) return true;  // (a block that is taken anyway)
+        const double x = double(value_of(k));
+        if (x > above) return true;
+        if (!(x >= from)) return false;
+        if (all) return true;
+        bool yes = false;
+        for (int i = 0; i < s.listed; ++i) yes = yes || (s.list[i] == j && s.win[i]);
+        return yes;
+    };
+    if constexpr (kPer > 0) {
+        // which of a thread's blocks are taken, and how many of each step of each wave
+        __shared__ int s_count[kPer * kWaves];
+        uint64_t m[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = i * kThreads + tid;
+            m[i] = __ballot(j < n && take(kept[i], j));
+            if (lane == 0) s_count[i * kWaves + wave] = __builtin_popcountll(m[i]);
+        }
+        __syncthreads();
+        // (kPer * kWaves <= 16 * 16 numbers: each wave adds up those before its own)
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int c = scan::row16(s_count[i * kWaves + min(lane & 15, kWaves - 1)]);
+            const int mine = before + (wave > 0 ? scan::lane_of(c, wave - 1) : 0);
+            before += scan::lane_of(c, kWaves - 1);
+            if ((m[i] >> lane) & 1) out[mine + __builtin_popcountll(m[i] & ((1ull << lane) - 1))] = i * kThreads + tid;
+        }
+    } else {
+        write_taken<kThreads>(out, n, s, [&](int, int j) __attribute__((always_inline)) { return take(load(j), j); });
     }
 }
 
@@ -282,12 +682,24 @@ hipError_t launch_select_blocks(const SelectParams& all, hipStream_t stream) {
     SelectParams p = all;
     for (int32_t t = 0; t < all.n_tokens; t += all.slab) {
         p.first_token = t;
-        const int32_t tokens = std::min(all.slab, all.n_tokens - t);
-        const dim3 grid(unsigned((p.row_blocks + 255) / 256), unsigned(tokens * p.h_kv));
-        hipLaunchKernelGGL(scores_kernel, grid, dim3(256), size_t(p.group) * p.chunks * 16 * 8, stream, p);
+        p.tokens = std::min(all.slab, all.n_tokens - t);
+        const unsigned groups = unsigned((p.tokens + p.pack - 1) / p.pack) * unsigned(p.h_kv);
+        const dim3 grid(unsigned((p.ranges + 3) / 4), groups);
+        if (p.chunks == 4)
+            hipLaunchKernelGGL(scores_kernel<64>, grid, dim3(256), 0, stream, p);
+        else
+            hipLaunchKernelGGL(scores_kernel<128>, grid, dim3(256), 0, stream, p);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(pick_kernel, dim3(unsigned(tokens * p.h_kv)), dim3(kPickThreads), 0, stream, p);
+        const dim3 picks(unsigned(p.tokens) * unsigned(p.h_kv));
+        if (p.row_blocks <= 1024)
+            hipLaunchKernelGGL((pick_kernel<256, 4>), picks, dim3(256), 0, stream, p);
+        else if (p.row_blocks <= 4096)
+            hipLaunchKernelGGL((pick_kernel<256, 16>), picks, dim3(256), 0, stream, p);
+        else if (p.row_blocks <= 16384)
+            hipLaunchKernelGGL((pick_kernel<1024, 16>), picks, dim3(1024), 0, stream, p);
+        else
+            hipLaunchKernelGGL((pick_kernel<1024, 0>), picks, dim3(1024), 0, stream, p);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -16,6 +16,7 @@
 // Bound by latency: a launch, and loads that wait for one another.
 #include "atf_internal.hpp"
 #include "rope.hpp"
+#include "scan.hpp"
 
 #include <algorithm>
 
@@ -27,57 +28,6 @@ constexpr int kPlanWaves = kPlanThreads / 64;
 constexpr int kPiece = 256;        // pages that a wave moves at once
 constexpr int kSlotThreads = 256;
 constexpr int kSlotRows = 2048;    // rows whose first tokens slots_kernel holds in LDS
-
-// Sum of each lane's and the lanes below it, by DPP: over rows of 16 lanes, then over the wave.
-template <int kCtrl, int kRows, typename Int>
-__device__ __forceinline__ Int dpp_add(Int x) {
-    if constexpr (sizeof(Int) == 4) {
-        return x + __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xF, false);
-    } else {
-        const int lo = __builtin_amdgcn_update_dpp(0, int(x), kCtrl, kRows, 0xF, false);
-        const int hi = __builtin_amdgcn_update_dpp(0, int(x >> 32), kCtrl, kRows, 0xF, false);
-        return x + (Int(hi) << 32 | uint32_t(lo));
-    }
-}
-template <typename Int>
-__device__ __forceinline__ Int scan_row16(Int x) {
-    x = dpp_add<0x111, 0xF>(x);  // from the lane 1, 2, 4, 8 below in the row of 16
-    x = dpp_add<0x112, 0xF>(x);
-    x = dpp_add<0x114, 0xF>(x);
-    return dpp_add<0x118, 0xF>(x);
-}
-template <typename Int>
-__device__ __forceinline__ Int scan_wave(Int x) {
-    x = scan_row16(x);
-    x = dpp_add<0x142, 0xA>(x);  // from the last lane of rows 0 and 2 to the rows after them
-    return dpp_add<0x143, 0xC>(x);  // from that of row 1 to rows 2 and 3
-}
-template <typename Int>
-__device__ __forceinline__ Int lane_of(Int x, int lane) {
-    if constexpr (sizeof(Int) == 4)
-        return __builtin_amdgcn_readlane(x, lane);
-    else
-        return Int(__builtin_amdgcn_readlane(int(x >> 32), lane)) << 32 | uint32_t(__builtin_amdgcn_readlane(int(x), lane));
-}
-
-// x: each thread's sums of the threads up to it; all: the sums of all.  `part` is free again after
-// the next barrier.
-template <int N, typename Int>
-__device__ __forceinline__ void scan_block(Int (&x)[N], Int (&all)[N], Int (*part)[kPlanWaves]) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = scan_wave(x[i]);
-        if (lane == 63) part[i][wave] = x[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const Int sums = scan_row16(part[i][lane & (kPlanWaves - 1)]);
-        all[i] = lane_of(sums, kPlanWaves - 1);
-        if (wave > 0) x[i] += lane_of(sums, wave - 1);
-    }
-}
 
 struct PlanRow {
     int n, grow;     // tokens it holds, tokens it is to get
@@ -197,7 +147,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanParams p) 
     int64_t f;
     if constexpr (kOne) {
         const Int back = x[0];
-        scan_block(x, all, s_part[0]);
+        scan::block<kPlanWaves>(x, all, s_part[0]);
         f = min(f0 + all[0], int64_t(p.free_capacity));
         if (all[0] > 0) {
             give(0, r, f0 + x[0] - back);
@@ -211,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanParams p) 
             r = plan_row(p, r0 + tid);
             Int y[1] = {Int(r.ends ? r.have : 0)}, sum[1];
             const Int back = y[0];
-            scan_block(y, sum, s_part[0]);
+            scan::block<kPlanWaves>(y, sum, s_part[0]);
             give(r0, r, f0 + given + y[0] - back);
             __syncthreads();
             give_pieces(r0);
@@ -231,7 +181,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanParams p) 
             x[0] = 0;
             x[1] = Int(r.need);
             x[2] = Int(min(r.grow, p.max_tokens + 1));
-            scan_block(x, all, s_part[1]);
+            scan::block<kPlanWaves>(x, all, s_part[1]);
         }
         const int64_t need_end = needed + x[1], end = tokens + x[2];
         const bool ok = r.grow > 0 && r.fits && need_end <= f && end <= p.max_tokens;
