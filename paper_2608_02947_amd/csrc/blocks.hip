@@ -200,15 +200,18 @@ __device__ __forceinline__ int max_columns(int x, int h, int G) {
 }
 
 // A wave: some tiles of 16 blocks, for the columns of `pack` tokens (of one row each time it goes
-// through the tiles) or one token's heads, 16 at a time.
+// through the tiles) or one token's heads, 16 at a time.  The queries' operands of the first kHeld times
+// 16 columns are in LDS, the next tile's bounds on their way while a tile is multiplied.
+constexpr int kHeld = 4;
+
 template <int D>
-__global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
+__global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     constexpr int kChunks = D / 16, kHalf = D / 2;
     __shared__ u32x4_t s_tile[4][kChunks][64];
+    extern __shared__ u32x4_t s_query[];  // [held][kChunks][64]
     const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int range = blockIdx.x * 4 + wave;
-    if (range >= p.ranges) return;
     const int g = int(blockIdx.y) % p.h_kv, t0 = int(blockIdx.y) / p.h_kv * p.pack;  // (of the slab)
     const int G = p.group, width = min(G, 16);
     const int my_w = lane < kHalf ? p.W[lane] : -1;
@@ -218,28 +221,27 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
     const bool is = at < p.pack && t < p.tokens;
     Token tok = {-1, 0, -1};
     if (is) tok = token_of(p, p.first_token + t);
+
+    // operand (column tile, chunk): the positive or the negative numbers of the columns' queries
+    const auto query_of = [&](int h0, int c) __attribute__((always_inline)) {
+        u32x4_t x = *reinterpret_cast<const u32x4_t*>(
+            p.q + (int64_t(p.first_token + (is ? t : t0)) * p.h_q + g * G + (h0 + h < G ? h0 + h : 0)) * D +
+            (g4 & 1) * kHalf + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] &= (((x[e] >> 15) & 0x00010001u) * 0xFFFFu) ^ (g4 >= 2 ? 0u : ~0u);
+        return x;
+    };
+    const int held = min((G + 15) / 16, kHeld);
+    for (int o = wave; o < held * kChunks; o += 4) s_query[64 * o + lane] = query_of(16 * (o / kChunks), o % kChunks);
+    __syncthreads();
+    if (range >= p.ranges) return;
+    const auto query = [&](int h0, int c) __attribute__((always_inline)) {
+        return h0 < 16 * kHeld ? s_query[(h0 / 16 * kChunks + c) * 64 + lane] : query_of(h0, c);
+    };
+
     bool todo = is && tok.row >= 0 && tok.last >= 0;
     float worst = 0.f;  // largest sum of magnitudes
     const int tile0 = range * p.range_tiles;
-
-    // the positive or the negative numbers of a column's query
-    const uint16_t* q = p.q + (int64_t(p.first_token + (is ? t : t0)) * p.h_q + g * G) * D + (g4 & 1) * kHalf;
-    const uint32_t sign = g4 >= 2 ? 0u : ~0u;
-    const auto part_of = [&](u32x4_t x) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] &= (((x[e] >> 15) & 0x00010001u) * 0xFFFFu) ^ sign;
-        return x;
-    };
-    u32x4_t b[kChunks];
-    const auto load_q = [&](int h0) __attribute__((always_inline)) {
-        const uint16_t* from = q + (h0 + h < G ? h0 + h : 0) * D;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) b[c] = *reinterpret_cast<const u32x4_t*>(from + 8 * c);
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) b[c] = part_of(b[c]);
-    };
-    load_q(0);
-
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
         const int row = __builtin_amdgcn_readlane(tok.row, __builtin_ctzll(rest));
         const bool mine = todo && tok.row == row;
@@ -251,19 +253,27 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
             last_pos = max(last_pos, pos);
             last_key = max(last_key, __builtin_amdgcn_readlane(tok.last, l));
         }
-        const int n = last_key / p.block_tokens + 1, tiles = (n + 15) / 16;
-        for (int tile = tile0; tile < min(tiles, tile0 + p.range_tiles); ++tile) {
-            const int j0 = 16 * tile, j15 = min(j0 + 15, n - 1);
-            const int far = last_pos - j0 * p.block_tokens;
-            const int near = max(0, first_pos - min(last_key, j15 * p.block_tokens + (p.block_tokens - 1)));
-            const uint64_t full = __ballot(my_w >= far), keep = __ballot(my_w >= near);
-            const uint16_t* src = bounds_of(p, row, g, min(j0 + r16, n - 1)) + 8 * g4;
-            u32x4_t a[kChunks];
+        const int n = last_key / p.block_tokens + 1, tile1 = min((n + 15) / 16, tile0 + p.range_tiles);
+        if (tile0 >= tile1) continue;
+        const auto where = [&](int tile) __attribute__((always_inline)) {
+            return bounds_of(p, row, g, min(16 * tile + r16, n - 1)) + 8 * g4;
+        };
+        const auto keep_of = [&](int tile) __attribute__((always_inline)) {
+            const int last = min(last_key, min(16 * tile + 15, n - 1) * p.block_tokens + (p.block_tokens - 1));
+            return __ballot(my_w >= max(0, first_pos - last));
+        };
+        u32x4_t a[kChunks];
+        const auto load = [&](const uint16_t* src, uint64_t keep) __attribute__((always_inline)) {
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                a[c] = u32x4_t{0u, 0u, 0u, 0u};
+            for (int c = 0; c < kChunks; ++c)
                 if ((keep >> (8 * c)) & 0xFFull) a[c] = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
-            }
+        };
+        uint64_t keep = keep_of(tile0);
+        load(where(tile0), keep);
+        const uint16_t* next = where(min(tile0 + 1, tile1 - 1));
+        for (int tile = tile0; tile < tile1; ++tile) {
+            const int j0 = 16 * tile;
+            const uint64_t full = __ballot(my_w >= last_pos - j0 * p.block_tokens);
             const uint64_t some = keep & ~full;  // pairs whose windows end in the tile
             if (some != 0) {
 #pragma unroll
@@ -272,25 +282,23 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
             int best[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
             for (int h0 = 0; h0 < G; h0 += 16) {
                 const bool live = mine && h0 + h < G;
-                if (G > 16) load_q(h0);
                 f32x4_t sum = {0.f, 0.f, 0.f, 0.f}, size = sum;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     const uint32_t whole = uint32_t(full >> (8 * c)) & 0xFFu;
-                    if (whole == 0xFFu) {
-                        sum = mfma16(a[c], b[c], sum);
-                        size = mfma16(magnitudes(a[c]), magnitudes(b[c]), size);
-                    } else if (whole != 0) {
-                        const u32x4_t x = keep_pairs(a[c], whole), y = keep_pairs(b[c], whole);
-                        sum = mfma16(x, y, sum);
-                        size = mfma16(magnitudes(x), magnitudes(y), size);
+                    if (whole == 0) continue;
+                    u32x4_t x = a[c], y = query(h0, c);
+                    if (whole != 0xFFu) {
+                        x = keep_pairs(x, whole);
+                        y = keep_pairs(y, whole);
                     }
+                    sum = mfma16(x, y, sum);
+                    size = mfma16(magnitudes(x), magnitudes(y), size);
                 }
                 for (uint64_t m = some; m != 0; m &= m - 1) {
                     const int r = __builtin_ctzll(m), c = r / 8, w = __builtin_amdgcn_readlane(my_w, r);
                     const u32x4_t x = keep_pairs(s_tile[wave][c][lane], 1u << (r % 8));
-                    const u32x4_t y = keep_pairs(
-                        part_of(*reinterpret_cast<const u32x4_t*>(q + (h0 + h < G ? h0 + h : 0) * D + 8 * c)), 1u << (r % 8));
+                    const u32x4_t y = keep_pairs(query(h0, c), 1u << (r % 8));
                     const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
                     const f32x4_t v = mfma16(magnitudes(x), magnitudes(y), f32x4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
@@ -303,6 +311,11 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
                         if (kept) sum[i] += x0;
                         if (kept) size[i] += v[i];
                     }
+                }
+                if (h0 + 16 >= G) {  // the tile is done with
+                    keep = keep_of(min(tile + 1, tile1 - 1));
+                    load(next, keep);
+                    next = where(min(tile + 2, tile1 - 1));
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -326,10 +339,22 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const SelectParams p) {
 
 __device__ __forceinline__ double widen(uint16_t x) { return double(__uint_as_float(uint32_t(x) << 16)); }
 
+// The sum over the wave's lanes.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double add_dpp(double x) {
+    const int64_t v = __double_as_longlong(x);
+    const int lo = __builtin_amdgcn_update_dpp(0, int(v), kCtrl, kRows, 0xF, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, int(v >> 32), kCtrl, kRows, 0xF, false);
+    return x + __longlong_as_double(int64_t(hi) << 32 | uint32_t(lo));
+}
 __device__ __forceinline__ double add_lanes(double x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
+    x = add_dpp<0x111, 0xF>(x);  // as scan::wave
+    x = add_dpp<0x112, 0xF>(x);
+    x = add_dpp<0x114, 0xF>(x);
+    x = add_dpp<0x118, 0xF>(x);
+    x = add_dpp<0x142, 0xA>(x);
+    x = add_dpp<0x143, 0xC>(x);
+    return __longlong_as_double(scan::lane_of(int64_t(__double_as_longlong(x)), 63));
 }
 
 // The score of block j in 64 bits, as an integer of the same order, NaN above all; a pair a lane.
@@ -345,11 +370,13 @@ __device__ __forceinline__ uint64_t exact_key(const SelectParams& p, const Token
     if (kept) hi0 = widen(at[0]), hi1 = widen(at[8]), lo0 = widen(at[16]), lo1 = widen(at[24]);
     double best = 0;
     bool none = false;
+    const int pair = min(lane, half - 1);
+#pragma unroll 4
     for (int h = 0; h < p.group; ++h) {
         const uint16_t* q = p.q + (int64_t(t) * p.h_q + g * p.group + h) * d;
+        const double q0 = widen(q[pair]), q1 = widen(q[pair + half]);
         double u = 0;
         if (kept) {
-            const double q0 = widen(q[lane]), q1 = widen(q[lane + half]);
             // (a query that is none stays so)
             u = (q0 < 0 ? 0 : q0) * hi0 + (q0 > 0 ? 0 : q0) * lo0;
             u += (q1 < 0 ? 0 : q1) * hi1 + (q1 > 0 ? 0 : q1) * lo1;
@@ -685,10 +712,11 @@ hipError_t launch_select_blocks(const SelectParams& all, hipStream_t stream) {
         p.tokens = std::min(all.slab, all.n_tokens - t);
         const unsigned groups = unsigned((p.tokens + p.pack - 1) / p.pack) * unsigned(p.h_kv);
         const dim3 grid(unsigned((p.ranges + 3) / 4), groups);
+        const size_t queries = size_t(std::min((p.group + 15) / 16, kHeld)) * size_t(p.chunks) * 1024;
         if (p.chunks == 4)
-            hipLaunchKernelGGL(scores_kernel<64>, grid, dim3(256), 0, stream, p);
+            hipLaunchKernelGGL(scores_kernel<64>, grid, dim3(256), queries, stream, p);
         else
-            hipLaunchKernelGGL(scores_kernel<128>, grid, dim3(256), 0, stream, p);
+            hipLaunchKernelGGL(scores_kernel<128>, grid, dim3(256), queries, stream, p);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const dim3 picks(unsigned(p.tokens) * unsigned(p.h_kv));
