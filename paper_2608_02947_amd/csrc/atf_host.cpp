@@ -1678,7 +1678,7 @@ int check_tokens(const char* fn, const QueryTokens& q) {
 }
 
 struct SelectLayout {
-    int32_t slab, pack, ranges, range_tiles, key_stride;
+    int32_t slab, pack, ranges, key_stride;
     size_t off_exact, off_sizes, total;  // total 0: too large
 };
 // Tokens of a row one behind the other share the columns of the matrix products: where there are more
@@ -1691,15 +1691,16 @@ SelectLayout select_layout(int64_t n_tokens, int32_t batch, int32_t h_q, int32_t
     n_tokens = std::max<int64_t>(n_tokens, 1);
     // (workspaces are sized without the rows: for one token of each)
     L.pack = group < 16 && n_tokens > 2 * int64_t(batch) ? 16 / group : 1;
-    const int64_t most_ranges = std::min<int64_t>(tiles, (4096 + h_kv - 1) / h_kv);
+    // (workgroups are of four waves)
+    const auto ranges = [&](int64_t groups) {
+        return std::min<int64_t>(tiles, (4096 + 4 * groups - 1) / (4 * groups) * 4);
+    };
+    const int64_t most_ranges = ranges(h_kv);
     const u128 each = u128(h_kv) * (u128(stride) * 12 + u128(most_ranges) * 4);
     int64_t slab = int64_t(std::min<u128>(u128(atf::kSelectSlabBytes) / each, u128(n_tokens)));
     slab = std::max<int64_t>(1, std::min<int64_t>(slab, 65535 / h_kv));
     if (slab * h_kv > 65535) return L;
-    const int64_t groups = (slab + L.pack - 1) / L.pack * h_kv;
-    const int64_t ranges = std::min<int64_t>(tiles, (4096 + groups - 1) / groups);
-    L.range_tiles = static_cast<int32_t>((tiles + ranges - 1) / ranges);
-    L.ranges = static_cast<int32_t>((tiles + L.range_tiles - 1) / L.range_tiles);
+    L.ranges = static_cast<int32_t>(ranges((slab + L.pack - 1) / L.pack * h_kv));
     L.slab = static_cast<int32_t>(slab);
     L.key_stride = static_cast<int32_t>(stride);
     const u128 keys = u128(slab) * u128(h_kv) * u128(stride);
@@ -1913,7 +1914,6 @@ int atf_select_blocks(const void* q, const void* bounds, int32_t* blocks, int64_
     p.key_stride = L.key_stride;
     p.pack = L.pack;
     p.ranges = L.ranges;
-    p.range_tiles = L.range_tiles;
     p.batch = batch;
     p.max_pages = max_pages_per_row;
     p.num_pages = num_pages;

@@ -250,7 +250,7 @@ struct SelectParams {
     const int32_t* positions;    // [n_tokens]
     const int32_t* n_k_rows;     // [batch], clamped to [0, max_n_k]
     // workspace: scores as integers of their order [slab][h_kv][key_stride], the same in 64 bits
-    // where fp32 does not do, and the largest sum of magnitudes of each range of tiles
+    // where fp32 does not do, and the largest sum of magnitudes that each wave met
     int32_t* keys;
     uint64_t* exact_keys;
     float* sizes;                // [slab][h_kv][ranges]
@@ -259,7 +259,7 @@ struct SelectParams {
     int32_t h_q, h_kv, group, chunks;
     int32_t key_stride;          // row_blocks rounded up to 16
     int32_t pack;                // tokens whose heads share the columns of a product
-    int32_t ranges, range_tiles; // waves of a (token, KV head), tiles of 16 blocks of each
+    int32_t ranges;              // waves of a (token, KV head): each takes every ranges-th tile
     int32_t slab, first_token, tokens;  // tokens of a launch at most; set by the launcher: the
                                  // first of this one, and their number
     int32_t W[kMaxPairs];

@@ -199,7 +199,7 @@ __device__ __forceinline__ int max_columns(int x, int h, int G) {
     return x;
 }
 
-// A wave: some tiles of 16 blocks, for the columns of `pack` tokens (of one row each time it goes
+// A wave: every `ranges`-th tile of 16 blocks, for the columns of `pack` tokens (of one row each time it goes
 // through the tiles) or one token's heads, 16 at a time.  The queries' operands of the first kHeld times
 // 16 columns are in LDS, the next tile's bounds on their way while a tile is multiplied.
 constexpr int kHeld = 4;
@@ -241,7 +241,6 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
 
     bool todo = is && tok.row >= 0 && tok.last >= 0;
     float worst = 0.f;  // largest sum of magnitudes
-    const int tile0 = range * p.range_tiles;
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
         const int row = __builtin_amdgcn_readlane(tok.row, __builtin_ctzll(rest));
         const bool mine = todo && tok.row == row;
@@ -253,8 +252,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
             last_pos = max(last_pos, pos);
             last_key = max(last_key, __builtin_amdgcn_readlane(tok.last, l));
         }
-        const int n = last_key / p.block_tokens + 1, tile1 = min((n + 15) / 16, tile0 + p.range_tiles);
-        if (tile0 >= tile1) continue;
+        const int n = last_key / p.block_tokens + 1, tiles = (n + 15) / 16;
+        if (range >= tiles) continue;
         const auto where = [&](int tile) __attribute__((always_inline)) {
             return bounds_of(p, row, g, min(16 * tile + r16, n - 1)) + 8 * g4;
         };
@@ -268,10 +267,10 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
             for (int c = 0; c < kChunks; ++c)
                 if ((keep >> (8 * c)) & 0xFFull) a[c] = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
         };
-        uint64_t keep = keep_of(tile0);
-        load(where(tile0), keep);
-        const uint16_t* next = where(min(tile0 + 1, tile1 - 1));
-        for (int tile = tile0; tile < tile1; ++tile) {
+        uint64_t keep = keep_of(range);
+        load(where(range), keep);
+        const uint16_t* next = where(min(range + p.ranges, tiles - 1));
+        for (int tile = range; tile < tiles; tile += p.ranges) {
             const int j0 = 16 * tile;
             const uint64_t full = __ballot(my_w >= last_pos - j0 * p.block_tokens);
             const uint64_t some = keep & ~full;  // pairs whose windows end in the tile
@@ -313,9 +312,9 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                     }
                 }
                 if (h0 + 16 >= G) {  // the tile is done with
-                    keep = keep_of(min(tile + 1, tile1 - 1));
+                    keep = keep_of(min(tile + p.ranges, tiles - 1));
                     load(next, keep);
-                    next = where(min(tile + 2, tile1 - 1));
+                    next = where(min(tile + 2 * p.ranges, tiles - 1));
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
