@@ -134,8 +134,9 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
 // tile of a row) has a product of its own, of which every block and column takes what its distance
 // allows; chunks without a kept pair are not read.
 //
-// These sums are in fp32, off by no more than their error bound: n additions, each at most 2^-23 of the
-// sum of magnitudes, which a second product has.  pick_kernel finds the border of the blocks taken
+// These sums are in fp32, off by no more than their error bound: the additions that a term goes through
+// (a product's 32, then one a chunk or pair), each at most 2^-23 of the sum of magnitudes, which a
+// second product has.  pick_kernel finds the border of the blocks taken
 // among them; blocks as near to it as the bound allows, mostly the one that is the border, are summed
 // again in 64 bits unless all or none of them are taken.
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -199,6 +200,17 @@ __device__ __forceinline__ int max_columns(int x, int h, int G) {
     return x;
 }
 
+// The largest of the wave's lanes.
+__device__ __forceinline__ int max_lanes(int x) {
+    x = max_dpp<0x111>(x, INT32_MIN, true);  // up to each lane of a row of 16, then of the wave
+    x = max_dpp<0x112>(x, INT32_MIN, true);
+    x = max_dpp<0x114>(x, INT32_MIN, true);
+    x = max_dpp<0x118>(x, INT32_MIN, true);
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x142, 0xA, 0xF, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x143, 0xC, 0xF, false));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // A wave: every `ranges`-th tile of 16 blocks, for the columns of `pack` tokens (of one row each time it goes
 // through the tiles) or one token's heads, 16 at a time.  The queries' operands of the first kHeld times
 // 16 columns are in LDS, the next tile's bounds on their way while a tile is multiplied.
@@ -240,7 +252,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     };
 
     bool todo = is && tok.row >= 0 && tok.last >= 0;
-    float worst = 0.f;  // largest sum of magnitudes
+    float worst = 0.f;  // largest sum of magnitudes times its additions
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
         const int row = __builtin_amdgcn_readlane(tok.row, __builtin_ctzll(rest));
         const bool mine = todo && tok.row == row;
@@ -291,13 +303,14 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                         x = keep_pairs(x, whole);
                         y = keep_pairs(y, whole);
                     }
-                    sum = mfma16(x, y, sum);
+                    // (a sum of its own for each chunk: fewer additions to a number)
+                    sum += mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
                     size = mfma16(magnitudes(x), magnitudes(y), size);
                 }
                 for (uint64_t m = some; m != 0; m &= m - 1) {
-                    const int r = __builtin_ctzll(m), c = r / 8, w = __builtin_amdgcn_readlane(my_w, r);
-                    const u32x4_t x = keep_pairs(s_tile[wave][c][lane], 1u << (r % 8));
-                    const u32x4_t y = keep_pairs(query(h0, c), 1u << (r % 8));
+                    const int r = __builtin_ctzll(m), w = __builtin_amdgcn_readlane(my_w, r);
+                    const u32x4_t x = keep_pairs(s_tile[wave][r / 8][lane], 1u << (r % 8));
+                    const u32x4_t y = keep_pairs(query(h0, r / 8), 1u << (r % 8));
                     const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
                     const f32x4_t v = mfma16(magnitudes(x), magnitudes(y), f32x4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
@@ -311,6 +324,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                         if (kept) size[i] += v[i];
                     }
                 }
+                // additions that a term goes through: those of a product of 32, the chunks', the pairs'
+                const float steps = float(32 + kChunks + __builtin_popcountll(some));
                 if (h0 + 16 >= G) {  // the tile is done with
                     keep = keep_of(min(tile + p.ranges, tiles - 1));
                     load(next, keep);
@@ -319,7 +334,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (live) best[i] = max(best[i], key_of(sum[i]));
-                    if (live) worst = fmaxf(worst, size[i]);
+                    if (live) worst = fmaxf(worst, size[i] * steps);
                 }
             }
 #pragma unroll
@@ -537,12 +552,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     });
     float size = 0.f;
     for (int i = tid; i < p.ranges; i += kThreads) size = fmaxf(size, p.sizes[at * p.ranges + i]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        low = min(low, __shfl_xor(low, o));
-        high = max(high, __shfl_xor(high, o));
-        size = fmaxf(size, __shfl_xor(size, o));
-    }
+    low = ~max_lanes(~low);  // (the complement is in the opposite order)
+    high = max_lanes(high);
+    size = __int_as_float(max_lanes(__float_as_int(size)));
     if (lane == 0) s.low[wave] = low, s.high[wave] = high, s.size[wave] = size;
     if (tid == 0) s.listed = s.sure = 0;
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
@@ -552,8 +564,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         high = max(high, s.high[w]);
         size = fmaxf(size, s.size[w]);
     }
-    // each of at most 2 d + 64 additions is off by 2^-23 of the magnitudes' sum, itself no further off
-    const double error = double(size) * (p.chunks * 32 + 128) * 0x1p-23;
+    // each addition is off by 2^-23 of the magnitudes' sum at most; that, and its product with their
+    // number, by less than 2^-10
+    const double error = double(size) * (0x1p-23 * (1 + 0x1p-10));
     bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
 
     double above = INFINITY, from = INFINITY;  // blocks over `above` are taken, those from `from` on maybe
