@@ -404,6 +404,22 @@ int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room) {
     return std::max<int64_t>(1, std::min(best, room));
 }
 
+// Attention over listed blocks: workgroups of 4 waves, of 8 where that leaves more waves than run at
+// once (2 a SIMD: 2,048) short of tiles no longer; a list is split where even so waves have more than 8
+// tiles and fewer than 2,048 run.
+AttendPlan attend_plan(int64_t groups, int64_t tiles) {
+    AttendPlan a = {4, 1, int32_t(std::min<int64_t>(tiles, INT32_MAX))};
+    groups = std::max<int64_t>(groups, 1);
+    if (groups * 8 <= 2048) a.waves = 8;
+    const int64_t room = 2048 / (groups * a.waves);
+    const int64_t splits = std::min(room, tiles / (4 * a.waves));
+    if (splits > 1) {
+        a.split_tiles = int32_t((tiles + splits - 1) / splits);
+        a.splits = int32_t((tiles + a.split_tiles - 1) / a.split_tiles);
+    }
+    return a;
+}
+
 }  // namespace atf
 
 extern "C" {
@@ -1942,7 +1958,9 @@ size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, i
         block_tokens < 32 || block_tokens % 32 != 0 || (head_dim != 64 && head_dim != 128) ||
         n_tokens > atf::kMaxTokenHeads / h_q)
         return 0;
-    return 256;
+    const int32_t group = h_q / h_kv, subgroups = (group + 31) / 32;
+    const atf::AttendPlan plan = atf::attend_plan(n_tokens * h_kv * subgroups, int64_t(top_blocks) * (block_tokens / 32));
+    return std::max<size_t>(256, plan.splits == 1 ? 0 : ws_layout(size_t(n_tokens) * size_t(plan.splits), h_q, head_dim, 0).total);
 }
 
 int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, void* o, float* lse, int64_t n_tokens,
@@ -2019,6 +2037,18 @@ int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, v
     p.group = h_q / h_kv;
     p.subgroups = (p.group + 31) / 32;
     p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
+    const atf::AttendPlan plan =
+        atf::attend_plan(n_tokens * h_kv * p.subgroups, int64_t(top_blocks) * (block_tokens / 32));
+    p.waves = plan.waves;
+    p.splits = plan.splits;
+    p.split_tiles = plan.split_tiles;
+    if (plan.splits > 1) {
+        const WsLayout L = ws_layout(size_t(n_tokens) * size_t(plan.splits), h_q, d, 0);
+        char* ws = static_cast<char*>(workspace);
+        p.ws_m = reinterpret_cast<float*>(ws + L.off_m);
+        p.ws_l = reinterpret_cast<float*>(ws + L.off_l);
+        p.ws_o = reinterpret_cast<float*>(ws + L.off_o);
+    }
     p.scale_log2 = scale * 1.4426950408889634f;
     std::memcpy(p.W, win.W, sizeof p.W);
     const hipError_t e = atf::launch_attend_blocks(p, d, static_cast<hipStream_t>(hip_stream));

@@ -280,6 +280,11 @@ struct AttendParams {
     int32_t batch, max_pages, num_pages, page_tokens, block_tokens;
     int32_t n_tokens, max_n_k, top, h_q, h_kv, group;
     int32_t heads_per_block, subgroups;  // as DecodeQ8Params
+    int32_t waves;               // of a workgroup: 2, 4 or 8
+    int32_t splits, split_tiles; // workgroups of a list, 32-token tiles of each
+    float* ws_m;                 // [n_tokens][h_q][splits], split lists, as the two below
+    float* ws_l;
+    float* ws_o;                 // [n_tokens][h_q][splits][d]
     float scale_log2;
     int32_t W[kMaxPairs];
 };
@@ -308,6 +313,12 @@ hipError_t launch_plan_pages(const PlanParams& p, hipStream_t stream);
 hipError_t launch_append_slots(const AppendSlotsParams& p, bool turn, int head_dim, hipStream_t stream);
 hipError_t launch_block_bounds(const BoundsParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_select_blocks(const SelectParams& p, hipStream_t stream);
+// Waves of a workgroup and workgroups of a list for `groups` (token, KV head, head subgroup)s of lists of
+// `tiles` 32-token tiles.
+struct AttendPlan {
+    int32_t waves, splits, split_tiles;
+};
+AttendPlan attend_plan(int64_t groups, int64_t tiles);
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_rotate_kcache(const RotateParams& p, int head_dim, hipStream_t stream);
 

@@ -10,9 +10,12 @@
 //     tokens whose scores it has.
 //
 // A pair is kept at distance z iff z <= W_r.  Per tile two ballots give the pairs kept at some token
-// and at every token: chunks without a kept pair are not read; keys lose the pairs kept nowhere, so
-// that a number that is none does not count there; where a window ends inside the tile they are
-// masked token by token.
+// and at every token: chunks without a kept pair are not read, and products of two such not made;
+// keys lose the pairs kept nowhere, so that a number that is none does not count there; where a window
+// ends inside the tile they are masked token by token.
+//
+// The NW waves of a workgroup take the list's tiles in turn and join their states in LDS.  Where tokens
+// are few a list is split over workgroups, whose partial states a second kernel joins.
 #include "atf_internal.hpp"
 
 namespace atf {
@@ -24,6 +27,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;
+constexpr float kRescale = 8.0f;  // lazy-rescale threshold, log2 units
 
 __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
@@ -42,6 +46,12 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t bits) {
     return u32x4_t{x[0] & pair_mask(bits, 0), x[1] & pair_mask(bits, 1), x[2] & pair_mask(bits, 2),
                    x[3] & pair_mask(bits, 3)};
 }
+
+// A lane looks up one tile of the list, 64 at a time; which of them are tokens of the row is a ballot.
+struct Tile {
+    int page, at;  // where its first token is
+    int first;     // that token's position
+};
 
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendParams p) {
@@ -62,9 +72,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
     const int r16 = lane & 15;
     const int g4 = lane >> 4;
     const int cols = p.h_kv * p.subgroups;
-    const int t = int(blockIdx.x) / cols;
-    const int col = int(blockIdx.x) % cols;
-    const int g = col / p.subgroups, sub = col % p.subgroups;
+    const int item = int(blockIdx.x) / cols;
+    const int col = int(blockIdx.x) - item * cols;
+    const int t = item / p.splits, split = item - t * p.splits;
+    const int g = col / p.subgroups, sub = col - g * p.subgroups;
     const int hq0 = g * p.group + sub * p.heads_per_block;
     const int NH = min(p.heads_per_block, p.group - sub * p.heads_per_block);
 
@@ -76,6 +87,77 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
 
     const int my_w = lane < kHalf ? p.W[lane] : -1;
     if (tid < kHalf) s_w[tid] = my_w;
+
+    // this wave's tiles of the split: every NW-th
+    const int per = p.block_tokens / kTile;
+    const int tile1 = min(p.top * per, (split + 1) * p.split_tiles);
+    const int32_t* list = p.blocks + (int64_t(t) * p.h_kv + g) * p.top;
+    int i0 = split * p.split_tiles + wave;
+    Tile mine = {0, 0, 0};
+    uint64_t found = 0;
+    const auto look = [&]() __attribute__((always_inline)) {
+        const int i = i0 + NW * lane;
+        bool is = false;
+        if (i < tile1) {
+            const int k = i / per, j = list[k];
+            if (j >= 0 && last >= 0 && j <= last / p.block_tokens) {
+                mine.first = j * p.block_tokens + (i - k * per) * kTile;
+                is = mine.first <= last;
+                if (is) {
+                    const int n = mine.first / p.page_tokens;
+                    mine.page = min(max(p.block_table[int64_t(row) * p.max_pages + n], 0), p.num_pages - 1);
+                    mine.at = mine.first - n * p.page_tokens;
+                }
+            }
+        }
+        found = __ballot(is);
+        i0 += 64 * NW;
+    };
+    const auto next = [&](Tile& x) __attribute__((always_inline)) {
+        while (found == 0) {
+            if (i0 >= tile1) return false;
+            look();
+        }
+        const int l = __builtin_ctzll(found);
+        found &= found - 1;
+        x.page = __builtin_amdgcn_readlane(mine.page, l);
+        x.at = __builtin_amdgcn_readlane(mine.at, l);
+        x.first = __builtin_amdgcn_readlane(mine.first, l);
+        return true;
+    };
+    const int tk = 16 * (r16 >> 3) + 4 * ((r16 >> 2) & 1) + (r16 & 3);  // this lane's token of s = 0
+    u32x4_t kf[2][kM], vf[kDB];
+    uint64_t full = 0, keep = 0;
+    const auto load_k = [&](const Tile& x) __attribute__((always_inline)) {
+        const int left = min(last - x.first, kTile - 1);
+        full = __ballot(my_w >= q_pos - x.first);
+        keep = __ballot(my_w >= q_pos - x.first - left);
+        const int64_t ph = int64_t(x.page) * p.h_kv + g;
+        const uint64_t at = reinterpret_cast<uint64_t>(p.k_pages) + (ph * kChunks * p.page_tokens + x.at) * 32 + 16 * (g4 & 1);
+#pragma unroll
+        for (int m = 0; m < kM; ++m) {
+            const int c = 2 * m + (g4 >> 1);
+            if (((keep >> (8 * c)) & 0xFFull) == 0) continue;
+            const uint64_t from = at + uint64_t(uint32_t(c) * uint32_t(p.page_tokens)) * 32;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) kf[s][m] = load16(from + 32 * min(tk + 8 * s, left));
+        }
+    };
+    const auto load_v = [&](const Tile& x) __attribute__((always_inline)) {
+        // (a 16-token block past the row's end is the one before it again, masked below)
+        const int block = 16 <= last - x.first ? g4 >> 1 : 0;
+        const uint64_t at = reinterpret_cast<uint64_t>(p.v_pages) +
+                            ((int64_t(x.page) * p.h_kv + g) * p.page_tokens + x.at + 16 * block) * (2 * D) + 16 * (g4 & 1) + 32 * r16;
+#pragma unroll
+        for (int i = 0; i < kDB; ++i) vf[i] = load16(at + 512 * i);
+    };
+
+    Tile x = {0, 0, 0};
+    bool have = next(x);
+    if (have) {
+        load_v(x);
+        load_k(x);
+    }
     // queries: operand (tile n, m)
     u32x4_t qf[kOps];
 #pragma unroll
@@ -89,157 +171,129 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
     __syncthreads();
 
     f32x4_t oacc[NT][kDB];
-    float m_run[NT], l_run[NT];
+    float m_run[NT], m_thr[NT], m_neg[NT], l_run[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int i = 0; i < kDB; ++i) oacc[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        m_run[n] = -INFINITY;
-        l_run[n] = 0.f;
+        m_run[n] = m_thr[n] = -INFINITY;
+        m_neg[n] = l_run[n] = 0.f;
     }
     const float sc = p.scale_log2;
-    const int tk = 16 * (r16 >> 3) + 4 * ((r16 >> 2) & 1) + (r16 & 3);  // this lane's token of s = 0
 
-    // tiles of the list: every NW-th is this wave's; a lane looks one up, 64 at a time
-    const int per = p.block_tokens / kTile, tiles = p.top * per;
-    const int32_t* list = p.blocks + (int64_t(t) * p.h_kv + g) * p.top;
-    for (int i0 = wave; i0 < tiles; i0 += 64 * NW) {
-        const int i = i0 + NW * lane;
-        int my_page = 0, my_at = 0, my_tb = -1;
-        if (i < tiles) {
-            const int j = list[i / per];
-            if (j >= 0 && last >= 0 && j <= last / p.block_tokens) {
-                const int tb = j * p.block_tokens + (i % per) * kTile;
-                if (tb <= last) {
-                    my_tb = tb;
-                    my_page = min(max(p.block_table[int64_t(row) * p.max_pages + tb / p.page_tokens], 0), p.num_pages - 1);
-                    my_at = tb % p.page_tokens;
+    while (have) {
+        const int left = last - x.first;  // the tile's last token that counts, if below 31
+        if (keep & ~full) {
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                int w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = s_w[8 * (2 * m + (g4 >> 1)) + e];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int z = q_pos - x.first - (tk + 8 * s);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        kf[s][m][e] &= (w[2 * e] >= z ? 0x0000FFFFu : 0u) | (w[2 * e + 1] >= z ? 0xFFFF0000u : 0u);
                 }
             }
         }
-        uint64_t todo = __ballot(my_tb >= 0);
-        while (todo) {
-            const int l = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const int page = __builtin_amdgcn_readlane(my_page, l), at = __builtin_amdgcn_readlane(my_at, l);
-            const int tb = __builtin_amdgcn_readlane(my_tb, l);
-            const int left = last - tb;  // the tile's last token that counts, if below 31
-            const uint64_t full = __ballot(my_w >= q_pos - tb);
-            const uint64_t keep = __ballot(my_w >= q_pos - tb - min(left, kTile - 1));
-            const int64_t ph = int64_t(page) * p.h_kv + g;
-            const uint64_t kb = reinterpret_cast<uint64_t>(p.k_pages) + (ph * kChunks * p.page_tokens + at) * 32;
-            const uint64_t vb = reinterpret_cast<uint64_t>(p.v_pages) + (ph * p.page_tokens + at) * (2 * D);
-            u32x4_t kf[2][kM], vf[kDB];
+        f32x4_t sacc[NT][2];
 #pragma unroll
-            for (int m = 0; m < kM; ++m) {
-                const int c = 2 * m + (g4 >> 1);
-                const bool kept = ((keep >> (8 * c)) & 0xFFull) != 0;
+        for (int n = 0; n < NT; ++n) sacc[n][0] = sacc[n][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    kf[s][m] = u32x4_t{0u, 0u, 0u, 0u};
-                    if (kept)
-                        kf[s][m] = load16(kb + (int64_t(c) * p.page_tokens + min(tk + 8 * s, left)) * 32 + 16 * (g4 & 1));
+        for (int m = 0; m < kM; ++m) {
+            const uint32_t both = uint32_t(keep >> (16 * m)) & 0xFFFFu;
+            if (both == 0xFFFFu) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) sacc[n][s] = mfma16(kf[s][m], qf[kM * n + m], sacc[n][s]);
+            } else if (both != 0) {
+                const uint32_t bits = both >> (8 * (g4 >> 1));
+                const u32x4_t k0 = keep_pairs(kf[0][m], bits), k1 = keep_pairs(kf[1][m], bits);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const u32x4_t q = keep_pairs(qf[kM * n + m], bits);
+                    sacc[n][0] = mfma16(k0, q, sacc[n][0]);
+                    sacc[n][1] = mfma16(k1, q, sacc[n][1]);
                 }
             }
+        }
+        // the next tile's keys, into the registers of this one's; its values follow below
+        Tile y = x;
+        have = next(y);
+        if (have) load_k(y);
+        // tokens past the row's keys: no probability, and no value that is not a number
+        if (left < kTile - 1) {
+            const int bound = left - 16 * (g4 >> 1) - 4 * (g4 & 1);
 #pragma unroll
-            for (int i = 0; i < kDB; ++i) {
-                vf[i] = u32x4_t{0u, 0u, 0u, 0u};
-                if (16 * (g4 >> 1) <= left) vf[i] = load16(vb + (g4 >> 1) * (32 * D) + (16 * i + r16) * 32 + 16 * (g4 & 1));
-            }
-            if (keep & ~full) {
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int m = 0; m < kM; ++m)
+                for (int v = 0; v < 4; ++v) {
+                    const bool out = 8 * s + v > bound;
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int z = q_pos - tb - (tk + 8 * s);
-                        uint32_t bits = 0;
+                    for (int n = 0; n < NT; ++n)
+                        if (out) sacc[n][s][v] = -INFINITY;
+                    // element 4 s + v of the lane's 8 values
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) bits |= s_w[8 * (2 * m + (g4 >> 1)) + e] >= z ? 1u << e : 0u;
-                        kf[s][m] = keep_pairs(kf[s][m], bits);
-                    }
-            } else {
-#pragma unroll
-                for (int m = 0; m < kM; ++m) {
-                    const uint32_t bits = uint32_t(keep >> (8 * (2 * m + (g4 >> 1)))) & 0xFFu;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) kf[s][m] = keep_pairs(kf[s][m], bits);
+                    for (int i = 0; i < kDB; ++i) vf[i][2 * s + v / 2] &= !out ? ~0u : v & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                 }
-            }
-            f32x4_t sacc[NT][2];
+        }
+        // P as two bf16 numbers, what fits and what is left over: one would round every probability to
+        // 2^-9, and the output's own rounding is that size
+        u32x4_t ph[NT], pl[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            float mx = -INFINITY;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    sacc[n][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int m = 0; m < kM; ++m) {
-                        const uint32_t bits = uint32_t(keep >> (8 * (2 * m + (g4 >> 1)))) & 0xFFu;
-                        sacc[n][s] = mfma16(kf[s][m], keep_pairs(qf[kM * n + m], bits), sacc[n][s]);
-                    }
-                }
-            // tokens past the row's keys: no probability, and no value that is not a number
-            if (left < kTile - 1) {
-                const int bound = left - 16 * (g4 >> 1) - 4 * (g4 & 1);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const bool out = 8 * s + v > bound;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            if (out) sacc[n][s][v] = -INFINITY;
-                        // element 4 s + v of the lane's 8 values
-                        if (out) {
-#pragma unroll
-                            for (int i = 0; i < kDB; ++i) vf[i][2 * s + v / 2] &= v & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                        }
-                    }
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sacc[n][s][v]);
+                for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sacc[n][s][v]);
+            if (__any(mx * sc > m_thr[n])) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
                 const float m_new = fmaxf(m_run[n], mx * sc);
                 const float m_use = m_new == -INFINITY ? 0.f : m_new;
                 const float alpha = exp2_fast(m_run[n] - m_use);
                 m_run[n] = m_new;
+                m_thr[n] = m_new + kRescale;
+                m_neg[n] = -m_use;
                 l_run[n] *= alpha;
 #pragma unroll
-                for (int i = 0; i < kDB; ++i) oacc[n][i] *= alpha;
-                // P as two bf16 numbers, what fits and what is left over: one would round every
-                // probability to 2^-9, and the output's own rounding is that size
-                u32x4_t ph_, pl_;
+                for (int i = 0; i < kDB; ++i)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        uint32_t h[2];
-                        bf16x2_t rest;
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float e = exp2_fast(__builtin_fmaf(sacc[n][s][2 * k + x], sc, -m_use));
-                            l_run[n] += e;
-                            h[x] = __float_as_uint(e) & 0xFFFF0000u;
-                            rest[x] = (__bf16)(e - __uint_as_float(h[x]));
-                        }
-                        ph_[2 * s + k] = h[0] >> 16 | h[1];
-                        pl_[2 * s + k] = __builtin_bit_cast(uint32_t, rest);
-                    }
-#pragma unroll
-                for (int i = 0; i < kDB; ++i) {
-                    oacc[n][i] = mfma16(vf[i], ph_, oacc[n][i]);
-                    oacc[n][i] = mfma16(vf[i], pl_, oacc[n][i]);
-                }
+                    for (int v = 0; v < 4; ++v) oacc[n][i][v] *= alpha;
             }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint32_t h[2];
+                    bf16x2_t rest;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float w = exp2_fast(__builtin_fmaf(sacc[n][s][2 * k + e], sc, m_neg[n]));
+                        l_run[n] += w;
+                        h[e] = __float_as_uint(w) & 0xFFFF0000u;
+                        rest[e] = (__bf16)(w - __uint_as_float(h[e]));
+                    }
+                    ph[n][2 * s + k] = h[0] >> 16 | h[1];
+                    pl[n][2 * s + k] = __builtin_bit_cast(uint32_t, rest);
+                }
         }
+#pragma unroll
+        for (int i = 0; i < kDB; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                oacc[n][i] = mfma16(vf[i], ph[n], oacc[n][i]);
+                oacc[n][i] = mfma16(vf[i], pl[n], oacc[n][i]);
+            }
+        if (have) load_v(y);
+        x = y;
     }
 
-    // ---- combine the waves' states, in wave order
+    // ---- combine the waves' states, in wave order, and write the output, or the split's partial
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         float l_lane = l_run[n] + __shfl_xor(l_run[n], 16);
@@ -266,7 +320,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         }
         __syncthreads();
         for (int e = tid; e < heads * (D / 4); e += NW * 64) {
-            const int r = e / (D / 4), x = 4 * (e % (D / 4)), h = 16 * n + r;
+            const int r = e / (D / 4), d = 4 * (e % (D / 4)), h = 16 * n + r;
             float M = -INFINITY;
 #pragma unroll
             for (int w = 0; w < NW; ++w) M = fmaxf(M, red_m[w][h]);
@@ -274,8 +328,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
             float L = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                o += *reinterpret_cast<const f32x4_t*>(&s_o[(16 * w + r) * kOStride + x]);
+                o += *reinterpret_cast<const f32x4_t*>(&s_o[(16 * w + r) * kOStride + d]);
                 if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
+            }
+            const int64_t to = int64_t(t) * p.h_q + hq0 + h;
+            if (p.splits > 1) {
+                const int64_t slot = to * p.splits + split;
+                if (d == 0) {
+                    p.ws_m[slot] = M;
+                    p.ws_l[slot] = L;
+                }
+                *reinterpret_cast<f32x4_t*>(&p.ws_o[slot * D + d]) = o;
+                continue;
             }
             const bool empty = L == 0.f;  // no key: O = 0, LSE = -inf
             bf16x2_t lo, hi;
@@ -283,31 +347,89 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
             lo[1] = (__bf16)(empty ? 0.f : o[1] / L);
             hi[0] = (__bf16)(empty ? 0.f : o[2] / L);
             hi[1] = (__bf16)(empty ? 0.f : o[3] / L);
-            const int64_t at = int64_t(t) * p.h_q + hq0 + h;
-            *reinterpret_cast<uint2*>(p.o + at * D + x) =
+            *reinterpret_cast<uint2*>(p.o + to * D + d) =
                 make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-            if (x == 0) p.lse[at] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
+            if (d == 0) p.lse[to] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
         }
     }
 }
 
+// Joins the splits' states of one (token, head), a wave; a lane has the same D / 64 dims of all.
 template <int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p) {
+    constexpr int kN = D / 64;
+    constexpr int kAhead = 8;  // states in flight
+    typedef float out_t __attribute__((ext_vector_type(kN)));
+    const int lane = threadIdx.x & 63;
+    const int64_t th = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (th >= int64_t(p.n_tokens) * p.h_q) return;
+    const int row = __builtin_amdgcn_readfirstlane(p.token_rows[th / p.h_q]);
+    if (row < 0 || row >= p.batch) return;
+    float M = -INFINITY, L = 0.f;
+    out_t O = {};
+    for (int s0 = 0; s0 < p.splits; s0 += kAhead) {
+        float m[kAhead], l[kAhead];
+        out_t o[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t at = th * p.splits + min(s0 + i, p.splits - 1);
+            m[i] = s0 + i < p.splits ? p.ws_m[at] : -INFINITY;
+            l[i] = p.ws_l[at];
+            o[i] = *reinterpret_cast<const out_t*>(p.ws_o + at * D + kN * lane);
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) top = fmaxf(top, m[i]);
+        if (top == -INFINITY) continue;  // splits without a key
+        const float f = exp2_fast(M - top);
+        M = top;
+        L *= f;
+        O *= f;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float w = exp2_fast(m[i] - M);
+            L += m[i] == -INFINITY ? 0.f : w * l[i];
+            O += m[i] == -INFINITY ? out_t{} : w * o[i];
+        }
+    }
+    const bool empty = L == 0.f;
+    if constexpr (kN == 2) {
+        bf16x2_t two;
+        two[0] = (__bf16)(empty ? 0.f : O[0] / L);
+        two[1] = (__bf16)(empty ? 0.f : O[1] / L);
+        *reinterpret_cast<uint32_t*>(p.o + th * D + 2 * lane) = __builtin_bit_cast(uint32_t, two);
+    } else {
+        p.o[th * D + lane] = __builtin_bit_cast(uint16_t, (__bf16)(empty ? 0.f : O[0] / L));
+    }
+    if (lane == 0) p.lse[th] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
+}
+
+template <int D, int NT>
 hipError_t launch_d(const AttendParams& p, hipStream_t stream) {
-    const int64_t blocks = int64_t(p.n_tokens) * p.h_kv * p.subgroups;
-    if (blocks * 256 > 0xFFFFFFFF) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<unsigned>(blocks));
-    if (p.heads_per_block > 16)
-        hipLaunchKernelGGL((attend_blocks_kernel<D, 2, 4>), grid, dim3(256), 0, stream, p);
+    const int64_t blocks = int64_t(p.n_tokens) * p.splits * p.h_kv * p.subgroups;
+    if (blocks * p.waves * 64 > 0xFFFFFFFF) return hipErrorInvalidConfiguration;
+    const dim3 grid(static_cast<unsigned>(blocks)), threads(unsigned(p.waves) * 64);
+    if (p.waves == 2)
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 2>), grid, threads, 0, stream, p);
+    else if (p.waves == 4)
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 4>), grid, threads, 0, stream, p);
     else
-        hipLaunchKernelGGL((attend_blocks_kernel<D, 1, 4>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 8>), grid, threads, 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const unsigned joins = unsigned((int64_t(p.n_tokens) * p.h_q + 3) / 4);
+    hipLaunchKernelGGL(attend_join_kernel<D>, dim3(joins), dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream) {
+    if ((p.waves != 2 && p.waves != 4 && p.waves != 8) || p.splits < 1 || p.split_tiles < 1) return hipErrorInvalidValue;
     (void)hipGetLastError();
-    return head_dim == 64 ? launch_d<64>(p, stream) : launch_d<128>(p, stream);
+    if (p.heads_per_block > 16)
+        return head_dim == 64 ? launch_d<64, 2>(p, stream) : launch_d<128, 2>(p, stream);
+    return head_dim == 64 ? launch_d<64, 1>(p, stream) : launch_d<128, 1>(p, stream);
 }
 
 }  // namespace atf
