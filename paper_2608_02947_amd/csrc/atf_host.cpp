@@ -404,16 +404,21 @@ int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room) {
     return std::max<int64_t>(1, std::min(best, room));
 }
 
-// Attention over listed blocks: workgroups of 4 waves, of 8 where that leaves more waves than run at
-// once (2 a SIMD: 2,048) short of tiles no longer; a list is split where even so waves have more than 8
-// tiles and fewer than 2,048 run.
+// Attention over listed blocks.  A workgroup has as many waves as bring those that run at once (2 a SIMD:
+// 2,048), no more than it has tiles: each state joined costs, with groups to spare more than the waves
+// gain (12,000 groups of 4 tiles, 24/8 heads of 128: 90 us with one wave, 103, 161 and 302 with 2, 4 and
+// 8; 1,024 of 512, 32/4 heads: 304 with 2, 331 and 392 with 4 and 8; 320 of 128, 24/8 heads: 136 with one,
+// 91, 87 and 92; 256 of 512, 32/4 heads: 234 with 2, 127 and 105).
+// Lists are split while there is room for their waves, a tile a wave at least, where that saves 20 tiles
+// or more of a workgroup's (fewer save less than joining the splits costs: 4 groups of 32 tiles 12.2 us whole, 9.9
+// in 4 or more; of 16 tiles 10.1 and 9.3 to 10.7; 128 of 32 tiles 9.9 whole, 10.9 in 2; 4 of 512 80.6 and 17.1).
 AttendPlan attend_plan(int64_t groups, int64_t tiles) {
-    AttendPlan a = {4, 1, int32_t(std::min<int64_t>(tiles, INT32_MAX))};
+    AttendPlan a = {1, 1, int32_t(std::min<int64_t>(tiles, INT32_MAX))};
     groups = std::max<int64_t>(groups, 1);
-    if (groups * 8 <= 2048) a.waves = 8;
-    const int64_t room = 2048 / (groups * a.waves);
-    const int64_t splits = std::min(room, tiles / (4 * a.waves));
-    if (splits > 1) {
+    const int32_t most = groups <= 256 ? 8 : groups <= 640 ? 4 : groups <= 2048 ? 2 : 1;
+    while (a.waves < most && a.waves < tiles) a.waves *= 2;
+    const int64_t splits = std::min(2048 / (groups * 8), tiles / 8);
+    if (a.waves == 8 && splits > 1 && tiles * (splits - 1) >= 20 * splits) {
         a.split_tiles = int32_t((tiles + splits - 1) / splits);
         a.splits = int32_t((tiles + a.split_tiles - 1) / a.split_tiles);
     }

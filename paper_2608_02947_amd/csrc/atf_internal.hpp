@@ -280,7 +280,7 @@ struct AttendParams {
     int32_t batch, max_pages, num_pages, page_tokens, block_tokens;
     int32_t n_tokens, max_n_k, top, h_q, h_kv, group;
     int32_t heads_per_block, subgroups;  // as DecodeQ8Params
-    int32_t waves;               // of a workgroup: 2, 4 or 8
+    int32_t waves;               // of a workgroup: 1, 2, 4 or 8
     int32_t splits, split_tiles; // workgroups of a list, 32-token tiles of each
     float* ws_m;                 // [n_tokens][h_q][splits], split lists, as the two below
     float* ws_l;

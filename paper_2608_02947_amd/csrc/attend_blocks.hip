@@ -36,6 +36,10 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
 __device__ __forceinline__ u32x4_t load16(uint64_t at) {
     return *(const __attribute__((address_space(1))) u32x4_t*)(at);
 }
+// what lanes read whose chunk no token of the tile keeps, and all after the last tile: as long as the
+// largest offset between a lane's loads
+__device__ const uint32_t g_zeros[1024] __attribute__((aligned(256))) = {};
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // halves of a register pair of bf16 numbers that bits 2t, 2t + 1 keep
@@ -126,37 +130,50 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         return true;
     };
     const int tk = 16 * (r16 >> 3) + 4 * ((r16 >> 2) & 1) + (r16 & 3);  // this lane's token of s = 0
+    const uint32_t k_lane = uint32_t(g4 >> 1) * (32 * uint32_t(p.page_tokens)) + 16 * (g4 & 1);
+    // (after the last tile zeros are read, so that the loads in flight, which the waits count, are the same
+    // on every path)
+    const uint64_t zeros = reinterpret_cast<uint64_t>(g_zeros);
     u32x4_t kf[2][kM], vf[kDB];
     uint64_t full = 0, keep = 0;
-    const auto load_k = [&](const Tile& x) __attribute__((always_inline)) {
+    const auto load_k = [&](const Tile& x, bool is) __attribute__((always_inline)) {
         const int left = min(last - x.first, kTile - 1);
         full = __ballot(my_w >= q_pos - x.first);
-        keep = __ballot(my_w >= q_pos - x.first - left);
+        keep = is ? __ballot(my_w >= q_pos - x.first - left) : 0ull;
         const int64_t ph = int64_t(x.page) * p.h_kv + g;
-        const uint64_t at = reinterpret_cast<uint64_t>(p.k_pages) + (ph * kChunks * p.page_tokens + x.at) * 32 + 16 * (g4 & 1);
+        const uint64_t at = reinterpret_cast<uint64_t>(p.k_pages) + (ph * kChunks * p.page_tokens + x.at) * 32 + k_lane;
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
-            const int c = 2 * m + (g4 >> 1);
-            if (((keep >> (8 * c)) & 0xFFull) == 0) continue;
-            const uint64_t from = at + uint64_t(uint32_t(c) * uint32_t(p.page_tokens)) * 32;
+            const bool kept = ((keep >> (8 * (2 * m + (g4 >> 1)))) & 0xFFull) != 0;
+            const uint64_t from = kept ? at + uint64_t(m) * (64 * uint32_t(p.page_tokens)) : zeros;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) kf[s][m] = load16(from + 32 * min(tk + 8 * s, left));
+            for (int s = 0; s < 2; ++s) kf[s][m] = load16(from + 32 * max(min(tk + 8 * s, left), 0));
         }
     };
-    const auto load_v = [&](const Tile& x) __attribute__((always_inline)) {
+    const auto load_v = [&](const Tile& x, bool is) __attribute__((always_inline)) {
         // (a 16-token block past the row's end is the one before it again, masked below)
         const int block = 16 <= last - x.first ? g4 >> 1 : 0;
         const uint64_t at = reinterpret_cast<uint64_t>(p.v_pages) +
                             ((int64_t(x.page) * p.h_kv + g) * p.page_tokens + x.at + 16 * block) * (2 * D) + 16 * (g4 & 1) + 32 * r16;
+        const uint64_t from = is ? at : zeros;
 #pragma unroll
-        for (int i = 0; i < kDB; ++i) vf[i] = load16(at + 512 * i);
+        for (int i = 0; i < kDB; ++i) vf[i] = load16(from + 512 * i);
+    };
+    // they have arrived
+    const auto wait_k = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < kM; ++m) asm volatile("" : "+v"(kf[0][m]), "+v"(kf[1][m]));
+    };
+    const auto wait_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kDB; ++i) asm volatile("" : "+v"(vf[i]));
     };
 
     Tile x = {0, 0, 0};
     bool have = next(x);
     if (have) {
-        load_v(x);
-        load_k(x);
+        load_v(x, true);
+        load_k(x, true);
     }
     // queries: operand (tile n, m)
     u32x4_t qf[kOps];
@@ -180,8 +197,23 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         m_neg[n] = l_run[n] = 0.f;
     }
     const float sc = p.scale_log2;
+    // masks of the pairs that are kept, and the queries so masked, of the last tile (d = 128 with two
+    // column tiles has no registers left for them)
+    constexpr bool kCached = NT == 1 || D == 64;
+    uint64_t q_keep = ~0ull;
+    [[maybe_unused]] u32x4_t masks[kM], qm[kOps];
+    if constexpr (kCached) {
+#pragma unroll
+        for (int m = 0; m < kM; ++m) masks[m] = u32x4_t{~0u, ~0u, ~0u, ~0u};
+#pragma unroll
+        for (int o = 0; o < kOps; ++o) qm[o] = qf[o];
+    }
 
+    // (nothing in flight: the loop's waits count its own loads alone)
+    wait_v();
+    wait_k();
     while (have) {
+        wait_k();
         const int left = last - x.first;  // the tile's last token that counts, if below 31
         if (keep & ~full) {
 #pragma unroll
@@ -198,18 +230,42 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                 }
             }
         }
+        // pairs kept nowhere in the tile: the queries and the keys (in lanes whose chunk was not read they
+        // are another tile's) lose them
+        if constexpr (kCached) {
+            if (keep != q_keep) {
+                q_keep = keep;
+#pragma unroll
+                for (int m = 0; m < kM; ++m) {
+                    const uint32_t bits = uint32_t(keep >> (16 * m + 8 * (g4 >> 1))) & 0xFFu;
+                    masks[m] = u32x4_t{pair_mask(bits, 0), pair_mask(bits, 1), pair_mask(bits, 2), pair_mask(bits, 3)};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) qm[kM * n + m] = qf[kM * n + m] & masks[m];
+                }
+            }
+        }
         f32x4_t sacc[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) sacc[n][0] = sacc[n][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
             const uint32_t both = uint32_t(keep >> (16 * m)) & 0xFFFFu;
-            if (both == 0xFFFFu) {
+            if (both == 0) continue;
+            if constexpr (kCached) {
+                if ((both ^ (both >> 1)) & 0x7F7Fu) {
+                    kf[0][m] &= masks[m];
+                    kf[1][m] &= masks[m];
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) sacc[n][s] = mfma16(kf[s][m], qm[kM * n + m], sacc[n][s]);
+            } else if (both == 0xFFFFu) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int s = 0; s < 2; ++s) sacc[n][s] = mfma16(kf[s][m], qf[kM * n + m], sacc[n][s]);
-            } else if (both != 0) {
+            } else {
                 const uint32_t bits = both >> (8 * (g4 >> 1));
                 const u32x4_t k0 = keep_pairs(kf[0][m], bits), k1 = keep_pairs(kf[1][m], bits);
 #pragma unroll
@@ -223,7 +279,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         // the next tile's keys, into the registers of this one's; its values follow below
         Tile y = x;
         have = next(y);
-        if (have) load_k(y);
+        load_k(y, have);
+        wait_v();
         // tokens past the row's keys: no probability, and no value that is not a number
         if (left < kTile - 1) {
             const int bound = left - 16 * (g4 >> 1) - 4 * (g4 & 1);
@@ -289,7 +346,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                 oacc[n][i] = mfma16(vf[i], ph[n], oacc[n][i]);
                 oacc[n][i] = mfma16(vf[i], pl[n], oacc[n][i]);
             }
-        if (have) load_v(y);
+        load_v(y, have);
         x = y;
     }
 
@@ -409,7 +466,9 @@ hipError_t launch_d(const AttendParams& p, hipStream_t stream) {
     const int64_t blocks = int64_t(p.n_tokens) * p.splits * p.h_kv * p.subgroups;
     if (blocks * p.waves * 64 > 0xFFFFFFFF) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), threads(unsigned(p.waves) * 64);
-    if (p.waves == 2)
+    if (p.waves == 1)
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 1>), grid, threads, 0, stream, p);
+    else if (p.waves == 2)
         hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 2>), grid, threads, 0, stream, p);
     else if (p.waves == 4)
         hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 4>), grid, threads, 0, stream, p);
@@ -425,7 +484,7 @@ hipError_t launch_d(const AttendParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream) {
-    if ((p.waves != 2 && p.waves != 4 && p.waves != 8) || p.splits < 1 || p.split_tiles < 1) return hipErrorInvalidValue;
+    if ((p.waves != 1 && p.waves != 2 && p.waves != 4 && p.waves != 8) || p.splits < 1 || p.split_tiles < 1) return hipErrorInvalidValue;
     (void)hipGetLastError();
     if (p.heads_per_block > 16)
         return head_dim == 64 ? launch_d<64, 2>(p, stream) : launch_d<128, 2>(p, stream);
