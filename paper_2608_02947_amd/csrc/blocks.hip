@@ -24,7 +24,8 @@ __device__ __forceinline__ s16x2_t ordered(uint32_t x) {
 // Lanes of equal parity then share their extremes: the smallest as the largest complement, so that
 // after the first step, which leaves one in the lower lanes and the other in the upper ones, both
 // go on together.
-// Bound by HBM reads.
+// Bound by HBM reads: 131,072 keys of 4 heads of 128 (138 MB) 26.0 us, 5.3 TB/s (a streaming read
+// reaches 5.57), 30.8 with loads that stay in the caches; 2 or 8 chunks a wave 30.6 and 31.2 against 30.8.
 constexpr int kBoundChunks = 4;
 
 template <int kCtrl>
@@ -71,8 +72,8 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
                 for (int c = 0; c < kBoundChunks; ++c)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        x[c][h] = *reinterpret_cast<const u32x4_t*>(
-                            src + (int64_t(c) * p.page_tokens + min(t0 + 32 * h + (lane >> 1), last)) * 16);
+                        x[c][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(
+                            src + (int64_t(c) * p.page_tokens + min(t0 + 32 * h + (lane >> 1), last)) * 16));
 #pragma unroll
                 for (int c = 0; c < kBoundChunks; ++c)
 #pragma unroll

@@ -95,7 +95,7 @@ class PlanState:
 @pytest.mark.parametrize("kind", ["step", "fits", "long", "short", "none", "tight", "idle"])
 @pytest.mark.parametrize("B,width,pt,T", [(1, 1, 32, 1), (1, 700, 32, 30000), (3, 5, 64, 40), (64, 9, 32, 64), (70, 20, 96, 900),
                                           (200, 30, 64, 300), (1024, 3, 32, 1500), (1025, 3, 32, 1500), (2500, 4, 64, 2600),
-                                          (24, 400, 32, 9000), (5, 3, 32, 0), (7, 40, 32, 8192), (7, 40, 32, 8193)])
+                                          (24, 400, 32, 9000), (5, 3, 32, 0), (7, 40, 32, 2048), (7, 40, 32, 2049), (7, 40, 32, 8193)])
 def test_plan(B, width, pt, T, kind):
     note(f"plan {B} {width} {pt} {T} {kind}")
     PlanState(B, width, pt, T, B + T, kind).run().check()
