@@ -432,7 +432,7 @@ __device__ __forceinline__ void write_taken(int32_t* out, int n, PickShared<kThr
     int taken = 0;
     for (int i = 0; i * kThreads < n; ++i) {
         const int j = i * kThreads + tid;
-        const bool yes = j < n && take(i, j);
+        const bool yes = j < n && take(j);
         const uint64_t m = __ballot(yes);
         if (lane == 0) s.part[i & 1][wave] = __builtin_popcountll(m);
         __syncthreads();
@@ -570,8 +570,8 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     const double error = double(size) * (0x1p-23 * (1 + 0x1p-10));
     bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
 
-    double above = INFINITY, from = INFINITY;  // blocks over `above` are taken, those from `from` on maybe
-    bool all = true;                           // the latter all are
+    int above = INT32_MAX, from = INT32_MAX;  // blocks over `above` are taken, those from `from` on maybe
+    bool all = true;                          // the latter all are
     if (want > 0 && !exact) {
         int left = want;
         int border = low;
@@ -629,15 +629,18 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
             __syncthreads();
         }
-        above = double(value_of(border)) + 2 * error;
-        from = double(value_of(border)) - 2 * error;
+        // (the numbers of fp32 next to the two limits on their inner sides)
+        const double over = double(value_of(border)) + 2 * error, under = double(value_of(border)) - 2 * error;
+        above = key_of(float(over));
+        above -= double(float(over)) > over && above != INT32_MAX;
+        from = key_of(float(under));
+        from = from == INT32_MAX ? INT32_MIN + 1 : from + (double(float(under)) < under);
         __syncthreads();
         int sure = 0;
         each([&](int j, int k) __attribute__((always_inline)) {
-            const double x = double(value_of(k));
-            if (x > above)
+            if (k > above)
                 ++sure;
-            else if (x >= from) {
+            else if (k >= from) {
                 const int i = atomicAdd(&s.listed, 1);
                 if (i < kListed) s.list[i] = j;
             }
@@ -667,28 +670,26 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         pick_exact<kThreads>(p, tok, t, g, n, want, p.exact_keys + at * p.key_stride, out, s);
         return;
     }
-    const auto take = [&](int k, int j) __attribute__((always_inline)) {
-        if (k == INT32_MIN) return true;  // (a block that is taken anyway)
-        const double x = double(value_of(k));
-        if (x > above) return true;
-        if (!(x >= from)) return false;
-        if (all) return true;
-        bool yes = false;
-        for (int i = 0; i < s.listed; ++i) yes = yes || (s.list[i] == j && s.win[i]);
-        return yes;
-    };
     if constexpr (kPer > 0) {
         // which of a thread's blocks are taken, and how many of each step of each wave
         __shared__ int s_count[kPer * kWaves];
+        uint32_t won = all ? ~0u : 0u;
+        if (!all)
+            for (int i = 0; i < s.listed; ++i) {
+                const int j = s.list[i], step = j / kThreads;
+                if (j - step * kThreads == tid && s.win[i]) won |= 1u << step;
+            }
         uint64_t m[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int j = i * kThreads + tid;
-            m[i] = __ballot(j < n && take(kept[i], j));
+            const int k = kept[i];
+            // (blocks that are taken anyway, below n, have the lowest key)
+            const bool yes = k == INT32_MIN ? i * kThreads + tid < n : k > above || (k >= from && ((won >> i) & 1u) != 0);
+            m[i] = __ballot(yes);
             if (lane == 0) s_count[i * kWaves + wave] = __builtin_popcountll(m[i]);
         }
         __syncthreads();
-        // (kPer * kWaves <= 16 * 16 numbers: each wave adds up those before its own)
+        // (each wave adds up the numbers of those before its own)
         int before = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -698,7 +699,14 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             if ((m[i] >> lane) & 1) out[mine + __builtin_popcountll(m[i] & ((1ull << lane) - 1))] = i * kThreads + tid;
         }
     } else {
-        write_taken<kThreads>(out, n, s, [&](int, int j) __attribute__((always_inline)) { return take(load(j), j); });
+        write_taken<kThreads>(out, n, s, [&](int j) __attribute__((always_inline)) {
+            const int k = load(j);
+            if (k == INT32_MIN || k > above) return true;
+            bool yes = all;
+            if (k >= from && !all)
+                for (int i = 0; i < s.listed; ++i) yes = yes || (s.list[i] == j && s.win[i]);
+            return k >= from && yes;
+        });
     }
 }
 
