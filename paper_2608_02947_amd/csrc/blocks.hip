@@ -155,7 +155,6 @@ __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t bits) {
         r[t] = x[t] & (((bits >> (2 * t)) & 1u ? 0x0000FFFFu : 0u) | ((bits >> (2 * t + 1)) & 1u ? 0xFFFF0000u : 0u));
     return r;
 }
-__device__ __forceinline__ u32x4_t magnitudes(u32x4_t x) { return x & 0x7FFF7FFFu; }
 
 // What a query token sees: its row (-1: padding), its position, and the last key that it reaches (below
 // 0: none).
@@ -252,6 +251,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         return h0 < 16 * kHeld ? s_query[(h0 / 16 * kChunks + c) * 64 + lane] : query_of(h0, c);
     };
 
+    // signs of the bounds' magnitudes: those of the queries' parts
+    const u32x4_t minus = u32x4_t{1u, 1u, 1u, 1u} * (g4 >= 2 ? 0x80008000u : 0u);
     bool todo = is && tok.row >= 0 && tok.last >= 0;
     float worst = 0.f;  // largest sum of magnitudes times its additions
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
@@ -306,14 +307,14 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                     }
                     // (a sum of its own for each chunk: fewer additions to a number)
                     sum += mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    size = mfma16(magnitudes(x), magnitudes(y), size);
+                    size = mfma16((x & 0x7FFF7FFFu) | minus, y, size);
                 }
                 for (uint64_t m = some; m != 0; m &= m - 1) {
                     const int r = __builtin_ctzll(m), w = __builtin_amdgcn_readlane(my_w, r);
                     const u32x4_t x = keep_pairs(s_tile[wave][r / 8][lane], 1u << (r % 8));
                     const u32x4_t y = keep_pairs(query(h0, r / 8), 1u << (r % 8));
                     const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    const f32x4_t v = mfma16(magnitudes(x), magnitudes(y), f32x4_t{0.f, 0.f, 0.f, 0.f});
+                    const f32x4_t v = mfma16((x & 0x7FFF7FFFu) | minus, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // (a tile past the row's end may reach past 2^31: wrapped, and not written)
@@ -408,11 +409,11 @@ __device__ __forceinline__ uint64_t exact_key(const SelectParams& p, const Token
 
 // The blocks of one token for one KV head.  kPer keys of a thread stay in registers; 0: they are read
 // again each time.
-constexpr int kBins = 2048;
-constexpr int kListed = 256;  // blocks that are ranked, or summed again, one against another
-
 template <int kThreads>
 struct PickShared {
+    static constexpr int kBits = kThreads == 64 ? 9 : 11, kBins = 1 << kBits;
+    // blocks that are ranked, or summed again, one against another
+    static constexpr int kListed = kThreads < 256 ? kThreads : 256;
     int hist[kBins];
     int part[2][kThreads / 64];
     int low[kThreads / 64], high[kThreads / 64];
@@ -511,6 +512,8 @@ __device__ __forceinline__ void pick_exact(const SelectParams& p, const Token& t
 template <int kThreads, int kPer>
 __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     constexpr int kWaves = kThreads / 64;
+    constexpr int kBits = PickShared<kThreads>::kBits, kBins = PickShared<kThreads>::kBins;
+    constexpr int kListed = PickShared<kThreads>::kListed;
     __shared__ PickShared<kThreads> s;
     __shared__ int s_scan[1][kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -577,7 +580,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         int border = low;
         for (;;) {
             const uint32_t reach = uint32_t(high) - uint32_t(low);
-            const int shift = max(0, 21 - __builtin_clz(reach | 1));  // bins are 11 bits
+            const int shift = max(0, 32 - kBits - __builtin_clz(reach | 1));
             each([&](int, int k) __attribute__((always_inline)) {
                 if (k >= low && k <= high) atomicAdd(&s.hist[(uint32_t(k) - uint32_t(low)) >> shift], 1);
             });
@@ -741,7 +744,10 @@ hipError_t launch_select_blocks(const SelectParams& all, hipStream_t stream) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const dim3 picks(unsigned(p.tokens) * unsigned(p.h_kv));
-        if (p.row_blocks <= 1024)
+        // (a wave a pick where they are many)
+        if (p.row_blocks <= 1024 && picks.x > 2048)
+            hipLaunchKernelGGL((pick_kernel<64, 16>), picks, dim3(64), 0, stream, p);
+        else if (p.row_blocks <= 1024)
             hipLaunchKernelGGL((pick_kernel<256, 4>), picks, dim3(256), 0, stream, p);
         else if (p.row_blocks <= 4096)
             hipLaunchKernelGGL((pick_kernel<256, 16>), picks, dim3(256), 0, stream, p);
