@@ -46,10 +46,6 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int t) {
     return ((bits >> (2 * t)) & 1u ? 0x0000FFFFu : 0u) | ((bits >> (2 * t + 1)) & 1u ? 0xFFFF0000u : 0u);
 }
-__device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t bits) {
-    return u32x4_t{x[0] & pair_mask(bits, 0), x[1] & pair_mask(bits, 1), x[2] & pair_mask(bits, 2),
-                   x[3] & pair_mask(bits, 3)};
-}
 
 // A lane looks up one tile of the list, 64 at a time; which of them are tokens of the row is a ballot.
 struct Tile {
@@ -175,15 +171,25 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         load_v(x, true);
         load_k(x, true);
     }
-    // queries: operand (tile n, m)
-    u32x4_t qf[kOps];
-#pragma unroll
-    for (int o = 0; o < kOps; ++o) {
+    // queries: operand (tile n, m).  d = 128 with two column tiles has no registers for them, nor for the
+    // masks below: they are in LDS then.
+    constexpr bool kCached = NT == 1 || D == 64;
+    const auto query_of = [&](int o) __attribute__((always_inline)) {
         const int h = 16 * (o / kM) + r16, m = o % kM;
-        qf[o] = u32x4_t{0u, 0u, 0u, 0u};
+        u32x4_t q = {0u, 0u, 0u, 0u};
         if (h < NH)
-            qf[o] = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(t) * p.h_q + hq0 + h) * D + (g4 & 1) * kHalf +
-                                                      8 * (2 * m + (g4 >> 1)));
+            q = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(t) * p.h_q + hq0 + h) * D + (g4 & 1) * kHalf +
+                                                  8 * (2 * m + (g4 >> 1)));
+        return q;
+    };
+    [[maybe_unused]] u32x4_t qf[kCached ? kOps : 1];
+    [[maybe_unused]] u32x4_t* const s_q = reinterpret_cast<u32x4_t*>(s_o) + lane;
+    if constexpr (kCached) {
+#pragma unroll
+        for (int o = 0; o < kOps; ++o) qf[o] = query_of(o);
+    } else {
+        static_assert(NW * 16 * kOStride * 4 >= kOps * 64 * 16, "the states' room holds the queries");
+        for (int o = wave; o < kOps; o += NW) s_q[64 * o] = query_of(o);
     }
     __syncthreads();
 
@@ -197,11 +203,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         m_neg[n] = l_run[n] = 0.f;
     }
     const float sc = p.scale_log2;
-    // masks of the pairs that are kept, and the queries so masked, of the last tile (d = 128 with two
-    // column tiles has no registers left for them)
-    constexpr bool kCached = NT == 1 || D == 64;
+    // masks of the pairs that are kept, and the queries so masked, of the last tile
     uint64_t q_keep = ~0ull;
-    [[maybe_unused]] u32x4_t masks[kM], qm[kOps];
+    [[maybe_unused]] u32x4_t masks[kCached ? kM : 1], qm[kCached ? kOps : 1];
     if constexpr (kCached) {
 #pragma unroll
         for (int m = 0; m < kM; ++m) masks[m] = u32x4_t{~0u, ~0u, ~0u, ~0u};
@@ -260,19 +264,19 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int s = 0; s < 2; ++s) sacc[n][s] = mfma16(kf[s][m], qm[kM * n + m], sacc[n][s]);
-            } else if (both == 0xFFFFu) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) sacc[n][s] = mfma16(kf[s][m], qf[kM * n + m], sacc[n][s]);
             } else {
-                const uint32_t bits = both >> (8 * (g4 >> 1));
-                const u32x4_t k0 = keep_pairs(kf[0][m], bits), k1 = keep_pairs(kf[1][m], bits);
+                u32x4_t mask = {~0u, ~0u, ~0u, ~0u};
+                if (both != 0xFFFFu) {
+                    const uint32_t bits = both >> (8 * (g4 >> 1));
+                    mask = u32x4_t{pair_mask(bits, 0), pair_mask(bits, 1), pair_mask(bits, 2), pair_mask(bits, 3)};
+                    kf[0][m] &= mask;
+                    kf[1][m] &= mask;
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const u32x4_t q = keep_pairs(qf[kM * n + m], bits);
-                    sacc[n][0] = mfma16(k0, q, sacc[n][0]);
-                    sacc[n][1] = mfma16(k1, q, sacc[n][1]);
+                    const u32x4_t q = s_q[64 * (kM * n + m)] & mask;
+                    sacc[n][0] = mfma16(kf[0][m], q, sacc[n][0]);
+                    sacc[n][1] = mfma16(kf[1][m], q, sacc[n][1]);
                 }
             }
         }
@@ -280,26 +284,17 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         Tile y = x;
         have = next(y);
         load_k(y, have);
-        wait_v();
-        // tokens past the row's keys: no probability, and no value that is not a number
+        // tokens past the row's keys: no probability, and (below) no value that is not a number
+        const int bound = left - 16 * (g4 >> 1) - 4 * (g4 & 1);
         if (left < kTile - 1) {
-            const int bound = left - 16 * (g4 >> 1) - 4 * (g4 & 1);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const bool out = 8 * s + v > bound;
+                for (int v = 0; v < 4; ++v)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        if (out) sacc[n][s][v] = -INFINITY;
-                    // element 4 s + v of the lane's 8 values
-#pragma unroll
-                    for (int i = 0; i < kDB; ++i) vf[i][2 * s + v / 2] &= !out ? ~0u : v & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                }
+                        if (8 * s + v > bound) sacc[n][s][v] = -INFINITY;
         }
-        // P as two bf16 numbers, what fits and what is left over: one would round every probability to
-        // 2^-9, and the output's own rounding is that size
-        u32x4_t ph[NT], pl[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float mx = -INFINITY;
@@ -322,6 +317,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
 #pragma unroll
                     for (int v = 0; v < 4; ++v) oacc[n][i][v] *= alpha;
             }
+            // P as two bf16 numbers, what fits and what is left over: one would round every probability
+            // to 2^-9, and the output's own rounding is that size
+            u32x4_t ph, pl;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -335,17 +333,27 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                         h[e] = __float_as_uint(w) & 0xFFFF0000u;
                         rest[e] = (__bf16)(w - __uint_as_float(h[e]));
                     }
-                    ph[n][2 * s + k] = h[0] >> 16 | h[1];
-                    pl[n][2 * s + k] = __builtin_bit_cast(uint32_t, rest);
+                    ph[2 * s + k] = h[0] >> 16 | h[1];
+                    pl[2 * s + k] = __builtin_bit_cast(uint32_t, rest);
                 }
-        }
+            if (n == 0) {
+                wait_v();
+                if (left < kTile - 1) {
+                    // (value 4 s + v of the lane's 8)
 #pragma unroll
-        for (int i = 0; i < kDB; ++i)
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t msk = 8 * (e / 4) + e % 4 <= bound ? ~0u : e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                oacc[n][i] = mfma16(vf[i], ph[n], oacc[n][i]);
-                oacc[n][i] = mfma16(vf[i], pl[n], oacc[n][i]);
+                        for (int i = 0; i < kDB; ++i) vf[i][e / 2] &= msk;
+                    }
+                }
             }
+#pragma unroll
+            for (int i = 0; i < kDB; ++i) {
+                oacc[n][i] = mfma16(vf[i], ph, oacc[n][i]);
+                oacc[n][i] = mfma16(vf[i], pl, oacc[n][i]);
+            }
+        }
         load_v(y, have);
         x = y;
     }

@@ -219,7 +219,7 @@ constexpr int kHeld = 4;
 template <int D>
 __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     constexpr int kChunks = D / 16, kHalf = D / 2;
-    __shared__ u32x4_t s_tile[4][kChunks][64];
+    __shared__ u32x4_t s_masks[256];  // keep_pairs' of each set of pairs
     extern __shared__ u32x4_t s_query[];  // [held][kChunks][64]
     const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -244,6 +244,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         return x;
     };
     const int held = min((G + 15) / 16, kHeld);
+    s_masks[threadIdx.x] = keep_pairs(u32x4_t{~0u, ~0u, ~0u, ~0u}, threadIdx.x);
     for (int o = wave; o < held * kChunks; o += 4) s_query[64 * o + lane] = query_of(16 * (o / kChunks), o % kChunks);
     __syncthreads();
     if (range >= p.ranges) return;
@@ -275,35 +276,41 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
             const int last = min(last_key, min(16 * tile + 15, n - 1) * p.block_tokens + (p.block_tokens - 1));
             return __ballot(my_w >= max(0, first_pos - last));
         };
-        u32x4_t a[kChunks];
+        // (one vector, for an index that is not known when this is compiled)
+        typedef uint32_t tile_t __attribute__((ext_vector_type(4 * kChunks)));
+        tile_t a = {};
+        const auto chunk = [&](int c) __attribute__((always_inline)) {
+            return u32x4_t{a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]};
+        };
         const auto load = [&](const uint16_t* src, uint64_t keep) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < kChunks; ++c)
-                if ((keep >> (8 * c)) & 0xFFull) a[c] = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
+                if ((keep >> (8 * c)) & 0xFFull) {
+                    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[4 * c + e] = x[e];
+                }
         };
         uint64_t keep = keep_of(range);
         load(where(range), keep);
         const uint16_t* next = where(min(range + p.ranges, tiles - 1));
         for (int tile = range; tile < tiles; tile += p.ranges) {
             const int j0 = 16 * tile;
-            const uint64_t full = __ballot(my_w >= last_pos - j0 * p.block_tokens);
+            uint64_t full = __ballot(my_w >= last_pos - j0 * p.block_tokens);
             const uint64_t some = keep & ~full;  // pairs whose windows end in the tile
-            if (some != 0) {
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) s_tile[wave][c][lane] = a[c];
-            }
             int best[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
             for (int h0 = 0; h0 < G; h0 += 16) {
                 const bool live = mine && h0 + h < G;
+                asm volatile("" : "+s"(full));  // (its chunks' parts are not kept from one time to the next)
                 f32x4_t sum = {0.f, 0.f, 0.f, 0.f}, size = sum;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     const uint32_t whole = uint32_t(full >> (8 * c)) & 0xFFu;
                     if (whole == 0) continue;
-                    u32x4_t x = a[c], y = query(h0, c);
+                    u32x4_t x = chunk(c), y = query(h0, c);
                     if (whole != 0xFFu) {
-                        x = keep_pairs(x, whole);
-                        y = keep_pairs(y, whole);
+                        x &= s_masks[whole];
+                        y &= s_masks[whole];
                     }
                     // (a sum of its own for each chunk: fewer additions to a number)
                     sum += mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
@@ -311,8 +318,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 }
                 for (uint64_t m = some; m != 0; m &= m - 1) {
                     const int r = __builtin_ctzll(m), w = __builtin_amdgcn_readlane(my_w, r);
-                    const u32x4_t x = keep_pairs(s_tile[wave][r / 8][lane], 1u << (r % 8));
-                    const u32x4_t y = keep_pairs(query(h0, r / 8), 1u << (r % 8));
+                    const u32x4_t mask = s_masks[1u << (r % 8)];
+                    const u32x4_t x = chunk(r / 8) & mask, y = query(h0, r / 8) & mask;
                     const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
                     const f32x4_t v = mfma16((x & 0x7FFF7FFFu) | minus, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
@@ -539,8 +546,10 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     const auto each = [&](auto body) __attribute__((always_inline)) {
         if constexpr (kPer > 0) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
+            for (int i = 0; i < kPer; ++i) {
+                asm volatile("" : "+v"(kept[i]));  // (its comparisons are not kept from one time to the next)
                 if (kept[i] != INT32_MIN) body(i * kThreads + tid, kept[i]);
+            }
         } else {
             for (int j = tid; j < n; j += kThreads) {
                 const int k = load(j);
@@ -682,14 +691,15 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
                 const int j = s.list[i], step = j / kThreads;
                 if (j - step * kThreads == tid && s.win[i]) won |= 1u << step;
             }
-        uint64_t m[kPer];
+        uint32_t taken = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int k = kept[i];
             // (blocks that are taken anyway, below n, have the lowest key)
             const bool yes = k == INT32_MIN ? i * kThreads + tid < n : k > above || (k >= from && ((won >> i) & 1u) != 0);
-            m[i] = __ballot(yes);
-            if (lane == 0) s_count[i * kWaves + wave] = __builtin_popcountll(m[i]);
+            taken |= uint32_t(yes) << i;
+            const uint64_t m = __ballot(yes);
+            if (lane == 0) s_count[i * kWaves + wave] = __builtin_popcountll(m);
         }
         __syncthreads();
         // (each wave adds up the numbers of those before its own)
@@ -699,7 +709,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             const int c = scan::row16(s_count[i * kWaves + min(lane & 15, kWaves - 1)]);
             const int mine = before + (wave > 0 ? scan::lane_of(c, wave - 1) : 0);
             before += scan::lane_of(c, kWaves - 1);
-            if ((m[i] >> lane) & 1) out[mine + __builtin_popcountll(m[i] & ((1ull << lane) - 1))] = i * kThreads + tid;
+            const bool yes = ((taken >> i) & 1u) != 0;
+            const uint64_t m = __ballot(yes);
+            if (yes) out[mine + __builtin_popcountll(m & ((1ull << lane) - 1))] = i * kThreads + tid;
         }
     } else {
         write_taken<kThreads>(out, n, s, [&](int j) __attribute__((always_inline)) {

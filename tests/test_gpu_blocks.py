@@ -374,6 +374,42 @@ def test_select_many_tokens():
     check_select(tok, q, random_bounds(tok.P, pt, bt, h_kv, d, 2), bt, win, W, 3, 1, 1)
 
 
+@pytest.mark.parametrize("what", ["random", "zeros", "NaN"])
+@pytest.mark.parametrize("queries", [(1, 1), (140, 80)])
+def test_select_many_picks(what, queries):
+    """More than 2,048 (token, KV head)s, and few, at the same sizes: alike, and the plain form's."""
+    note(f"select picks {what} {queries}")
+    d, h, pt, bt = 64, 16, 64, 32
+    win, W = windows(d, "exact")
+    tok = Tokens([180, 130], queries, pt, 3)
+    q = torch.randn((tok.T, h, d), generator=torch.Generator().manual_seed(1)).to(BF)
+    b = random_bounds(tok.P, pt, bt, h, d, 2)
+    if what == "zeros":
+        b.zero_()
+    elif what == "NaN":
+        b.view(-1)[torch.arange(0, b.numel(), 4001)] = math.nan
+    check_select(tok, q, b, bt, win, W, 3, 0, 1)
+
+
+def test_select_many_equal_blocks_of_many_tokens():
+    """More blocks at the border than are listed (64 where a wave picks, else 256), nearly all alike."""
+    note("select equal, many")
+    d, h, pt, bt = 64, 16, 32, 32
+    win, W = windows(d, "off")
+    for queries, n in (((130, 3), 4000), ((1, 1), 12000)):
+        tok = Tokens([n, 90], queries, pt, 3)
+        q = torch.randint(-1, 2, (tok.T, h, d), generator=torch.Generator().manual_seed(1)).to(BF)
+        b = torch.ones(random_bounds(tok.P, pt, bt, h, d, 2).shape, dtype=BF)
+        b[::7] = 2.0
+        got = selected(tok, q.to(DEV), b.to(DEV), bt, win, 30, 1, 1).cpu().numpy()
+        # one token's in the plain form; the others choose by their own queries, two of them checked
+        for t in {0, min(5, tok.T - 3), tok.T - 3}:
+            one = np.full((1,) + got.shape[1:], 777)
+            R.select(q[t:t + 1].double().numpy(), b.double().numpy(), tok.table, tok.rows[t:t + 1], tok.pos[t:t + 1],
+                     tok.lens, n, W, pt, bt, 30, 1, 1, one)
+            assert np.array_equal(got[t], one[0])
+
+
 @pytest.mark.parametrize("what", ["zeros", "equal", "shared", "integers", "close"])
 def test_select_ties_go_to_the_lower_block(what):
     note(f"select ties {what}")
@@ -414,6 +450,19 @@ def test_select_numbers_that_are_none(kind):
         b = random_bounds(tok.P, pt, bt, h_kv, d, 7)
         b.view(-1)[torch.tensor(rng.integers(0, b.numel(), count))] = x
         check_select(tok, q, b, bt, win, W, top, 1, 1)
+
+
+def test_select_tiny_and_huge_numbers():
+    """Denormal bounds beside queries that bring their products to size, and sums past fp32."""
+    note("select tiny and huge")
+    d, h_q, h_kv, pt, bt = 64, 4, 2, 32, 32
+    win, W = windows(d, "off")
+    tok = Tokens([640, 333], [2, 1], pt, 4)
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn((tok.T, h_q, d), generator=g)
+    b = random_bounds(tok.P, pt, bt, h_kv, d, 5).float()
+    for x, y in ((2.0 ** 100, 2.0 ** -129), (2.0 ** 60, 2.0 ** 70), (2.0 ** 120, 2.0 ** -131), (2.0 ** -126, 2.0 ** 3)):
+        check_select(tok, (q * x).to(BF), (b * y).to(BF), bt, win, W, 6, 1, 1)
 
 
 def test_select_of_entries_out_of_range():
@@ -475,7 +524,7 @@ def check_attend(tok, q, kp, vp, lists, bt, win, W, scale=0.0):
     empty = np.isneginf(wl)
     assert np.array_equal(np.isneginf(lse), empty)
     tol_l = e + n * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(np.where(empty, 0, wl)))
-    assert (np.abs(lse - wl)[~empty] <= tol_l[~empty]).all()
+    assert (np.abs(lse[~empty] - wl[~empty]) <= tol_l[~empty]).all()
     return o, lse
 
 
@@ -519,10 +568,12 @@ def test_attend(d, h_q, h_kv, pt, bt, top, kind):
         check_attend(tok, q, kp, vp, random_lists(tok, h_kv, top, bt, seed), bt, win, W, 0.0 if seed != 1 else 0.3)
 
 
-@pytest.mark.parametrize("n,top,tokens", [(40000, 300, 1), (9000, 4096, 1), (5000, 60, 2), (3000, 40, 70)])
-def test_attend_long_lists(n, top, tokens):
-    note(f"attend long {n} {top} {tokens}")
-    d, h_q, h_kv, pt, bt = 64, 7, 1, 64, 32
+@pytest.mark.parametrize("n,top,tokens,d,h_q", [(40000, 300, 1, 64, 7), (9000, 4096, 1, 64, 7), (5000, 60, 2, 64, 7), (3000, 40, 70, 64, 7),
+                                                (20000, 200, 1, 128, 3), (6000, 100, 1, 128, 24), (6000, 100, 3, 64, 40),
+                                                (700, 9, 300, 64, 20), (700, 9, 300, 128, 20), (700, 9, 300, 128, 3)])
+def test_attend_long_lists(n, top, tokens, d, h_q):
+    note(f"attend long {n} {top} {tokens} {d} {h_q}")
+    h_kv, pt, bt = 1, 64, 32
     win, W = windows(d, "exact")
     tok = Tokens([n, n // 2], [tokens, 1], pt, n)
     q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(n)).to(BF)
@@ -530,9 +581,11 @@ def test_attend_long_lists(n, top, tokens):
     check_attend(tok, q, kp, vp, random_lists(tok, h_kv, top, bt, n, wild=False), bt, win, W)
 
 
-def test_attend_many_heads_and_tokens():
-    note("attend many")
-    d, h_q, h_kv, pt, bt, top = 64, 16, 16, 32, 32, 2
+@pytest.mark.parametrize("d,h_q,h_kv", [(64, 16, 16), (128, 16, 16), (64, 17 * 5, 5), (128, 20 * 12, 12)])
+def test_attend_many_heads_and_tokens(d, h_q, h_kv):
+    """Workgroups of one wave, or two."""
+    note(f"attend many {d} {h_q}/{h_kv}")
+    pt, bt, top = 32, 32, 2
     win, W = windows(d, "exact")
     tok = Tokens([150, 90], [120, 90], pt, 3)
     q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(3)).to(BF)
