@@ -646,7 +646,7 @@ int atf_cache_append_slots_rotated(const void *k_new, const void *v_new, void *k
  *           16 largest, then the 16 smallest, dims as in the K cache    (device, written)
  * Table entries are clamped to [0, num_pages).  Blocks that a call writes must be one row's.
  * Errors: ATF_EINVAL (NULL or misaligned pointer, bounds that overlap an input, batch < 1, h_kv < 1,
- * max_new < 0, more than 2^30 blocks times h_kv in a row's pages, bad page or block arguments);
+ * max_new < 0, more than 2^29 blocks times h_kv in a row's pages, bad page or block arguments);
  * ATF_EUNSUPPORTED (d not 64 or 128); ATF_EHIP. */
 int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_table,
                      int32_t max_pages_per_row, int32_t num_pages, int32_t page_tokens,
@@ -700,7 +700,8 @@ int atf_select_blocks(const void *q, const void *bounds, int32_t *blocks, int64_
  * window such a number does not count.  softmax_scale <= 0 selects 1/sqrt(d).  Any group size is
  * built: up to 32 query heads of a KV head share a workgroup.  Table entries are clamped to [0, num_pages).
  * n_tokens == 0 is a no-op.  Deterministic.
- * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite. */
+ * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite or top_blocks *
+ * block_tokens above 2^31 - 1. */
 size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int32_t top_blocks,
                                   int32_t block_tokens, int32_t head_dim);
 int atf_attend_blocks(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,

@@ -1830,8 +1830,8 @@ int atf_block_bounds(const void* k_pages, void* bounds, const int32_t* block_tab
     if (rc != ATF_OK) return rc;
     if (batch < 1 || h_kv < 1 || max_new < 0)
         return fail(ATF_EINVAL, "%s: need batch >= 1, h_kv >= 1, max_new >= 0", fn);
-    if (cap / block_tokens > (int64_t(1) << 30) / h_kv)
-        return fail(ATF_EINVAL, "%s: more than 2^30 blocks times h_kv in a row's pages", fn);
+    if (cap / block_tokens > (int64_t(1) << 29) / h_kv)
+        return fail(ATF_EINVAL, "%s: more than 2^29 blocks times h_kv in a row's pages", fn);
     if (!k_pages || !bounds || !n_k_rows || !n_new_rows) return fail(ATF_EINVAL, "%s: NULL pointer", fn);
     if (!aligned(k_pages, 16) || !aligned(bounds, 16) || !aligned(n_k_rows, 4) || !aligned(n_new_rows, 4))
         return fail(ATF_EINVAL, "%s: tensors must be 16-byte, row arrays 4-byte aligned", fn);
@@ -1961,7 +1961,7 @@ size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, i
                                   int32_t block_tokens, int32_t head_dim) {
     if (n_tokens < 0 || h_q < 1 || h_kv < 1 || h_q % h_kv || top_blocks < 1 || top_blocks > atf::kMaxTopBlocks ||
         block_tokens < 32 || block_tokens % 32 != 0 || (head_dim != 64 && head_dim != 128) ||
-        n_tokens > atf::kMaxTokenHeads / h_q)
+        n_tokens > atf::kMaxTokenHeads / h_q || int64_t(top_blocks) * block_tokens > kPosLimit)
         return 0;
     const int32_t group = h_q / h_kv, subgroups = (group + 31) / 32;
     const atf::AttendPlan plan = atf::attend_plan(n_tokens * h_kv * subgroups, int64_t(top_blocks) * (block_tokens / 32));
@@ -1987,6 +1987,8 @@ int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, v
     if (rc != ATF_OK) return rc;
     if (top_blocks < 1 || top_blocks > atf::kMaxTopBlocks)
         return fail(ATF_EINVAL, "%s: need 1 <= top_blocks <= %d", fn, atf::kMaxTopBlocks);
+    if (int64_t(top_blocks) * block_tokens > kPosLimit)
+        return fail(ATF_EINVAL, "%s: top_blocks * block_tokens above 2^31 - 1", fn);
     if (!std::isfinite(softmax_scale)) return fail(ATF_EINVAL, "%s: softmax_scale must be finite", fn);
     atf::WindowTable win;
     rc = build_table(w, &win);

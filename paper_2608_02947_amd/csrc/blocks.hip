@@ -435,7 +435,7 @@ struct PickShared {
 
 // Blocks j where take(j), in order, behind each other: a step of kThreads blocks at a time.
 template <int kThreads, typename Take>
-__device__ __forceinline__ void write_taken(int32_t* out, int n, PickShared<kThreads>& s, Take take) {
+__device__ __forceinline__ void write_taken(int32_t* out, int top, int n, PickShared<kThreads>& s, Take take) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int taken = 0;
     for (int i = 0; i * kThreads < n; ++i) {
@@ -450,7 +450,7 @@ __device__ __forceinline__ void write_taken(int32_t* out, int n, PickShared<kThr
             at += w < wave ? s.part[i & 1][w] : 0;
             taken += s.part[i & 1][w];
         }
-        if (yes) out[at] = j;
+        if (yes && at < top) out[at] = j;
     }
 }
 
@@ -511,7 +511,7 @@ __device__ __forceinline__ void pick_exact(const SelectParams& p, const Token& t
             at += w < wave ? s.part[1][w] : 0;
             taken += s.part[1][w];
         }
-        if (yes) out[at] = j;
+        if (yes && at < p.top) out[at] = j;
         __syncthreads();
     }
 }
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
 
     int above = INT32_MAX, from = INT32_MAX;  // blocks over `above` are taken, those from `from` on maybe
-    bool all = true;                          // the latter all are
+    bool all = want > 0;                      // the latter all are
     if (want > 0 && !exact) {
         int left = want;
         int border = low;
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         // which of a thread's blocks are taken, and how many of each step of each wave
         __shared__ int s_count[kPer * kWaves];
         uint32_t won = all ? ~0u : 0u;
-        if (!all)
+        if (!all && want > 0)
             for (int i = 0; i < s.listed; ++i) {
                 const int j = s.list[i], step = j / kThreads;
                 if (j - step * kThreads == tid && s.win[i]) won |= 1u << step;
@@ -711,14 +711,15 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             before += scan::lane_of(c, kWaves - 1);
             const bool yes = ((taken >> i) & 1u) != 0;
             const uint64_t m = __ballot(yes);
-            if (yes) out[mine + __builtin_popcountll(m & ((1ull << lane) - 1))] = i * kThreads + tid;
+            const int to = mine + __builtin_popcountll(m & ((1ull << lane) - 1));
+            if (yes && to < p.top) out[to] = i * kThreads + tid;
         }
     } else {
-        write_taken<kThreads>(out, n, s, [&](int j) __attribute__((always_inline)) {
+        write_taken<kThreads>(out, p.top, n, s, [&](int j) __attribute__((always_inline)) {
             const int k = load(j);
             if (k == INT32_MIN || k > above) return true;
             bool yes = all;
-            if (k >= from && !all)
+            if (k >= from && !all && want > 0)
                 for (int i = 0; i < s.listed; ++i) yes = yes || (s.list[i] == j && s.win[i]);
             return k >= from && yes;
         });

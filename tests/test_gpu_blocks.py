@@ -452,6 +452,25 @@ def test_select_numbers_that_are_none(kind):
         check_select(tok, q, b, bt, win, W, top, 1, 1)
 
 
+@pytest.mark.parametrize("n,queries", [(640, (2, 1)), (640, (130, 9)), (9000, (1, 1)), (40000, (1, 1)), (600000, (1, 1))])
+def test_select_only_what_is_taken_anyway(n, queries):
+    """first_blocks + last_blocks = top_blocks: no other block, though some have scores that are none; the lists
+    behind each other, so that one too long would show in the next."""
+    note(f"select forced {n} {queries}")
+    d, h, pt, bt = 64, 16, 64, 32
+    win, W = windows(d, "off")
+    tok = Tokens([n, 333], queries, pt, 4)
+    q = torch.randn((tok.T, h, d), generator=torch.Generator().manual_seed(6)).to(BF)
+    b = torch.full(random_bounds(1, pt, bt, h, d, 5).shape, math.nan, dtype=BF).expand(tok.P, -1, -1, -1, -1, -1)
+    got = selected(tok, q.to(DEV), b.to(DEV).contiguous(), bt, win, 5, 3, 2).cpu().numpy()
+    for t in range(tok.T - 2):
+        last = tok.pos[t] // bt
+        want = list(range(min(3, last + 1))) + list(range(max(3, last - 1), last + 1))
+        want = sorted(set(want)) if last >= 5 else list(range(last + 1))
+        assert (got[t] == np.array(want + [-1] * (5 - len(want)))).all(), t
+    assert (got[tok.T - 2:] == 777).all()
+
+
 def test_select_tiny_and_huge_numbers():
     """Denormal bounds beside queries that bring their products to size, and sums past fp32."""
     note("select tiny and huge")
