@@ -701,7 +701,7 @@ int atf_select_blocks(const void *q, const void *bounds, int32_t *blocks, int64_
  * built: up to 32 query heads of a KV head share a workgroup.  Table entries are clamped to [0, num_pages).
  * n_tokens == 0 is a no-op.  Deterministic.
  * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite or top_blocks *
- * block_tokens above 2^31 - 1. */
+ * block_tokens above 2^31 - 1, and ATF_EUNSUPPORTED for page_tokens above 2^26. */
 size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int32_t top_blocks,
                                   int32_t block_tokens, int32_t head_dim);
 int atf_attend_blocks(const void *q, const void *k_pages, const void *v_pages, void *o, float *lse,

@@ -1987,6 +1987,8 @@ int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, v
     if (rc != ATF_OK) return rc;
     if (top_blocks < 1 || top_blocks > atf::kMaxTopBlocks)
         return fail(ATF_EINVAL, "%s: need 1 <= top_blocks <= %d", fn, atf::kMaxTopBlocks);
+    if (page_tokens > 1 << 26)  // (a lane's offset within a chunk pair's tokens has 32 bits)
+        return fail(ATF_EUNSUPPORTED, "%s: pages of more than 2^26 tokens are not built", fn);
     if (int64_t(top_blocks) * block_tokens > kPosLimit)
         return fail(ATF_EINVAL, "%s: top_blocks * block_tokens above 2^31 - 1", fn);
     if (!std::isfinite(softmax_scale)) return fail(ATF_EINVAL, "%s: softmax_scale must be finite", fn);

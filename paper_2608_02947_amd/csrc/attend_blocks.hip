@@ -33,12 +33,12 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                    __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ u32x4_t load16(uint64_t at) {
-    return *(const __attribute__((address_space(1))) u32x4_t*)(at);
+// 16 bytes a lane at base + off (base wave-uniform), or zeros, nothing read, where off is kOutOfRange
+constexpr uint32_t kOutOfRange = 0xFFFFFFFFu;
+__device__ __forceinline__ u32x4_t load16(const char* base, uint32_t off, int more) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, int(0xFFFFFFF0u), 0x00020000);
+    return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, int(off), more, 0));
 }
-// what lanes read whose chunk no token of the tile keeps, and all after the last tile: as long as the
-// largest offset between a lane's loads
-__device__ const uint32_t g_zeros[1024] __attribute__((aligned(256))) = {};
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -53,7 +53,7 @@ struct Tile {
     int first;     // that token's position
 };
 
-template <int D, int NT, int NW>
+template <int D, int NT, int NW, bool kHalves>
 __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendParams p) {
     constexpr int kChunks = D / 16;
     constexpr int kHalf = D / 2;
@@ -61,9 +61,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
     constexpr int kDB = D / 16;  // 16-dim blocks of the output
     constexpr int kOps = kM * NT;
     constexpr int kOStride = D + 4;
+    static_assert(!kHalves || NT == 1, "8 heads are half of a tile's columns");
     __shared__ float red_m[NW][16 * NT];
     __shared__ float red_l[NW][16 * NT];
     __shared__ int s_w[kHalf];
+    __shared__ u32x4_t s_masks[256];  // of each set of a chunk's pairs
     __shared__ __attribute__((aligned(16))) float s_o[NW * 16 * kOStride];
 
     const int tid = threadIdx.x;
@@ -71,6 +73,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15;
     const int g4 = lane >> 4;
+    const bool rests = kHalves && r16 >= 8;  // the column has what is left over of its head's probabilities
     const int cols = p.h_kv * p.subgroups;
     const int item = int(blockIdx.x) / cols;
     const int col = int(blockIdx.x) - item * cols;
@@ -87,6 +90,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
 
     const int my_w = lane < kHalf ? p.W[lane] : -1;
     if (tid < kHalf) s_w[tid] = my_w;
+    for (int e = tid; e < 256; e += NW * 64)
+        s_masks[e] = u32x4_t{pair_mask(e, 0), pair_mask(e, 1), pair_mask(e, 2), pair_mask(e, 3)};
 
     // this wave's tiles of the split: every NW-th
     const int per = p.block_tokens / kTile;
@@ -126,34 +131,35 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         return true;
     };
     const int tk = 16 * (r16 >> 3) + 4 * ((r16 >> 2) & 1) + (r16 & 3);  // this lane's token of s = 0
+    // (after the last tile nothing is read, but all loads are issued: those in flight, which the waits
+    // count, are the same on every path)
     const uint32_t k_lane = uint32_t(g4 >> 1) * (32 * uint32_t(p.page_tokens)) + 16 * (g4 & 1);
-    // (after the last tile zeros are read, so that the loads in flight, which the waits count, are the same
-    // on every path)
-    const uint64_t zeros = reinterpret_cast<uint64_t>(g_zeros);
+    const uint32_t v_lane = 16 * (g4 & 1) + 32 * r16;
     u32x4_t kf[2][kM], vf[kDB];
     uint64_t full = 0, keep = 0;
     const auto load_k = [&](const Tile& x, bool is) __attribute__((always_inline)) {
-        const int left = min(last - x.first, kTile - 1);
+        const int left = max(min(last - x.first, kTile - 1), 0);
         full = __ballot(my_w >= q_pos - x.first);
         keep = is ? __ballot(my_w >= q_pos - x.first - left) : 0ull;
         const int64_t ph = int64_t(x.page) * p.h_kv + g;
-        const uint64_t at = reinterpret_cast<uint64_t>(p.k_pages) + (ph * kChunks * p.page_tokens + x.at) * 32 + k_lane;
+        const char* base = reinterpret_cast<const char*>(p.k_pages) + (ph * kChunks * p.page_tokens + x.at) * 32;
+        const uint32_t t0 = k_lane + 32 * min(tk, left), t1 = k_lane + 32 * min(tk + 8, left);
+        const uint64_t mine = keep >> (8 * (g4 >> 1));  // of this lane's chunk of each two
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
-            const bool kept = ((keep >> (8 * (2 * m + (g4 >> 1)))) & 0xFFull) != 0;
-            const uint64_t from = kept ? at + uint64_t(m) * (64 * uint32_t(p.page_tokens)) : zeros;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) kf[s][m] = load16(from + 32 * max(min(tk + 8 * s, left), 0));
+            const bool kept = (uint32_t(mine >> (16 * m)) & 0xFFu) != 0;
+            const char* from = base + int64_t(m) * (64 * int64_t(p.page_tokens));
+            kf[0][m] = load16(from, kept ? t0 : kOutOfRange, 0);
+            kf[1][m] = load16(from, kept ? t1 : kOutOfRange, 0);
         }
     };
     const auto load_v = [&](const Tile& x, bool is) __attribute__((always_inline)) {
-        // (a 16-token block past the row's end is the one before it again, masked below)
-        const int block = 16 <= last - x.first ? g4 >> 1 : 0;
-        const uint64_t at = reinterpret_cast<uint64_t>(p.v_pages) +
-                            ((int64_t(x.page) * p.h_kv + g) * p.page_tokens + x.at + 16 * block) * (2 * D) + 16 * (g4 & 1) + 32 * r16;
-        const uint64_t from = is ? at : zeros;
+        const char* base = reinterpret_cast<const char*>(p.v_pages) +
+                           ((int64_t(x.page) * p.h_kv + g) * p.page_tokens + x.at) * (2 * D);
+        // (a 16-token block past the row's end is not read)
+        const uint32_t off = is && 16 * (g4 >> 1) <= last - x.first ? v_lane + (g4 >> 1) * (32 * D) : kOutOfRange;
 #pragma unroll
-        for (int i = 0; i < kDB; ++i) vf[i] = load16(from + 512 * i);
+        for (int i = 0; i < kDB; ++i) vf[i] = load16(base + 512 * i, off, 0);
     };
     // they have arrived
     const auto wait_k = [&]() __attribute__((always_inline)) {
@@ -175,7 +181,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
     // masks below: they are in LDS then.
     constexpr bool kCached = NT == 1 || D == 64;
     const auto query_of = [&](int o) __attribute__((always_inline)) {
-        const int h = 16 * (o / kM) + r16, m = o % kM;
+        const int h = 16 * (o / kM) + (kHalves ? r16 & 7 : r16), m = o % kM;
         u32x4_t q = {0u, 0u, 0u, 0u};
         if (h < NH)
             q = *reinterpret_cast<const u32x4_t*>(p.q + (int64_t(t) * p.h_q + hq0 + h) * D + (g4 & 1) * kHalf +
@@ -241,8 +247,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                 q_keep = keep;
 #pragma unroll
                 for (int m = 0; m < kM; ++m) {
-                    const uint32_t bits = uint32_t(keep >> (16 * m + 8 * (g4 >> 1))) & 0xFFu;
-                    masks[m] = u32x4_t{pair_mask(bits, 0), pair_mask(bits, 1), pair_mask(bits, 2), pair_mask(bits, 3)};
+                    masks[m] = s_masks[uint32_t(keep >> (16 * m + 8 * (g4 >> 1))) & 0xFFu];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) qm[kM * n + m] = qf[kM * n + m] & masks[m];
                 }
@@ -267,8 +272,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
             } else {
                 u32x4_t mask = {~0u, ~0u, ~0u, ~0u};
                 if (both != 0xFFFFu) {
-                    const uint32_t bits = both >> (8 * (g4 >> 1));
-                    mask = u32x4_t{pair_mask(bits, 0), pair_mask(bits, 1), pair_mask(bits, 2), pair_mask(bits, 3)};
+                    mask = s_masks[(both >> (8 * (g4 >> 1))) & 0xFFu];
                     kf[0][m] &= mask;
                     kf[1][m] &= mask;
                 }
@@ -318,23 +322,24 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                     for (int v = 0; v < 4; ++v) oacc[n][i][v] *= alpha;
             }
             // P as two bf16 numbers, what fits and what is left over: one would round every probability
-            // to 2^-9, and the output's own rounding is that size
+            // to 2^-9, and the output's own rounding is that size.  Up to 8 heads have a column for each.
             u32x4_t ph, pl;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     uint32_t h[2];
-                    bf16x2_t rest;
+                    bf16x2_t two;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float w = exp2_fast(__builtin_fmaf(sacc[n][s][2 * k + e], sc, m_neg[n]));
                         l_run[n] += w;
                         h[e] = __float_as_uint(w) & 0xFFFF0000u;
-                        rest[e] = (__bf16)(w - __uint_as_float(h[e]));
+                        const float rest = w - __uint_as_float(h[e]);
+                        two[e] = (__bf16)(kHalves && !rests ? __uint_as_float(h[e]) : rest);
                     }
-                    ph[2 * s + k] = h[0] >> 16 | h[1];
-                    pl[2 * s + k] = __builtin_bit_cast(uint32_t, rest);
+                    if constexpr (!kHalves) ph[2 * s + k] = h[0] >> 16 | h[1];
+                    pl[2 * s + k] = __builtin_bit_cast(uint32_t, two);
                 }
             if (n == 0) {
                 wait_v();
@@ -350,7 +355,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
             }
 #pragma unroll
             for (int i = 0; i < kDB; ++i) {
-                oacc[n][i] = mfma16(vf[i], ph, oacc[n][i]);
+                if constexpr (!kHalves) oacc[n][i] = mfma16(vf[i], ph, oacc[n][i]);
                 oacc[n][i] = mfma16(vf[i], pl, oacc[n][i]);
             }
         }
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
         for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, red_m[w][16 * n + r16]);
         const float f = m_run[n] == -INFINITY ? 0.f : exp2_fast(m_run[n] - m_all);
         const int heads = min(NH - 16 * n, 16);
-        if (r16 < heads) {
+        if ((kHalves ? r16 & 7 : r16) < heads) {
 #pragma unroll
             for (int i = 0; i < kDB; ++i)
                 *reinterpret_cast<f32x4_t*>(&s_o[(16 * wave + r16) * kOStride + 16 * i + 4 * g4]) = oacc[n][i] * f;
@@ -394,6 +399,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 o += *reinterpret_cast<const f32x4_t*>(&s_o[(16 * w + r) * kOStride + d]);
+                if constexpr (kHalves) o += *reinterpret_cast<const f32x4_t*>(&s_o[(16 * w + r + 8) * kOStride + d]);
                 if (red_m[w][h] != -INFINITY) L += red_l[w][h] * exp2_fast(red_m[w][h] - M);
             }
             const int64_t to = int64_t(t) * p.h_q + hq0 + h;
@@ -469,19 +475,19 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p) 
     if (lane == 0) p.lse[th] = empty ? -INFINITY : M * 0.69314718055994531f + logf(L);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool kHalves>
 hipError_t launch_d(const AttendParams& p, hipStream_t stream) {
     const int64_t blocks = int64_t(p.n_tokens) * p.splits * p.h_kv * p.subgroups;
     if (blocks * p.waves * 64 > 0xFFFFFFFF) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), threads(unsigned(p.waves) * 64);
     if (p.waves == 1)
-        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 1>), grid, threads, 0, stream, p);
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 1, kHalves>), grid, threads, 0, stream, p);
     else if (p.waves == 2)
-        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 2>), grid, threads, 0, stream, p);
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 2, kHalves>), grid, threads, 0, stream, p);
     else if (p.waves == 4)
-        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 4>), grid, threads, 0, stream, p);
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 4, kHalves>), grid, threads, 0, stream, p);
     else
-        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 8>), grid, threads, 0, stream, p);
+        hipLaunchKernelGGL((attend_blocks_kernel<D, NT, 8, kHalves>), grid, threads, 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const unsigned joins = unsigned((int64_t(p.n_tokens) * p.h_q + 3) / 4);
@@ -489,14 +495,18 @@ hipError_t launch_d(const AttendParams& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_heads(const AttendParams& p, hipStream_t stream) {
+    if (p.heads_per_block > 16) return launch_d<D, 2, false>(p, stream);
+    return p.heads_per_block > 8 ? launch_d<D, 1, false>(p, stream) : launch_d<D, 1, true>(p, stream);
+}
+
 }  // namespace
 
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream) {
     if ((p.waves != 1 && p.waves != 2 && p.waves != 4 && p.waves != 8) || p.splits < 1 || p.split_tiles < 1) return hipErrorInvalidValue;
     (void)hipGetLastError();
-    if (p.heads_per_block > 16)
-        return head_dim == 64 ? launch_d<64, 2>(p, stream) : launch_d<128, 2>(p, stream);
-    return head_dim == 64 ? launch_d<64, 1>(p, stream) : launch_d<128, 1>(p, stream);
+    return head_dim == 64 ? launch_heads<64>(p, stream) : launch_heads<128>(p, stream);
 }
 
 }  // namespace atf

@@ -108,6 +108,7 @@ BAD = [("plan", dict(page_tokens=48), EINVAL), ("plan", dict(page_tokens=0), EIN
        ("attend", dict(o=addr(0)), EINVAL), ("attend", dict(lse=addr(9)), EINVAL), ("attend", dict(n_tokens=-1), EINVAL),
        ("attend", dict(batch=0), EINVAL), ("attend", dict(lse=ctypes.c_void_p(addr(4).value + 2)), EINVAL),
        ("attend", dict(top=4096, page_tokens=1 << 19, block_tokens=1 << 19), EINVAL),
+       ("attend", dict(page_tokens=(1 << 26) + 32, block_tokens=32, max_pages=1), EUNSUPPORTED),
        ("bounds", dict(page_tokens=32, max_pages=(1 << 26) - 1, h_kv=9), EINVAL),
        ("attend", dict(k_pages=ctypes.c_void_p(addr(1).value + 8)), EINVAL), ("attend", dict(num_pages=0), EINVAL)]
 BAD += [(call, {name: None}, EINVAL) for call, (_, make) in CALLS.items() for name, value in make().items()
