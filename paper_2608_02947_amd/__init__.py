@@ -1036,6 +1036,17 @@ def bounds_shape(num_pages: int, page_tokens: int, block_tokens: int, h_kv: int,
     return (num_pages, h_kv, page_tokens // block_tokens, head_dim // 16, 2, 16)
 
 
+def _flat(t, dtype, dev, name, n):
+    """_vector of a tensor that must be given, its size first where nothing is wrong."""
+    try:
+        if t.dtype is dtype and t.numel() == n and t.dim() == 1 and t.get_device() == dev and dev >= 0 and \
+                t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _vector(t, dtype, dev, name, n)
+
+
 def atf_plan_pages(block_table, page_tokens: int, free_pages, free_count, n_k_rows, n_new_rows, n_k_out,
                    row_starts, slots, token_rows, positions, counts, stream=None):
     """Rows that end give back their pages, rows that grow take new ones, and every new token gets
@@ -1045,35 +1056,33 @@ def atf_plan_pages(block_table, page_tokens: int, free_pages, free_count, n_k_ro
     [3] (free pages left, packed tokens, rows refused).  All on the device, int32 but slots."""
     fn = "atf_plan_pages"
     ty, dev, st = _call()
-    if len(block_table.shape) != 2 or len(free_pages.shape) != 1 or len(slots.shape) != 1:
-        raise ValueError(f"{fn}: block_table must be [B, max_pages], free_pages [F], slots [T]")
-    B, width = block_table.shape
-    F, T = free_pages.shape[0], slots.shape[0]
-    if free_count.numel() < 1 or counts.shape != (3,):
-        raise ValueError(f"{fn}: free_count must hold a number, counts three")
+    F, T = free_pages.numel(), slots.numel()
+    if free_count.numel() < 1:
+        raise ValueError(f"{fn}: free_count must hold a number")
+    tp, B, width = _rows_table(fn, ty, dev, block_table)
     _check(_lib.atf_plan_pages(
-        _ptr(block_table, ty.i32, dev, "block_table"), width, int(page_tokens),
-        _ptr(free_pages, ty.i32, dev, "free_pages"), F, _ptr(free_count, ty.i32, dev, "free_count"), B,
-        _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), _vector(n_new_rows, ty.i32, dev, "n_new_rows", B),
-        _vector(n_k_out, ty.i32, dev, "n_k_out", B), _vector(row_starts, ty.i32, dev, "row_starts", B + 1), T,
-        _ptr(slots, ty.i64, dev, "slots"), _vector(token_rows, ty.i32, dev, "token_rows", T),
-        _vector(positions, ty.i32, dev, "positions", T), _ptr(counts, ty.i32, dev, "counts"),
+        tp, width, int(page_tokens),
+        _flat(free_pages, ty.i32, dev, "free_pages", F), F, _ptr(free_count, ty.i32, dev, "free_count"), B,
+        _flat(n_k_rows, ty.i32, dev, "n_k_rows", B), _flat(n_new_rows, ty.i32, dev, "n_new_rows", B),
+        _flat(n_k_out, ty.i32, dev, "n_k_out", B), _flat(row_starts, ty.i32, dev, "row_starts", B + 1), T,
+        _flat(slots, ty.i64, dev, "slots", T), _flat(token_rows, ty.i32, dev, "token_rows", T),
+        _flat(positions, ty.i32, dev, "positions", T), _flat(counts, ty.i32, dev, "counts", 3),
         st if stream is None else stream.cuda_stream))
 
 
 def _slot_args(fn, ty, dev, k_new, v_new, k_pages, v_pages, slots):
     """(pointers of k_new, v_new, k_pages, v_pages, slots), T, pages, tokens of a page, h_kv, d."""
-    T, h_kv, d = k_new.shape
-    ks = k_pages.shape
+    new, ks = k_new.shape, k_pages.shape
+    T, h_kv, d = new
     if len(ks) != 5:
         raise ValueError(f"{fn}: page pools must be 5-d (see kpages_shape, vpages_shape)")
     pages, tokens = ks[0], ks[3]
-    if v_new.shape != k_new.shape or ks != (pages, h_kv, d // 16, tokens, 16) or \
-            v_pages.shape != (pages, h_kv, tokens // 16, d, 16) or slots.shape != (T,):
+    if v_new.shape != new or ks != (pages, h_kv, d // 16, tokens, 16) or \
+            v_pages.shape != (pages, h_kv, tokens // 16, d, 16):
         raise ValueError(f"{fn}: inconsistent shapes")
     return ((_ptr(k_new, ty.bf16, dev, "k_new"), _ptr(v_new, ty.bf16, dev, "v_new"),
              _ptr(k_pages, ty.bf16, dev, "k_pages"), _ptr(v_pages, ty.bf16, dev, "v_pages"),
-             _ptr(slots, ty.i64, dev, "slots")), T, pages, tokens, h_kv, d)
+             _flat(slots, ty.i64, dev, "slots", T)), T, pages, tokens, h_kv, d)
 
 
 def atf_cache_append_slots(k_new, v_new, k_pages, v_pages, slots, stream=None):
@@ -1096,23 +1105,24 @@ def atf_cache_append_slots_rotated(k_new, v_new, k_pages, v_pages, slots, positi
         raise ValueError(f"{fn}: inconsistent shapes")
     cw, keep = window.as_c()
     fp, keep2 = _rope_freq(rope_inv_freq, d)
-    _check(_lib.atf_cache_append_slots_rotated(*ptrs, _vector(positions, ty.i32, dev, "positions", T), T, pages,
+    _check(_lib.atf_cache_append_slots_rotated(*ptrs, _flat(positions, ty.i32, dev, "positions", T), T, pages,
                                                tokens, h_kv, cw, fp, st if stream is None else stream.cuda_stream))
 
 
 def _bounds(fn, ty, dev, bounds, page_tokens, h_kv, d):
-    """(pointer of the bounds, tokens of a block) of pages of page_tokens tokens."""
+    """(pointer of the bounds, tokens of a block, pages) of pages of page_tokens tokens."""
     bs = bounds.shape
-    if len(bs) != 6 or bs != (bs[0], h_kv, bs[2], d // 16, 2, 16) or bs[2] < 1 or page_tokens % bs[2]:
+    if len(bs) != 6 or bs[1] != h_kv or bs[3] != d // 16 or bs[4] != 2 or bs[5] != 16 or bs[2] < 1 or page_tokens % bs[2]:
         raise ValueError(f"{fn}: bounds must be [pages, h_kv, blocks of a page, d/16, 2, 16] (see bounds_shape)")
-    return _ptr(bounds, ty.bf16, dev, "bounds"), page_tokens // bs[2]
+    return _ptr(bounds, ty.bf16, dev, "bounds"), page_tokens // bs[2], bs[0]
 
 
 def _rows_table(fn, ty, dev, block_table):
     """(table pointer, rows, pages of a row)."""
-    if len(block_table.shape) != 2:
+    ts = block_table.shape
+    if len(ts) != 2:
         raise ValueError(f"{fn}: block_table must be [B, max_pages]")
-    return _ptr(block_table, ty.i32, dev, "block_table"), block_table.shape[0], block_table.shape[1]
+    return _ptr(block_table, ty.i32, dev, "block_table"), ts[0], ts[1]
 
 
 def atf_block_bounds(k_pages, bounds, block_table, n_k_rows, n_new_rows, max_new: int, stream=None):
@@ -1121,14 +1131,17 @@ def atf_block_bounds(k_pages, bounds, block_table, n_k_rows, n_new_rows, max_new
     of bounds_shape."""
     fn = "atf_block_bounds"
     ty, dev, st = _call()
-    if len(k_pages.shape) != 5 or k_pages.shape[4] != 16 or bounds.shape[0] != k_pages.shape[0]:
+    ks = k_pages.shape
+    if len(ks) != 5 or ks[4] != 16:
         raise ValueError(f"{fn}: inconsistent shapes")
-    pages, h_kv, nc, pt, _ = k_pages.shape
-    bp, bt = _bounds(fn, ty, dev, bounds, pt, h_kv, 16 * nc)
+    pages, h_kv, nc, pt, _ = ks
+    bp, bt, lead = _bounds(fn, ty, dev, bounds, pt, h_kv, 16 * nc)
+    if lead != pages:
+        raise ValueError(f"{fn}: inconsistent shapes")
     tp, B, width = _rows_table(fn, ty, dev, block_table)
     _check(_lib.atf_block_bounds(_ptr(k_pages, ty.bf16, dev, "k_pages"), bp, tp, width, pages, pt, bt, B,
-                                 _vector(n_k_rows, ty.i32, dev, "n_k_rows", B),
-                                 _vector(n_new_rows, ty.i32, dev, "n_new_rows", B), int(max_new), h_kv, 16 * nc,
+                                 _flat(n_k_rows, ty.i32, dev, "n_k_rows", B),
+                                 _flat(n_new_rows, ty.i32, dev, "n_new_rows", B), int(max_new), h_kv, 16 * nc,
                                  st if stream is None else stream.cuda_stream))
 
 
@@ -1147,16 +1160,17 @@ def atf_select_blocks(q, bounds, blocks, block_table, page_tokens: int, token_ro
     fn = "atf_select_blocks"
     ty, dev, st = _call()
     T, h_q, d = q.shape
-    if len(blocks.shape) != 3 or blocks.shape[0] != T or window.head_dim != d:
+    bs = blocks.shape
+    if len(bs) != 3 or bs[0] != T or window.head_dim != d:
         raise ValueError(f"{fn}: inconsistent shapes")
-    h_kv, top = blocks.shape[1], blocks.shape[2]
-    bp, bt = _bounds(fn, ty, dev, bounds, int(page_tokens), h_kv, d)
+    h_kv, top = bs[1], bs[2]
+    bp, bt, pages = _bounds(fn, ty, dev, bounds, int(page_tokens), h_kv, d)
     tp, B, width = _rows_table(fn, ty, dev, block_table)
     cw, keep = window.as_c()
     _check(_lib.atf_select_blocks(
-        _ptr(q, ty.bf16, dev, "q"), bp, _ptr(blocks, ty.i32, dev, "blocks"), T, tp, width, bounds.shape[0],
-        int(page_tokens), bt, B, _vector(token_rows, ty.i32, dev, "token_rows", T),
-        _vector(positions, ty.i32, dev, "positions", T), _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), int(max_n_k),
+        _ptr(q, ty.bf16, dev, "q"), bp, _ptr(blocks, ty.i32, dev, "blocks"), T, tp, width, pages,
+        int(page_tokens), bt, B, _flat(token_rows, ty.i32, dev, "token_rows", T),
+        _flat(positions, ty.i32, dev, "positions", T), _flat(n_k_rows, ty.i32, dev, "n_k_rows", B), int(max_n_k),
         top, int(first_blocks), int(last_blocks), h_q, h_kv, cw, _ptr(workspace, ty.u8, dev, "workspace"),
         workspace.numel(), st if stream is None else stream.cuda_stream))
 
@@ -1173,18 +1187,19 @@ def atf_attend_blocks(q, k_pages, v_pages, o, lse, block_table, token_rows, posi
     atf_attend_workspace_bytes()."""
     fn = "atf_attend_blocks"
     ty, dev, st = _call()
-    T, h_q, d = q.shape
+    qs, bs, ts = q.shape, blocks.shape, block_table.shape
+    T, h_q, d = qs
     h_kv = k_pages.shape[1]
-    if o.shape != q.shape or lse.shape != (T, h_q) or len(blocks.shape) != 3 or blocks.shape[:2] != (T, h_kv) or \
-            window.head_dim != d:
+    if o.shape != qs or lse.shape != (T, h_q) or len(bs) != 3 or bs[0] != T or bs[1] != h_kv or window.head_dim != d or \
+            len(ts) != 2:
         raise ValueError(f"{fn}: inconsistent shapes")
-    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, block_table.shape[0], h_kv, d)
-    B = block_table.shape[0]
+    B = ts[0]
+    pools = _pools(fn, ty, dev, k_pages, v_pages, block_table, B, h_kv, d)
     cw, keep = window.as_c()
     _check(_lib.atf_attend_blocks(
         _ptr(q, ty.bf16, dev, "q"), _ptr(k_pages, ty.bf16, dev, "k_pages"), _ptr(v_pages, ty.bf16, dev, "v_pages"),
         *_decode_out(ty, dev, o, lse), T, *pools, int(block_tokens), B,
-        _vector(token_rows, ty.i32, dev, "token_rows", T), _vector(positions, ty.i32, dev, "positions", T),
-        _vector(n_k_rows, ty.i32, dev, "n_k_rows", B), _ptr(blocks, ty.i32, dev, "blocks"), blocks.shape[2], h_q,
+        _flat(token_rows, ty.i32, dev, "token_rows", T), _flat(positions, ty.i32, dev, "positions", T),
+        _flat(n_k_rows, ty.i32, dev, "n_k_rows", B), _ptr(blocks, ty.i32, dev, "blocks"), bs[2], h_q,
         h_kv, cw, softmax_scale, _ptr(workspace, ty.u8, dev, "workspace"), workspace.numel(),
         st if stream is None else stream.cuda_stream))
