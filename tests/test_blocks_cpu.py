@@ -19,8 +19,13 @@ def addr(i):
     return ctypes.c_void_p(A * 1024 * (i + 1))
 
 
+KEPT = []  # the arrays that the windows below point to
+
+
 def window(d=128, **kw):
-    return atf.Window(d, 1e4, 2.0, **kw).as_c()[0]
+    w, arrays = atf.Window(d, 1e4, 2.0, **kw).as_c()
+    KEPT.append(arrays)
+    return w
 
 
 def plan_args(**kw):
