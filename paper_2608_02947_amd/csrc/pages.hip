@@ -13,7 +13,8 @@
 // token's row by a search in the rows' first tokens, and the row's first position, or -1 if the row got
 // nothing, where the plan left it: at the row's first token.
 //
-// Bound by latency: a launch, and loads that wait for one another.
+// Bound by latency: a launch, and loads that wait for one another (200 rows of a step with 5,900 tokens 10.2
+// us in a captured graph, 24 prompts with 274,000 tokens 11.2).
 #include "atf_internal.hpp"
 #include "rope.hpp"
 #include "scan.hpp"
@@ -302,7 +303,9 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(const PlanParams p)
 //   values: a whole block's as rotate.hip's appends take them: 2 dims x the 8 tokens of one half of the
 //     slots (slot 8h + e holds token 8(e/4) + 4h + e%4) a lane, two 16-byte stores; of others 2 dims a
 //     lane, 8 tokens loaded before the first is stored, 2 bytes a store
-// Bound by HBM where tokens are many.
+// Bound by HBM where tokens are many: 11,991 of 8 heads of 128, keys turned (98 MB), 24.0 us, 4.1 TB/s of
+// the 5.4 that a large copy reaches, which takes 18.2 for the bytes; the rest is start and end.  Loads
+// past the caches take 24.3 us, stores past them 36.8, lanes in the order of the tokens 25.4.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <int D, bool kTurn, int kWindow>
