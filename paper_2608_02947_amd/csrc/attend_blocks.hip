@@ -247,8 +247,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_blocks_kernel(const AttendP
                 }
             }
         }
-        // pairs kept nowhere in the tile: the queries and the keys (in lanes whose chunk was not read they
-        // are another tile's) lose them
+        // pairs kept nowhere in the tile: the queries and the keys (zeros in lanes whose chunk was not read)
+        // lose them
         if constexpr (kCached) {
             if (keep != q_keep) {
                 q_keep = keep;

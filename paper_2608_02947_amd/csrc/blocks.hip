@@ -137,9 +137,9 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
 //
 // These sums are in fp32, off by no more than their error bound: the additions that a term goes through
 // (a product's 32, then one a chunk or pair), each at most 2^-23 of the sum of magnitudes, which a
-// second product has.  pick_kernel finds the border of the blocks taken
-// among them; blocks as near to it as the bound allows, mostly the one that is the border, are summed
-// again in 64 bits unless all or none of them are taken.
+// second product has, and what fp32 loses below its smallest normal number.  pick_kernel finds the
+// border of the blocks taken among them; blocks as near to it as the bound allows, mostly the one that
+// is the border, are summed again in 64 bits unless all or none of them are taken.
 //
 // Bound by latency for single tokens (1,048,576 keys in 16,384 blocks, 28/4 heads of 128: scores 15 us, of
 // which 12 MB of bounds are 2, the choice 14; summing every block in 64 bits took 326 in all), by
@@ -585,8 +585,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         size = fmaxf(size, s.size[w]);
     }
     // each addition is off by 2^-23 of the magnitudes' sum at most; that, and its product with their
-    // number, by less than 2^-10
-    const double error = double(size) * (0x1p-23 * (1 + 0x1p-10));
+    // number, by less than 2^-10; and the products and additions, fewer than 2^10, that come out below the
+    // smallest normal number by no more than that, 2^-126, each
+    const double error = double(size) * (0x1p-23 * (1 + 0x1p-10)) + 0x1p-115;
     bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
 
     int above = INT32_MAX, from = INT32_MAX;  // blocks over `above` are taken, those from `from` on maybe

@@ -484,6 +484,19 @@ def test_select_tiny_and_huge_numbers():
         check_select(tok, (q * x).to(BF), (b * y).to(BF), bt, win, W, 6, 1, 1)
 
 
+@pytest.mark.parametrize("queries", [(2, 1), (130, 9)])
+def test_select_products_below_fp32(queries):
+    """Products that fp32 holds with few bits or none: the blocks are those of sums in 64 bits all the same."""
+    note(f"select products below fp32 {queries}")
+    d, h_q, h_kv, pt, bt = 128, 4, 2, 32, 32
+    win, W = windows(d, "exact")
+    tok = Tokens([3000, 700], list(queries), pt, 4)
+    q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(8))
+    b = random_bounds(tok.P, pt, bt, h_kv, d, 6).float()
+    for e in (-66, -70, -73, -78):
+        check_select(tok, (q * 2.0 ** e).to(BF), (b * 2.0 ** e).to(BF), bt, win, W, 9, 1, 1)
+
+
 def test_select_of_entries_out_of_range():
     """Table entries and lengths outside their ranges are clamped."""
     note("select clamps")
