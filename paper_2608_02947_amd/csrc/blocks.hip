@@ -421,8 +421,8 @@ __device__ __forceinline__ uint64_t exact_key(const SelectParams& p, const Token
     return uint64_t(v ^ ((v >> 63) & 0x7FFFFFFFFFFFFFFFll)) ^ 0x8000000000000000ull;
 }
 
-// The blocks of one token for one KV head.  kPer keys of a thread stay in registers; 0: they are read
-// again each time.
+// The blocks of one token for one KV head.  A thread's kPer keys, one behind the other, stay in registers;
+// 0: they are read again each time.
 template <int kThreads>
 struct PickShared {
     static constexpr int kBits = kThreads == 64 ? 9 : 11, kBins = 1 << kBits;
@@ -440,7 +440,7 @@ struct PickShared {
     uint8_t win[kListed];
 };
 
-// Blocks j where take(j), in order, behind each other: a step of kThreads blocks at a time.
+// Blocks j where take(j), in order, one behind the other: a step of kThreads blocks at a time.
 template <int kThreads, typename Take>
 __device__ __forceinline__ void write_taken(int32_t* out, int top, int n, PickShared<kThreads>& s, Take take) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -547,15 +547,23 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     const auto load = [&](int j) { return j >= p.first_blocks && j < n - p.last_blocks ? keys[j] : INT32_MIN; };
     [[maybe_unused]] int kept[kPer > 0 ? kPer : 1];
     if constexpr (kPer > 0) {
+        const int j0 = tid * kPer;
+        int4 x[kPer / 4] = {};
+        if (j0 < n)  // (the row's keys fill up to 16)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) kept[i] = load(i * kThreads + tid);
+            for (int i = 0; i < kPer / 4; ++i) x[i] = *reinterpret_cast<const int4*>(keys + j0 + 4 * i);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = j0 + i, k = i % 4 == 0 ? x[i / 4].x : i % 4 == 1 ? x[i / 4].y : i % 4 == 2 ? x[i / 4].z : x[i / 4].w;
+            kept[i] = j >= p.first_blocks && j < n - p.last_blocks ? k : INT32_MIN;
+        }
     }
     const auto each = [&](auto body) __attribute__((always_inline)) {
         if constexpr (kPer > 0) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 asm volatile("" : "+v"(kept[i]));  // (its comparisons are not kept from one time to the next)
-                if (kept[i] != INT32_MIN) body(i * kThreads + tid, kept[i]);
+                if (kept[i] != INT32_MIN) body(tid * kPer + i, kept[i]);
             }
         } else {
             for (int j = tid; j < n; j += kThreads) {
@@ -691,37 +699,27 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         return;
     }
     if constexpr (kPer > 0) {
-        // which of a thread's blocks are taken, and how many of each step of each wave
-        __shared__ int s_count[kPer * kWaves];
+        // which of a thread's blocks are taken
         uint32_t won = all ? ~0u : 0u;
         if (!all && want > 0)
             for (int i = 0; i < s.listed; ++i) {
-                const int j = s.list[i], step = j / kThreads;
-                if (j - step * kThreads == tid && s.win[i]) won |= 1u << step;
+                const int j = s.list[i];
+                if (j / kPer == tid && s.win[i]) won |= 1u << (j % kPer);
             }
         uint32_t taken = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int k = kept[i];
             // (blocks that are taken anyway, below n, have the lowest key)
-            const bool yes = k == INT32_MIN ? i * kThreads + tid < n : k > above || (k >= from && ((won >> i) & 1u) != 0);
+            const bool yes = k == INT32_MIN ? tid * kPer + i < n : k > above || (k >= from && ((won >> i) & 1u) != 0);
             taken |= uint32_t(yes) << i;
-            const uint64_t m = __ballot(yes);
-            if (lane == 0) s_count[i * kWaves + wave] = __builtin_popcountll(m);
         }
-        __syncthreads();
-        // (each wave adds up the numbers of those before its own)
-        int before = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int c = scan::row16(s_count[i * kWaves + min(lane & 15, kWaves - 1)]);
-            const int mine = before + (wave > 0 ? scan::lane_of(c, wave - 1) : 0);
-            before += scan::lane_of(c, kWaves - 1);
-            const bool yes = ((taken >> i) & 1u) != 0;
-            const uint64_t m = __ballot(yes);
-            const int to = mine + __builtin_popcountll(m & ((1ull << lane) - 1));
-            if (yes && to < p.top) out[to] = i * kThreads + tid;
-        }
+        int upto[1] = {int(__builtin_popcount(taken))}, total[1];
+        int to = -upto[0];
+        scan::block<kWaves>(upto, total, s_scan);
+        to += upto[0];
+        for (; taken != 0; taken &= taken - 1, ++to)
+            if (to < p.top) out[to] = tid * kPer + __builtin_ctz(taken);
     } else {
         write_taken<kThreads>(out, p.top, n, s, [&](int j) __attribute__((always_inline)) {
             const int k = load(j);
