@@ -433,9 +433,9 @@ struct PickShared {
     int low[kThreads / 64], high[kThreads / 64];
     float size[kThreads / 64];
     int bin, above, inside;
-    int listed, sure;
+    int listed, sure, maybe;
     int border;
-    int list[kListed];
+    int list[kListed], key[kListed];
     uint64_t exact[kListed];
     uint8_t win[kListed];
 };
@@ -563,28 +563,33 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 asm volatile("" : "+v"(kept[i]));  // (its comparisons are not kept from one time to the next)
-                if (kept[i] != INT32_MIN) body(tid * kPer + i, kept[i]);
+                body(tid * kPer + i, kept[i]);
             }
         } else {
-            for (int j = tid; j < n; j += kThreads) {
-                const int k = load(j);
-                if (k != INT32_MIN) body(j, k);
-            }
+            for (int j = tid; j < n; j += kThreads) body(j, load(j));
         }
     };
-    // extremes, and the error bound
-    int low = INT32_MAX, high = INT32_MIN;
+    // lo <= k <= hi, lo above the lowest key, in one comparison
+    const auto within = [](int k, int lo, int hi) __attribute__((always_inline)) {
+        return uint32_t(k) - uint32_t(lo) <= uint32_t(hi) - uint32_t(lo);
+    };
+    // extremes (the lowest key comes last among those so counted), and the error bound
+    constexpr uint32_t kLast = 0x80000001u;
+    uint32_t least = ~0u;
+    int high = INT32_MIN;
     each([&](int, int k) __attribute__((always_inline)) {
-        low = min(low, k);
+        least = min(least, uint32_t(k) - kLast);
         high = max(high, k);
     });
+    int low = int(least + kLast);
+    if (least == ~0u) low = INT32_MAX;
     float size = 0.f;
     for (int i = tid; i < p.ranges; i += kThreads) size = fmaxf(size, p.sizes[at * p.ranges + i]);
     low = ~max_lanes(~low);  // (the complement is in the opposite order)
     high = max_lanes(high);
     size = __int_as_float(max_lanes(__float_as_int(size)));
     if (lane == 0) s.low[wave] = low, s.high[wave] = high, s.size[wave] = size;
-    if (tid == 0) s.listed = s.sure = 0;
+    if (tid == 0) s.listed = s.sure = s.maybe = 0;
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
     __syncthreads();
     for (int w = 0; w < kWaves; ++w) {
@@ -597,17 +602,29 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     // smallest normal number by no more than that, 2^-126, each
     const double error = double(size) * (0x1p-23 * (1 + 0x1p-10)) + 0x1p-115;
     bool exact = want > 0 && (high == INT32_MAX || !(error < 1e300));
+    // of the keys of scores that may be as large as one of key k, the lowest; as small, the highest (the
+    // numbers of fp32 next to the limits on their inner sides)
+    const auto lowest_of = [&](int k) __attribute__((always_inline)) {
+        const double x = double(value_of(k)) - 2 * error;
+        const int y = key_of(float(x));
+        return y == INT32_MAX ? INT32_MIN + 1 : y + (double(float(x)) < x);
+    };
+    const auto highest_of = [&](int k) __attribute__((always_inline)) {
+        const double x = double(value_of(k)) + 2 * error;
+        const int y = key_of(float(x));
+        return y - (double(float(x)) > x && y != INT32_MAX);
+    };
 
     int above = INT32_MAX, from = INT32_MAX;  // blocks over `above` are taken, those from `from` on maybe
     bool all = want > 0;                      // the latter all are
     if (want > 0 && !exact) {
-        int left = want;
-        int border = low;
+        // the bin of the border, and so on in it until the blocks that may be at the border can be listed
+        int left = want, listed;
         for (;;) {
             const uint32_t reach = uint32_t(high) - uint32_t(low);
             const int shift = max(0, 32 - kBits - __builtin_clz(reach | 1));
             each([&](int, int k) __attribute__((always_inline)) {
-                if (k >= low && k <= high) atomicAdd(&s.hist[(uint32_t(k) - uint32_t(low)) >> shift], 1);
+                if (within(k, low, high)) atomicAdd(&s.hist[(uint32_t(k) - uint32_t(low)) >> shift], 1);
             });
             __syncthreads();
             // the bin where `left` is reached, from the highest
@@ -633,65 +650,70 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             left -= s.above;
             low = int(uint32_t(low) + (uint32_t(s.bin) << shift));
             high = min(high, int(uint32_t(low) + ((1u << shift) - 1)));
-            border = low;
-            if (shift == 0) break;
-            if (s.inside <= kListed) {
-                each([&](int, int k) __attribute__((always_inline)) {
-                    if (k >= low && k <= high) s.list[atomicAdd(&s.listed, 1)] = k;
-                });
-                __syncthreads();
-                if (tid < s.inside) {
-                    const int k = s.list[tid];
-                    int over = 0, same = 0;
-                    for (int i = 0; i < s.inside; ++i) {
-                        over += s.list[i] > k;
-                        same += s.list[i] == k;
+            from = lowest_of(low);
+            above = highest_of(high);
+            listed = s.inside;
+            if (listed <= kListed) {
+                int sure = 0;
+                each([&](int j, int k) __attribute__((always_inline)) {
+                    sure += k > above;
+                    if (within(k, from, above)) {
+                        const int i = atomicAdd(&s.listed, 1);
+                        if (i < kListed) s.list[i] = j, s.key[i] = k;
                     }
-                    if (over < left && left <= over + same) s.border = k;
-                }
+                });
+                sure = scan::lane_of(scan::wave(sure), 63);
+                if (lane == 0 && sure > 0) atomicAdd(&s.sure, sure);
                 __syncthreads();
-                border = s.border;
-                if (tid == 0) s.listed = 0;
-                break;
+                listed = s.listed;
             }
+            if (listed <= kListed || shift == 0) break;
             for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
             __syncthreads();
+            if (tid == 0) s.listed = s.sure = 0;
         }
-        // (the numbers of fp32 next to the two limits on their inner sides)
-        const double over = double(value_of(border)) + 2 * error, under = double(value_of(border)) - 2 * error;
-        above = key_of(float(over));
-        above -= double(float(over)) > over && above != INT32_MAX;
-        from = key_of(float(under));
-        from = from == INT32_MAX ? INT32_MIN + 1 : from + (double(float(under)) < under);
-        __syncthreads();
-        int sure = 0;
-        each([&](int j, int k) __attribute__((always_inline)) {
-            if (k > above)
-                ++sure;
-            else if (k >= from) {
-                const int i = atomicAdd(&s.listed, 1);
-                if (i < kListed) s.list[i] = j;
-            }
-        });
-        sure = scan::lane_of(scan::wave(sure), 63);
-        if (lane == 0 && sure > 0) atomicAdd(&s.sure, sure);
-        __syncthreads();
-        const int listed = s.listed, rest = want - s.sure;
-        all = listed == rest;
-        exact = !all && listed > kListed;
-        if (!all && !exact) {
-            for (int i = wave; i < listed; i += kWaves) {
-                const uint64_t k = exact_key(p, tok, t, g, __builtin_amdgcn_readfirstlane(s.list[i]));
-                if (lane == 0) s.exact[i] = k;
-            }
-            __syncthreads();
+        exact = listed > kListed;
+        if (!exact) {
+            // the border: the key whose place is the last one taken
+            const int sure = s.sure, mine = tid < listed ? s.key[tid] : INT32_MIN;
             if (tid < listed) {
-                int over = 0;
-                for (int i = 0; i < listed; ++i)
-                    over += s.exact[i] > s.exact[tid] || (s.exact[i] == s.exact[tid] && s.list[i] < s.list[tid]);
-                s.win[tid] = over < rest;
+                int over = sure, same = 0;
+                for (int i = 0; i < listed; ++i) {
+                    over += s.key[i] > mine;
+                    same += s.key[i] == mine;
+                }
+                if (over < want && want <= over + same) s.border = mine;
             }
             __syncthreads();
+            from = lowest_of(s.border);
+            above = highest_of(s.border);
+            const int over = __builtin_popcountll(__ballot(tid < listed && mine > above));
+            const int maybe = __builtin_popcountll(__ballot(tid < listed && within(mine, from, above)));
+            if (lane == 0 && over > 0) atomicAdd(&s.sure, over);
+            if (lane == 0 && maybe > 0) atomicAdd(&s.maybe, maybe);
+            __syncthreads();
+            const int rest = want - s.sure;
+            all = s.maybe == rest;
+            if (!all) {
+                for (int i = wave; i < listed; i += kWaves) {
+                    if (!within(__builtin_amdgcn_readfirstlane(s.key[i]), from, above)) continue;
+                    const uint64_t k = exact_key(p, tok, t, g, __builtin_amdgcn_readfirstlane(s.list[i]));
+                    if (lane == 0) s.exact[i] = k;
+                }
+                __syncthreads();
+                if (tid < listed) {
+                    bool win = false;
+                    if (within(mine, from, above)) {
+                        int better = 0;
+                        for (int i = 0; i < listed; ++i)
+                            better += within(s.key[i], from, above) &&
+                                      (s.exact[i] > s.exact[tid] || (s.exact[i] == s.exact[tid] && s.list[i] < s.list[tid]));
+                        win = better < rest;
+                    }
+                    s.win[tid] = win;
+                }
+                __syncthreads();
+            }
         }
     }
     if (exact) {
@@ -699,21 +721,18 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
         return;
     }
     if constexpr (kPer > 0) {
-        // which of a thread's blocks are taken
-        uint32_t won = all ? ~0u : 0u;
+        // which of a thread's blocks are taken: those taken anyway, those over a limit, and the listed ones
+        // that won
+        const auto below = [&](int j) __attribute__((always_inline)) { return (1u << min(max(j - tid * kPer, 0), kPer)) - 1; };
+        uint32_t taken = below(n) & (below(p.first_blocks) | ~below(n - p.last_blocks));
+        const int limit = all ? from - 1 : above;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) taken |= uint32_t(kept[i] > limit) << i;
         if (!all && want > 0)
             for (int i = 0; i < s.listed; ++i) {
                 const int j = s.list[i];
-                if (j / kPer == tid && s.win[i]) won |= 1u << (j % kPer);
+                if (j / kPer == tid && s.win[i]) taken |= 1u << (j % kPer);
             }
-        uint32_t taken = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int k = kept[i];
-            // (blocks that are taken anyway, below n, have the lowest key)
-            const bool yes = k == INT32_MIN ? tid * kPer + i < n : k > above || (k >= from && ((won >> i) & 1u) != 0);
-            taken |= uint32_t(yes) << i;
-        }
         int upto[1] = {int(__builtin_popcount(taken))}, total[1];
         int to = -upto[0];
         scan::block<kWaves>(upto, total, s_scan);
