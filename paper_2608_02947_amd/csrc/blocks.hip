@@ -342,8 +342,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 }
                 // additions that a term goes through: those of a product of 32, the chunks', the pairs'
                 const float steps = float(32 + kChunks + __builtin_popcountll(some));
-                if (h0 + 16 >= G) {  // the tile is done with
-                    keep = keep_of(min(tile + p.ranges, tiles - 1));
+                if (h0 + 16 >= G && tile + p.ranges < tiles) {  // the tile is done with
+                    keep = keep_of(tile + p.ranges);
                     load(next, keep);
                     next = where(min(tile + 2 * p.ranges, tiles - 1));
                 }
@@ -558,6 +558,8 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
             kept[i] = j >= p.first_blocks && j < n - p.last_blocks ? k : INT32_MIN;
         }
     }
+    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+    float size = p.sizes[at * p.ranges + min(tid, p.ranges - 1)];  // (on its way with the keys)
     const auto each = [&](auto body) __attribute__((always_inline)) {
         if constexpr (kPer > 0) {
 #pragma unroll
@@ -583,14 +585,12 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const SelectParams p) {
     });
     int low = int(least + kLast);
     if (least == ~0u) low = INT32_MAX;
-    float size = 0.f;
-    for (int i = tid; i < p.ranges; i += kThreads) size = fmaxf(size, p.sizes[at * p.ranges + i]);
+    for (int i = tid + kThreads; i < p.ranges; i += kThreads) size = fmaxf(size, p.sizes[at * p.ranges + i]);
     low = ~max_lanes(~low);  // (the complement is in the opposite order)
     high = max_lanes(high);
     size = __int_as_float(max_lanes(__float_as_int(size)));
     if (lane == 0) s.low[wave] = low, s.high[wave] = high, s.size[wave] = size;
     if (tid == 0) s.listed = s.sure = s.maybe = 0;
-    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
     __syncthreads();
     for (int w = 0; w < kWaves; ++w) {
         low = min(low, s.low[w]);
