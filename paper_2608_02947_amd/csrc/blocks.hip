@@ -179,11 +179,14 @@ __device__ __forceinline__ Token token_of(const SelectParams& p, int t) {
     return x;
 }
 
-// The bounds of block j of a row, for KV head g.
-__device__ __forceinline__ const uint16_t* bounds_of(const SelectParams& p, int row, int g, int j) {
-    const uint32_t per = uint32_t(p.page_blocks), i = uint32_t(j) / per;
-    const int page = min(max(p.block_table[int64_t(row) * p.max_pages + i], 0), p.num_pages - 1);
-    return p.bounds + ((int64_t(page) * p.h_kv + g) * per + (uint32_t(j) - i * per)) * p.chunks * 32;
+// The bounds of block j of a row, for KV head g: the table's entry, and where they are by it.
+__device__ __forceinline__ int page_of(const SelectParams& p, int row, int j) {
+    return p.block_table[int64_t(row) * p.max_pages + uint32_t(j) / uint32_t(p.page_blocks)];
+}
+__device__ __forceinline__ const uint16_t* bounds_of(const SelectParams& p, int page, int g, int j) {
+    const uint32_t per = uint32_t(p.page_blocks);
+    page = min(max(page, 0), p.num_pages - 1);
+    return p.bounds + ((int64_t(page) * p.h_kv + g) * per + uint32_t(j) % per) * p.chunks * 32;
 }
 
 // fp32 numbers as integers of the same order and back; what is not finite above all
@@ -276,9 +279,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         }
         const int n = last_key / p.block_tokens + 1, tiles = (n + 15) / 16;
         if (range >= tiles) continue;
-        const auto where = [&](int tile) __attribute__((always_inline)) {
-            return bounds_of(p, row, g, min(16 * tile + r16, n - 1)) + 8 * g4;
-        };
+        const auto block_of = [&](int tile) __attribute__((always_inline)) { return min(16 * tile + r16, n - 1); };
         const auto keep_of = [&](int tile) __attribute__((always_inline)) {
             const int last = min(last_key, min(16 * tile + 15, n - 1) * p.block_tokens + (p.block_tokens - 1));
             return __ballot(my_w >= max(0, first_pos - last));
@@ -289,7 +290,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         const auto chunk = [&](int c) __attribute__((always_inline)) {
             return u32x4_t{a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]};
         };
-        const auto load = [&](const uint16_t* src, uint64_t keep) __attribute__((always_inline)) {
+        const auto load = [&](int tile, int page, uint64_t keep) __attribute__((always_inline)) {
+            const uint16_t* src = bounds_of(p, page, g, block_of(tile)) + 8 * g4;
 #pragma unroll
             for (int c = 0; c < kChunks; ++c)
                 if ((keep >> (8 * c)) & 0xFFull) {
@@ -299,8 +301,9 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 }
         };
         uint64_t keep = keep_of(range);
-        load(where(range), keep);
-        const uint16_t* next = where(min(range + p.ranges, tiles - 1));
+        load(range, page_of(p, row, block_of(range)), keep);
+        // (what is not looked at before the next tile's loads is not waited for with this one's)
+        int next = page_of(p, row, block_of(min(range + p.ranges, tiles - 1)));
         for (int tile = range; tile < tiles; tile += p.ranges) {
             const int j0 = 16 * tile;
             uint64_t full = __ballot(my_w >= last_pos - j0 * p.block_tokens);
@@ -344,8 +347,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 const float steps = float(32 + kChunks + __builtin_popcountll(some));
                 if (h0 + 16 >= G && tile + p.ranges < tiles) {  // the tile is done with
                     keep = keep_of(tile + p.ranges);
-                    load(next, keep);
-                    next = where(min(tile + 2 * p.ranges, tiles - 1));
+                    load(tile + p.ranges, next, keep);
+                    next = page_of(p, row, block_of(min(tile + 2 * p.ranges, tiles - 1)));
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -395,7 +398,7 @@ __device__ __forceinline__ uint64_t exact_key(const SelectParams& p, const Token
     const int far = tok.pos - first, near = tok.pos - min(first + (p.block_tokens - 1), tok.last);
     const int w = lane < half ? p.W[lane] : -1;
     const bool kept = lane < half && w >= near;
-    const uint16_t* at = bounds_of(p, tok.row, g, j) + lane / 8 * 32 + lane % 8;
+    const uint16_t* at = bounds_of(p, page_of(p, tok.row, j), g, j) + lane / 8 * 32 + lane % 8;
     double hi0 = 0, hi1 = 0, lo0 = 0, lo1 = 0;
     if (kept) hi0 = widen(at[0]), hi1 = widen(at[8]), lo0 = widen(at[16]), lo1 = widen(at[24]);
     double best = 0;
