@@ -154,6 +154,14 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                    __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+// The same of two numbers a lane, the others 0.
+typedef short bf16x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4_t mfma16_pair(uint32_t a, uint32_t b) {
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, u32x2_t{a, 0u}),
+                                                     __builtin_bit_cast(bf16x4_t, u32x2_t{b, 0u}),
+                                                     f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+}
 // pairs of a chunk that bits of `bits` keep
 __device__ __forceinline__ u32x4_t keep_pairs(u32x4_t x, uint32_t bits) {
     u32x4_t r;
@@ -262,8 +270,15 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         return h0 < 16 * kHeld ? s_query[(h0 / 16 * kChunks + c) * 64 + lane] : query_of(h0, c);
     };
 
+    // registers of two pairs each
+    const auto query_pairs = [&](int h0, int e) __attribute__((always_inline)) {
+        if (h0 < 16 * kHeld) return reinterpret_cast<const uint32_t*>(&s_query[(h0 / 16 * kChunks + e / 4) * 64 + lane])[e % 4];
+        const u32x4_t x = query_of(h0, e / 4);
+        return e % 4 == 0 ? x[0] : e % 4 == 1 ? x[1] : e % 4 == 2 ? x[2] : x[3];
+    };
+
     // signs of the bounds' magnitudes: those of the queries' parts
-    const u32x4_t minus = u32x4_t{1u, 1u, 1u, 1u} * (g4 >= 2 ? 0x80008000u : 0u);
+    const uint32_t minus = g4 >= 2 ? 0x80008000u : 0u;
     bool todo = is && tok.row >= 0 && tok.last >= 0;
     float worst = 0.f;  // largest sum of magnitudes times its additions
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
@@ -328,10 +343,11 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 }
                 for (uint64_t m = some; m != 0; m &= m - 1) {
                     const int r = __builtin_ctzll(m), w = __builtin_amdgcn_readlane(my_w, r);
-                    const u32x4_t mask = s_masks[1u << (r % 8)];
-                    const u32x4_t x = chunk(r / 8) & mask, y = query(h0, r / 8) & mask;
-                    const f32x4_t u = mfma16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    const f32x4_t v = mfma16((x & 0x7FFF7FFFu) | minus, y, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                    // (a pair is half a register of each lane)
+                    const uint32_t half = r & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+                    const uint32_t x = a[r / 2] & half, y = query_pairs(h0, r / 2) & half;
+                    const f32x4_t u = mfma16_pair(x, y);
+                    const f32x4_t v = mfma16_pair((x & 0x7FFF7FFFu) | (minus & half), y);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // (a tile past the row's end may reach past 2^31: wrapped, and not written)
