@@ -177,14 +177,10 @@ struct Token {
     int row, pos, last;
 };
 __device__ __forceinline__ Token token_of(const SelectParams& p, int t) {
-    Token x = {p.token_rows[t], p.positions[t], -1};
-    if (x.row < 0 || x.row >= p.batch) {
-        x.row = -1;
-        return x;
-    }
-    x.pos = min(x.pos, 0x7FFFFFFD);
-    x.last = min(min(max(p.n_k_rows[x.row], 0), p.max_n_k) - 1, x.pos);
-    return x;
+    const int row = p.token_rows[t], pos = min(p.positions[t], 0x7FFFFFFD);
+    const bool is = row >= 0 && row < p.batch;
+    const int keys = p.n_k_rows[is ? row : 0];
+    return {is ? row : -1, pos, is ? min(min(max(keys, 0), p.max_n_k) - 1, pos) : -1};
 }
 
 // The bounds of block j of a row, for KV head g: the table's entry, and where they are by it.
@@ -249,9 +245,6 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     const int at = r16 / width, h = r16 - at * width;
     const int t = t0 + at;
     const bool is = at < p.pack && t < p.tokens;
-    Token tok = {-1, 0, -1};
-    if (is) tok = token_of(p, p.first_token + t);
-
     // operand (column tile, chunk): the positive or the negative numbers of the columns' queries
     const auto query_of = [&](int h0, int c) __attribute__((always_inline)) {
         u32x4_t x = *reinterpret_cast<const u32x4_t*>(
@@ -261,9 +254,21 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
         for (int e = 0; e < 4; ++e) x[e] &= (((x[e] >> 15) & 0x00010001u) * 0xFFFFu) ^ (g4 >= 2 ? 0u : ~0u);
         return x;
     };
+    // (what the loads do not need of each other is on its way at once: the first queries, the tokens, the
+    // first tile's pages by the first token's row and any number of keys)
+    u32x4_t early[kChunks / 4];
+#pragma unroll
+    for (int i = 0; i < kChunks / 4; ++i) early[i] = query_of(0, wave + 4 * i);
+    Token tok = token_of(p, p.first_token + (is ? t : t0));
+    const int early_row = max(__builtin_amdgcn_readfirstlane(tok.row), 0);
+    const int early_page = page_of(p, early_row, min(16 * range + r16, p.row_blocks - 1));
+    if (!is) tok = {-1, 0, -1};
+
     const int held = min((G + 15) / 16, kHeld);
     s_masks[threadIdx.x] = keep_pairs(u32x4_t{~0u, ~0u, ~0u, ~0u}, threadIdx.x);
-    for (int o = wave; o < held * kChunks; o += 4) s_query[64 * o + lane] = query_of(16 * (o / kChunks), o % kChunks);
+#pragma unroll
+    for (int i = 0; i < kChunks / 4; ++i) s_query[64 * (wave + 4 * i) + lane] = early[i];
+    for (int o = wave + kChunks; o < held * kChunks; o += 4) s_query[64 * o + lane] = query_of(16 * (o / kChunks), o % kChunks);
     __syncthreads();
     if (range >= p.ranges) return;
     const auto query = [&](int h0, int c) __attribute__((always_inline)) {
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
                 }
         };
         uint64_t keep = keep_of(range);
-        load(range, page_of(p, row, block_of(range)), keep);
+        load(range, row == early_row && 16 * range + 15 < n ? early_page : page_of(p, row, block_of(range)), keep);
         // (what is not looked at before the next tile's loads is not waited for with this one's)
         int next = page_of(p, row, block_of(min(range + p.ranges, tiles - 1)));
         for (int tile = range; tile < tiles; tile += p.ranges) {
