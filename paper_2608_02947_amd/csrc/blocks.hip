@@ -141,12 +141,13 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
 // border of the blocks taken among them; blocks as near to it as the bound allows, mostly the one that
 // is the border, are summed again in 64 bits unless all or none of them are taken.
 //
-// Bound by latency for single tokens (1,048,576 keys in 16,384 blocks, 28/4 heads of 128: scores 15 us, of
-// which 12 MB of bounds are 2, the choice 14; summing every block in 64 bits took 326 in all), by
-// vector work for turns (1,460 tokens against up to 516 blocks, 24/8 heads: 67 and 31 us, 4,097 in 64 bits).
+// Bound by latency for single tokens (1,048,576 keys in 16,384 blocks, 28/4 heads of 128: scores 13 us, of
+// which 12 MB of bounds are 2, the choice 8.6; summing every block in 64 bits took 326 in all), by
+// vector work for turns (1,460 tokens against up to 516 blocks, 24/8 heads: 59 and 22 us, 4,097 in 64 bits).
 // Tokens that share the columns of a product, and 16 blocks a tile, are what keeps the vector work per
-// score small; the tile's bounds stay in registers, indexed by the pair whose window ends in it
-// (through LDS they took 90 us for the 67, at three workgroups' room a CU).
+// score small; the tile's bounds stay in registers, indexed by the pair whose window ends in it (through LDS
+// they took 90 us where registers took 67, at three workgroups' room a CU).  The row's last tile, where
+// most windows end, shared among a workgroup's waves: 31.9 us for 30.5 (24 rows), 88 for 83 (turns).
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
