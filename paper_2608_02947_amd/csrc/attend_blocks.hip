@@ -18,11 +18,13 @@
 // are few a list is split over workgroups, whose partial states a second kernel joins.
 //
 // Bound by HBM reads where rows are many: 63 rows of up to 4,096 keys, 24/8 heads of 128 (813 MB), 148 us,
-// 5.5 TB/s (a streaming read reaches 5.57).  By the caches where many tokens read one row's: 1,460
-// tokens of 2,048 keys, 32/4 heads of 128, 219 us, 5 GB through the L2s.  There a wave that walks its
-// list alone and in order stays near the others of its XCD: 238 us with one wave a token and head, 281
-// with four; three waves a SIMD (the masks formed for each tile) take 242 for 220.  A single token's call is a launch
-// and a chain of loads (token, row, list, table, keys): 7 us for 16 blocks of 32, 14/2 heads of 64.
+// 5.5 TB/s (a streaming read reaches 5.57).  Inside the CUs where many tokens read one row's: 1,460 tokens of
+// 2,048 keys, 32/4 heads of 128, 219 us, and 200 with one tile's keys and values read for all (a copy of the
+// kernel): 16 loads of 1 KB a tile into registers, each byte used for one token's 8 heads, and 170 vector
+// instructions (ALU busy 0.51) by two waves a SIMD.  There a wave that walks its list alone and in order
+// stays near the others of its XCD: 238 us with one wave a token and head, 281 with four; three waves a SIMD
+// (the masks formed for each tile) take 242 for 220.  A single token's call is a launch and a chain of loads
+// (token, row, list, table, keys): 7 us for 16 blocks of 32, 14/2 heads of 64.
 #include "atf_internal.hpp"
 
 namespace atf {
