@@ -253,6 +253,22 @@ def test_block_bounds(d, h_kv, pt, bt, lens, news):
         assert np.array_equal(bits(out).numpy() == SENTINEL, bits(torch.tensor(want).to(BF)).numpy() == SENTINEL)
 
 
+@pytest.mark.parametrize("rows,pages,pt,h_kv", [(1, 4300, 64, 4), (1300, 3, 32, 2)])
+def test_block_bounds_of_long_rows_and_many(rows, pages, pt, h_kv):
+    """More blocks of a row, and more rows, than a launch has workgroups for at once."""
+    import paper_2608_02947_amd as atf
+    note(f"bounds {rows} rows of {pages} pages")
+    d, bt, P = 64, 32, rows * pages
+    k = torch.randn(atf.kpages_shape(P, pt, h_kv, d), generator=torch.Generator().manual_seed(rows)).to(BF)
+    x = k.view(P, h_kv, d // 16, pt // bt, bt, 16).permute(0, 1, 3, 2, 4, 5)
+    want = torch.stack([x.amax(dim=4), x.amin(dim=4)], dim=4)
+    out = filled(atf.bounds_shape(P, pt, bt, h_kv, d))
+    n = np.full(rows, pages * pt)
+    atf.atf_block_bounds(k.to(DEV), out, dev32(np.arange(P).reshape(rows, pages)), dev32(n), dev32(n), pages * pt)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), want)
+
+
 def test_block_bounds_nan_of_either_sign():
     import paper_2608_02947_amd as atf
     note("bounds of NaNs")
@@ -372,6 +388,28 @@ def test_select_many_tokens():
     tok = Tokens(lens, queries, pt, 3)
     q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(1)).to(BF)
     check_select(tok, q, random_bounds(tok.P, pt, bt, h_kv, d, 2), bt, win, W, 3, 1, 1)
+
+
+@pytest.mark.parametrize("what", ["random", "zeros", "NaN"])
+def test_select_more_tokens_than_a_workspace_holds(what):
+    """Rows that may be long: the workspace holds some of the call's tokens at a time."""
+    import paper_2608_02947_amd as atf
+    note(f"select workspace {what}")
+    d, h_q, h_kv, pt, bt = 64, 6, 2, 32, 32
+    win, W = windows(d, "exact")
+    tok = Tokens([600, 333], [130, 100], pt, 3)
+    pages = 1 << 17
+    most = pages * pt
+    assert atf.atf_select_workspace_bytes(tok.T, h_q, h_kv, most, bt, d) < \
+        tok.T // 2 * atf.atf_select_workspace_bytes(1, h_q, h_kv, most, bt, d)
+    tok.table = np.pad(tok.table, ((0, 0), (0, pages - tok.table.shape[1])), constant_values=-1)
+    q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(1)).to(BF)
+    b = random_bounds(tok.P, pt, bt, h_kv, d, 2)
+    if what == "zeros":
+        b.zero_()
+    elif what == "NaN":
+        b.view(-1)[torch.arange(0, b.numel(), 3001)] = math.nan
+    check_select(tok, q, b, bt, win, W, 5, 1, 1, max_n_k=most)
 
 
 @pytest.mark.parametrize("what", ["random", "zeros", "NaN"])
