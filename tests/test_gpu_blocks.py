@@ -733,6 +733,42 @@ def test_attend_of_all_blocks_is_the_paged_decode():
     assert (lse - lse2)[live].abs().max() <= 1e-4
 
 
+def test_pages_past_32_bits():
+    """Pages further on than 2^32 bytes: the same bits as in a small pool."""
+    import paper_2608_02947_amd as atf
+    note("pages past 32 bits")
+    h_q, h_kv, d, pt, bt, T, top = 24, 8, 128, 256, 64, 700, 5
+    big, width = 2 ** 32 // (h_kv * d * 2 * pt) + 40, 3
+    win, _ = windows(d, "exact")
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn((T, h_q, d), generator=g).to(BF).to(DEV)
+    k, v = (torch.randn((T, h_kv, d), generator=g).to(BF).to(DEV) for _ in range(2))
+    got = []
+    for pages, ids in ((3, [2, 0, 1]), (big, [big - 1, big - 9, big - 17])):
+        table = dev32([ids])
+        kp = torch.empty(atf.kpages_shape(pages, pt, h_kv, d), dtype=BF, device=DEV)
+        vp = torch.empty(atf.vpages_shape(pages, pt, h_kv, d), dtype=BF, device=DEV)
+        bnd = torch.empty(atf.bounds_shape(pages, pt, bt, h_kv, d), dtype=BF, device=DEV)
+        at = torch.arange(T, device=DEV)
+        slots = table[0].long()[at // pt] * pt + at % pt
+        pos, rows, n = dev32(np.arange(T)), dev32(np.zeros(T)), dev32([T])
+        atf.atf_cache_append_slots_rotated(k, v, kp, vp, slots, pos, win)
+        atf.atf_block_bounds(kp, bnd, table, n, n, T)
+        blocks = dev32(np.full((T, h_kv, top), 777))
+        ws = torch.empty(atf.atf_select_workspace_bytes(T, h_q, h_kv, T, bt, d), dtype=torch.uint8, device=DEV)
+        atf.atf_select_blocks(q, bnd, blocks, table, pt, rows, pos, n, T, win, ws)
+        o, lse = torch.empty_like(q), torch.empty((T, h_q), device=DEV)
+        ws = torch.empty(atf.atf_attend_workspace_bytes(T, h_q, h_kv, top, bt, d), dtype=torch.uint8, device=DEV)
+        atf.atf_attend_blocks(q, kp, vp, o, lse, table, rows, pos, n, blocks, bt, win, ws)
+        torch.cuda.synchronize()
+        got.append((kp[ids].cpu(), bnd[ids].cpu(), blocks.cpu(), o.cpu(), lse.cpu()))
+        del kp, vp, bnd
+    # (the third page's last tokens are nobody's)
+    assert torch.equal(got[0][0][:2], got[1][0][:2]) and torch.equal(got[0][1][:2], got[1][1][:2])
+    for x, y in zip(got[0][2:], got[1][2:]):
+        assert torch.equal(x, y)
+
+
 # ---- a serving step of all of them
 
 class Engine:
