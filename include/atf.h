@@ -694,12 +694,15 @@ int atf_select_blocks(const void *q, const void *bounds, int32_t *blocks, int64_
  *   q, o     bf16 [n_tokens][h_q][d];  lse  fp32 [n_tokens][h_q]
  *   blocks   int32 [n_tokens][h_kv][top_blocks], as atf_select_blocks writes it   (device, read)
  *   n_k_rows int32 [batch], clamped to what a row's pages hold
- *   workspace: device, >= atf_attend_workspace_bytes(n_tokens, h_q, h_kv, top_blocks, block_tokens, d)
- *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each
+ *   workspace: device, 16-byte aligned, >= 256 bytes, contents are scratch; calls that may run at once
+ *            need one each.  Lists of few tokens are split over workgroups as far as their partial
+ *            states have room: the whole plan takes atf_attend_workspace_bytes(n_tokens, h_q, h_kv,
+ *            top_blocks, block_tokens, d) bytes, more for few tokens than for many; 256 * (h_q / h_kv) *
+ *            (4 d + 8) + 768 bytes hold the plans of every n_tokens and top_blocks
  * A row gives NaN where a number of a key is NaN in a pair that the window keeps; past its pair's
  * window such a number does not count.  softmax_scale <= 0 selects 1/sqrt(d).  Any group size is
  * built: up to 32 query heads of a KV head share a workgroup.  Table entries are clamped to [0, num_pages).
- * n_tokens == 0 is a no-op.  Deterministic.
+ * n_tokens == 0 is a no-op.  Deterministic: equal inputs and an equal workspace_bytes give equal bits.
  * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite or top_blocks *
  * block_tokens above 2^31 - 1, and ATF_EUNSUPPORTED for page_tokens above 2^26. */
 size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, int32_t top_blocks,

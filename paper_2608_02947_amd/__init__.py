@@ -1184,7 +1184,7 @@ def atf_attend_blocks(q, k_pages, v_pages, o, lse, block_table, token_rows, posi
                       block_tokens: int, window: Window, workspace, softmax_scale: float = 0.0, stream=None):
     """Windowed attention of query tokens q [T, h_q, d] over the blocks [T, h_kv, N] of their rows
     (int32; negative: none) -> o like q, lse [T, h_q] fp32; workspace: uint8 of
-    atf_attend_workspace_bytes()."""
+    atf_attend_workspace_bytes(), or of 256 bytes at least: lists are split as far as it has room."""
     fn = "atf_attend_blocks"
     ty, dev, st = _call()
     qs, bs, ts = q.shape, blocks.shape, block_table.shape

@@ -412,18 +412,20 @@ int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room) {
 // Lists are split while there is room for their waves, a tile a wave at least, where that saves 20 tiles
 // or more of a workgroup's (fewer save less than joining the splits costs: 4 groups of 32 tiles 12.2 us whole, 9.9
 // in 4 or more; of 16 tiles 10.1 and 9.3 to 10.7; 128 of 32 tiles 9.9 whole, 10.9 in 2; 4 of 512 80.6 and 17.1).
-AttendPlan attend_plan(int64_t groups, int64_t tiles) {
+// `room`: splits whose states the workspace holds.
+AttendPlan attend_plan(int64_t groups, int64_t tiles, int64_t room) {
     AttendPlan a = {1, 1, int32_t(std::min<int64_t>(tiles, INT32_MAX))};
     groups = std::max<int64_t>(groups, 1);
     const int32_t most = groups <= 256 ? 8 : groups <= 640 ? 4 : groups <= 2048 ? 2 : 1;
     while (a.waves < most && a.waves < tiles) a.waves *= 2;
-    const int64_t splits = std::min(2048 / (groups * 8), tiles / 8);
+    const int64_t splits = std::min({2048 / (groups * 8), tiles / 8, room});
     if (a.waves == 8 && splits > 1 && tiles * (splits - 1) >= 20 * splits) {
         a.split_tiles = int32_t((tiles + splits - 1) / splits);
         a.splits = int32_t((tiles + a.split_tiles - 1) / a.split_tiles);
     }
     return a;
 }
+AttendPlan attend_plan(int64_t groups, int64_t tiles) { return attend_plan(groups, tiles, tiles); }
 
 }  // namespace atf
 
@@ -1698,6 +1700,22 @@ int check_tokens(const char* fn, const QueryTokens& q) {
     return ATF_OK;
 }
 
+// States of split lists; without splits there are none.
+WsLayout attend_states(int64_t n_tokens, const atf::AttendPlan& plan, int32_t h_q, int32_t d) {
+    return ws_layout(plan.splits == 1 ? 0 : size_t(n_tokens) * size_t(plan.splits), h_q, d, 0);
+}
+constexpr size_t kAttendLeastBytes = 256;
+// The plan of a call in a workspace of `bytes`: as many splits as have room, at worst one.  Lists of many
+// tokens are not split, so that a workspace for them is smaller than one for few.
+atf::AttendPlan attend_plan_in(size_t bytes, int64_t n_tokens, int32_t h_q, int64_t columns, int64_t tiles, int32_t d) {
+    const int64_t groups = n_tokens * columns;
+    const atf::AttendPlan plan = atf::attend_plan(groups, tiles);
+    if (attend_states(n_tokens, plan, h_q, d).total <= bytes) return plan;
+    // (three arrays, each rounded up to 256 bytes)
+    const size_t split = size_t(n_tokens) * size_t(h_q) * size_t(d + 2) * 4;
+    return atf::attend_plan(groups, tiles, int64_t((bytes - std::min<size_t>(bytes, 3 * 256)) / split));
+}
+
 struct SelectLayout {
     int32_t slab, pack, ranges, key_stride;
     size_t off_exact, off_sizes, total;  // total 0: too large
@@ -1965,7 +1983,7 @@ size_t atf_attend_workspace_bytes(int64_t n_tokens, int32_t h_q, int32_t h_kv, i
         return 0;
     const int32_t group = h_q / h_kv, subgroups = (group + 31) / 32;
     const atf::AttendPlan plan = atf::attend_plan(n_tokens * h_kv * subgroups, int64_t(top_blocks) * (block_tokens / 32));
-    return std::max<size_t>(256, plan.splits == 1 ? 0 : ws_layout(size_t(n_tokens) * size_t(plan.splits), h_q, head_dim, 0).total);
+    return std::max(kAttendLeastBytes, attend_states(n_tokens, plan, h_q, head_dim).total);
 }
 
 int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, void* o, float* lse, int64_t n_tokens,
@@ -2000,11 +2018,14 @@ int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, v
     if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(o, 16) || !aligned(lse, 4) ||
         !aligned(blocks, 4))
         return fail(ATF_EINVAL, "%s: q/k/v/o must be 16-byte, lse and blocks 4-byte aligned", fn);
-    const size_t need = atf_attend_workspace_bytes(n_tokens, h_q, h_kv, top_blocks, block_tokens, d);
-    if (workspace == nullptr || workspace_bytes < need)
-        return fail(ATF_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+    if (workspace == nullptr || workspace_bytes < kAttendLeastBytes)
+        return fail(ATF_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, kAttendLeastBytes,
                     workspace == nullptr ? size_t(0) : workspace_bytes);
     if (!aligned(workspace, 16)) return fail(ATF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+    const int32_t group = h_q / h_kv, subgroups = (group + 31) / 32;
+    const atf::AttendPlan plan = attend_plan_in(workspace_bytes, n_tokens, h_q, int64_t(h_kv) * subgroups,
+                                                int64_t(top_blocks) * (block_tokens / 32), d);
+    const size_t need = std::max(kAttendLeastBytes, attend_states(n_tokens, plan, h_q, d).total);
     const size_t tokens = size_t(n_tokens) * 4, rows = tokens / 2 * size_t(h_q) * size_t(d);
     const size_t pool = pool_bytes(pg, h_kv, 2 * int64_t(d));
     const Span spans[] = {{"o", o, rows, true},
@@ -2043,16 +2064,14 @@ int atf_attend_blocks(const void* q, const void* k_pages, const void* v_pages, v
     p.top = top_blocks;
     p.h_q = h_q;
     p.h_kv = h_kv;
-    p.group = h_q / h_kv;
-    p.subgroups = (p.group + 31) / 32;
-    p.heads_per_block = (p.group + p.subgroups - 1) / p.subgroups;
-    const atf::AttendPlan plan =
-        atf::attend_plan(n_tokens * h_kv * p.subgroups, int64_t(top_blocks) * (block_tokens / 32));
+    p.group = group;
+    p.subgroups = subgroups;
+    p.heads_per_block = (group + subgroups - 1) / subgroups;
     p.waves = plan.waves;
     p.splits = plan.splits;
     p.split_tiles = plan.split_tiles;
     if (plan.splits > 1) {
-        const WsLayout L = ws_layout(size_t(n_tokens) * size_t(plan.splits), h_q, d, 0);
+        const WsLayout L = attend_states(n_tokens, plan, h_q, d);
         char* ws = static_cast<char*>(workspace);
         p.ws_m = reinterpret_cast<float*>(ws + L.off_m);
         p.ws_l = reinterpret_cast<float*>(ws + L.off_l);

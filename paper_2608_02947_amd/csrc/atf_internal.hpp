@@ -314,11 +314,12 @@ hipError_t launch_append_slots(const AppendSlotsParams& p, bool turn, int head_d
 hipError_t launch_block_bounds(const BoundsParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_select_blocks(const SelectParams& p, hipStream_t stream);
 // Waves of a workgroup and workgroups of a list for `groups` (token, KV head, head subgroup)s of lists of
-// `tiles` 32-token tiles.
+// `tiles` 32-token tiles; the second: where a workspace holds the states of `room` splits.
 struct AttendPlan {
     int32_t waves, splits, split_tiles;
 };
 AttendPlan attend_plan(int64_t groups, int64_t tiles);
+AttendPlan attend_plan(int64_t groups, int64_t tiles, int64_t room);
 hipError_t launch_attend_blocks(const AttendParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_rotate_kcache(const RotateParams& p, int head_dim, hipStream_t stream);
 

@@ -1,0 +1,42 @@
+"""Workspaces of the operators over blocks, sized once for calls of several sizes, on the host."""
+import ctypes
+import random
+
+import pytest
+
+import test_blocks_cpu as C
+from test_blocks_plan_cpu import Plan
+
+atf = pytest.importorskip("paper_2608_02947_amd")
+
+_fit = ctypes.CDLL(atf.LIB_PATH)["_ZN3atf11attend_planElll"]
+_fit.restype, _fit.argtypes = Plan, [ctypes.c_int64] * 3
+_plan = ctypes.CDLL(atf.LIB_PATH)["_ZN3atf11attend_planEll"]
+_plan.restype, _plan.argtypes = Plan, [ctypes.c_int64] * 2
+
+
+def test_attention_splits_no_further_than_its_room():
+    rng = random.Random(2)
+    for _ in range(20000):
+        groups, tiles, room = int(2 ** rng.uniform(0, 9)), int(2 ** rng.uniform(0, 14)), rng.choice([0, 1, 2, 7, 30, 300])
+        p, whole = _fit(groups, tiles, room), _plan(groups, tiles)
+        assert 1 <= p.splits <= max(1, min(room, 256 // groups, tiles // 8))
+        assert p.waves == whole.waves and p.splits * p.split_tiles >= tiles > (p.splits - 1) * p.split_tiles
+        if room >= tiles:
+            assert (p.splits, p.split_tiles) == (whole.splits, whole.split_tiles)
+
+
+def test_attention_workspace_that_serves_every_call():
+    """The bound that atf.h names."""
+    for h_q, h_kv, d in ((32, 4, 128), (14, 2, 64), (40, 1, 64), (72, 1, 128), (16, 16, 64), (300, 300, 64)):
+        most = 256 * (h_q // h_kv) * (4 * d + 8) + 768
+        for n in list(range(1, 300)) + [900, 5000]:
+            for top, bt in ((1, 32), (16, 32), (27, 32), (64, 64), (300, 32), (4096, 128)):
+                assert 256 <= atf.atf_attend_workspace_bytes(n, h_q, h_kv, top, bt, d) <= most
+
+
+@pytest.mark.parametrize("size", [0, 255])
+def test_attention_workspaces_below_the_least_are_refused(size):
+    fn, make = C.CALLS["attend"]
+    assert fn(*make(bytes=size).values()) == atf.ATF_EWORKSPACE
+    assert atf.atf_last_error()

@@ -1,0 +1,47 @@
+"""Selection of blocks and attention over them in workspaces of other sizes than the call's own."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_blocks as B
+from parity import note
+
+pytestmark = B.pytestmark
+
+
+class Room:
+    """A workspace of `size` bytes inside a larger buffer whose other bytes are looked at."""
+
+    def __init__(self, size):
+        self.all = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=B.DEV)
+        self.part, self.size = self.all[:size], size
+
+    def check(self):
+        assert bool((self.all[self.size:] == 0x5A).all())
+
+
+@pytest.mark.parametrize("d,h_q,h_kv", [(128, 32, 4), (64, 40, 1)])
+def test_attend_in_the_workspace_of_another_step(monkeypatch, d, h_q, h_kv):
+    """A workspace made for a prompt's tokens serves single ones, and any size from 256 bytes on serves any call,
+    without a byte written past it; the whole plan's size and the one that serves every call give the same bits."""
+    import paper_2608_02947_amd as atf
+    note(f"attend workspaces {d} {h_q}/{h_kv}")
+    pt, bt, top = 64, 64, 64
+    win, W = B.windows(d, "exact")
+    for queries in ((1,), (3, 1)):
+        tok = B.Tokens([4500, 3000][:len(queries)], queries, pt, 7)
+        q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(7)).to(B.BF)
+        kp, vp = B.random_pools(tok.P, pt, h_kv, d, 7)
+        lists = B.random_lists(tok, h_kv, top, bt, 7, wild=False)
+        size = lambda n: atf.atf_attend_workspace_bytes(n, h_q, h_kv, top, bt, d)
+        own, prompt, every = size(tok.T), size(900), 256 * (h_q // h_kv) * (4 * d + 8) + 768
+        assert prompt < own <= every
+        got = {}
+        attended = B.attended
+        for bytes_ in (prompt, own // 5, own // 2, own - 256, own, every):
+            room = Room(bytes_ // 16 * 16)
+            monkeypatch.setattr(B, "attended", lambda *a: attended(*a, ws=room.part))
+            got[bytes_] = B.check_attend(tok, q, kp, vp, lists, bt, win, W)
+            room.check()
+        monkeypatch.setattr(B, "attended", attended)
+        assert all(np.array_equal(x, y) for x, y in zip(got[own], got[every]))
