@@ -669,7 +669,8 @@ int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_tab
  *   blocks  int32 [n_tokens][h_kv][top_blocks], ascending, then -1 where the row has fewer (device, written)
  *   token_rows, positions  int32 [n_tokens];  n_k_rows  int32 [batch], clamped to [0, max_n_k]
  *   workspace: device, >= atf_select_workspace_bytes(n_tokens, h_q, h_kv, max_n_k, block_tokens, d)
- *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each
+ *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each.  A
+ *            workspace serves fewer tokens and a smaller max_n_k too
  * Table entries are clamped to [0, num_pages).  n_tokens == 0 is a no-op.  Deterministic.
  * Errors: ATF_EINVAL (NULL window or pointer, misaligned pointer, written buffers that overlap another
  * one, batch < 1, n_tokens < 0, n_tokens * h_q > 2^23, heads < 1, h_q % h_kv != 0, max_n_k < 1 or more than a

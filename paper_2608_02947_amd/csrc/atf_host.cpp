@@ -1718,7 +1718,7 @@ atf::AttendPlan attend_plan_in(size_t bytes, int64_t n_tokens, int32_t h_q, int6
 
 struct SelectLayout {
     int32_t slab, pack, ranges, key_stride;
-    size_t off_exact, off_sizes, total;  // total 0: too large
+    size_t off_exact, off_sizes, total;  // total 0: too large; else no less than for fewer tokens or keys
 };
 // Tokens of a row one behind the other share the columns of the matrix products: where there are more
 // than two a row they are taken to.  A wave has a tile of 16 blocks at least, and waves are 4,096 in all
@@ -1746,7 +1746,10 @@ SelectLayout select_layout(int64_t n_tokens, int32_t batch, int32_t h_q, int32_t
     if (keys * 16 > u128(1) << 46) return L;
     L.off_exact = align_up(size_t(keys) * 4, 256);
     L.off_sizes = L.off_exact + align_up(size_t(keys) * 8, 256);
-    L.total = L.off_sizes + align_up(size_t(slab) * size_t(h_kv) * size_t(most_ranges) * 4, 256);
+    // (slab * each, and three arrays rounded up; a slab that kSelectSlabBytes bounds leaves less than `each` of
+    // them, more or less of it as rows get longer)
+    const u128 most = u128(std::min<int64_t>(n_tokens, 65535 / h_kv)) * each;
+    L.total = size_t(std::min(most, std::max(u128(atf::kSelectSlabBytes), each))) + 3 * 256;
     return L;
 }
 

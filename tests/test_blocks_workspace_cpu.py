@@ -40,3 +40,18 @@ def test_attention_workspaces_below_the_least_are_refused(size):
     fn, make = C.CALLS["attend"]
     assert fn(*make(bytes=size).values()) == atf.ATF_EWORKSPACE
     assert atf.atf_last_error()
+
+
+def test_selection_workspace_serves_smaller_calls():
+    """Fewer tokens and fewer keys take no more; what the tokens of one launch need is there: 12 bytes a block
+    for as many tokens as 256 MB hold."""
+    for h_q, h_kv, bt, d in ((6, 2, 64, 128), (32, 8, 64, 128), (64, 64, 32, 128), (40, 2, 32, 64), (3000, 3000, 64, 64)):
+        rng = random.Random(h_q)
+        tokens = sorted({0, 1, 2, 64} | {int(2 ** rng.uniform(0, 11)) for _ in range(20)})
+        keys = sorted({1, 500000, 1 << 20, 2000000, 6 << 20, 2 ** 31 - 1} | {int(2 ** rng.uniform(0, 31)) for _ in range(40)})
+        size = [[atf.atf_select_workspace_bytes(n, h_q, h_kv, k, bt, d) for k in keys] for n in tokens]
+        for i, n in enumerate(tokens):
+            for j, k in enumerate(keys):
+                assert size[i][j] >= size[max(i - 1, 0)][j] and size[i][j] >= size[i][max(j - 1, 0)]
+                each = 12 * h_kv * -(-k // (16 * bt)) * 16
+                assert size[i][j] >= each * max(1, min(n, 65535 // h_kv, (1 << 28) // (2 * each)))

@@ -45,3 +45,45 @@ def test_attend_in_the_workspace_of_another_step(monkeypatch, d, h_q, h_kv):
             room.check()
         monkeypatch.setattr(B, "attended", attended)
         assert all(np.array_equal(x, y) for x, y in zip(got[own], got[every]))
+
+
+@pytest.mark.parametrize("what", ["random", "zeros"])
+def test_select_in_the_workspace_of_longer_rows(what):
+    """A workspace made for rows of 6 M keys serves rows of 1 M, whose tokens fill more of it; nothing is written
+    past it."""
+    import paper_2608_02947_amd as atf
+    note(f"select workspace of longer rows {what}")
+    d, h, pt, bt, top = 64, 64, 32, 32, 3
+    win, W = B.windows(d, "exact")
+    tok = B.Tokens([200, 333], [40, 22], pt, 3)
+    assert tok.T == 64
+    most = 1 << 20
+    tok.table = np.pad(tok.table, ((0, 0), (0, most // pt - tok.table.shape[1])), constant_values=-1)
+    q = torch.randn((tok.T, h, d), generator=torch.Generator().manual_seed(1)).to(B.BF)
+    b = B.random_bounds(tok.P, pt, bt, h, d, 2)
+    if what == "zeros":
+        b.zero_()
+    room = Room(atf.atf_select_workspace_bytes(tok.T, h, h, 6 * most, bt, d))
+    got = B.selected(tok, q.to(B.DEV), b.to(B.DEV), bt, win, top, 1, 1, max_n_k=most, ws=room.part)
+    room.check()
+    want = np.full(got.shape, 777)
+    B.R.select(q.double().numpy(), b.double().numpy(), tok.table, tok.rows, tok.pos, tok.lens, most, W, pt, bt, top, 1, 1, want)
+    assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("T,most", [(1, 1), (1, 70000), (70, 3000), (232, 1 << 22)])
+def test_select_writes_no_further_than_its_size(T, most):
+    import paper_2608_02947_amd as atf
+    note(f"select workspace end {T} {most}")
+    d, h_q, h_kv, pt, bt = 64, 6, 2, 32, 32
+    win, _ = B.windows(d, "exact")
+    n = min(most, 3000)
+    tok = B.Tokens([n, n], [T - T // 2, T // 2], pt, 3, pad=0)
+    tok.pos = np.maximum(tok.pos, 0)
+    tok.table = np.pad(tok.table, ((0, 0), (0, max(0, -(-most // pt) - tok.table.shape[1]))), constant_values=-1)
+    q = torch.randn((T, h_q, d), generator=torch.Generator().manual_seed(1)).to(B.BF).to(B.DEV)
+    for b in (B.random_bounds(tok.P, pt, bt, h_kv, d, 2), torch.zeros(atf.bounds_shape(tok.P, pt, bt, h_kv, d), dtype=B.BF)):
+        room = Room(atf.atf_select_workspace_bytes(T, h_q, h_kv, most, bt, d))
+        out = B.selected(tok, q, b.to(B.DEV), bt, win, 5, 1, 1, max_n_k=most, ws=room.part)
+        room.check()
+        assert torch.equal(out, B.selected(tok, q, b.to(B.DEV), bt, win, 5, 1, 1, max_n_k=most))
