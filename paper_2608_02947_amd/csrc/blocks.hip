@@ -138,7 +138,8 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsParams p)
 // These sums are in fp32, off by no more than their error bound: the additions that a term goes through
 // (a product's 32, then one a chunk or pair), each at most 2^-23 of the sum of magnitudes, which a
 // second product has, and what fp32 loses below its smallest normal number.  pick_kernel finds the
-// border of the blocks taken among them; blocks as near to it as the bound allows, mostly the one that
+// border of the blocks taken among them (those taken anyway, first or last, are not compared, and their magnitudes
+// do not count: they may be any); blocks as near to it as the bound allows, mostly the one that
 // is the border, are summed again in 64 bits unless all or none of them are taken.
 //
 // Bound by latency for single tokens (1,048,576 keys in 16,384 blocks, 28/4 heads of 128: scores 13 us, of
@@ -264,6 +265,8 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     const int early_row = max(__builtin_amdgcn_readfirstlane(tok.row), 0);
     const int early_page = page_of(p, early_row, min(16 * range + r16, p.row_blocks - 1));
     if (!is) tok = {-1, 0, -1};
+    // blocks that the column's choice compares, from first_blocks on
+    const uint32_t compared = uint32_t(max(0, tok.last / p.block_tokens + 1 - p.last_blocks - p.first_blocks));
 
     const int held = min((G + 15) / 16, kHeld);
     s_masks[threadIdx.x] = keep_pairs(u32x4_t{~0u, ~0u, ~0u, ~0u}, threadIdx.x);
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
     // signs of the bounds' magnitudes: those of the queries' parts
     const uint32_t minus = g4 >= 2 ? 0x80008000u : 0u;
     bool todo = is && tok.row >= 0 && tok.last >= 0;
-    float worst = 0.f;  // largest sum of magnitudes times its additions
+    float worst = 0.f;  // largest sum of magnitudes times its additions, of the blocks compared
     for (uint64_t rest = __ballot(todo); rest != 0; rest = __ballot(todo)) {
         const int row = __builtin_amdgcn_readlane(tok.row, __builtin_ctzll(rest));
         const bool mine = todo && tok.row == row;
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(256, 3) void scores_kernel(const SelectParams p) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (live) best[i] = max(best[i], key_of(sum[i]));
-                    if (live) worst = fmaxf(worst, size[i] * steps);
+                    if (live && uint32_t(j0 + 4 * g4 + i - p.first_blocks) < compared) worst = fmaxf(worst, size[i] * steps);
                 }
             }
 #pragma unroll

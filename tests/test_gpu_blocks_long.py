@@ -184,6 +184,39 @@ def test_select_whatever_the_blocks_taken_anyway_hold(x, queries):
     check(tok, q, b, bt, win, W, 7, 1, 1)
 
 
+@pytest.mark.parametrize("x", [math.inf, math.nan, 1e37, 3000.0])
+@pytest.mark.parametrize("n,queries", [(3000, (1, 1)), (3000, (70, 60)), (70000, (1, 1))])
+def test_select_without_sums_in_64_bits_for_blocks_taken_anyway(n, queries, x):
+    """What the blocks taken anyway hold, and those past a token's position that others of its row reach, leaves
+    the sums in 64 bits of all other blocks undone: their place in the workspace, behind 4 bytes for each block
+    and token, keeps what it holds."""
+    import paper_2608_02947_amd as atf
+    note(f"select forced, no sums {n} {queries} {x}")
+    d, h, pt, bt = 64, 16, 32, 32
+    win, W = B.windows(d, "off")
+    tok = B.Tokens([n, 640], queries, pt, 9, pad=0)
+    q = torch.randn((tok.T, h, d), generator=torch.Generator().manual_seed(9)).to(B.BF)
+    plain = B.random_bounds(tok.P, pt, bt, h, d, 9)
+    keys = tok.T * h * (-(-n // (16 * bt)) * 16)
+    at = -(-4 * keys // 256) * 256
+    for j, summed in ((0, False), (-1, False), (n // bt // 2, True)):
+        b = plain.clone()
+        for row, pos in zip(tok.rows, tok.pos):
+            if j != -1:
+                b[tok.table[row, j if row == 0 or not summed else 9]] = x
+        if j == -1:  # the last blocks that any token of a row reaches: nobody compares them
+            for row in range(2):
+                last = tok.pos[tok.rows == row]
+                b[tok.table[row, last.min() // bt: last.max() // bt + 1]] = x
+        ws = torch.full((atf.atf_select_workspace_bytes(tok.T, h, h, n, bt, d),), 0x5A, dtype=torch.uint8, device=B.DEV)
+        got = B.selected(tok, q.to(B.DEV), b.to(B.DEV), bt, win, 7, 1, 3, ws=ws).cpu().numpy()
+        assert np.array_equal(got, chosen(tok, q.double().numpy(), b.double().numpy(), bt, W, 7, 1, 3))
+        if summed and not math.isfinite(x):
+            assert not bool((ws[at: at + 8 * keys] == 0x5A).all())
+        elif not summed:
+            assert bool((ws[at: at + 8 * keys] == 0x5A).all())
+
+
 @pytest.mark.parametrize("kind", ["exact", "sliding"])
 def test_select_for_queries_that_are_none(kind):
     """NaN and infinities in queries: scores that are none, or infinite; past its pair's window such a number does
