@@ -52,10 +52,6 @@ def plan(table, pt, free, count, n_k, n_new, T):
                 positions=np.array(positions), counts=np.array([top, starts[-1], refused]))
 
 
-def k_place(t):
-    return t
-
-
 def v_slot(t):
     """Slot of token t of a 16-token V block."""
     return 8 * (t // 4 % 2) + 4 * (t // 8) + t % 4

@@ -232,6 +232,35 @@ def test_select_for_queries_that_are_none(kind):
         check(tok, q, B.random_bounds(tok.P, pt, bt, h_kv, d, 7), bt, win, W, 9, 1, 1)
 
 
+@pytest.mark.parametrize("x", [math.inf, math.nan])
+@pytest.mark.parametrize("d,h_q", [(64, 5), (128, 20)])
+def test_attend_for_queries_that_are_none(d, h_q, x):
+    """Such a number is its own head's and token's: all others stay within check_attend's errors of what they are
+    without it (twice, once for each call: their sums may be scaled at other tiles)."""
+    note(f"attend queries {d} {h_q} {x}")
+    h_kv, pt, bt = 1, 64, 32
+    win, W = B.windows(d, "sliding")
+    tok = B.Tokens([333, 150], [1, 2], pt, 5)
+    q = torch.randn((tok.T, h_q, d), generator=torch.Generator().manual_seed(1)).to(B.BF)
+    kp, vp = B.random_pools(tok.P, pt, h_kv, d, 2)
+    lists = B.random_lists(tok, h_kv, 4, bt, 1, wild=False)
+    lists[0, 0] = [6, 7, 9, 10]  # the newest and those where the windows of 100 tokens end
+    o, lse = B.check_attend(tok, q, kp, vp, lists, bt, win, W)
+    wo, _, mass, size = R.attend(q.double().numpy(), kp.double().numpy(), vp.double().numpy(), tok.table, tok.rows, tok.pos,
+                                 tok.lens, lists, W, pt, bt, d ** -0.5)
+    bad = q.clone()
+    bad[0, 1, 3] = x
+    o2, lse2 = (B.to64(y)[:3] for y in B.attended(tok, bad.to(B.DEV), kp.to(B.DEV), vp.to(B.DEV), lists, bt, win))
+    assert np.isnan(o2[0, 1]).all() and np.isnan(lse2[0, 1])
+    e = (d + 2) * 2.0 ** -23 * size[:3] + 2.0 ** -22 * (size[:3] + 1)
+    tol = 2.0 ** -7 * np.abs(wo[:3]) + 2 * (2 * e + 2.0 ** -15 + 4 * bt * 2.0 ** -23)[..., None] * mass[:3]
+    rest = np.ones((3, h_q), dtype=bool)
+    rest[0, 1] = False
+    assert (np.abs(o2 - o) <= tol)[rest].all()
+    tol_l = 2 * (e + 4 * bt * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(lse)))
+    assert (np.abs(lse2 - lse) <= tol_l)[rest].all()
+
+
 # ---- at once
 
 def test_two_streams_with_their_work_queued():
