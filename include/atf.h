@@ -663,7 +663,7 @@ int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_tab
  * The query heads of one KV head take the same blocks: a block counts by its largest score of them.
  * Taken are, top_blocks in all: the first first_blocks blocks and the last last_blocks; blocks
  * with a score that is NaN; then those with the largest scores; of equal ones the lower block.  Scores
- * are compared as exact sums would be: summed in 64 bits wherever fp32 cannot tell.
+ * are compared as sums in 64 bits would be: they are summed so wherever fp32 cannot tell.
  *   q       bf16 [n_tokens][h_q][d], rotated                       (device, read)
  *   bounds  as atf_block_bounds                                    (device, read)
  *   blocks  int32 [n_tokens][h_kv][top_blocks], ascending, then -1 where the row has fewer (device, written)
@@ -671,7 +671,9 @@ int atf_block_bounds(const void *k_pages, void *bounds, const int32_t *block_tab
  *   workspace: device, >= atf_select_workspace_bytes(n_tokens, h_q, h_kv, max_n_k, block_tokens, d)
  *            bytes, 16-byte aligned, contents are scratch; calls that may run at once need one each.  A
  *            workspace serves fewer tokens and a smaller max_n_k too
- * Table entries are clamped to [0, num_pages).  n_tokens == 0 is a no-op.  Deterministic.
+ * A token and KV head with a score that is not finite, or with hundreds of blocks that may be the last taken
+ * (windows that end before most of them leave scores of 0), has all its blocks summed in 64 bits, which is
+ * far slower.  Table entries are clamped to [0, num_pages).  n_tokens == 0 is a no-op.  Deterministic.
  * Errors: ATF_EINVAL (NULL window or pointer, misaligned pointer, written buffers that overlap another
  * one, batch < 1, n_tokens < 0, n_tokens * h_q > 2^23, heads < 1, h_q % h_kv != 0, max_n_k < 1 or more than a
  * row's pages hold, top_blocks < 1 or > 4096, first_blocks or last_blocks < 0 or their sum above top_blocks,
@@ -701,7 +703,9 @@ int atf_select_blocks(const void *q, const void *bounds, int32_t *blocks, int64_
  *            top_blocks, block_tokens, d) bytes, more for few tokens than for many; 256 * (h_q / h_kv) *
  *            (4 d + 8) + 768 bytes hold the plans of every n_tokens and top_blocks
  * A row gives NaN where a number of a key is NaN in a pair that the window keeps; past its pair's
- * window such a number does not count.  softmax_scale <= 0 selects 1/sqrt(d).  Any group size is
+ * window such a number does not count.  A query's number that is infinite gives its head NaN also where
+ * its pair's window ends among the 32 tokens of a tile (atf_decode_paged keeps the tokens past the window apart
+ * there).  softmax_scale <= 0 selects 1/sqrt(d).  Any group size is
  * built: up to 32 query heads of a KV head share a workgroup.  Table entries are clamped to [0, num_pages).
  * n_tokens == 0 is a no-op.  Deterministic: equal inputs and an equal workspace_bytes give equal bits.
  * Errors: as atf_select_blocks, plus ATF_EINVAL for a scale that is not finite or top_blocks *

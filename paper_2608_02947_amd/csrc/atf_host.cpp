@@ -408,7 +408,9 @@ int64_t decode_q8_splits(int64_t groups, int64_t slots, int64_t room) {
 // 2,048), no more than it has tiles: each state joined costs, with groups to spare more than the waves
 // gain (12,000 groups of 4 tiles, 24/8 heads of 128: 90 us with one wave, 103, 161 and 302 with 2, 4 and
 // 8; 1,024 of 512, 32/4 heads: 304 with 2, 331 and 392 with 4 and 8; 320 of 128, 24/8 heads: 136 with one,
-// 91, 87 and 92; 256 of 512, 32/4 heads: 234 with 2, 127 and 105).
+// 91, 87 and 92; 256 of 512, 32/4 heads: 234 with 2, 127 and 105; d = 64, 16/16 heads: 256 of 32 12.2 with 8, 12.7
+// with 4; 640 of 128 38.5 with 4, 41.8 with 8; 1,024 of 32 19.6 with 2, 17.9 with 4; 4,096 of 32 44.4 with one, 48.7
+// with 2; but 2,496 of 128, little more than one round, 125 with one, 99 with 4).
 // Lists are split while there is room for their waves, a tile a wave at least, where that saves 20 tiles
 // or more of a workgroup's (fewer save less than joining the splits costs: 4 groups of 32 tiles 12.2 us whole, 9.9
 // in 4 or more; of 16 tiles 10.1 and 9.3 to 10.7; 128 of 32 tiles 9.9 whole, 10.9 in 2; 4 of 512 80.6 and 17.1).

@@ -490,7 +490,8 @@ __device__ __forceinline__ void write_taken(int32_t* out, int top, int n, PickSh
 }
 
 // Every block's score in 64 bits, the border found 8 bits at a time: where fp32 tells nothing (numbers
-// that are not finite, many equal blocks).
+// that are not finite, many equal blocks).  Bound by the latency of a wave's blocks one behind the other (16,384
+// blocks of 7 heads, 16 waves: 4.2 ms).
 template <int kThreads>
 __device__ __forceinline__ void pick_exact(const SelectParams& p, const Token& tok, int t, int g, int n, int want,
                                                      uint64_t* keys, int32_t* out, PickShared<kThreads>& s) {
@@ -810,7 +811,11 @@ hipError_t launch_select_blocks(const SelectParams& all, hipStream_t stream) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const dim3 picks(unsigned(p.tokens) * unsigned(p.h_kv));
-        // (a wave a pick where they are many)
+        // A wave a pick where they are many (us of a selection, picks by 256 threads and by 64; 24/8 heads, 516
+        // blocks: 1,008 picks 28.2 and 29.5, 2,040 34.2 and 33.6, 8,184 81.5 and 71.9; 94 blocks: 24.7 and 26.7,
+        // 23.2 and 22.9, 53.6 and 43.0; 14/2 heads of 64, 938 blocks: 2,046 57.5 and 57.5, 4,092 79.6 and 78.6).
+        // Past 16,384 blocks a row a thread's keys have no room in registers (32,768 blocks of 4 heads: 47 us; 8.5
+        // for 16,384)
         if (p.row_blocks <= 1024 && picks.x > 2048)
             hipLaunchKernelGGL((pick_kernel<64, 16>), picks, dim3(64), 0, stream, p);
         else if (p.row_blocks <= 1024)
